@@ -415,6 +415,180 @@ CIERA_API int ciera_select_shards(const ciera_gain_in* shards, uint32_t n_shards
                                   int with_sender_cache, uint32_t* ranking_out, uint8_t* selected_out,
                                   double* gains_out, uint64_t* footprints_out, uint64_t* used_bytes_out);
 
+/* ---- the MoE layer behind the gather ---------------------------------------------------------- */
+
+/* What the gathered experts are needed for (no counterpart in the paper, which leaves the layer to the training
+ * framework): tokens are routed to experts, their rows laid out expert by expert, multiplied with the experts'
+ * matrices in 8-bit floating point, and summed back.  All calls only enqueue work on `stream`, read every size that
+ * depends on the routing on the device, keep nothing between calls, and give the same bits for the same inputs.
+ * dtype arguments are ciera_dtype values; strides count elements; every tensor's last dimension is contiguous.  Buffers
+ * of one call do not overlap.  Base pointers of 16-, 32- and 64-bit data are aligned to one value; wider alignment is
+ * used where it is there. */
+
+typedef enum ciera_score { CIERA_SCORE_SOFTMAX = 0, CIERA_SCORE_SIGMOID = 1 } ciera_score;
+
+/* Routing.  For each token with logits l[0 .. n_experts):
+ *   s = softmax(l) or, value by value, sigmoid(l);   c = s + bias (bias 0 if NULL)
+ *   an expert whose logit is -inf or NaN, or whose c is -inf or NaN, is closed: its s is 0 where the logit closes it,
+ *   and it is never chosen; +inf counts as the largest finite number
+ *   groups of n_experts / n_groups neighbours; a group's value is the sum of its `group_best` (1 or 2) largest c; the
+ *   top_groups groups of the largest values stay (a group without an open expert never does)
+ *   the top_k largest c among them are chosen, in falling order; equal values go to the lower index
+ *   w = scale * s of the chosen, divided by the sum of their s if `renormalise` (0 where that sum is 0)
+ * Choices are those of 64-bit arithmetic.  Where fewer than top_k experts are open, the rest has index -1 and weight 0.
+ * Limits: n_experts 1 .. 1024, top_k 1 .. 32 and at most top_groups * (n_experts / n_groups), n_groups 1 .. 32 and a
+ * divisor of n_experts, scale finite. */
+typedef struct ciera_route_config {
+    uint32_t n_experts, top_k, n_groups, top_groups, group_best;
+    int32_t score;       /* ciera_score */
+    int32_t renormalise; /* 0 or 1 */
+    float scale;
+} ciera_route_config;
+
+/*   logits   device, n_tokens rows of n_experts values, logits_stride apart
+ *   bias     device, n_experts fp32, or NULL: added for the choice only
+ *   experts  device, n_tokens x top_k int32;  weights  device, n_tokens x top_k fp32 */
+CIERA_API int ciera_route(const ciera_route_config* config, int dtype, const void* logits_dev, uint64_t n_tokens,
+                          uint64_t logits_stride, const float* bias_dev, int32_t* experts_dev, float* weights_dev,
+                          void* stream);
+/* Gradient of the logits from that of the weights, for the choice in `experts` (entries outside 0 .. n_experts - 1 and
+ * their dweights are passed over).  Through the scores and, if asked for, the renormalisation; the choice and the bias
+ * have none.  Closed experts get 0.  dlogits has the logits' type; every value of its rows is written. */
+CIERA_API int ciera_route_backward(const ciera_route_config* config, int dtype, const void* logits_dev, uint64_t n_tokens,
+                                   uint64_t logits_stride, const int32_t* experts_dev, const float* dweights_dev,
+                                   void* dlogits_dev, uint64_t dlogits_stride, void* stream);
+
+/* Rows of a segment are a multiple of this, and so many values share a scale. */
+#define CIERA_FP8_BLOCK 128
+
+/* Layout of n_slots slots (token * top_k + choice) by expert: expert e's slots in rising order at rows starts[e] ..
+ * starts[e] + counts[e] - 1, its segment ends at starts[e + 1], a multiple of 128.  Slots whose expert is outside
+ * 0 .. n_experts - 1 get no row (-1).
+ *   starts       device, n_experts + 1 int32;  counts  device, n_experts int32
+ *   row_of_slot  device, n_slots int32
+ *   slot_of_row  device, ciera_expert_rows_capacity() int32: -1 for the rows that fill a segment up; rows from
+ *                starts[n_experts] on are left as they were
+ *   workspace    device, ciera_expert_layout_workspace_bytes(); any contents, not shared by calls that may overlap
+ * Limits: n_experts 1 .. 1024, at most 2^30 slots. */
+CIERA_API uint64_t ciera_expert_rows_capacity(uint64_t n_slots, uint32_t n_experts);
+CIERA_API size_t ciera_expert_layout_workspace_bytes(uint64_t n_slots, uint32_t n_experts);
+CIERA_API int ciera_expert_layout(const int32_t* experts_dev, uint64_t n_slots, uint32_t n_experts, int32_t* starts_dev,
+                                  int32_t* counts_dev, int32_t* row_of_slot_dev, int32_t* slot_of_row_dev, void* workspace,
+                                  void* stream);
+
+/* Operands in e4m3 (finite, largest 448) with a power of two for each block of 128 values.  With the block's largest
+ * magnitude a, s is the least integer >= -126 with a <= 448 * 2^s (0 for a block of zeros); the scale byte is s + 127 and
+ * stands for 2^s; a value y is stored as y * 2^-s rounded to nearest, ties to even.  A block that holds an infinity or a
+ * NaN has byte 255 and NaN in all its places.
+ * Scale bytes of an operand [rows, cols] whose blocks lie along the columns: byte (column / 128) * stride + row. */
+typedef enum ciera_fp8_source {
+    CIERA_SOURCE_ROWS = 0,           /* y = x, or x of the row's token (slot_of_row), or row_weights[slot] * that           */
+    CIERA_SOURCE_SWIGLU = 1,         /* y[:, j] = silu(x[:, j]) * x[:, cols + j]; x has 2 * cols columns                     */
+    CIERA_SOURCE_SWIGLU_BACKWARD = 2 /* gradient of that by x: cols even, x has cols columns, grad has cols / 2              */
+} ciera_fp8_source;
+
+/* Rows of an operand, formed from `x` and rounded in one pass.
+ *   q, scales      blocks along the columns: q [rows, cols], ceil(cols / 128) rows of scale bytes
+ *   qt, scales_t   or NULL, NULL: the same y transposed, blocks of 128 rows: qt [cols, rows], ceil(rows / 128) rows of
+ *                  scale bytes (one for each column of y)
+ *   slot_of_row    or NULL.  With CIERA_SOURCE_ROWS row r is made from x's row slot_of_row[r] / top_k; with the others
+ *                  from x's row r.  Rows without a slot (negative, or beyond x_rows * top_k) are zero.
+ *   row_weights    or NULL; x_rows * top_k fp32 (CIERA_SOURCE_ROWS with slot_of_row only)
+ *   starts         or NULL: rows from starts[n_experts] on are left as they were, in q, qt and the scales alike
+ * q and qt are 16-byte aligned with strides that are multiples of 16 and at least cols / rows.  Limits: rows and cols
+ * 1 .. 2^31 - 256.  Arithmetic in 32 bits; the scale is that of 64-bit arithmetic where silu stands in between. */
+typedef struct ciera_fp8_rows {
+    int32_t source, dtype; /* dtype of x and grad */
+    uint64_t rows, cols, x_rows;
+    const void* x;
+    uint64_t x_stride;
+    const void* grad;
+    uint64_t grad_stride;
+    const int32_t* slot_of_row;
+    const float* row_weights;
+    const int32_t* starts;
+    uint32_t top_k, n_experts;
+    void* q;
+    uint64_t q_stride;
+    uint8_t* scales;
+    uint64_t scales_stride;
+    void* qt;
+    uint64_t qt_stride;
+    uint8_t* scales_t;
+    uint64_t scales_t_stride;
+} ciera_fp8_rows;
+CIERA_API int ciera_fp8_quantize_rows(const ciera_fp8_rows* args, void* stream);
+
+/* Matrices with one scale for each block of 128 x 128: x is `matrices` matrices [rows, cols], x_stride between rows,
+ * x_matrix_stride between matrices.  scales: byte (matrix, row / 128, column / 128) at matrix * scales_matrix_stride +
+ * (row / 128) * scales_stride + column / 128.  qt, scales_t (or NULL, NULL): the transposed matrices [cols, rows]. */
+typedef struct ciera_fp8_blocks {
+    int32_t dtype;
+    uint32_t matrices;
+    uint64_t rows, cols;
+    const void* x;
+    uint64_t x_stride, x_matrix_stride;
+    void* q;
+    uint64_t q_stride, q_matrix_stride;
+    uint8_t* scales;
+    uint64_t scales_stride, scales_matrix_stride;
+    void* qt;
+    uint64_t qt_stride, qt_matrix_stride;
+    uint8_t* scales_t;
+    uint64_t scales_t_stride, scales_t_matrix_stride;
+} ciera_fp8_blocks;
+CIERA_API int ciera_fp8_quantize_blocks(const ciera_fp8_blocks* args, void* stream);
+
+/* Products of such operands, out = sum over blocks of 2^(sa + sb) * (a_block * b_block^T), summed in fp32.
+ *   CIERA_PRODUCT_DENSE     out [m, n] = a [m, k] * b [n, k]^T
+ *   CIERA_PRODUCT_ROWS      rows starts[e] .. starts[e + 1] - 1 of a and out with matrix e of b [n_experts][n, k]; rows of
+ *                           out from starts[n_experts] on are left as they were
+ *   CIERA_PRODUCT_CONTRACT  out [n_experts][m, n]: a [m, k] * b [n, k]^T over the columns starts[e] .. starts[e + 1] - 1
+ *                           alone; zeros for an empty segment
+ * a has a scale for each row and 128 columns; b the same (b_blocks 0, CONTRACT and DENSE) or one for each block of
+ * 128 x 128 (b_blocks 1, DENSE and ROWS; strides as in ciera_fp8_blocks).
+ * starts rise from 0, are multiples of 128 and end at or below m (ROWS) or k (CONTRACT): otherwise CIERA_ERR_CORRUPT is
+ * written to *status, if given, and no output.  a, b are 16-byte aligned, their strides multiples of 16 and at most
+ * 2^40 - 16.  Limits: m, n, k 1 .. 2^31 - 256, n_experts 1 .. 1024. */
+typedef enum ciera_product_mode {
+    CIERA_PRODUCT_DENSE = 0,
+    CIERA_PRODUCT_ROWS = 1,
+    CIERA_PRODUCT_CONTRACT = 2
+} ciera_product_mode;
+typedef struct ciera_fp8_product {
+    int32_t mode, out_dtype, b_blocks;
+    uint32_t n_experts;
+    uint64_t m, n, k;
+    const void* a;
+    uint64_t a_stride;
+    const uint8_t* a_scales;
+    uint64_t a_scales_stride;
+    const void* b;
+    uint64_t b_stride, b_matrix_stride;
+    const uint8_t* b_scales;
+    uint64_t b_scales_stride, b_scales_matrix_stride;
+    const int32_t* starts;
+    void* out;
+    uint64_t out_stride, out_matrix_stride;
+    int32_t* status;
+} ciera_fp8_product;
+CIERA_API int ciera_fp8_matmul(const ciera_fp8_product* args, void* stream);
+
+/* Weighted sum of a token's rows: out[t] = sum over j of weights[t, j] * rows[row_of_slot[t, j]], in fp32, rounded once;
+ * weights NULL: 1.  Entries of row_of_slot outside 0 .. n_rows - 1 are passed over (a token without any gets zeros).
+ *   rows  device, n_rows rows of `cols` values of `dtype`;  out  device, n_tokens rows, same type
+ * Limits: top_k 1 .. 32, cols 1 .. 2^31 - 256, n_tokens * top_k and n_rows up to 2^31 - 256. */
+CIERA_API int ciera_expert_combine(int dtype, const void* rows_dev, uint64_t n_rows, uint64_t rows_stride,
+                                   const int32_t* row_of_slot_dev, const float* weights_dev, uint64_t n_tokens,
+                                   uint32_t top_k, uint64_t cols, void* out_dev, uint64_t out_stride, void* stream);
+/* Its gradients from that of out: dweights[t, j] = sum of dout[t] * rows[row] in fp32 (0 for entries passed over), and,
+ * if drows is given, drows[row] = weights[t, j] * dout[t] (rows that no entry names are left as they were; entries name
+ * different rows). */
+CIERA_API int ciera_expert_combine_backward(int dtype, const void* dout_dev, uint64_t dout_stride, const void* rows_dev,
+                                            uint64_t n_rows, uint64_t rows_stride, const int32_t* row_of_slot_dev,
+                                            const float* weights_dev, uint64_t n_tokens, uint32_t top_k, uint64_t cols,
+                                            float* dweights_dev, void* drows_dev, uint64_t drows_stride, void* stream);
+
 /* ---- diagnostics ---------------------------------------------------------------------------- */
 
 /* Self-test of the device-side failure path (no counterpart in the paper: Algorithm 1 has no failure

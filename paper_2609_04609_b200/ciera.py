@@ -44,6 +44,42 @@ _u64, _u32, _i32, _vp, _sz, _dbl = (ctypes.c_uint64, ctypes.c_uint32, ctypes.c_i
                                     ctypes.c_size_t, ctypes.c_double)
 
 
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+FP8_BLOCK = 128
+SOURCE_ROWS, SOURCE_SWIGLU, SOURCE_SWIGLU_BACKWARD = 0, 1, 2
+PRODUCT_DENSE, PRODUCT_ROWS, PRODUCT_CONTRACT = 0, 1, 2
+
+
+class RouteConfig(ctypes.Structure):
+    """How tokens choose experts (see ``ciera_route_config`` in ciera.h); fields by keyword, the rest zero."""
+
+    _fields_ = [("n_experts", _u32), ("top_k", _u32), ("n_groups", _u32), ("top_groups", _u32), ("group_best", _u32),
+                ("score", ctypes.c_int32), ("renormalise", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class _Fp8Rows(ctypes.Structure):
+    _fields_ = [("source", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rows", _u64), ("cols", _u64), ("x_rows", _u64),
+                ("x", _vp), ("x_stride", _u64), ("grad", _vp), ("grad_stride", _u64), ("slot_of_row", _vp),
+                ("row_weights", _vp), ("starts", _vp), ("top_k", _u32), ("n_experts", _u32), ("q", _vp), ("q_stride", _u64),
+                ("scales", _vp), ("scales_stride", _u64), ("qt", _vp), ("qt_stride", _u64), ("scales_t", _vp),
+                ("scales_t_stride", _u64)]
+
+
+class _Fp8Blocks(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("matrices", _u32), ("rows", _u64), ("cols", _u64), ("x", _vp),
+                ("x_stride", _u64), ("x_matrix_stride", _u64), ("q", _vp), ("q_stride", _u64), ("q_matrix_stride", _u64),
+                ("scales", _vp), ("scales_stride", _u64), ("scales_matrix_stride", _u64), ("qt", _vp), ("qt_stride", _u64),
+                ("qt_matrix_stride", _u64), ("scales_t", _vp), ("scales_t_stride", _u64), ("scales_t_matrix_stride", _u64)]
+
+
+class _Fp8Product(ctypes.Structure):
+    _fields_ = [("mode", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("b_blocks", ctypes.c_int32), ("n_experts", _u32),
+                ("m", _u64), ("n", _u64), ("k", _u64), ("a", _vp), ("a_stride", _u64), ("a_scales", _vp),
+                ("a_scales_stride", _u64), ("b", _vp), ("b_stride", _u64), ("b_matrix_stride", _u64), ("b_scales", _vp),
+                ("b_scales_stride", _u64), ("b_scales_matrix_stride", _u64), ("starts", _vp), ("out", _vp),
+                ("out_stride", _u64), ("out_matrix_stride", _u64), ("status", _vp)]
+
+
 class GainIn(ctypes.Structure):
     _fields_ = [
         ("n_values", _u64), ("dtype", ctypes.c_int32), ("block", _u32), ("q", _dbl),
@@ -87,6 +123,17 @@ _SIGS = {
     "ciera_roundtrip_host": ([_vp, _vp, _sz, _vp, _vp, _vp, _vp], _i32),
     "ciera_should_compress": ([ctypes.POINTER(GainIn), ctypes.POINTER(_dbl), ctypes.POINTER(_i32)], _i32),
     "ciera_select_shards": ([ctypes.POINTER(GainIn), _u32, _u64, _i32, _vp, _vp, _vp, _vp, _vp], _i32),
+    "ciera_route": ([ctypes.POINTER(RouteConfig), _i32, _vp, _u64, _u64, _vp, _vp, _vp, _vp], _i32),
+    "ciera_route_backward": ([ctypes.POINTER(RouteConfig), _i32, _vp, _u64, _u64, _vp, _vp, _vp, _u64, _vp], _i32),
+    "ciera_expert_rows_capacity": ([_u64, _u32], _u64),
+    "ciera_expert_layout_workspace_bytes": ([_u64, _u32], _sz),
+    "ciera_expert_layout": ([_vp, _u64, _u32] + [_vp] * 6, _i32),
+    "ciera_fp8_quantize_rows": ([ctypes.POINTER(_Fp8Rows), _vp], _i32),
+    "ciera_fp8_quantize_blocks": ([ctypes.POINTER(_Fp8Blocks), _vp], _i32),
+    "ciera_fp8_matmul": ([ctypes.POINTER(_Fp8Product), _vp], _i32),
+    "ciera_expert_combine": ([_i32, _vp, _u64, _u64, _vp, _vp, _u64, _u32, _u64, _vp, _u64, _vp], _i32),
+    "ciera_expert_combine_backward": ([_i32, _vp, _u64, _vp, _u64, _u64, _vp, _vp, _u64, _u32, _u64, _vp, _vp, _u64, _vp],
+                                      _i32),
     "ciera_selftest_bounded_waits": ([_u32, _vp, _vp, _vp, _vp], _i32),
     "ciera_last_cuda_error": ([], _i32),
     "ciera_kernel_launch_count": ([], _u64),
@@ -324,6 +371,259 @@ def roundtrip_host(plan: Plan, weights_host: torch.Tensor, weights_out_host: tor
     _check("ciera_roundtrip_host",
            _lib.ciera_roundtrip_host(plan.handle, _ptr(weights_host), nbytes, _ptr(weights_out_host),
                                      _ptr(wire_bytes_host), ctypes.addressof(bufs), _stream(stream)))
+
+
+# ------------------------------------------------------------------------------ the MoE layer behind the gather
+
+_CODE_OF = {torch.bfloat16: BF16, torch.float32: FP32, torch.float16: FP16}
+_E4M3 = torch.float8_e4m3fn
+_I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
+
+
+def _refuse(where: str, status: int = ERR_INVALID_ARG):
+    raise CieraError(where, status)
+
+
+def _need(where: str, t, dim: int, *dtypes) -> None:
+    """``t`` is a CUDA tensor of ``dim`` dimensions and one of the types, its values of the last dimension neighbours."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == dim and t.dtype in dtypes):
+        _refuse(where)
+    if dim and t.stride(-1) != 1 and t.shape[-1] > 1:
+        _refuse(where)
+
+
+def _whole(where: str, t, shape, dtype) -> None:
+    """``t`` is a contiguous CUDA tensor of this shape and type."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.shape == shape and t.dtype is dtype and t.is_contiguous()):
+        _refuse(where)
+
+
+def _call(where: str, f, first: torch.Tensor, others, stream, *args) -> None:
+    """Calls the library on the tensors' device, which need not be the current one."""
+    device = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != device:
+            _refuse(where)
+    if device == _current_device():
+        status = f(*args, _stream(stream))
+    else:
+        with torch.cuda.device(device):
+            status = f(*args, _stream(stream))
+    if status != OK:
+        raise CieraError(where, status)
+
+
+def route(config: RouteConfig, logits, bias, experts, weights, stream=None) -> None:
+    """Scores of ``logits`` [T, E], the top k experts of every token (``experts`` int32 [T, k], -1 where none is left) and their
+    ``weights`` (fp32 [T, k]); ``bias`` (fp32 [E] or None) counts for the choice only."""
+    w = "ciera_route"
+    _need(w, logits, 2, *_CODE_OF)
+    t, e = logits.shape
+    if e != config.n_experts:
+        _refuse(w)
+    _whole(w, experts, (t, config.top_k), _I32)
+    _whole(w, weights, (t, config.top_k), _F32)
+    if bias is not None:
+        _whole(w, bias, (e,), _F32)
+    _call(w, _lib.ciera_route, logits, (bias, experts, weights), stream, config, _CODE_OF[logits.dtype], logits.data_ptr(), t,
+          logits.stride(0), _ptr(bias), experts.data_ptr(), weights.data_ptr())
+
+
+def route_backward(config: RouteConfig, logits, experts, dweights, dlogits, stream=None) -> None:
+    """Gradient of the logits (``dlogits``, their shape and type) from that of the weights, for the choice in ``experts``."""
+    w = "ciera_route_backward"
+    _need(w, logits, 2, *_CODE_OF)
+    t, e = logits.shape
+    _need(w, dlogits, 2, logits.dtype)
+    if e != config.n_experts or dlogits.shape != logits.shape:
+        _refuse(w)
+    _whole(w, experts, (t, config.top_k), _I32)
+    _whole(w, dweights, (t, config.top_k), _F32)
+    _call(w, _lib.ciera_route_backward, logits, (experts, dweights, dlogits), stream, config, _CODE_OF[logits.dtype],
+          logits.data_ptr(), t, logits.stride(0), experts.data_ptr(), dweights.data_ptr(), dlogits.data_ptr(), dlogits.stride(0))
+
+
+def expert_rows_capacity(n_slots: int, n_experts: int) -> int:
+    """Rows that the experts' segments can take at most."""
+    return int(_lib.ciera_expert_rows_capacity(n_slots, n_experts))
+
+
+def expert_layout_workspace_bytes(n_slots: int, n_experts: int) -> int:
+    return int(_lib.ciera_expert_layout_workspace_bytes(n_slots, n_experts))
+
+
+def expert_layout(experts, n_experts: int, starts, counts, row_of_slot, slot_of_row, workspace, stream=None) -> None:
+    """Slots (``experts``, int32, any shape) in the order of the experts, segments of a multiple of 128 rows: ``starts`` int32
+    [E + 1], ``counts`` int32 [E], ``row_of_slot`` int32 of the shape of ``experts``, ``slot_of_row`` int32
+    [expert_rows_capacity], ``workspace`` uint8 [expert_layout_workspace_bytes]."""
+    w = "ciera_expert_layout"
+    if not isinstance(experts, torch.Tensor):
+        _refuse(w)
+    n = experts.numel()
+    _whole(w, experts, experts.shape, _I32)
+    _whole(w, starts, (n_experts + 1,), _I32)
+    _whole(w, counts, (n_experts,), _I32)
+    _whole(w, row_of_slot, experts.shape, _I32)
+    _need(w, slot_of_row, 1, _I32)
+    _need(w, workspace, 1, _U8)
+    if slot_of_row.numel() < expert_rows_capacity(n, n_experts) or \
+            workspace.numel() < expert_layout_workspace_bytes(n, n_experts):
+        _refuse(w, ERR_CAPACITY)
+    _call(w, _lib.ciera_expert_layout, experts, (starts, counts, row_of_slot, slot_of_row, workspace), stream,
+          experts.data_ptr(), n, n_experts, starts.data_ptr(), counts.data_ptr(), row_of_slot.data_ptr(),
+          slot_of_row.data_ptr(), workspace.data_ptr())
+
+
+def _scale_rows(where: str, s, cols: int, rows: int) -> None:
+    _need(where, s, 2, _U8)
+    if s.shape[0] != -(-cols // FP8_BLOCK) or s.shape[1] < rows:
+        _refuse(where)
+
+
+def fp8_quantize_rows(x, q, scales, qt=None, scales_t=None, *, kind: int = SOURCE_ROWS, grad=None, slot_of_row=None,
+                      top_k: int = 1, row_weights=None, starts=None, stream=None) -> None:
+    """Rows formed from ``x`` and rounded to e4m3: ``q`` [rows, cols] with ``scales`` uint8 [ceil(cols / 128), >= rows], and, if
+    given, the transposed ``qt`` [cols, rows] with ``scales_t`` uint8 [ceil(rows / 128), >= cols] (see ``ciera_fp8_rows``)."""
+    w = "ciera_fp8_quantize_rows"
+    _need(w, x, 2, *_CODE_OF)
+    _need(w, q, 2, _E4M3)
+    rows, cols = q.shape
+    _scale_rows(w, scales, cols, rows)
+    if x.shape[1] != (2 * cols if kind == SOURCE_SWIGLU else cols):
+        _refuse(w)
+    if (qt is None) != (scales_t is None):
+        _refuse(w)
+    if qt is not None:
+        _need(w, qt, 2, _E4M3)
+        _scale_rows(w, scales_t, rows, cols)
+        if qt.shape != (cols, rows):
+            _refuse(w)
+    if (grad is not None) != (kind == SOURCE_SWIGLU_BACKWARD):
+        _refuse(w)
+    if grad is not None:
+        _need(w, grad, 2, x.dtype)
+        if grad.shape != (x.shape[0], cols // 2):
+            _refuse(w)
+    if slot_of_row is not None:
+        _need(w, slot_of_row, 1, _I32)
+        if slot_of_row.numel() < rows:
+            _refuse(w)
+    if row_weights is not None:
+        _whole(w, row_weights, (x.shape[0], top_k), _F32)
+    if starts is not None:
+        _whole(w, starts, starts.shape, _I32)
+    args = _Fp8Rows(kind, _CODE_OF[x.dtype], rows, cols, x.shape[0], x.data_ptr(), x.stride(0), _ptr(grad),
+                    0 if grad is None else grad.stride(0), _ptr(slot_of_row), _ptr(row_weights), _ptr(starts), top_k,
+                    0 if starts is None else starts.numel() - 1, q.data_ptr(), q.stride(0), scales.data_ptr(),
+                    scales.stride(0), _ptr(qt), 0 if qt is None else qt.stride(0), _ptr(scales_t),
+                    0 if scales_t is None else scales_t.stride(0))
+    _call(w, _lib.ciera_fp8_quantize_rows, x, (q, scales, qt, scales_t, grad, slot_of_row, row_weights, starts), stream, args)
+
+
+def fp8_quantize_blocks(x, q, scales, qt=None, scales_t=None, stream=None) -> None:
+    """Matrices ``x`` [matrices, rows, cols] rounded to e4m3 with one scale for each 128 x 128 block: ``q`` of that shape with
+    ``scales`` uint8 [matrices, ceil(rows / 128), ceil(cols / 128)], and, if given, the transposed ``qt`` and ``scales_t``."""
+    w = "ciera_fp8_quantize_blocks"
+    _need(w, x, 3, *_CODE_OF)
+    _need(w, q, 3, _E4M3)
+    _need(w, scales, 3, _U8)
+    m, r, c = x.shape
+    rb, cb = -(-r // FP8_BLOCK), -(-c // FP8_BLOCK)
+    if q.shape != x.shape or scales.shape != (m, rb, cb) or (qt is None) != (scales_t is None):
+        _refuse(w)
+    t = ()
+    if qt is not None:
+        _need(w, qt, 3, _E4M3)
+        _need(w, scales_t, 3, _U8)
+        if qt.shape != (m, c, r) or scales_t.shape != (m, cb, rb):
+            _refuse(w)
+        t = (qt.data_ptr(), qt.stride(1), qt.stride(0), scales_t.data_ptr(), scales_t.stride(1), scales_t.stride(0))
+    args = _Fp8Blocks(_CODE_OF[x.dtype], m, r, c, x.data_ptr(), x.stride(1), x.stride(0), q.data_ptr(), q.stride(1),
+                      q.stride(0), scales.data_ptr(), scales.stride(1), scales.stride(0), *t)
+    _call(w, _lib.ciera_fp8_quantize_blocks, x, (q, scales, qt, scales_t), stream, args)
+
+
+def fp8_matmul(a, a_scales, b, b_scales, out, starts=None, contract: bool = False, status=None, stream=None) -> None:
+    """``out`` = ``a`` times ``b`` transposed, of operands as the two calls above make them (see ``ciera_fp8_product``).
+
+    ``starts`` None: a [m, k], b [n, k] with a scale for each row and 128 columns, or b [1, n, k] with one for each block.
+    ``starts`` int32 [E + 1]: rows of ``a`` and ``out`` [rows, n] by segments, each with its own matrix of b [E, n, k]; with
+    ``contract`` a [m, rows], b [n, rows], out [E, m, n], each from the columns of its own segment."""
+    w = "ciera_fp8_matmul"
+    _need(w, a, 2, _E4M3)
+    m, k = a.shape
+    _scale_rows(w, a_scales, k, m)
+    blocks = isinstance(b, torch.Tensor) and b.dim() == 3
+    _need(w, b, 3 if blocks else 2, _E4M3)
+    n, experts = b.shape[-2], 0
+    if b.shape[-1] != k:
+        _refuse(w)
+    if starts is not None:
+        _whole(w, starts, starts.shape, _I32)
+        experts = starts.numel() - 1
+    mode = PRODUCT_DENSE if starts is None else PRODUCT_CONTRACT if contract else PRODUCT_ROWS
+    if (contract and (starts is None or blocks)) or (mode == PRODUCT_ROWS and not blocks):
+        _refuse(w)
+    if blocks:
+        _need(w, b_scales, 3, _U8)
+        if b.shape[0] != (experts if mode == PRODUCT_ROWS else 1) or \
+                b_scales.shape != (b.shape[0], -(-n // FP8_BLOCK), -(-k // FP8_BLOCK)):
+            _refuse(w)
+        bs = (b.stride(1), b.stride(0), b_scales.data_ptr(), b_scales.stride(1), b_scales.stride(0))
+    else:
+        _scale_rows(w, b_scales, k, n)
+        bs = (b.stride(0), 0, b_scales.data_ptr(), b_scales.stride(0), 0)
+    _need(w, out, 3 if contract else 2, *_CODE_OF)
+    if out.shape != ((experts, m, n) if contract else (m, n)):
+        _refuse(w)
+    if status is not None:
+        _whole(w, status, (1,), _I32)
+    args = _Fp8Product(mode, _CODE_OF[out.dtype], int(blocks), experts, m, n, k, a.data_ptr(), a.stride(0),
+                       a_scales.data_ptr(), a_scales.stride(0), b.data_ptr(), *bs, _ptr(starts), out.data_ptr(),
+                       out.stride(-2), out.stride(0) if contract else 0, _ptr(status))
+    _call(w, _lib.ciera_fp8_matmul, a, (a_scales, b, b_scales, out, starts, status), stream, args)
+
+
+def expert_combine(rows, row_of_slot, weights, out, stream=None) -> None:
+    """``out`` [T, cols] = the weighted sum of every token's ``rows`` (``row_of_slot`` int32 [T, k], entries outside passed
+    over; ``weights`` fp32 [T, k], or None for 1)."""
+    w = "ciera_expert_combine"
+    _need(w, rows, 2, *_CODE_OF)
+    _need(w, out, 2, rows.dtype)
+    _need(w, row_of_slot, 2, _I32)
+    t, k = row_of_slot.shape
+    _whole(w, row_of_slot, (t, k), _I32)
+    if out.shape != (t, rows.shape[1]):
+        _refuse(w)
+    if weights is not None:
+        _whole(w, weights, (t, k), _F32)
+    _call(w, _lib.ciera_expert_combine, out, (rows, row_of_slot, weights), stream, _CODE_OF[rows.dtype], rows.data_ptr(),
+          rows.shape[0], rows.stride(0), row_of_slot.data_ptr(), _ptr(weights), t, k, rows.shape[1], out.data_ptr(),
+          out.stride(0))
+
+
+def expert_combine_backward(dout, rows, row_of_slot, weights, dweights, drows=None, stream=None) -> None:
+    """Gradients of ``expert_combine``: ``dweights`` fp32 [T, k] and, if given, ``drows`` (shape and type of ``rows``; rows that
+    no slot names are left as they were)."""
+    w = "ciera_expert_combine_backward"
+    _need(w, rows, 2, *_CODE_OF)
+    _need(w, dout, 2, rows.dtype)
+    _need(w, row_of_slot, 2, _I32)
+    t, k = row_of_slot.shape
+    _whole(w, row_of_slot, (t, k), _I32)
+    _whole(w, dweights, (t, k), _F32)
+    if dout.shape != (t, rows.shape[1]):
+        _refuse(w)
+    if weights is not None:
+        _whole(w, weights, (t, k), _F32)
+    if drows is not None:
+        _need(w, drows, 2, rows.dtype)
+        if drows.shape != rows.shape:
+            _refuse(w)
+    _call(w, _lib.ciera_expert_combine_backward, dout, (rows, row_of_slot, weights, dweights, drows), stream,
+          _CODE_OF[rows.dtype], dout.data_ptr(), dout.stride(0), rows.data_ptr(), rows.shape[0], rows.stride(0),
+          row_of_slot.data_ptr(), _ptr(weights), t, k, rows.shape[1], dweights.data_ptr(), _ptr(drows),
+          0 if drows is None else drows.stride(0))
 
 
 # ------------------------------------------------------------------------------ gain rule (host)
