@@ -4,15 +4,21 @@
 // (kind::mxf8f6f4), so a block's scale is handed to them four times over and the sum over all blocks stays in tensor memory in
 // fp32: no result passes through registers before the last block.
 //
-// One persistent block of threads per SM takes tiles of 128 rows x BN columns:
+// Persistent pairs of blocks of threads (a cluster on two SMs) take tiles of 256 columns x 256 (or 128) rows of out.  b's rows
+// are the tensor cores' first operand, 128 to a block, a's rows the second, half of them to a block: a block then moves 32 KB
+// through its shared memory for 128 values of the contraction, where one of its own would move 48 KB and be bound by that
+// (measured: 8192^3 at 2180 TFLOP/s with one block on 128 x 256).  b's rows in front, since segments of a's end at
+// any multiple of 128: a tile's second half is left out where its segment has no rows for it, in both blocks.
 //   warp 0      copies tiles of a and b (128 values of the contraction) into a ring of stages by tensor maps
-//   warp 1      copies a stage's scales into tensor memory and starts its four products
-//   warps 2, 3  read the scale bytes, a stage each in turn, and lay them out as the tensor cores want them: row r's byte four
-//               times over in word r / 32 of line r % 32
-//   warps 4-7   read finished sums, round them and write them, 128 bytes of a row at a time through shared memory
-// Two sums are in flight, so a tile's products run while the one before is written.  Tensor memory has 512 columns: with
-// BN = 256 the two sums share 64 columns, which are the first that are read (the next tile's products wait for them alone),
-// and 64 columns hold the scales, a slot for each stage.
+//   warp 1      of the first block: starts a stage's four products; before every fourth stage of a tile it copies the scales
+//               of four into tensor memory
+//   warps 2, 3  read the scale bytes of four stages at a time, each in turn, and lay them out as the tensor cores want them:
+//               row r's four bytes in word r / 32 of line r % 32.  (A stage at a time, with its byte four times over, cost a
+//               third of the time of the whole: 8192^3 took 606 us, 399 without any scales.)
+//   warps 4-7   read finished sums (a lane is a column of out), turn them in shared memory and write them row by row
+// Two sums are in flight, so a tile's products run while the one before is written.  Tensor memory has 512 columns: the two sums
+// share 64 of them, which are the first that are read (the next tile's products wait for them alone), and 64 hold the scales of
+// four groups of stages.
 #include <cuda.h>
 
 #include <type_traits>
@@ -23,9 +29,12 @@
 namespace ciera {
 
 constexpr int kProductThreads = 256;
-constexpr int kStages = 4;
-constexpr uint32_t kTileM = 128;
+constexpr int kStages = 6;
+constexpr uint32_t kTileN = 256;  // columns of a pair's tile
+constexpr int kGroup = 4;   // stages whose scales go together: a byte each in a word
+constexpr int kGroups = 4;  // such groups in shared and in tensor memory
 constexpr uint32_t kMaxSegments = 1024;
+constexpr uint32_t kShared = 64, kSecondSum = 256 - kShared, kScalesAt = kSecondSum + 256;  // columns of tensor memory
 
 struct ProductArgs {
     uint64_t a_scales_stride, b_scales_stride, b_scales_matrix_stride, out_stride, out_matrix_stride;
@@ -36,62 +45,65 @@ struct ProductArgs {
     uint32_t m, n, k, n_experts;
     int32_t a_words, b_words;  // scale bytes of rows may be read four at a time
     int32_t b_blocks;
-    int32_t wide_out;  // rows of out start at multiples of 16 bytes
+    int32_t wide_out;     // rows of out start at multiples of 16 bytes
+    uint32_t tile_m;      // rows of a tile: 256 or 128
 };
 
-template <int BN>
 struct alignas(1024) ProductSmem {
-    uint8_t a[kStages][kTileM * 128];
-    uint8_t b[kStages][BN * 128];
-    uint4 a_scales[kStages][32];
-    uint4 b_scales[kStages][BN / 128][32];
-    uint4 out[4][32 * 8];  // 32 rows of 128 bytes of each writing warp
-    uint64_t full[kStages], empty[kStages], sums_full[2], sums_free[2], done;
+    uint8_t b[kStages][128 * 128];
+    uint8_t a[kStages][128 * 128];
+    uint32_t b_scales[kGroups][128];
+    uint32_t a_scales[kGroups][2][128];
+    uint4 out[4][256];  // 32 rows of up to 128 bytes of each writing warp
+    uint64_t full[kStages], empty[kStages], scales_full[kGroups], scales_empty[kGroups], sums_full[2], sums_free[2], done;
     uint32_t tmem;
     int abort;
     int32_t starts[kMaxSegments + 1];
+    uint32_t first_tile[kMaxSegments + 1];  // rows' tiles before each segment
 };
 
-// Where a sum and the scales of a stage are in tensor memory.
-template <int BN>
-__device__ __forceinline__ uint32_t sum_column(uint32_t which) { return which * (BN == 256 ? 192 : 128); }
-template <int BN>
-__device__ __forceinline__ uint32_t scales_column(uint32_t stage) { return (BN == 256 ? 448 : 256) + 16 * stage; }
+static_assert(sizeof(ProductSmem) + 1024 <= 227 * 1024, "more than a block may have");
 
-// The tiles of a block of threads, in order, and the blocks of the contraction in each.
-template <int MODE, int BN>
+// The tiles of a pair, in order, and the blocks of the contraction in each.
+template <int MODE>
 struct Walk {
     const ProductArgs& p;
-    const int32_t* starts;
+    const ProductSmem& sm;
     uint32_t n_tiles, m_tiles, all, at;
     uint32_t e = 0, m0 = 0, n0 = 0, m1 = 0, kb0 = 0, kb1 = 0;
 
-    __device__ Walk(const ProductArgs& p_, const int32_t* starts_) : p(p_), starts(starts_), at(blockIdx.x) {
-        n_tiles = (p.n + BN - 1) / BN;
-        m_tiles = MODE == CIERA_PRODUCT_ROWS ? (uint32_t)starts[p.n_experts] / kTileM : (p.m + kTileM - 1) / kTileM;
+    __device__ Walk(const ProductArgs& p_, const ProductSmem& sm_) : p(p_), sm(sm_), at(blockIdx.x >> 1) {
+        n_tiles = (p.n + kTileN - 1) / kTileN;
+        m_tiles = MODE == CIERA_PRODUCT_ROWS ? sm.first_tile[p.n_experts] : (p.m + p.tile_m - 1) / p.tile_m;
         all = m_tiles * n_tiles * (MODE == CIERA_PRODUCT_CONTRACT ? p.n_experts : 1u);
     }
     __device__ bool next() {  // false behind the last tile
         if (at >= all) return false;
         const uint32_t row = at / n_tiles;
-        n0 = (at - row * n_tiles) * BN;
+        n0 = (at - row * n_tiles) * kTileN;
         if (MODE == CIERA_PRODUCT_CONTRACT) {
             e = row / m_tiles;
-            m0 = (row - e * m_tiles) * kTileM;
+            m0 = (row - e * m_tiles) * p.tile_m;
             m1 = p.m;
-            kb0 = (uint32_t)starts[e] / 128;
-            kb1 = (uint32_t)starts[e + 1] / 128;
+            kb0 = (uint32_t)sm.starts[e] / 128;
+            kb1 = (uint32_t)sm.starts[e + 1] / 128;
         } else {
-            m0 = row * kTileM;
-            m1 = p.m;
-            if (MODE == CIERA_PRODUCT_ROWS)
-                while ((uint32_t)starts[e + 1] <= m0) ++e;  // (tiles come in rising order)
+            if (MODE == CIERA_PRODUCT_ROWS) {
+                while (sm.first_tile[e + 1] <= row) ++e;  // (tiles come in rising order)
+                m0 = (uint32_t)sm.starts[e] + (row - sm.first_tile[e]) * p.tile_m;
+                m1 = (uint32_t)sm.starts[e + 1];
+            } else {
+                m0 = row * p.tile_m;
+                m1 = p.m;
+            }
             kb0 = 0;
             kb1 = (p.k + 127) / 128;
         }
-        at += gridDim.x;
+        at += gridDim.x >> 1;
         return true;
     }
+    // rows of the tile that the products are made for
+    __device__ uint32_t height() const { return m1 - m0 > 128 && p.tile_m == 256 ? 256u : 128u; }
 };
 
 // 128 scale bytes of a block, four rows a lane: rows row0 + 4 * lane ...; rows from `rows` on count as 1
@@ -104,82 +116,91 @@ __device__ __forceinline__ uint32_t row_scales(const uint8_t* line, uint32_t row
         if (r + i < rows) v = (v & ~(255u << (8 * i))) | (uint32_t)__ldg(line + r + i) << (8 * i);
     return v;
 }
-// ... as the tensor cores want them: line `lane` has rows lane, 32 + lane, 64 + lane, 96 + lane
-__device__ __forceinline__ uint4 spread_scales(uint32_t four, int lane) {
-    const uint32_t pick = 0x1111u * (lane & 3);
-    uint4 v;
-    v.x = __byte_perm(__shfl_sync(~0u, four, lane >> 2), 0, pick);
-    v.y = __byte_perm(__shfl_sync(~0u, four, 8 + (lane >> 2)), 0, pick);
-    v.z = __byte_perm(__shfl_sync(~0u, four, 16 + (lane >> 2)), 0, pick);
-    v.w = __byte_perm(__shfl_sync(~0u, four, 24 + (lane >> 2)), 0, pick);
-    return v;
+// Scale bytes of four blocks, four rows a lane in each, to words of a row's four bytes: row r in word r / 32 of line r % 32.
+__device__ __forceinline__ void lay_out_scales(uint32_t* to, const uint32_t (&v)[kGroup], int lane) {
+    const uint32_t lo01 = __byte_perm(v[0], v[1], 0x5140), hi01 = __byte_perm(v[0], v[1], 0x7362);
+    const uint32_t lo23 = __byte_perm(v[2], v[3], 0x5140), hi23 = __byte_perm(v[2], v[3], 0x7362);
+    uint32_t* w = to + (lane & 7) * 16 + (lane >> 3);
+    w[0] = __byte_perm(lo01, lo23, 0x5410);
+    w[4] = __byte_perm(lo01, lo23, 0x7632);
+    w[8] = __byte_perm(hi01, hi23, 0x5410);
+    w[12] = __byte_perm(hi01, hi23, 0x7632);
 }
 
-// 32 columns of 16-byte units: `units` of them hold the sums of 64 (16-bit types) or 32 columns, rounded
+// Two sums rounded to a 16-bit type, the first in the low half.
 template <int DT>
-__device__ __forceinline__ uint4 pack_unit(const uint32_t* r) {
-    if constexpr (DT == CIERA_FP32) {
-        return make_uint4(r[0], r[1], r[2], r[3]);
+__device__ __forceinline__ uint32_t pack_two(uint32_t lo, uint32_t hi) {
+    const float x = __uint_as_float(lo), y = __uint_as_float(hi);
+    if constexpr (DT == CIERA_BF16) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+        return *reinterpret_cast<const uint32_t*>(&h);
     } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float lo = __uint_as_float(r[2 * i]), hi = __uint_as_float(r[2 * i + 1]);
-            if constexpr (DT == CIERA_BF16) {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-                w[i] = *reinterpret_cast<const uint32_t*>(&h);
-            } else {
-                const __half2 h = __floats2half2_rn(lo, hi);
-                w[i] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
+        const __half2 h = __floats2half2_rn(x, y);
+        return *reinterpret_cast<const uint32_t*>(&h);
     }
 }
 
-// Writes 128 bytes of each of the warp's 32 rows: `unit(u)` gives the lane's row's unit u.  `stage`: 4 KB of the warp's own.
-template <int DT, class F>
-__device__ __forceinline__ void write_rows(F&& unit, uint4* stage, value_t<DT>* out, uint64_t stride, uint32_t rows_left, uint32_t col,
-                                           uint32_t n, bool wide, int lane) {
-    constexpr uint32_t V = 16 / sizeof(value_t<DT>);
+// Writes 32 columns x 32 rows of out of which the lane has column `lane` in r: through the warp's own shared memory, then 16
+// bytes a lane, neighbouring columns in neighbouring lanes.
+template <int DT>
+__device__ __forceinline__ void write_part(const uint32_t (&r)[32], uint4* stage, value_t<DT>* out, uint64_t stride, uint32_t row,
+                                           uint32_t rows, uint32_t col, uint32_t cols, bool wide, int lane) {
+    if (row >= rows) return;
+    constexpr uint32_t V = 16 / sizeof(value_t<DT>), U = 32 / V;  // columns in 16 bytes, such units in a row
+    uint32_t* words = reinterpret_cast<uint32_t*>(stage);
+    __syncwarp();
+    if constexpr (DT == CIERA_FP32) {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) words[c * 32 + lane] = r[c];
+    } else {
+        // two columns to a word: an even lane puts those of row c together, its neighbour those of row c + 1
+        const bool odd = lane & 1;
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) {
+            const uint32_t other = __shfl_xor_sync(~0u, odd ? r[c] : r[c + 1], 1);
+            words[(c + odd) * 16 + (lane >> 1)] = odd ? pack_two<DT>(other, r[c + 1]) : pack_two<DT>(r[c], other);
+        }
+    }
     __syncwarp();
 #pragma unroll
-    for (int u = 0; u < 8; ++u) stage[lane * 8 + (u ^ (lane & 7))] = unit(u);
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t r = 4 * i + (lane >> 3), u = lane & 7, c = col + u * V;
-        if (r >= rows_left || c >= n) continue;
-        const uint4 v = stage[r * 8 + (u ^ (r & 7))];
-        value_t<DT>* to = out + r * stride + c;
-        if (wide && c + V <= n) {
+    for (int i = 0; i < (int)U; ++i) {
+        const uint32_t at = i * 32 + lane, m = row + at / U, n = col + at % U * V;
+        if (m >= rows || n >= cols) continue;
+        const uint4 v = stage[at];
+        value_t<DT>* to = out + m * stride + n;
+        if (wide && n + V <= cols) {
             *reinterpret_cast<uint4*>(to) = v;
         } else {
             const Pack<value_t<DT>, (int)V> w = *reinterpret_cast<const Pack<value_t<DT>, (int)V>*>(&v);
 #pragma unroll
             for (uint32_t q = 0; q < V; ++q)
-                if (c + q < n) to[q] = w.v[q];
+                if (n + q < cols) to[q] = w.v[q];
         }
     }
 }
 
-template <int MODE, int DT, int BN>
+template <int MODE, int DT>
 __global__ void __launch_bounds__(kProductThreads, 1)
     product_kernel(const ProductArgs p, const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                    value_t<DT>* __restrict__ out) {
     extern __shared__ uint8_t product_smem[];
-    ProductSmem<BN>& sm = *reinterpret_cast<ProductSmem<BN>*>(product_smem + (-smem_u32(product_smem) & 1023u));
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    ProductSmem& sm = *reinterpret_cast<ProductSmem*>(product_smem + (-smem_u32(product_smem) & 1023u));
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(~0u, (int)(threadIdx.x >> 5), 0);
+    const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
         prefetch_map(&a_map);
         prefetch_map(&b_map);
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&sm.full[s], 2);  // the copies' thread and the scales' warp
+            mbar_init(&sm.full[s], 1);
             mbar_init(&sm.empty[s], 1);
+        }
+        for (int g = 0; g < kGroups; ++g) {
+            mbar_init(&sm.scales_full[g], 2);  // (the first block's) a warp of each block
+            mbar_init(&sm.scales_empty[g], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sm.sums_full[i], 1);
-            mbar_init(&sm.sums_free[i], 4);
+            mbar_init(&sm.sums_free[i], 8);  // (the first block's) both blocks' writing warps
         }
         mbar_init(&sm.done, 1);
         sm.abort = 0;
@@ -200,132 +221,175 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         }
     }
     bad = __syncthreads_or(bad);
+    if (MODE == CIERA_PRODUCT_ROWS && !bad) {
+        if (warp == 0) {
+            uint32_t run = 0;
+            for (uint32_t e0 = 0; e0 < p.n_experts; e0 += 32) {
+                const uint32_t e = e0 + lane;
+                const uint32_t v = e < p.n_experts ? ((uint32_t)(sm.starts[e + 1] - sm.starts[e]) + p.tile_m - 1) / p.tile_m : 0;
+                uint32_t s = v;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const uint32_t o = __shfl_up_sync(~0u, s, d);
+                    if (lane >= d) s += o;
+                }
+                if (e < p.n_experts) sm.first_tile[e] = run + s - v;
+                run += __shfl_sync(~0u, s, 31);
+            }
+            if (lane == 0) sm.first_tile[p.n_experts] = run;
+        }
+    }
+    tensor_fence_before();
+    cluster_sync();  // barriers, tables and tensor memory of both blocks are there
     tensor_fence_after();
     const uint32_t tmem = sm.tmem;
-    if (bad) {
-        if (p.status && threadIdx.x == 0) atomicCAS(p.status, 0, (int32_t)CIERA_ERR_CORRUPT);
+    if (bad) {  // (in both blocks: they read the same table)
+        if (p.status && threadIdx.x == 0 && rank == 0) atomicCAS(p.status, 0, (int32_t)CIERA_ERR_CORRUPT);
         if (warp == 1) tmem_free(tmem, 512);
         return;
     }
-    Walk<MODE, BN> w(p, sm.starts);
+    Walk<MODE> w(p, sm);
     volatile int* abort = &sm.abort;
     uint32_t it = 0;  // blocks of the contraction so far
 
     if (warp == 0) {
-        if (lane == 0) {
-            bool ok = true;
-            while (ok && w.next()) {
-                for (uint32_t kb = w.kb0; kb < w.kb1; ++kb, ++it) {
-                    const uint32_t s = it % kStages;
-                    if (!mbar_wait(&sm.empty[s], ((it / kStages) & 1) ^ 1, abort, p.status)) {
-                        ok = false;
-                        break;
-                    }
-                    mbar_arrive_expect_tx(&sm.full[s], kTileM * 128 + BN * 128);
-                    map_load2(sm.a[s], &a_map, (int32_t)(kb * 128), (int32_t)w.m0, &sm.full[s]);
-                    map_load3(sm.b[s], &b_map, (int32_t)(kb * 128), (int32_t)w.n0, MODE == CIERA_PRODUCT_ROWS ? (int32_t)w.e : 0, &sm.full[s]);
+        bool ok = true;
+        uint32_t s = 0, odd = 1;  // stage, and the parity of its last phase
+        while (ok && w.next()) {
+            const uint32_t half = w.height() / 2;
+            const int32_t m0 = (int32_t)(w.m0 + rank * half), n0 = (int32_t)(w.n0 + rank * 128);
+            for (uint32_t kb = w.kb0; kb < w.kb1; ++kb, ++it) {
+                if (!mbar_wait_soon(&sm.empty[s], odd, abort, p.status)) {
+                    ok = false;
+                    break;
                 }
+                if (elect_one()) {
+                    if (rank == 0) mbar_arrive_expect_tx(&sm.full[s], 2 * (128 * 128 + half * 128));
+                    const uint32_t full = in_first_block(&sm.full[s]);
+                    const int32_t k0 = (int32_t)(kb * 128);
+                    map_load3(sm.b[s], &b_map, k0, n0, MODE == CIERA_PRODUCT_ROWS ? (int32_t)w.e : 0, full);
+                    map_load3(sm.a[s], &a_map, k0, m0, 0, full);
+                    if (half == 128) map_load3(sm.a[s] + 64 * 128, &a_map, k0, m0 + 64, 0, full);
+                }
+                __syncwarp();
+                if (++s == kStages) s = 0, odd ^= 1;
             }
-            // given up: the copies in flight end before the block does
-            if (!ok)
-                for (uint32_t i = it < kStages ? 0 : it - kStages; i < it; ++i) {
-                    int none = 0;
-                    mbar_wait(&sm.full[i % kStages], (i / kStages) & 1, &none, p.status, 1024);
-                }
         }
+        // given up: the copies in flight (they report to the first block) end before the cluster does
+        if (!ok && rank == 0 && lane == 0)
+            for (uint32_t i = it < kStages ? 0 : it - kStages; i < it; ++i) {
+                int none = 0;
+                mbar_wait(&sm.full[i % kStages], (i / kStages) & 1, &none, p.status, 1024);
+            }
+        __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t instruction = mx_instruction(kTileM, BN);
-            uint32_t tile = 0;
+        if (rank == 0) {
+            uint32_t tile = 0, g = 0, g_odd = 0, s = 0, odd = 0;
             bool ok = true;
+            const uint64_t db0 = operand_descriptor(sm.b[0]), da0 = operand_descriptor(sm.a[0]);
             while (ok && w.next()) {
                 if (w.kb0 == w.kb1) continue;
-                // BN = 128: the sum before the last one has been read.  BN = 256: the columns shared with the last one have.
-                if (BN == 256 ? tile >= 1 : tile >= 2) {
-                    const uint32_t of = tile - (BN == 256 ? 1 : 2);
-                    if (!mbar_wait(&sm.sums_free[of & 1], (of >> 1) & 1, abort, p.status)) break;
+                if (tile) {  // the columns shared with the sum before have been read
+                    if (!mbar_wait_soon(&sm.sums_free[(tile - 1) & 1], ((tile - 1) >> 1) & 1, abort, p.status)) break;
                     tensor_fence_after();
                 }
-                const uint32_t d = tmem + sum_column<BN>(tile & 1);
-                for (uint32_t kb = w.kb0; kb < w.kb1; ++kb, ++it) {
-                    const uint32_t s = it % kStages;
-                    if (!mbar_wait(&sm.full[s], (it / kStages) & 1, abort, p.status)) {
+                const uint32_t first = mx_instruction(256, w.height(), 0), d = tmem + (tile & 1) * kSecondSum;
+                uint32_t j = 0;
+                for (uint32_t kb = w.kb0; kb < w.kb1; ++kb) {
+                    const uint32_t sc = tmem + kScalesAt + 16 * g;
+                    if (!mbar_wait_soon(&sm.full[s], odd, abort, p.status) ||
+                        (j == 0 && !mbar_wait_soon(&sm.scales_full[g], g_odd, abort, p.status))) {
                         ok = false;
                         break;
                     }
                     tensor_fence_after();
-                    const uint32_t sc = tmem + scales_column<BN>(s);
-                    tmem_copy_scales(sc, scales_descriptor(sm.a_scales[s]));
+                    const bool last = kb + 1 == w.kb1;
+                    if (elect_one()) {
+                        if (j == 0) {
+                            tmem_copy_scales(sc, scales_descriptor(sm.b_scales[g]));
+                            tmem_copy_scales(sc + 8, scales_descriptor(sm.a_scales[g][0]));
+                            tmem_copy_scales(sc + 12, scales_descriptor(sm.a_scales[g][1]));
+                        }
+                        const uint64_t db = db0 + s * (128 * 128 / 16), da = da0 + s * (128 * 128 / 16);
+                        const uint32_t instruction = first + j * mx_byte(1);
 #pragma unroll
-                    for (int h = 0; h < BN / 128; ++h) tmem_copy_scales(sc + 8 + 4 * h, scales_descriptor(sm.b_scales[s][h]));
-                    const uint64_t da = operand_descriptor(sm.a[s]), db = operand_descriptor(sm.b[s]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) tensor_mma_mx(d, da + 2 * j, db + 2 * j, instruction, sc, sc + 8, kb > w.kb0 || j > 0);
-                    tensor_commit(&sm.empty[s]);
+                        for (int i = 0; i < 4; ++i) tensor_mma_mx(d, db + 2 * i, da + 2 * i, instruction, sc, sc + 8, kb > w.kb0 || i > 0);
+                        tensor_commit(&sm.empty[s]);
+                        if (j == kGroup - 1 || last) tensor_commit(&sm.scales_empty[g]);
+                        if (last) tensor_commit(&sm.sums_full[tile & 1]);
+                    }
+                    __syncwarp();
+                    if (++s == kStages) s = 0, odd ^= 1;
+                    if (++j == kGroup || last) {
+                        j = 0;
+                        if (++g == kGroups) g = 0, g_odd ^= 1;
+                    }
                 }
-                if (ok) tensor_commit(&sm.sums_full[tile & 1]);
                 ++tile;
             }
-            // nothing of this thread's is in flight when the tensor memory is given back
-            tensor_commit(&sm.done);
+            // nothing that this warp started is in flight when the tensor memory is given back
+            if (elect_one()) tensor_commit(&sm.done);
             int none = 0;
             mbar_wait(&sm.done, 0, &none, p.status);
         }
         __syncwarp();
     } else if (warp < 4) {
-        // this warp's blocks are every other one; the bytes of the next are fetched before it waits for room for the last
-        uint32_t kb = 0;
-        bool more = true, some = false;
-        auto advance = [&](uint32_t by) {
-            while (by) {
-                if (some && kb + 1 < w.kb1) {
-                    ++kb, --by;
-                    continue;
-                }
-                do {
-                    if (!w.next()) {
-                        more = false;
-                        return;
-                    }
-                } while (w.kb0 == w.kb1);
-                some = true;
+        // this warp's groups are every other one; the bytes of its next are fetched before it lays out the last
+        uint32_t kb = 0, group = 0;
+        bool more = w.next();
+        auto settle = [&]() {  // to the next block of the contraction that there is
+            while (more && kb >= w.kb1) {
+                more = w.next();
                 kb = w.kb0;
-                --by;
             }
         };
-        uint32_t va, vb[BN / 128];
+        auto skip = [&]() {
+            if (more) kb = min(kb + kGroup, w.kb1);
+            settle();
+        };
+        uint32_t vb[kGroup], va0[kGroup], va1[kGroup];
+        bool some = false;
         auto fetch = [&]() {
-            va = row_scales(p.a_scales + kb * p.a_scales_stride, w.m0, w.m1, p.a_words, lane);
+            some = more;
+            if (!more) return;
+            const uint32_t n0 = w.n0 + 128 * rank;
 #pragma unroll
-            for (int h = 0; h < BN / 128; ++h) {
-                const uint32_t n0 = w.n0 + 128 * h;
-                if (p.b_blocks)
-                    vb[h] = n0 < p.n ? __ldg(p.b_scales + (MODE == CIERA_PRODUCT_ROWS ? w.e : 0) * p.b_scales_matrix_stride +
-                                             (uint64_t)(n0 / 128) * p.b_scales_stride + kb) * 0x01010101u
-                                     : 0x7f7f7f7fu;
-                else
-                    vb[h] = row_scales(p.b_scales + kb * p.b_scales_stride, n0, p.n, p.b_words, lane);
+            for (int j = 0; j < kGroup; ++j) {
+                vb[j] = va0[j] = va1[j] = 0x7f7f7f7fu;
+                if (kb + j >= w.kb1) continue;
+                if (!p.b_blocks)
+                    vb[j] = row_scales(p.b_scales + (kb + j) * p.b_scales_stride, n0, p.n, p.b_words, lane);
+                else if (n0 < p.n)
+                    vb[j] = __ldg(p.b_scales + (MODE == CIERA_PRODUCT_ROWS ? w.e : 0) * p.b_scales_matrix_stride +
+                                  (uint64_t)(n0 / 128) * p.b_scales_stride + kb + j) * 0x01010101u;
+                va0[j] = row_scales(p.a_scales + (kb + j) * p.a_scales_stride, w.m0, w.m1, p.a_words, lane);
+                va1[j] = row_scales(p.a_scales + (kb + j) * p.a_scales_stride, w.m0 + 128, w.m1, p.a_words, lane);
             }
+            skip();
         };
-        it = warp - 2;
-        advance(1 + it);
-        if (more) fetch();
-        while (more) {
-            const uint32_t s = it % kStages, turn = it / kStages;
-            const uint4 sa = spread_scales(va, lane);
-            uint4 sb[BN / 128];
+        kb = w.kb0;
+        settle();
+        if (warp == 3) {
+            skip();
+            group = 1;
+        }
+        fetch();
+        skip();
+        while (some) {
+            uint32_t b_now[kGroup], a0_now[kGroup], a1_now[kGroup];
 #pragma unroll
-            for (int h = 0; h < BN / 128; ++h) sb[h] = p.b_blocks ? make_uint4(vb[h], vb[h], vb[h], vb[h]) : spread_scales(vb[h], lane);
-            it += 2;
-            advance(2);
-            if (more) fetch();
-            if (!mbar_wait(&sm.empty[s], (turn & 1) ^ 1, abort, p.status)) break;
-            sm.a_scales[s][lane] = sa;
-#pragma unroll
-            for (int h = 0; h < BN / 128; ++h) sm.b_scales[s][h][lane] = sb[h];
+            for (int j = 0; j < kGroup; ++j) b_now[j] = vb[j], a0_now[j] = va0[j], a1_now[j] = va1[j];
+            fetch();
+            skip();
+            const uint32_t g = group % kGroups;
+            if (!mbar_wait_soon(&sm.scales_empty[g], ((group / kGroups) & 1) ^ 1, abort, p.status)) break;
+            lay_out_scales(sm.b_scales[g], b_now, lane);
+            lay_out_scales(sm.a_scales[g][0], a0_now, lane);
+            lay_out_scales(sm.a_scales[g][1], a1_now, lane);
             fence_async_shared();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.full[s]);
+            if (lane == 0) mbar_arrive_cluster(in_first_block(&sm.scales_full[g]));
+            group += 2;
         }
         __syncwarp();
     } else {
@@ -333,48 +397,45 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         uint4* stage = sm.out[quarter];
         uint32_t tile = 0;
         while (w.next()) {
-            const uint32_t m = w.m0 + quarter * 32;
-            const uint32_t rows_left = m < w.m1 ? w.m1 - m : 0;
-            value_t<DT>* o = out + (MODE == CIERA_PRODUCT_CONTRACT ? w.e * p.out_matrix_stride : 0) + m * p.out_stride;
+            const uint32_t n = w.n0 + rank * 128 + quarter * 32;
+            value_t<DT>* o = out + (MODE == CIERA_PRODUCT_CONTRACT ? w.e * p.out_matrix_stride : 0);
+            auto write = [&](const uint32_t(&r)[32], uint32_t part) {
+                write_part<DT>(r, stage, o, p.out_stride, w.m0 + 32 * part, w.m1, n, p.n, p.wide_out, lane);
+            };
+            const uint32_t parts = w.height() / 32;
             if (w.kb0 == w.kb1) {  // nothing to add up
-                for (uint32_t c = 0; c < BN; c += 128 / sizeof(value_t<DT>))
-                    write_rows<DT>([&](int) { return make_uint4(0, 0, 0, 0); }, stage, o, p.out_stride, rows_left, w.n0 + c, p.n, p.wide_out, lane);
+                const uint32_t zero[32] = {};
+                for (uint32_t i = 0; i < parts; ++i) write(zero, i);
                 continue;
             }
             const uint32_t which = tile & 1;
-            if (!mbar_wait(&sm.sums_full[which], (tile >> 1) & 1, abort, p.status, kMaxBarrierPolls + (w.kb1 - w.kb0))) break;
+            if (!mbar_wait_soon(&sm.sums_full[which], (tile >> 1) & 1, abort, p.status, kMaxBarrierPolls + (w.kb1 - w.kb0))) break;
             __syncwarp();
             tensor_fence_after();
-            const uint32_t from = tmem + ((uint32_t)quarter << 21) + sum_column<BN>(which);
-            constexpr int kParts = BN / 64;
-            for (int i = 0; i < kParts; ++i) {
-                // the columns shared with the other sum first
-                const uint32_t c = BN == 256 && which == 0 ? ((i + 3) & 3) * 64 : i * 64;
-                uint32_t r[2][32];
-                tmem_load32(from + c, r[0]);
-                tmem_load32(from + c + 32, r[1]);
-                tmem_wait_load();
-                if (BN == 256 ? i == 0 : i == kParts - 1) {
-                    tensor_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sm.sums_free[which]);
-                }
-                if constexpr (DT == CIERA_FP32) {
+            const uint32_t from = tmem + ((uint32_t)quarter << 21) + which * kSecondSum;
+            // the columns shared with the other sum first: the second's first two parts, the first's last two of eight
+            const uint32_t first = which == 0 && parts == 8 ? 6 : 0;
+            uint32_t r[2][32];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        write_rows<DT>([&](int u) { return pack_unit<DT>(r[h] + 4 * u); }, stage, o, p.out_stride, rows_left,
-                                       w.n0 + c + 32 * h, p.n, p.wide_out, lane);
-                } else {
-                    write_rows<DT>([&](int u) { return pack_unit<DT>(r[u >> 2] + 8 * (u & 3)); }, stage, o, p.out_stride, rows_left,
-                                   w.n0 + c, p.n, p.wide_out, lane);
-                }
+            for (int i = 0; i < 2; ++i) tmem_load32(from + 32 * (first + i), r[i]);
+            tmem_wait_load();
+            tensor_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(in_first_block(&sm.sums_free[which]));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) write(r[i], first + i);
+            for (uint32_t i = 2; i < parts; ++i) {
+                const uint32_t part = first ? i - 2 : i;
+                tmem_load32(from + 32 * part, r[0]);
+                tmem_wait_load();
+                write(r[0], part);
             }
             ++tile;
         }
         __syncwarp();
     }
     tensor_fence_before();
-    __syncthreads();
+    cluster_sync();  // neither block's memory is in use by the other
     if (warp == 1) {
         tensor_fence_after();
         tmem_free(tmem, 512);
@@ -404,7 +465,7 @@ static bool operand_map(CUtensorMap* map, const void* p, uint64_t k, uint64_t ro
     if (matrices <= 1) matrix_stride = stride;
     const cuuint64_t dims[3] = {k, rows, matrices}, strides[2] = {stride, matrix_stride};
     const cuuint32_t boxes[3] = {128, box, 1}, steps[3] = {1, 1, 1};
-    return encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, matrices ? 3 : 2, const_cast<void*>(p), dims, strides, boxes, steps,
+    return encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(p), dims, strides, boxes, steps,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -421,13 +482,26 @@ static int sm_count(int* n) {
     return CIERA_OK;
 }
 
-template <int MODE, int DT, int BN>
-static cudaError_t launch_product(const ProductArgs& a, const CUtensorMap& am, const CUtensorMap& bm, void* out, uint32_t grid, cudaStream_t s) {
-    constexpr size_t smem = sizeof(ProductSmem<BN>) + 1024;  // (the ring starts at a multiple of 1024)
-    auto kernel = product_kernel<MODE, DT, BN>;
+template <int MODE, int DT>
+static cudaError_t launch_product(const ProductArgs& a, const CUtensorMap& am, const CUtensorMap& bm, void* out, uint32_t pairs, cudaStream_t s) {
+    constexpr size_t smem = sizeof(ProductSmem) + 1024;  // (the ring starts at a multiple of 1024)
+    auto kernel = product_kernel<MODE, DT>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    return launch_after(kernel, dim3(grid), kProductThreads, smem, s, a, am, bm, (value_t<DT>*)out);
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = 2;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * pairs);
+    cfg.blockDim = dim3(kProductThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a, am, bm, (value_t<DT>*)out);
 }
 
 }  // namespace ciera
@@ -460,31 +534,30 @@ extern "C" int ciera_fp8_matmul(const ciera_fp8_product* p, void* stream) {
     int sms = 0;
     const int rc = sm_count(&sms);
     if (rc) return rc;
-    // tiles of 256 columns read a third less than two of 128; narrower ones where the wide ones would leave SMs without work
-    const uint64_t mt = (p->m + kTileM - 1) / kTileM, groups = contract ? p->n_experts : 1;
-    const uint64_t wide = mt * ((p->n + 255) / 256) * groups, narrow = mt * nb * groups;
-    const bool bn256 = wide >= (uint64_t)sms;
-    if (narrow > 0xffffffffull - 65536) return CIERA_ERR_UNSUPPORTED;
-    const uint64_t tiles = bn256 ? wide : narrow;
-    const uint32_t grid = (uint32_t)(tiles < (uint64_t)sms ? tiles : sms);
+    // tiles of 128 rows where those of 256 would leave SMs without work (every segment has at most one more than its rows fill)
+    const uint64_t groups = contract ? p->n_experts : 1, n_tiles = (p->n + kTileN - 1) / kTileN, pairs = sms / 2;
+    const auto tiles_of = [&](uint64_t h) { return ((p->m + h - 1) / h) * n_tiles * groups; };
+    const uint32_t tile_m = tiles_of(256) >= pairs ? 256 : 128;
+    const uint64_t tiles = tiles_of(tile_m) + (rows && tile_m == 256 ? p->n_experts * n_tiles : 0);
+    if (tiles > 0xffffffffull - 65536) return CIERA_ERR_UNSUPPORTED;
+    const uint32_t grid = (uint32_t)(tiles < pairs ? tiles : pairs);
     const uint64_t v = dtype_bytes(p->out_dtype);
     const bool words_a = aligned_to(p->a_scales, 4) && !(p->a_scales_stride & 3), words_b = aligned_to(p->b_scales, 4) && !(p->b_scales_stride & 3);
     const bool wide_out = aligned_to(p->out, 16) && !(p->out_stride * v & 15) && (!contract || !(p->out_matrix_stride * v & 15));
     const ProductArgs a{p->a_scales_stride, p->b_scales_stride, p->b_scales_matrix_stride, p->out_stride, p->out_matrix_stride,
                         p->a_scales, p->b_scales, p->starts, p->status, (uint32_t)p->m, (uint32_t)p->n, (uint32_t)p->k, p->n_experts,
-                        words_a, words_b, p->b_blocks, wide_out};
+                        words_a, words_b, p->b_blocks, wide_out, tile_m};
     if (!encode_tiled()) return record_cuda_error(cudaErrorNotSupported);
     CUtensorMap am, bm;
-    if (!operand_map(&am, p->a, p->k, p->m, 0, p->a_stride, 0, kTileM) ||
-        !operand_map(&bm, p->b, p->k, p->n, rows ? p->n_experts : 1, p->b_stride, p->b_matrix_stride, bn256 ? 256 : 128))
+    if (!operand_map(&am, p->a, p->k, p->m, 1, p->a_stride, 0, 64) ||
+        !operand_map(&bm, p->b, p->k, p->n, rows ? p->n_experts : 1, p->b_stride, p->b_matrix_stride, 128))
         return record_cuda_error(cudaErrorInvalidValue);
     cudaError_t e = cudaSuccess;
     with_dtype(p->out_dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         auto go = [&](auto mode_c) {
             constexpr int MODE = decltype(mode_c)::value;
-            e = bn256 ? launch_product<MODE, DT, 256>(a, am, bm, p->out, grid, (cudaStream_t)stream)
-                      : launch_product<MODE, DT, 128>(a, am, bm, p->out, grid, (cudaStream_t)stream);
+            e = launch_product<MODE, DT>(a, am, bm, p->out, grid, (cudaStream_t)stream);
         };
         if (rows) go(std::integral_constant<int, CIERA_PRODUCT_ROWS>());
         else if (contract) go(std::integral_constant<int, CIERA_PRODUCT_CONTRACT>());

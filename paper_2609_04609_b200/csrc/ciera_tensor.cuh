@@ -5,20 +5,70 @@
 
 namespace ciera {
 
-// ---- tensor memory: 128 lanes x 512 columns of 32 bits; an address is lane << 16 | column
+// Two blocks of threads on neighbouring SMs (a cluster of 2) work on one product: each holds its own 128 rows of the one
+// operand, half of the other, and its rows' sums; one thread of the first block starts the products of both.
 
-__device__ __forceinline__ void tmem_alloc(uint32_t* where, uint32_t columns) {  // whole warp; blocks until there is room
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(columns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
 }
-__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t columns) {  // the same warp
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// the first block's address of something that lies at `p` in each block
+__device__ __forceinline__ uint32_t in_first_block(const void* p) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(p)));
+    return a;
+}
+// An arrival on a barrier of either block.  What it hands over is tensor memory that has been read (behind a tensor_fence_before)
+// or shared memory that only tensor copies read (behind a fence_async_shared): nothing that a wider release would have to wait
+// for.  (With .release.cluster here and .acquire.cluster in the waits the products of 8192^3 took a third longer.)
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// true in one lane of the warp, the same one every time.  Tensor work and tensor-map copies are started under this, by a warp that
+// otherwise runs as one: under `lane == 0` the compiler does not see that one thread is left and wraps each in a loop (a stage of
+// products then took 700 cycles to start, more than the 512 that the tensor cores need for it).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+// mbar_wait for phases that are mostly over or about to be: without the suspension of its polls at first, which wakes up late
+__device__ __forceinline__ bool mbar_wait_soon(uint64_t* bar, uint32_t parity, volatile int* abort, int32_t* status,
+                                               uint32_t max_polls = kMaxBarrierPolls) {
+    for (int i = 0; i < 256; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(smem_u32(bar)), "r"(parity)
+            : "memory");
+        if (ok) return true;
+    }
+    return mbar_wait(bar, parity, abort, status, max_polls);
+}
+
+// ---- tensor memory: 128 lanes x 512 columns of 32 bits in each block; an address is lane << 16 | column
+
+__device__ __forceinline__ void tmem_alloc(uint32_t* where, uint32_t columns) {  // a whole warp of each block
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t columns) {  // the same warps
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
 }
 __device__ __forceinline__ void tensor_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tensor_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// arrives on `bar` when all the thread's tensor work so far has finished
+// arrives on the barrier at `bar` in both blocks when all the thread's tensor work so far has finished
 __device__ __forceinline__ void tensor_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+                 "h"((uint16_t)3)
+                 : "memory");
 }
 // 32 columns of the warp's 32 lanes: lane i gets its lane's values
 __device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t (&r)[32]) {
@@ -44,20 +94,22 @@ __device__ __forceinline__ uint64_t operand_descriptor(const void* tile) {
 __device__ __forceinline__ uint64_t scales_descriptor(const void* rows) {
     return (uint64_t)((smem_u32(rows) & 0x3ffff) >> 4) | 1ull << 16 | (uint64_t)(128 >> 4) << 32 | 1ull << 46;
 }
-// 32 rows of 128 bits to 4 columns, the same in each quarter of the lanes
+// 32 rows of 128 bits to 4 columns, the same in each quarter of the lanes; in both blocks, each from its own shared memory
 __device__ __forceinline__ void tmem_copy_scales(uint32_t to, uint64_t rows) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(rows) : "memory");
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(rows) : "memory");
 }
 
-// e4m3 operands with a power of two for each row and 32 values of the contraction, fp32 sums
-__host__ __device__ constexpr uint32_t mx_instruction(uint32_t m, uint32_t n) {
-    return (n >> 3) << 17 | 1u << 23 /* scales are powers of two */ | (m >> 4) << 24;
+// e4m3 operands with a power of two for each row and 32 values of the contraction, fp32 sums; the scales are byte `byte` of
+// the words in tensor memory
+__host__ __device__ constexpr uint32_t mx_byte(uint32_t byte) { return byte << 4 | byte << 29; }
+__host__ __device__ constexpr uint32_t mx_instruction(uint32_t m, uint32_t n, uint32_t byte) {
+    return (n >> 3) << 17 | 1u << 23 /* scales are powers of two */ | (m >> 4) << 24 | mx_byte(byte);
 }
 __device__ __forceinline__ void tensor_mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, uint32_t a_scales,
                                               uint32_t b_scales, bool add) {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
         "l"(a), "l"(b), "r"(instruction), "r"(a_scales), "r"(b_scales), "r"((uint32_t)add)
         : "memory");
 }
@@ -67,17 +119,13 @@ __device__ __forceinline__ void tensor_mma_mx(uint32_t d, uint64_t a, uint64_t b
 __device__ __forceinline__ void prefetch_map(const void* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
-__device__ __forceinline__ void map_load2(void* dst, const void* map, int32_t x, int32_t y, uint64_t* bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-                     smem_u32(dst)),
-                 "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
-                 : "memory");
-}
-__device__ __forceinline__ void map_load3(void* dst, const void* map, int32_t x, int32_t y, int32_t z, uint64_t* bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
-                     smem_u32(dst)),
-                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
-                 : "memory");
+// to the block's own shared memory; `bar`: a barrier of either block
+__device__ __forceinline__ void map_load3(void* dst, const void* map, int32_t x, int32_t y, int32_t z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+            smem_u32(dst)),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
 }
 
 }  // namespace ciera
