@@ -15,7 +15,7 @@
 //   warps 2, 3  read the scale bytes of four stages at a time, each in turn, and lay them out as the tensor cores want them:
 //               row r's four bytes in word r / 32 of line r % 32.  (A stage at a time, with its byte four times over, cost a
 //               third of the time of the whole: 8192^3 took 606 us, 399 without any scales.)
-//   warps 4-7   read finished sums (a lane is a column of out), turn them in shared memory and write them row by row
+//   warps 4-7   read finished sums (a lane is a column of out) and write them
 // Two sums are in flight, so a tile's products run while the one before is written.  Tensor memory has 512 columns: the two sums
 // share 64 of them, which are the first that are read (the next tile's products wait for them alone), and 64 hold the scales of
 // four groups of stages.
@@ -45,7 +45,7 @@ struct ProductArgs {
     uint32_t m, n, k, n_experts;
     int32_t a_words, b_words;  // scale bytes of rows may be read four at a time
     int32_t b_blocks;
-    int32_t wide_out;     // rows of out start at multiples of 16 bytes
+    int32_t wide_out;     // 16-bit columns of out may be written two at a time
     uint32_t tile_m;      // rows of a tile: 256 or 128
 };
 
@@ -54,7 +54,6 @@ struct alignas(1024) ProductSmem {
     uint8_t a[kStages][128 * 128];
     uint32_t b_scales[kGroups][128];
     uint32_t a_scales[kGroups][2][128];
-    uint4 out[4][256];  // 32 rows of up to 128 bytes of each writing warp
     uint64_t full[kStages], empty[kStages], scales_full[kGroups], scales_empty[kGroups], sums_full[2], sums_free[2], done;
     uint32_t tmem;
     int abort;
@@ -140,42 +139,38 @@ __device__ __forceinline__ uint32_t pack_two(uint32_t lo, uint32_t hi) {
     }
 }
 
-// Writes 32 columns x 32 rows of out of which the lane has column `lane` in r: through the warp's own shared memory, then 16
-// bytes a lane, neighbouring columns in neighbouring lanes.
+// Writes 32 columns x 32 rows of out of which the lane has column `col` in r: neighbouring columns are in neighbouring lanes, so
+// a row goes out as it is, 16-bit values two at a time: an even lane puts row c's together, its neighbour row c + 1's.
 template <int DT>
-__device__ __forceinline__ void write_part(const uint32_t (&r)[32], uint4* stage, value_t<DT>* out, uint64_t stride, uint32_t row,
-                                           uint32_t rows, uint32_t col, uint32_t cols, bool wide, int lane) {
-    if (row >= rows) return;
-    constexpr uint32_t V = 16 / sizeof(value_t<DT>), U = 32 / V;  // columns in 16 bytes, such units in a row
-    uint32_t* words = reinterpret_cast<uint32_t*>(stage);
-    __syncwarp();
+__device__ __forceinline__ void write_part(const uint32_t (&r)[32], value_t<DT>* out, uint64_t stride, uint32_t row, uint32_t rows,
+                                           uint32_t col, uint32_t cols, bool wide, int lane) {
     if constexpr (DT == CIERA_FP32) {
+        uint32_t* to = reinterpret_cast<uint32_t*>(out + row * stride + col);
+        if (col >= cols) return;
+        if (row + 32 <= rows) {
 #pragma unroll
-        for (int c = 0; c < 32; ++c) words[c * 32 + lane] = r[c];
-    } else {
-        // two columns to a word: an even lane puts those of row c together, its neighbour those of row c + 1
-        const bool odd = lane & 1;
-#pragma unroll
-        for (int c = 0; c < 32; c += 2) {
-            const uint32_t other = __shfl_xor_sync(~0u, odd ? r[c] : r[c + 1], 1);
-            words[(c + odd) * 16 + (lane >> 1)] = odd ? pack_two<DT>(other, r[c + 1]) : pack_two<DT>(r[c], other);
-        }
-    }
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < (int)U; ++i) {
-        const uint32_t at = i * 32 + lane, m = row + at / U, n = col + at % U * V;
-        if (m >= rows || n >= cols) continue;
-        const uint4 v = stage[at];
-        value_t<DT>* to = out + m * stride + n;
-        if (wide && n + V <= cols) {
-            *reinterpret_cast<uint4*>(to) = v;
+            for (int c = 0; c < 32; ++c, to += stride) *to = r[c];
         } else {
-            const Pack<value_t<DT>, (int)V> w = *reinterpret_cast<const Pack<value_t<DT>, (int)V>*>(&v);
 #pragma unroll
-            for (uint32_t q = 0; q < V; ++q)
-                if (n + q < cols) to[q] = w.v[q];
+            for (int c = 0; c < 32; ++c, to += stride)
+                if (row + c < rows) *to = r[c];
         }
+    } else if (wide) {
+        const uint32_t odd = lane & 1;
+        uint32_t* to = reinterpret_cast<uint32_t*>(out + (row + odd) * stride + (col - odd));
+        const bool some = col - odd < cols;  // (cols is even)
+        const bool all = row + 32 <= rows;
+#pragma unroll
+        for (int c = 0; c < 32; c += 2, to += stride) {
+            const uint32_t other = __shfl_xor_sync(~0u, odd ? r[c] : r[c + 1], 1);
+            const uint32_t both = odd ? pack_two<DT>(other, r[c + 1]) : pack_two<DT>(r[c], other);
+            if (some && (all || row + c + odd < rows)) *to = both;
+        }
+    } else {
+        value_t<DT>* to = out + row * stride + col;
+#pragma unroll
+        for (int c = 0; c < 32; ++c, to += stride)
+            if (col < cols && row + c < rows) *to = ValueOf<DT>::put(__uint_as_float(r[c]));
     }
 }
 
@@ -394,13 +389,12 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         __syncwarp();
     } else {
         const int quarter = warp & 3;
-        uint4* stage = sm.out[quarter];
         uint32_t tile = 0;
         while (w.next()) {
             const uint32_t n = w.n0 + rank * 128 + quarter * 32;
             value_t<DT>* o = out + (MODE == CIERA_PRODUCT_CONTRACT ? w.e * p.out_matrix_stride : 0);
             auto write = [&](const uint32_t(&r)[32], uint32_t part) {
-                write_part<DT>(r, stage, o, p.out_stride, w.m0 + 32 * part, w.m1, n, p.n, p.wide_out, lane);
+                write_part<DT>(r, o, p.out_stride, w.m0 + 32 * part, w.m1, n + lane, p.n, p.wide_out, lane);
             };
             const uint32_t parts = w.height() / 32;
             if (w.kb0 == w.kb1) {  // nothing to add up
@@ -541,9 +535,8 @@ extern "C" int ciera_fp8_matmul(const ciera_fp8_product* p, void* stream) {
     const uint64_t tiles = tiles_of(tile_m) + (rows && tile_m == 256 ? p->n_experts * n_tiles : 0);
     if (tiles > 0xffffffffull - 65536) return CIERA_ERR_UNSUPPORTED;
     const uint32_t grid = (uint32_t)(tiles < pairs ? tiles : pairs);
-    const uint64_t v = dtype_bytes(p->out_dtype);
     const bool words_a = aligned_to(p->a_scales, 4) && !(p->a_scales_stride & 3), words_b = aligned_to(p->b_scales, 4) && !(p->b_scales_stride & 3);
-    const bool wide_out = aligned_to(p->out, 16) && !(p->out_stride * v & 15) && (!contract || !(p->out_matrix_stride * v & 15));
+    const bool wide_out = aligned_to(p->out, 4) && !((p->n | p->out_stride | (contract ? p->out_matrix_stride : 0)) & 1);
     const ProductArgs a{p->a_scales_stride, p->b_scales_stride, p->b_scales_matrix_stride, p->out_stride, p->out_matrix_stride,
                         p->a_scales, p->b_scales, p->starts, p->status, (uint32_t)p->m, (uint32_t)p->n, (uint32_t)p->k, p->n_experts,
                         words_a, words_b, p->b_blocks, wide_out, tile_m};
