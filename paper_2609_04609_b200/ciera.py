@@ -378,37 +378,74 @@ def roundtrip_host(plan: Plan, weights_host: torch.Tensor, weights_out_host: tor
 _CODE_OF = {torch.bfloat16: BF16, torch.float32: FP32, torch.float16: FP16}
 _E4M3 = torch.float8_e4m3fn
 _I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
+_Tensor = torch.Tensor
 
 
 def _refuse(where: str, status: int = ERR_INVALID_ARG):
     raise CieraError(where, status)
 
 
-def _need(where: str, t, dim: int, *dtypes) -> None:
-    """``t`` is a CUDA tensor of ``dim`` dimensions and one of the types, its values of the last dimension neighbours."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == dim and t.dtype in dtypes):
-        _refuse(where)
-    if dim and t.stride(-1) != 1 and t.shape[-1] > 1:
-        _refuse(where)
+def _device_of(where: str, t) -> int:
+    """The CUDA device that the call's first tensor lives on; the others have to live there too."""
+    device = t.get_device() if isinstance(t, _Tensor) else -1
+    if device < 0:
+        raise CieraError(where, ERR_INVALID_ARG)
+    return device
 
 
-def _whole(where: str, t, shape, dtype) -> None:
-    """``t`` is a contiguous CUDA tensor of this shape and type."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.shape == shape and t.dtype is dtype and t.is_contiguous()):
-        _refuse(where)
+def _whole(where: str, device: int, t, shape, dtype) -> int:
+    """The address of a contiguous tensor of this shape and type."""
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.shape != shape or t.get_device() != device \
+            or not t.is_contiguous():
+        raise CieraError(where, ERR_INVALID_ARG)
+    return t.data_ptr()
 
 
-def _call(where: str, f, first: torch.Tensor, others, stream, *args) -> None:
-    """Calls the library on the tensors' device, which need not be the current one."""
-    device = first.get_device()
-    for t in others:
-        if t is not None and t.get_device() != device:
-            _refuse(where)
+def _matrix(where: str, device: int, t, shape, dtype):
+    """The address and the stride of the rows of a 2-D tensor of this type and, unless None, shape."""
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.get_device() != device or t.dim() != 2 \
+            or (shape is not None and t.shape != shape):
+        raise CieraError(where, ERR_INVALID_ARG)
+    stride = t.stride()
+    if stride[1] != 1 and t.shape[1] > 1:
+        raise CieraError(where, ERR_INVALID_ARG)
+    return t.data_ptr(), stride[0]
+
+
+def _matrices(where: str, device: int, t, shape, dtype):
+    """The address and the strides of the rows and of the matrices of a 3-D tensor of this type and, unless None, shape."""
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.get_device() != device or t.dim() != 3 \
+            or (shape is not None and t.shape != shape):
+        raise CieraError(where, ERR_INVALID_ARG)
+    stride = t.stride()
+    if stride[2] != 1 and t.shape[2] > 1:
+        raise CieraError(where, ERR_INVALID_ARG)
+    return t.data_ptr(), stride[1], stride[0]
+
+
+def _scale_lines(where: str, device: int, t, cols: int, rows: int):
+    """The same of scale bytes [ceil(cols / 128), at least rows]."""
+    at = _matrix(where, device, t, None, _U8)
+    shape = t.shape
+    if shape[0] != -(-cols // FP8_BLOCK) or shape[1] < rows:
+        raise CieraError(where, ERR_INVALID_ARG)
+    return at
+
+
+def _code(where: str, t) -> int:
+    code = _CODE_OF.get(t.dtype)
+    if code is None:
+        raise CieraError(where, ERR_INVALID_ARG)
+    return code
+
+
+def _enqueue(where: str, device: int, stream, f, *args) -> None:
+    """Calls the library for tensors on ``device``, which need not be the current one."""
     if device == _current_device():
-        status = f(*args, _stream(stream))
+        status = f(*args, (_current_raw_stream(device) if stream is None else stream.cuda_stream) or None)
     else:
         with torch.cuda.device(device):
-            status = f(*args, _stream(stream))
+            status = f(*args, (_current_raw_stream(device) if stream is None else stream.cuda_stream) or None)
     if status != OK:
         raise CieraError(where, status)
 
@@ -417,30 +454,32 @@ def route(config: RouteConfig, logits, bias, experts, weights, stream=None) -> N
     """Scores of ``logits`` [T, E], the top k experts of every token (``experts`` int32 [T, k], -1 where none is left) and their
     ``weights`` (fp32 [T, k]); ``bias`` (fp32 [E] or None) counts for the choice only."""
     w = "ciera_route"
-    _need(w, logits, 2, *_CODE_OF)
+    device = _device_of(w, logits)
+    code = _code(w, logits)
+    at, stride = _matrix(w, device, logits, None, logits.dtype)
     t, e = logits.shape
     if e != config.n_experts:
         _refuse(w)
-    _whole(w, experts, (t, config.top_k), _I32)
-    _whole(w, weights, (t, config.top_k), _F32)
-    if bias is not None:
-        _whole(w, bias, (e,), _F32)
-    _call(w, _lib.ciera_route, logits, (bias, experts, weights), stream, config, _CODE_OF[logits.dtype], logits.data_ptr(), t,
-          logits.stride(0), _ptr(bias), experts.data_ptr(), weights.data_ptr())
+    k = config.top_k
+    _enqueue(w, device, stream, _lib.ciera_route, config, code, at, t, stride,
+             None if bias is None else _whole(w, device, bias, (e,), _F32), _whole(w, device, experts, (t, k), _I32),
+             _whole(w, device, weights, (t, k), _F32))
 
 
 def route_backward(config: RouteConfig, logits, experts, dweights, dlogits, stream=None) -> None:
     """Gradient of the logits (``dlogits``, their shape and type) from that of the weights, for the choice in ``experts``."""
     w = "ciera_route_backward"
-    _need(w, logits, 2, *_CODE_OF)
-    t, e = logits.shape
-    _need(w, dlogits, 2, logits.dtype)
-    if e != config.n_experts or dlogits.shape != logits.shape:
+    device = _device_of(w, logits)
+    code = _code(w, logits)
+    at, stride = _matrix(w, device, logits, None, logits.dtype)
+    shape = logits.shape
+    t, e = shape
+    if e != config.n_experts:
         _refuse(w)
-    _whole(w, experts, (t, config.top_k), _I32)
-    _whole(w, dweights, (t, config.top_k), _F32)
-    _call(w, _lib.ciera_route_backward, logits, (experts, dweights, dlogits), stream, config, _CODE_OF[logits.dtype],
-          logits.data_ptr(), t, logits.stride(0), experts.data_ptr(), dweights.data_ptr(), dlogits.data_ptr(), dlogits.stride(0))
+    k = config.top_k
+    _enqueue(w, device, stream, _lib.ciera_route_backward, config, code, at, t, stride,
+             _whole(w, device, experts, (t, k), _I32), _whole(w, device, dweights, (t, k), _F32),
+             *_matrix(w, device, dlogits, shape, logits.dtype))
 
 
 def expert_rows_capacity(n_slots: int, n_experts: int) -> int:
@@ -457,27 +496,18 @@ def expert_layout(experts, n_experts: int, starts, counts, row_of_slot, slot_of_
     [E + 1], ``counts`` int32 [E], ``row_of_slot`` int32 of the shape of ``experts``, ``slot_of_row`` int32
     [expert_rows_capacity], ``workspace`` uint8 [expert_layout_workspace_bytes]."""
     w = "ciera_expert_layout"
-    if not isinstance(experts, torch.Tensor):
-        _refuse(w)
+    device = _device_of(w, experts)
+    shape = experts.shape
     n = experts.numel()
-    _whole(w, experts, experts.shape, _I32)
-    _whole(w, starts, (n_experts + 1,), _I32)
-    _whole(w, counts, (n_experts,), _I32)
-    _whole(w, row_of_slot, experts.shape, _I32)
-    _need(w, slot_of_row, 1, _I32)
-    _need(w, workspace, 1, _U8)
-    if slot_of_row.numel() < expert_rows_capacity(n, n_experts) or \
-            workspace.numel() < expert_layout_workspace_bytes(n, n_experts):
+    room = slot_of_row.numel() if isinstance(slot_of_row, _Tensor) else -1
+    scratch = workspace.numel() if isinstance(workspace, _Tensor) else -1
+    args = (_whole(w, device, experts, shape, _I32), n, n_experts, _whole(w, device, starts, (n_experts + 1,), _I32),
+            _whole(w, device, counts, (n_experts,), _I32), _whole(w, device, row_of_slot, shape, _I32),
+            _whole(w, device, slot_of_row, (room,), _I32), _whole(w, device, workspace, (scratch,), _U8))
+    if room < _lib.ciera_expert_rows_capacity(n, n_experts) or \
+            scratch < _lib.ciera_expert_layout_workspace_bytes(n, n_experts):
         _refuse(w, ERR_CAPACITY)
-    _call(w, _lib.ciera_expert_layout, experts, (starts, counts, row_of_slot, slot_of_row, workspace), stream,
-          experts.data_ptr(), n, n_experts, starts.data_ptr(), counts.data_ptr(), row_of_slot.data_ptr(),
-          slot_of_row.data_ptr(), workspace.data_ptr())
-
-
-def _scale_rows(where: str, s, cols: int, rows: int) -> None:
-    _need(where, s, 2, _U8)
-    if s.shape[0] != -(-cols // FP8_BLOCK) or s.shape[1] < rows:
-        _refuse(where)
+    _enqueue(w, device, stream, _lib.ciera_expert_layout, *args)
 
 
 def fp8_quantize_rows(x, q, scales, qt=None, scales_t=None, *, kind: int = SOURCE_ROWS, grad=None, slot_of_row=None,
@@ -485,62 +515,55 @@ def fp8_quantize_rows(x, q, scales, qt=None, scales_t=None, *, kind: int = SOURC
     """Rows formed from ``x`` and rounded to e4m3: ``q`` [rows, cols] with ``scales`` uint8 [ceil(cols / 128), >= rows], and, if
     given, the transposed ``qt`` [cols, rows] with ``scales_t`` uint8 [ceil(rows / 128), >= cols] (see ``ciera_fp8_rows``)."""
     w = "ciera_fp8_quantize_rows"
-    _need(w, x, 2, *_CODE_OF)
-    _need(w, q, 2, _E4M3)
+    device = _device_of(w, x)
+    code = _code(w, x)
+    x_at = _matrix(w, device, x, None, x.dtype)
+    x_rows, x_cols = x.shape
+    q_at = _matrix(w, device, q, None, _E4M3)
     rows, cols = q.shape
-    _scale_rows(w, scales, cols, rows)
-    if x.shape[1] != (2 * cols if kind == SOURCE_SWIGLU else cols):
+    if x_cols != (2 * cols if kind == SOURCE_SWIGLU else cols) or (qt is None) != (scales_t is None) or \
+            (grad is None) == (kind == SOURCE_SWIGLU_BACKWARD):
         _refuse(w)
-    if (qt is None) != (scales_t is None):
-        _refuse(w)
+    s_at = _scale_lines(w, device, scales, cols, rows)
+    t_at, st_at, g_at = (None, 0), (None, 0), (None, 0)
     if qt is not None:
-        _need(w, qt, 2, _E4M3)
-        _scale_rows(w, scales_t, rows, cols)
-        if qt.shape != (cols, rows):
-            _refuse(w)
-    if (grad is not None) != (kind == SOURCE_SWIGLU_BACKWARD):
-        _refuse(w)
+        t_at = _matrix(w, device, qt, (cols, rows), _E4M3)
+        st_at = _scale_lines(w, device, scales_t, rows, cols)
     if grad is not None:
-        _need(w, grad, 2, x.dtype)
-        if grad.shape != (x.shape[0], cols // 2):
-            _refuse(w)
+        g_at = _matrix(w, device, grad, (x_rows, cols // 2), x.dtype)
+    slots = weights = begin = None
+    n_experts = 0
     if slot_of_row is not None:
-        _need(w, slot_of_row, 1, _I32)
-        if slot_of_row.numel() < rows:
+        slots = _whole(w, device, slot_of_row, slot_of_row.shape, _I32)
+        if slot_of_row.dim() != 1 or slot_of_row.numel() < rows:
             _refuse(w)
     if row_weights is not None:
-        _whole(w, row_weights, (x.shape[0], top_k), _F32)
+        weights = _whole(w, device, row_weights, (x_rows, top_k), _F32)
     if starts is not None:
-        _whole(w, starts, starts.shape, _I32)
-    args = _Fp8Rows(kind, _CODE_OF[x.dtype], rows, cols, x.shape[0], x.data_ptr(), x.stride(0), _ptr(grad),
-                    0 if grad is None else grad.stride(0), _ptr(slot_of_row), _ptr(row_weights), _ptr(starts), top_k,
-                    0 if starts is None else starts.numel() - 1, q.data_ptr(), q.stride(0), scales.data_ptr(),
-                    scales.stride(0), _ptr(qt), 0 if qt is None else qt.stride(0), _ptr(scales_t),
-                    0 if scales_t is None else scales_t.stride(0))
-    _call(w, _lib.ciera_fp8_quantize_rows, x, (q, scales, qt, scales_t, grad, slot_of_row, row_weights, starts), stream, args)
+        n_experts = starts.numel() - 1
+        begin = _whole(w, device, starts, (n_experts + 1,), _I32)
+    args = _Fp8Rows(kind, code, rows, cols, x_rows, *x_at, *g_at, slots, weights, begin, top_k, max(n_experts, 0), *q_at, *s_at,
+                    *t_at, *st_at)
+    _enqueue(w, device, stream, _lib.ciera_fp8_quantize_rows, args)
 
 
 def fp8_quantize_blocks(x, q, scales, qt=None, scales_t=None, stream=None) -> None:
     """Matrices ``x`` [matrices, rows, cols] rounded to e4m3 with one scale for each 128 x 128 block: ``q`` of that shape with
     ``scales`` uint8 [matrices, ceil(rows / 128), ceil(cols / 128)], and, if given, the transposed ``qt`` and ``scales_t``."""
     w = "ciera_fp8_quantize_blocks"
-    _need(w, x, 3, *_CODE_OF)
-    _need(w, q, 3, _E4M3)
-    _need(w, scales, 3, _U8)
-    m, r, c = x.shape
+    device = _device_of(w, x)
+    code = _code(w, x)
+    x_at = _matrices(w, device, x, None, x.dtype)
+    shape = x.shape
+    m, r, c = shape
     rb, cb = -(-r // FP8_BLOCK), -(-c // FP8_BLOCK)
-    if q.shape != x.shape or scales.shape != (m, rb, cb) or (qt is None) != (scales_t is None):
+    if (qt is None) != (scales_t is None):
         _refuse(w)
-    t = ()
-    if qt is not None:
-        _need(w, qt, 3, _E4M3)
-        _need(w, scales_t, 3, _U8)
-        if qt.shape != (m, c, r) or scales_t.shape != (m, cb, rb):
-            _refuse(w)
-        t = (qt.data_ptr(), qt.stride(1), qt.stride(0), scales_t.data_ptr(), scales_t.stride(1), scales_t.stride(0))
-    args = _Fp8Blocks(_CODE_OF[x.dtype], m, r, c, x.data_ptr(), x.stride(1), x.stride(0), q.data_ptr(), q.stride(1),
-                      q.stride(0), scales.data_ptr(), scales.stride(1), scales.stride(0), *t)
-    _call(w, _lib.ciera_fp8_quantize_blocks, x, (q, scales, qt, scales_t), stream, args)
+    turned = () if qt is None else (*_matrices(w, device, qt, (m, c, r), _E4M3),
+                                    *_matrices(w, device, scales_t, (m, cb, rb), _U8))
+    args = _Fp8Blocks(code, m, r, c, *x_at, *_matrices(w, device, q, shape, _E4M3),
+                      *_matrices(w, device, scales, (m, rb, cb), _U8), *turned)
+    _enqueue(w, device, stream, _lib.ciera_fp8_quantize_blocks, args)
 
 
 def fp8_matmul(a, a_scales, b, b_scales, out, starts=None, contract: bool = False, status=None, stream=None) -> None:
@@ -550,80 +573,76 @@ def fp8_matmul(a, a_scales, b, b_scales, out, starts=None, contract: bool = Fals
     ``starts`` int32 [E + 1]: rows of ``a`` and ``out`` [rows, n] by segments, each with its own matrix of b [E, n, k]; with
     ``contract`` a [m, rows], b [n, rows], out [E, m, n], each from the columns of its own segment."""
     w = "ciera_fp8_matmul"
-    _need(w, a, 2, _E4M3)
+    device = _device_of(w, a)
+    a_at = _matrix(w, device, a, None, _E4M3)
     m, k = a.shape
-    _scale_rows(w, a_scales, k, m)
-    blocks = isinstance(b, torch.Tensor) and b.dim() == 3
-    _need(w, b, 3 if blocks else 2, _E4M3)
-    n, experts = b.shape[-2], 0
-    if b.shape[-1] != k:
-        _refuse(w)
+    begin, experts = None, 0
+    mode = PRODUCT_DENSE
     if starts is not None:
-        _whole(w, starts, starts.shape, _I32)
         experts = starts.numel() - 1
-    mode = PRODUCT_DENSE if starts is None else PRODUCT_CONTRACT if contract else PRODUCT_ROWS
-    if (contract and (starts is None or blocks)) or (mode == PRODUCT_ROWS and not blocks):
+        begin = _whole(w, device, starts, (experts + 1,), _I32)
+        mode = PRODUCT_CONTRACT if contract else PRODUCT_ROWS
+    elif contract:
+        _refuse(w)
+    blocks = isinstance(b, _Tensor) and b.dim() == 3
+    if blocks != (mode == PRODUCT_ROWS) and mode != PRODUCT_DENSE:
         _refuse(w)
     if blocks:
-        _need(w, b_scales, 3, _U8)
-        if b.shape[0] != (experts if mode == PRODUCT_ROWS else 1) or \
-                b_scales.shape != (b.shape[0], -(-n // FP8_BLOCK), -(-k // FP8_BLOCK)):
+        b_at = _matrices(w, device, b, None, _E4M3)
+        matrices, n, bk = b.shape
+        if matrices != (experts if mode == PRODUCT_ROWS else 1):
             _refuse(w)
-        bs = (b.stride(1), b.stride(0), b_scales.data_ptr(), b_scales.stride(1), b_scales.stride(0))
+        bs_at = _matrices(w, device, b_scales, (matrices, -(-n // FP8_BLOCK), -(-k // FP8_BLOCK)), _U8)
     else:
-        _scale_rows(w, b_scales, k, n)
-        bs = (b.stride(0), 0, b_scales.data_ptr(), b_scales.stride(0), 0)
-    _need(w, out, 3 if contract else 2, *_CODE_OF)
-    if out.shape != ((experts, m, n) if contract else (m, n)):
+        b_at = (*_matrix(w, device, b, None, _E4M3), 0)
+        n, bk = b.shape
+        bs_at = (*_scale_lines(w, device, b_scales, k, n), 0)
+    if bk != k:
         _refuse(w)
-    if status is not None:
-        _whole(w, status, (1,), _I32)
-    args = _Fp8Product(mode, _CODE_OF[out.dtype], int(blocks), experts, m, n, k, a.data_ptr(), a.stride(0),
-                       a_scales.data_ptr(), a_scales.stride(0), b.data_ptr(), *bs, _ptr(starts), out.data_ptr(),
-                       out.stride(-2), out.stride(0) if contract else 0, _ptr(status))
-    _call(w, _lib.ciera_fp8_matmul, a, (a_scales, b, b_scales, out, starts, status), stream, args)
+    code = _code(w, out)
+    if contract:
+        o_at = _matrices(w, device, out, (experts, m, n), out.dtype)
+    else:
+        o_at = (*_matrix(w, device, out, (m, n), out.dtype), 0)
+    args = _Fp8Product(mode, code, blocks, max(experts, 0), m, n, k, *a_at, *_scale_lines(w, device, a_scales, k, m), *b_at,
+                       *bs_at, begin, *o_at, None if status is None else _whole(w, device, status, (1,), _I32))
+    _enqueue(w, device, stream, _lib.ciera_fp8_matmul, args)
 
 
 def expert_combine(rows, row_of_slot, weights, out, stream=None) -> None:
     """``out`` [T, cols] = the weighted sum of every token's ``rows`` (``row_of_slot`` int32 [T, k], entries outside passed
     over; ``weights`` fp32 [T, k], or None for 1)."""
     w = "ciera_expert_combine"
-    _need(w, rows, 2, *_CODE_OF)
-    _need(w, out, 2, rows.dtype)
-    _need(w, row_of_slot, 2, _I32)
-    t, k = row_of_slot.shape
-    _whole(w, row_of_slot, (t, k), _I32)
-    if out.shape != (t, rows.shape[1]):
+    device = _device_of(w, rows)
+    code = _code(w, rows)
+    r_at = _matrix(w, device, rows, None, rows.dtype)
+    n_rows, cols = rows.shape
+    if not isinstance(row_of_slot, _Tensor) or row_of_slot.dim() != 2:
         _refuse(w)
-    if weights is not None:
-        _whole(w, weights, (t, k), _F32)
-    _call(w, _lib.ciera_expert_combine, out, (rows, row_of_slot, weights), stream, _CODE_OF[rows.dtype], rows.data_ptr(),
-          rows.shape[0], rows.stride(0), row_of_slot.data_ptr(), _ptr(weights), t, k, rows.shape[1], out.data_ptr(),
-          out.stride(0))
+    shape = row_of_slot.shape
+    t, k = shape
+    _enqueue(w, device, stream, _lib.ciera_expert_combine, code, r_at[0], n_rows, r_at[1],
+             _whole(w, device, row_of_slot, shape, _I32), None if weights is None else _whole(w, device, weights, shape, _F32),
+             t, k, cols, *_matrix(w, device, out, (t, cols), rows.dtype))
 
 
 def expert_combine_backward(dout, rows, row_of_slot, weights, dweights, drows=None, stream=None) -> None:
     """Gradients of ``expert_combine``: ``dweights`` fp32 [T, k] and, if given, ``drows`` (shape and type of ``rows``; rows that
     no slot names are left as they were)."""
     w = "ciera_expert_combine_backward"
-    _need(w, rows, 2, *_CODE_OF)
-    _need(w, dout, 2, rows.dtype)
-    _need(w, row_of_slot, 2, _I32)
-    t, k = row_of_slot.shape
-    _whole(w, row_of_slot, (t, k), _I32)
-    _whole(w, dweights, (t, k), _F32)
-    if dout.shape != (t, rows.shape[1]):
+    device = _device_of(w, rows)
+    code = _code(w, rows)
+    r_at = _matrix(w, device, rows, None, rows.dtype)
+    n_rows, cols = rows.shape
+    if not isinstance(row_of_slot, _Tensor) or row_of_slot.dim() != 2:
         _refuse(w)
-    if weights is not None:
-        _whole(w, weights, (t, k), _F32)
-    if drows is not None:
-        _need(w, drows, 2, rows.dtype)
-        if drows.shape != rows.shape:
-            _refuse(w)
-    _call(w, _lib.ciera_expert_combine_backward, dout, (rows, row_of_slot, weights, dweights, drows), stream,
-          _CODE_OF[rows.dtype], dout.data_ptr(), dout.stride(0), rows.data_ptr(), rows.shape[0], rows.stride(0),
-          row_of_slot.data_ptr(), _ptr(weights), t, k, rows.shape[1], dweights.data_ptr(), _ptr(drows),
-          0 if drows is None else drows.stride(0))
+    shape = row_of_slot.shape
+    t, k = shape
+    d_at = (None, 0) if drows is None else _matrix(w, device, drows, (n_rows, cols), rows.dtype)
+    _enqueue(w, device, stream, _lib.ciera_expert_combine_backward, code, *_matrix(w, device, dout, (t, cols), rows.dtype), r_at[0],
+             n_rows, r_at[1], _whole(w, device, row_of_slot, shape, _I32),
+             None if weights is None else _whole(w, device, weights, shape, _F32), t, k, cols,
+             _whole(w, device, dweights, shape, _F32), *d_at)
 
 
 # ------------------------------------------------------------------------------ gain rule (host)

@@ -464,24 +464,28 @@ static bool operand_map(CUtensorMap* map, const void* p, uint64_t k, uint64_t ro
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-static int sm_count(int* n) {
+// the current device and its SMs
+static int device_and_sms(int* dev, int* n) {
     static std::atomic<int> known[64];
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    cudaError_t e = cudaGetDevice(dev);
     if (e != cudaSuccess) return record_cuda_error(e);
-    if (dev < 64 && (*n = known[dev].load(std::memory_order_relaxed)) > 0) return CIERA_OK;
-    e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
+    if (*dev < 64 && (*n = known[*dev].load(std::memory_order_relaxed)) > 0) return CIERA_OK;
+    e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, *dev);
     if (e != cudaSuccess) return record_cuda_error(e);
-    if (dev < 64) known[dev].store(*n, std::memory_order_relaxed);
+    if (*dev < 64) known[*dev].store(*n, std::memory_order_relaxed);
     return CIERA_OK;
 }
 
 template <int MODE, int DT>
-static cudaError_t launch_product(const ProductArgs& a, const CUtensorMap& am, const CUtensorMap& bm, void* out, uint32_t pairs, cudaStream_t s) {
+static cudaError_t launch_product(const ProductArgs& a, const CUtensorMap& am, const CUtensorMap& bm, void* out, uint32_t pairs, int dev, cudaStream_t s) {
+    static std::atomic<uint64_t> allowed{0};  // devices on which this instance may have its shared memory
     constexpr size_t smem = sizeof(ProductSmem) + 1024;  // (the ring starts at a multiple of 1024)
     auto kernel = product_kernel<MODE, DT>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -525,8 +529,8 @@ extern "C" int ciera_fp8_matmul(const ciera_fp8_product* p, void* stream) {
         return CIERA_ERR_MISALIGNED;
     if ((p->m > 1 && p->a_stride >= 1ull << 40) || (p->n > 1 && p->b_stride >= 1ull << 40) || (several && p->b_matrix_stride >= 1ull << 40))
         return CIERA_ERR_UNSUPPORTED;
-    int sms = 0;
-    const int rc = sm_count(&sms);
+    int dev = 0, sms = 0;
+    const int rc = device_and_sms(&dev, &sms);
     if (rc) return rc;
     // tiles of 128 rows where those of 256 would leave SMs without work (every segment has at most one more than its rows fill)
     const uint64_t groups = contract ? p->n_experts : 1, n_tiles = (p->n + kTileN - 1) / kTileN, pairs = sms / 2;
@@ -550,7 +554,7 @@ extern "C" int ciera_fp8_matmul(const ciera_fp8_product* p, void* stream) {
         constexpr int DT = decltype(dt)::value;
         auto go = [&](auto mode_c) {
             constexpr int MODE = decltype(mode_c)::value;
-            e = launch_product<MODE, DT>(a, am, bm, p->out, grid, (cudaStream_t)stream);
+            e = launch_product<MODE, DT>(a, am, bm, p->out, grid, dev, (cudaStream_t)stream);
         };
         if (rows) go(std::integral_constant<int, CIERA_PRODUCT_ROWS>());
         else if (contract) go(std::integral_constant<int, CIERA_PRODUCT_CONTRACT>());
