@@ -2,7 +2,8 @@
 //
 // A block of threads has a tile of 128 x 128 values.  A warp has 16 rows, a lane 4 neighbouring columns of each, so a row's
 // largest magnitude is one reduction over the warp and the tile is read and kept in registers once for both orientations;
-// the transposed copy goes through shared memory to be written 128 bytes at a time.  Memory bounds it.
+// the transposed copy goes through shared memory to be written 128 bytes at a time.  Memory bounds it.  Tiles beside each
+// other come one behind the other, so that blocks that run together read and write whole rows.
 #include <type_traits>
 
 #include "ciera_numeric.cuh"
@@ -11,7 +12,6 @@ namespace ciera {
 
 constexpr int kTileThreads = 256;
 constexpr int kTileRows = 16;  // rows of a warp
-constexpr int kTransposedPitch = 128 + 16;
 
 struct RowsArgs {
     uint64_t x_stride, grad_stride, q_stride, scales_stride, qt_stride, scales_t_stride;
@@ -19,7 +19,7 @@ struct RowsArgs {
     const int32_t* slot_of_row;
     const float* row_weights;
     const int32_t* starts;
-    uint32_t rows, cols, top_k, n_experts;
+    uint32_t rows, cols, col_tiles, top_k, n_experts;
     uint8_t* q;
     uint8_t* scales;
     uint8_t* qt;
@@ -47,20 +47,53 @@ __device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d
 
 __device__ __forceinline__ float sigmoid32(float g) { return 1.f / (1.f + expf(-g)); }
 
-// One value of the rows: x's, silu(g) * u, or one of their gradients.
-template <int DT, int SRC>
-__device__ __forceinline__ float source_value(const value_t<DT>* __restrict__ x, const value_t<DT>* __restrict__ grad, uint32_t c,
-                                              uint32_t cols) {
+// Four neighbouring values of a row: x's, silu(g) * u, or one of their gradients.  WIDE: one access for each four of an input.
+template <int DT, int SRC, bool WIDE>
+__device__ __forceinline__ void source_values(const value_t<DT>* __restrict__ x, const value_t<DT>* __restrict__ grad, uint32_t c,
+                                              uint32_t cols, float (&v)[4]) {
+    const auto get = [&](const value_t<DT>* p, uint32_t c0, float(&to)[4]) {
+        if constexpr (WIDE) {
+            load_values<DT, 4>(p, to);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to[j] = c0 + j < cols ? ValueOf<DT>::get(p[j]) : 0.f;
+        }
+    };
     if constexpr (SRC == CIERA_SOURCE_ROWS) {
-        return ValueOf<DT>::get(x[c]);
+        get(x + c, c, v);
     } else if constexpr (SRC == CIERA_SOURCE_SWIGLU) {
-        const float g = ValueOf<DT>::get(x[c]), u = ValueOf<DT>::get(x[cols + c]);
-        return g * sigmoid32(g) * u;
+        float g[4], u[4];
+        get(x + c, c, g);
+        get(x + cols + c, c, u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = g[j] * sigmoid32(g[j]) * u[j];
+    } else if constexpr (WIDE) {  // (the four are on one side)
+        const uint32_t f = cols / 2, at = c < f ? c : c - f;
+        float g[4], u[4], d[4];
+        get(x + at, c, g);
+        get(grad + at, c, d);
+        if (c < f) {
+            get(x + f + at, c, u);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float s = sigmoid32(g[j]);
+                v[j] = d[j] * u[j] * s * (1.f + g[j] * (1.f - s));
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = d[j] * g[j] * sigmoid32(g[j]);
+        }
     } else {
-        const uint32_t f = cols / 2, j = c < f ? c : c - f;
-        const float g = ValueOf<DT>::get(x[j]), u = ValueOf<DT>::get(x[f + j]), d = ValueOf<DT>::get(grad[j]);
-        const float s = sigmoid32(g);
-        return c < f ? d * u * s * (1.f + g * (1.f - s)) : d * g * s;
+        const uint32_t f = cols / 2;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[j] = 0.f;
+            if (c + j >= cols) continue;
+            const uint32_t at = c + j < f ? c + j : c + j - f;
+            const float g = ValueOf<DT>::get(x[at]), u = ValueOf<DT>::get(x[f + at]), d = ValueOf<DT>::get(grad[at]);
+            const float s = sigmoid32(g);
+            v[j] = c + j < f ? d * u * s * (1.f + g * (1.f - s)) : d * g * s;
+        }
     }
 }
 
@@ -89,73 +122,109 @@ __device__ __forceinline__ uint32_t settle(uint32_t amax, double exact) {
     return exact > (double)__uint_as_float(border) ? border + 1u : border;
 }
 
-template <int DT, int SRC, bool T>
-__global__ void __launch_bounds__(kTileThreads) quantize_rows_kernel(const RowsArgs a, const value_t<DT>* __restrict__ x,
-                                                                     const value_t<DT>* __restrict__ grad) {
+// The tile's four values of each row, rounded with a scale for each row, to q.
+__device__ __forceinline__ void put_four(uint8_t* to, uint32_t q, uint32_t c0, uint32_t cols) {
+    if (c0 + 3 < cols) {
+        *reinterpret_cast<uint32_t*>(to) = q;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+            if (c0 + j < cols) to[j] = (uint8_t)(q >> (8 * j));
+    }
+}
+
+// 16 rounded values of one column go to line `c` of `turned` (128 bytes, in units of 16 whose places are mixed by the
+// column, so that neither the columns of a warp nor the units of a column meet in a bank) ...
+__device__ __forceinline__ void turn_in(uint4* turned, uint32_t c, uint32_t unit, const float (&v)[kTileRows][4], int j, float inv) {
+    uint32_t q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = to_e4m3x4(v[4 * i][j], v[4 * i + 1][j], v[4 * i + 2][j], v[4 * i + 3][j], inv);
+    turned[c * 8 + (unit ^ (c >> 2 & 7))] = make_uint4(q[0], q[1], q[2], q[3]);
+}
+// ... and from there to the transposed tile's rows.
+__device__ __forceinline__ void turn_out(const uint4* turned, uint8_t* qt, uint64_t stride, uint32_t col0, uint32_t cols, uint32_t row0,
+                                         uint32_t rows) {
+    for (int k = threadIdx.x; k < 128 * 8; k += kTileThreads) {
+        const uint32_t c = k >> 3, r = row0 + (k & 7) * 16;
+        if (col0 + c >= cols || r >= rows) continue;
+        const uint4 q = turned[c * 8 + ((k & 7) ^ (c >> 2 & 7))];
+        uint8_t* to = qt + (uint64_t)(col0 + c) * stride + r;
+        if (r + 15 < rows) {
+            *reinterpret_cast<uint4*>(to) = q;
+        } else {
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+            for (uint32_t i = 0; r + i < rows; ++i) to[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+        }
+    }
+}
+
+template <int DT, int SRC, bool T, bool WIDE>
+__global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const RowsArgs a, const value_t<DT>* __restrict__ x,
+                                                                        const value_t<DT>* __restrict__ grad) {
     __shared__ uint32_t col_max[T ? kTileThreads / 32 : 1][128];
-    __shared__ __align__(16) uint8_t turned[T ? 128 * kTransposedPitch : 16];
+    __shared__ uint4 turned[T ? 128 * 8 : 1];
     pdl_wait();
-    const uint32_t row0 = blockIdx.x * 128u, col0 = blockIdx.y * 128u;
+    const uint32_t row_tile = blockIdx.x / a.col_tiles, col_tile = blockIdx.x - row_tile * a.col_tiles;
+    const uint32_t row0 = row_tile * 128u, col0 = col_tile * 128u;
     const uint32_t rows = a.starts ? min((uint32_t)max(a.starts[a.n_experts], 0), a.rows) : a.rows;
     if (row0 >= rows) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t c0 = col0 + lane * 4;
+    const uint32_t c0 = col0 + lane * 4, first = row0 + warp * kTileRows;
+    // lane i: where row i of the warp comes from
+    uint32_t from = first + lane;
+    float weight = 1.f;
+    bool some = lane < kTileRows && from < rows;
+    if (a.slot_of_row) {
+        const int32_t slot = some ? a.slot_of_row[from] : -1;
+        some = slot >= 0 && (uint64_t)slot < a.x_rows * a.top_k;
+        if (SRC == CIERA_SOURCE_ROWS) from = (uint32_t)max(slot, 0) / a.top_k;
+        if (some && a.row_weights) weight = a.row_weights[slot];
+    } else {
+        some = some && from < a.x_rows;
+    }
+    const uint32_t live = __ballot_sync(~0u, some);
+    const bool whole = c0 + 3 < a.cols;
     float v[kTileRows][4];
-    const value_t<DT>* xr[kTileRows];
 #pragma unroll
     for (int i = 0; i < kTileRows; ++i) {
-        const uint32_t r = row0 + warp * kTileRows + i;
-        uint64_t from = r;
-        float w = 1.f;
-        bool some = r < rows;
-        if (some && a.slot_of_row) {
-            const int32_t slot = a.slot_of_row[r];
-            some = slot >= 0 && (uint64_t)slot < a.x_rows * a.top_k;
-            if (SRC == CIERA_SOURCE_ROWS) from = (uint32_t)max(slot, 0) / a.top_k;
-            if (some && a.row_weights) w = a.row_weights[slot];
-        } else if (some) {
-            some = r < a.x_rows;
-        }
-        xr[i] = some ? x + from * a.x_stride : nullptr;
+        const uint32_t r = __shfl_sync(~0u, from, i);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[i][j] = 0.f;
-            if (some && c0 + j < a.cols) {
-                v[i][j] = source_value<DT, SRC>(xr[i], SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + from * a.grad_stride : nullptr,
-                                                c0 + j, a.cols);
-                if (SRC == CIERA_SOURCE_ROWS && a.row_weights) v[i][j] *= w;
-            }
+        for (int j = 0; j < 4; ++j) v[i][j] = 0.f;
+        if (live >> i & 1 && (WIDE ? whole : c0 < a.cols))
+            source_values<DT, SRC, WIDE>(x + r * a.x_stride, SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + r * a.grad_stride : nullptr, c0, a.cols, v[i]);
+    }
+    if (SRC == CIERA_SOURCE_ROWS && a.row_weights) {
+#pragma unroll
+        for (int i = 0; i < kTileRows; ++i) {
+            const float w = __shfl_sync(~0u, weight, i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i][j] *= w;
         }
     }
+    uint32_t bytes = 0;  // lane i: the scale of row i
 #pragma unroll
     for (int i = 0; i < kTileRows; ++i) {
-        const uint32_t r = row0 + warp * kTileRows + i;
+        const uint32_t r = first + i;
         uint32_t amax = max(max(magnitude(v[i][0]), magnitude(v[i][1])), max(magnitude(v[i][2]), magnitude(v[i][3])));
         amax = __reduce_max_sync(~0u, amax);
         if constexpr (SRC != CIERA_SOURCE_ROWS) {
             if (at_border(amax)) {
                 double m = 0.0;
                 for (int j = 0; j < 4; ++j)
-                    if (xr[i] && c0 + j < a.cols)
-                        m = fmax(m, source_magnitude<DT, SRC>(xr[i], SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + (uint64_t)r * a.grad_stride : nullptr,
-                                                              c0 + j, a.cols));
+                    if (live >> i & 1 && c0 + j < a.cols)
+                        m = fmax(m, source_magnitude<DT, SRC>(x + (uint64_t)r * a.x_stride,
+                                                              SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + (uint64_t)r * a.grad_stride : nullptr, c0 + j, a.cols));
 #pragma unroll
                 for (int d = 16; d; d >>= 1) m = fmax(m, __shfl_xor_sync(~0u, m, d));
                 amax = settle(amax, m);
             }
         }
         const uint32_t byte = scale_byte(amax);
-        if (r >= rows) continue;
-        if (lane == 0) a.scales[(uint64_t)blockIdx.y * a.scales_stride + r] = (uint8_t)byte;
-        const uint32_t q = to_e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3], inverse_scale(byte));
-        uint8_t* to = a.q + (uint64_t)r * a.q_stride + c0;
-        if (c0 + 3 < a.cols) {
-            *reinterpret_cast<uint32_t*>(to) = q;
-        } else {
-            for (int j = 0; j < 3; ++j)
-                if (c0 + j < a.cols) to[j] = (uint8_t)(q >> (8 * j));
-        }
+        if (lane == i) bytes = byte;
+        if (r < rows && c0 < a.cols)
+            put_four(a.q + (uint64_t)r * a.q_stride + c0, to_e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3], inverse_scale(byte)), c0, a.cols);
     }
+    if (lane < kTileRows && first + lane < rows) a.scales[(uint64_t)col_tile * a.scales_stride + first + lane] = (uint8_t)bytes;
     if constexpr (T) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -186,26 +255,11 @@ __global__ void __launch_bounds__(kTileThreads) quantize_rows_kernel(const RowsA
                 }
             }
             const uint32_t byte = scale_byte(amax);
-            const float inv = inverse_scale(byte);
-            if (warp == 0 && c < a.cols) a.scales_t[(uint64_t)blockIdx.x * a.scales_t_stride + c] = (uint8_t)byte;
-            uint32_t q[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = to_e4m3x4(v[4 * i][j], v[4 * i + 1][j], v[4 * i + 2][j], v[4 * i + 3][j], inv);
-            *reinterpret_cast<uint4*>(turned + (lane * 4 + j) * kTransposedPitch + warp * kTileRows) = make_uint4(q[0], q[1], q[2], q[3]);
+            if (warp == 0 && c < a.cols) a.scales_t[(uint64_t)row_tile * a.scales_t_stride + c] = (uint8_t)byte;
+            turn_in(turned, lane * 4 + j, warp, v, j, inverse_scale(byte));
         }
         __syncthreads();
-        for (int k = threadIdx.x; k < 128 * 8; k += kTileThreads) {
-            const uint32_t c = col0 + (k >> 3), r = row0 + (k & 7) * 16;
-            if (c >= a.cols || r >= rows) continue;
-            const uint4 q = *reinterpret_cast<const uint4*>(turned + (k >> 3) * kTransposedPitch + (k & 7) * 16);
-            uint8_t* to = a.qt + (uint64_t)c * a.qt_stride + r;
-            if (r + 15 < rows) {
-                *reinterpret_cast<uint4*>(to) = q;
-            } else {
-                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-                for (uint32_t i = 0; r + i < rows; ++i) to[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
-            }
-        }
+        turn_out(turned, a.qt, a.qt_stride, col0, a.cols, row0, rows);
     }
 }
 
@@ -219,27 +273,30 @@ struct BlocksArgs {
     uint8_t* scales_t;
 };
 
-template <int DT, bool T>
-__global__ void __launch_bounds__(kTileThreads) quantize_blocks_kernel(const BlocksArgs a, const value_t<DT>* __restrict__ x) {
+template <int DT, bool T, bool WIDE>
+__global__ void __launch_bounds__(kTileThreads, 2) quantize_blocks_kernel(const BlocksArgs a, const value_t<DT>* __restrict__ x) {
     __shared__ uint32_t warp_max[kTileThreads / 32];
-    __shared__ __align__(16) uint8_t turned[T ? 128 * kTransposedPitch : 16];
+    __shared__ uint4 turned[T ? 128 * 8 : 1];
     pdl_wait();
-    const uint32_t matrix = blockIdx.x / a.row_blocks, rb = blockIdx.x % a.row_blocks;
-    const uint32_t row0 = rb * 128u, col0 = blockIdx.y * 128u;
+    const uint32_t row = blockIdx.x / a.col_blocks, cb = blockIdx.x - row * a.col_blocks;
+    const uint32_t matrix = row / a.row_blocks, rb = row - matrix * a.row_blocks;
+    const uint32_t row0 = rb * 128u, col0 = cb * 128u;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t c0 = col0 + lane * 4;
+    const uint32_t c0 = col0 + lane * 4, first = row0 + warp * kTileRows;
+    const value_t<DT>* xm = x + matrix * a.x_matrix_stride;
     float v[kTileRows][4];
     uint32_t amax = 0;
 #pragma unroll
     for (int i = 0; i < kTileRows; ++i) {
-        const uint32_t r = row0 + warp * kTileRows + i;
-        const value_t<DT>* xr = x + matrix * a.x_matrix_stride + r * a.x_stride;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[i][j] = r < a.rows && c0 + j < a.cols ? ValueOf<DT>::get(xr[c0 + j]) : 0.f;
-            amax = max(amax, magnitude(v[i][j]));
-        }
+        for (int j = 0; j < 4; ++j) v[i][j] = 0.f;
+        if (first + i < a.rows && (WIDE ? c0 + 3 < a.cols : c0 < a.cols))
+            source_values<DT, CIERA_SOURCE_ROWS, WIDE>(xm + (first + i) * a.x_stride, nullptr, c0, a.cols, v[i]);
     }
+#pragma unroll
+    for (int i = 0; i < kTileRows; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) amax = max(amax, magnitude(v[i][j]));
     amax = __reduce_max_sync(~0u, amax);
     if (lane == 0) warp_max[warp] = amax;
     __syncthreads();
@@ -248,43 +305,19 @@ __global__ void __launch_bounds__(kTileThreads) quantize_blocks_kernel(const Blo
     const uint32_t byte = scale_byte(amax);
     const float inv = inverse_scale(byte);
     if (threadIdx.x == 0) {
-        a.scales[matrix * a.scales_matrix_stride + rb * a.scales_stride + blockIdx.y] = (uint8_t)byte;
-        if (T) a.scales_t[matrix * a.scales_t_matrix_stride + blockIdx.y * a.scales_t_stride + rb] = (uint8_t)byte;
+        a.scales[matrix * a.scales_matrix_stride + rb * a.scales_stride + cb] = (uint8_t)byte;
+        if (T) a.scales_t[matrix * a.scales_t_matrix_stride + cb * a.scales_t_stride + rb] = (uint8_t)byte;
     }
+    uint8_t* q = a.q + matrix * a.q_matrix_stride + c0;
 #pragma unroll
-    for (int i = 0; i < kTileRows; ++i) {
-        const uint32_t r = row0 + warp * kTileRows + i;
-        if (r >= a.rows) break;
-        const uint32_t q = to_e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3], inv);
-        uint8_t* to = a.q + matrix * a.q_matrix_stride + r * a.q_stride + c0;
-        if (c0 + 3 < a.cols) {
-            *reinterpret_cast<uint32_t*>(to) = q;
-        } else {
-            for (int j = 0; j < 3; ++j)
-                if (c0 + j < a.cols) to[j] = (uint8_t)(q >> (8 * j));
-        }
-    }
+    for (int i = 0; i < kTileRows; ++i)
+        if (first + i < a.rows && c0 < a.cols)
+            put_four(q + (first + i) * a.q_stride, to_e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3], inv), c0, a.cols);
     if constexpr (T) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t q[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = to_e4m3x4(v[4 * i][j], v[4 * i + 1][j], v[4 * i + 2][j], v[4 * i + 3][j], inv);
-            *reinterpret_cast<uint4*>(turned + (lane * 4 + j) * kTransposedPitch + warp * kTileRows) = make_uint4(q[0], q[1], q[2], q[3]);
-        }
+        for (int j = 0; j < 4; ++j) turn_in(turned, lane * 4 + j, warp, v, j, inv);
         __syncthreads();
-        for (int k = threadIdx.x; k < 128 * 8; k += kTileThreads) {
-            const uint32_t c = col0 + (k >> 3), r = row0 + (k & 7) * 16;
-            if (c >= a.cols || r >= a.rows) continue;
-            const uint4 q = *reinterpret_cast<const uint4*>(turned + (k >> 3) * kTransposedPitch + (k & 7) * 16);
-            uint8_t* to = a.qt + matrix * a.qt_matrix_stride + c * a.qt_stride + r;
-            if (r + 15 < a.rows) {
-                *reinterpret_cast<uint4*>(to) = q;
-            } else {
-                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-                for (uint32_t i = 0; r + i < a.rows; ++i) to[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
-            }
-        }
+        turn_out(turned, a.qt + matrix * a.qt_matrix_stride, a.qt_stride, col0, a.cols, row0, a.rows);
     }
 }
 
@@ -316,20 +349,31 @@ extern "C" int ciera_fp8_quantize_rows(const ciera_fp8_rows* p, void* stream) {
         !aligned_to(p->grad, dtype_bytes(p->dtype)) || !aligned_to(p->slot_of_row, 4) || !aligned_to(p->row_weights, 4) ||
         !aligned_to(p->starts, 4))
         return CIERA_ERR_MISALIGNED;
-    if ((p->cols + 127) / 128 > 65535) return CIERA_ERR_UNSUPPORTED;
+    const uint64_t col_tiles = (p->cols + 127) / 128, tiles = (p->rows + 127) / 128 * col_tiles;
+    if (tiles > kMaxExtent) return CIERA_ERR_UNSUPPORTED;
+    // four values at a time where every row's start and, for gate and up, each half's is a multiple of four
+    const uint64_t four = 4 * dtype_bytes(p->dtype) - 1;
+    const bool wide = !(((uint64_t)p->x | (uint64_t)p->grad | p->x_stride * dtype_bytes(p->dtype) | p->grad_stride * dtype_bytes(p->dtype)) & four) &&
+                      !(p->cols & (back ? 7 : 3));
     const RowsArgs a{p->x_stride, p->grad_stride, p->q_stride, p->scales_stride, p->qt_stride, p->scales_t_stride, p->x_rows,
-                     p->slot_of_row, p->row_weights, p->starts, (uint32_t)p->rows, (uint32_t)p->cols,
+                     p->slot_of_row, p->row_weights, p->starts, (uint32_t)p->rows, (uint32_t)p->cols, (uint32_t)col_tiles,
                      p->slot_of_row ? p->top_k : 1u, p->n_experts, (uint8_t*)p->q, p->scales, (uint8_t*)p->qt, p->scales_t};
-    const dim3 grid((uint32_t)((p->rows + 127) / 128), (uint32_t)((p->cols + 127) / 128));
     cudaError_t e = cudaSuccess;
     with_dtype(p->dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        auto go = [&](auto kernel) {
-            e = launch_after(kernel, grid, kTileThreads, 0, (cudaStream_t)stream, a, (const value_t<DT>*)p->x, (const value_t<DT>*)p->grad);
+        const auto go = [&](auto source, auto both, auto four_wide) {
+            e = launch_after(quantize_rows_kernel<DT, decltype(source)::value, decltype(both)::value, decltype(four_wide)::value>, dim3((uint32_t)tiles),
+                             kTileThreads, 0, (cudaStream_t)stream, a, (const value_t<DT>*)p->x, (const value_t<DT>*)p->grad);
         };
-        if (src == CIERA_SOURCE_ROWS) turned ? go(quantize_rows_kernel<DT, CIERA_SOURCE_ROWS, true>) : go(quantize_rows_kernel<DT, CIERA_SOURCE_ROWS, false>);
-        else if (!back) turned ? go(quantize_rows_kernel<DT, CIERA_SOURCE_SWIGLU, true>) : go(quantize_rows_kernel<DT, CIERA_SOURCE_SWIGLU, false>);
-        else turned ? go(quantize_rows_kernel<DT, CIERA_SOURCE_SWIGLU_BACKWARD, true>) : go(quantize_rows_kernel<DT, CIERA_SOURCE_SWIGLU_BACKWARD, false>);
+        const auto pick = [&](auto source) {
+            const std::true_type yes;
+            const std::false_type no;
+            if (turned) wide ? go(source, yes, yes) : go(source, yes, no);
+            else wide ? go(source, no, yes) : go(source, no, no);
+        };
+        if (src == CIERA_SOURCE_ROWS) pick(std::integral_constant<int, CIERA_SOURCE_ROWS>());
+        else if (!back) pick(std::integral_constant<int, CIERA_SOURCE_SWIGLU>());
+        else pick(std::integral_constant<int, CIERA_SOURCE_SWIGLU_BACKWARD>());
     });
     if (e != cudaSuccess) return record_cuda_error(e);
     count_launch();
@@ -351,16 +395,23 @@ extern "C" int ciera_fp8_quantize_blocks(const ciera_fp8_blocks* p, void* stream
         (turned && (!fp8_tensor_ok(p->qt, p->cols, p->qt_stride) || (several && (p->qt_matrix_stride & 15)))) ||
         !aligned_to(p->x, dtype_bytes(p->dtype)))
         return CIERA_ERR_MISALIGNED;
-    if (cb > 65535 || rb * p->matrices > kMaxExtent) return CIERA_ERR_UNSUPPORTED;
+    if (rb * p->matrices > kMaxExtent || rb * p->matrices * cb > kMaxExtent) return CIERA_ERR_UNSUPPORTED;
+    const uint64_t v = dtype_bytes(p->dtype);
+    const bool wide = !(((uint64_t)p->x | p->x_stride * v | p->x_matrix_stride * v) & (4 * v - 1)) && !(p->cols & 3);
     const BlocksArgs a{p->x_stride, p->x_matrix_stride, p->q_stride, p->q_matrix_stride, p->scales_stride, p->scales_matrix_stride,
                        p->qt_stride, p->qt_matrix_stride, p->scales_t_stride, p->scales_t_matrix_stride,
                        (uint32_t)p->rows, (uint32_t)p->cols, (uint32_t)rb, (uint32_t)cb, (uint8_t*)p->q, p->scales, (uint8_t*)p->qt, p->scales_t};
-    const dim3 grid((uint32_t)(rb * p->matrices), (uint32_t)cb);
     cudaError_t e = cudaSuccess;
     with_dtype(p->dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        auto go = [&](auto kernel) { e = launch_after(kernel, grid, kTileThreads, 0, (cudaStream_t)stream, a, (const value_t<DT>*)p->x); };
-        turned ? go(quantize_blocks_kernel<DT, true>) : go(quantize_blocks_kernel<DT, false>);
+        const auto go = [&](auto both, auto four_wide) {
+            e = launch_after(quantize_blocks_kernel<DT, decltype(both)::value, decltype(four_wide)::value>, dim3((uint32_t)(rb * p->matrices * cb)),
+                             kTileThreads, 0, (cudaStream_t)stream, a, (const value_t<DT>*)p->x);
+        };
+        const std::true_type yes;
+        const std::false_type no;
+        if (turned) wide ? go(yes, yes) : go(yes, no);
+        else wide ? go(no, yes) : go(no, no);
     });
     if (e != cudaSuccess) return record_cuda_error(e);
     count_launch();
