@@ -1,6 +1,6 @@
 // Operands of the 8-bit products: rows or matrices rounded to e4m3 with a power of two for each 128 values.
 //
-// A block of threads has a tile of 128 x 128 values.  A warp has 16 rows, a lane 4 neighbouring columns of each, so a row's
+// A block of threads has a tile of 128 x 128 values.  A warp has 8 rows, a lane 4 neighbouring columns of each, so a row's
 // largest magnitude is one reduction over the warp and the tile is read and kept in registers once for both orientations;
 // the transposed copy goes through shared memory to be written 128 bytes at a time.  Memory bounds it.  Tiles beside each
 // other come one behind the other, so that blocks that run together read and write whole rows.
@@ -10,8 +10,10 @@
 
 namespace ciera {
 
-constexpr int kTileThreads = 256;
-constexpr int kTileRows = 16;  // rows of a warp
+// 16 warps of 8 rows: 32 values a thread leave room for two blocks of 512 threads on an SM, and their loads in flight.  (8 warps
+// of 16 rows, two blocks of 256: dispatch of 4096 x 8 rows of 2048 in 113 us, 64 matrices of 2048 x 1024 in 205 us.)
+constexpr int kTileThreads = 512;
+constexpr int kTileRows = 8;  // rows of a warp
 
 struct RowsArgs {
     uint64_t x_stride, grad_stride, q_stride, scales_stride, qt_stride, scales_t_stride;
@@ -133,21 +135,28 @@ __device__ __forceinline__ void put_four(uint8_t* to, uint32_t q, uint32_t c0, u
     }
 }
 
-// 16 rounded values of one column go to line `c` of `turned` (128 bytes, in units of 16 whose places are mixed by the
-// column, so that neither the columns of a warp nor the units of a column meet in a bank) ...
-__device__ __forceinline__ void turn_in(uint4* turned, uint32_t c, uint32_t unit, const float (&v)[kTileRows][4], int j, float inv) {
-    uint32_t q[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) q[i] = to_e4m3x4(v[4 * i][j], v[4 * i + 1][j], v[4 * i + 2][j], v[4 * i + 3][j], inv);
-    turned[c * 8 + (unit ^ (c >> 2 & 7))] = make_uint4(q[0], q[1], q[2], q[3]);
+// Four words of four bytes, turned: byte i of word j to byte j of word i.
+__device__ __forceinline__ void turn_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t (&t)[4]) {
+    const uint32_t ab = __byte_perm(a, b, 0x5140), ab2 = __byte_perm(a, b, 0x7362);
+    const uint32_t cd = __byte_perm(c, d, 0x5140), cd2 = __byte_perm(c, d, 0x7362);
+    t[0] = __byte_perm(ab, cd, 0x5410);
+    t[1] = __byte_perm(ab, cd, 0x7632);
+    t[2] = __byte_perm(ab2, cd2, 0x5410);
+    t[3] = __byte_perm(ab2, cd2, 0x7632);
 }
-// ... and from there to the transposed tile's rows.
-__device__ __forceinline__ void turn_out(const uint4* turned, uint8_t* qt, uint64_t stride, uint32_t col0, uint32_t cols, uint32_t row0,
+// The 8 rounded values of warp `warp` in column 4 * lane + j go to that column's line of `turned`, 16 units of 8 bytes whose
+// places are mixed by the lane, so that neither the columns of a warp nor the units of a column meet in a bank ...
+__device__ __forceinline__ void turn_in(uint2* turned, int lane, int j, int warp, uint32_t lo, uint32_t hi) {
+    turned[(lane * 4 + j) * 16 + (((warp >> 1) ^ (lane & 7)) << 1 | ((warp & 1) ^ (lane >> 3 & 1)))] = make_uint2(lo, hi);
+}
+// ... and from there to the transposed tile's rows, 16 bytes a thread.
+__device__ __forceinline__ void turn_out(const uint2* turned, uint8_t* qt, uint64_t stride, uint32_t col0, uint32_t cols, uint32_t row0,
                                          uint32_t rows) {
     for (int k = threadIdx.x; k < 128 * 8; k += kTileThreads) {
-        const uint32_t c = k >> 3, r = row0 + (k & 7) * 16;
+        const uint32_t c = k >> 3, unit = k & 7, r = row0 + unit * 16, of = c >> 2;  // (the lane that put it there)
         if (col0 + c >= cols || r >= rows) continue;
-        const uint4 q = turned[c * 8 + ((k & 7) ^ (c >> 2 & 7))];
+        uint4 q = *reinterpret_cast<const uint4*>(turned + c * 16 + ((unit ^ (of & 7)) << 1));
+        if (of >> 3 & 1) q = make_uint4(q.z, q.w, q.x, q.y);
         uint8_t* to = qt + (uint64_t)(col0 + c) * stride + r;
         if (r + 15 < rows) {
             *reinterpret_cast<uint4*>(to) = q;
@@ -161,8 +170,9 @@ __device__ __forceinline__ void turn_out(const uint4* turned, uint8_t* qt, uint6
 template <int DT, int SRC, bool T, bool WIDE>
 __global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const RowsArgs a, const value_t<DT>* __restrict__ x,
                                                                         const value_t<DT>* __restrict__ grad) {
-    __shared__ uint32_t col_max[T ? kTileThreads / 32 : 1][128];
-    __shared__ uint4 turned[T ? 128 * 8 : 1];
+    __shared__ __align__(16) uint32_t col_max[T ? kTileThreads / 32 : 1][128];
+    __shared__ __align__(16) float col_inv[128];
+    __shared__ __align__(16) uint2 turned[T ? 128 * 16 : 2];
     pdl_wait();
     const uint32_t row_tile = blockIdx.x / a.col_tiles, col_tile = blockIdx.x - row_tile * a.col_tiles;
     const uint32_t row0 = row_tile * 128u, col0 = col_tile * 128u;
@@ -201,63 +211,73 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const Ro
             for (int j = 0; j < 4; ++j) v[i][j] *= w;
         }
     }
-    uint32_t bytes = 0;  // lane i: the scale of row i
+    uint32_t row_max = 0;  // lane i: the largest magnitude of row i
 #pragma unroll
     for (int i = 0; i < kTileRows; ++i) {
-        const uint32_t r = first + i;
         uint32_t amax = max(max(magnitude(v[i][0]), magnitude(v[i][1])), max(magnitude(v[i][2]), magnitude(v[i][3])));
         amax = __reduce_max_sync(~0u, amax);
         if constexpr (SRC != CIERA_SOURCE_ROWS) {
             if (at_border(amax)) {
+                const uint64_t r = first + i;
                 double m = 0.0;
                 for (int j = 0; j < 4; ++j)
                     if (live >> i & 1 && c0 + j < a.cols)
-                        m = fmax(m, source_magnitude<DT, SRC>(x + (uint64_t)r * a.x_stride,
-                                                              SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + (uint64_t)r * a.grad_stride : nullptr, c0 + j, a.cols));
+                        m = fmax(m, source_magnitude<DT, SRC>(x + r * a.x_stride, SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + r * a.grad_stride : nullptr, c0 + j, a.cols));
 #pragma unroll
                 for (int d = 16; d; d >>= 1) m = fmax(m, __shfl_xor_sync(~0u, m, d));
                 amax = settle(amax, m);
             }
         }
-        const uint32_t byte = scale_byte(amax);
-        if (lane == i) bytes = byte;
-        if (r < rows && c0 < a.cols)
-            put_four(a.q + (uint64_t)r * a.q_stride + c0, to_e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3], inverse_scale(byte)), c0, a.cols);
+        if (lane == i) row_max = amax;
     }
-    if (lane < kTileRows && first + lane < rows) a.scales[(uint64_t)col_tile * a.scales_stride + first + lane] = (uint8_t)bytes;
+    const uint32_t row_byte = scale_byte(row_max);
+    const float row_inv = inverse_scale(row_byte);
+    if (lane < kTileRows && first + lane < rows) a.scales[(uint64_t)col_tile * a.scales_stride + first + lane] = (uint8_t)row_byte;
+    uint8_t* q = a.q + (uint64_t)first * a.q_stride + c0;
+#pragma unroll
+    for (int i = 0; i < kTileRows; ++i) {
+        const float inv = __shfl_sync(~0u, row_inv, i);
+        if (first + i < rows && c0 < a.cols) put_four(q + i * a.q_stride, to_e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3], inv), c0, a.cols);
+    }
     if constexpr (T) {
+        uint32_t m[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            uint32_t m = 0;
+            m[j] = 0;
 #pragma unroll
-            for (int i = 0; i < kTileRows; ++i) m = max(m, magnitude(v[i][j]));
-            col_max[warp][lane * 4 + j] = m;
+            for (int i = 0; i < kTileRows; ++i) m[j] = max(m[j], magnitude(v[i][j]));
         }
+        *reinterpret_cast<uint4*>(&col_max[warp][lane * 4]) = make_uint4(m[0], m[1], m[2], m[3]);
         __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t c = c0 + j;
+        if (threadIdx.x < 128) {  // a thread for each column
+            const uint32_t c = col0 + threadIdx.x;
             uint32_t amax = 0;
 #pragma unroll
-            for (int w = 0; w < kTileThreads / 32; ++w) amax = max(amax, col_max[w][lane * 4 + j]);
+            for (int w = 0; w < kTileThreads / 32; ++w) amax = max(amax, col_max[w][threadIdx.x]);
             if constexpr (SRC != CIERA_SOURCE_ROWS) {
-                if (at_border(amax)) {  // (the same in every warp; each goes over the whole column)
-                    double m = 0.0;
+                if (at_border(amax)) {
+                    double most = 0.0;
                     for (uint32_t r = row0; r < min(row0 + 128u, rows) && c < a.cols; ++r) {
                         if (a.slot_of_row) {
                             const int32_t slot = a.slot_of_row[r];
                             if (slot < 0 || (uint64_t)slot >= a.x_rows * a.top_k) continue;
                         } else if (r >= a.x_rows) continue;
-                        m = fmax(m, source_magnitude<DT, SRC>(x + (uint64_t)r * a.x_stride,
-                                                              SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + (uint64_t)r * a.grad_stride : nullptr, c, a.cols));
+                        most = fmax(most, source_magnitude<DT, SRC>(x + (uint64_t)r * a.x_stride,
+                                                                    SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + (uint64_t)r * a.grad_stride : nullptr, c, a.cols));
                     }
-                    amax = settle(amax, m);
+                    amax = settle(amax, most);
                 }
             }
             const uint32_t byte = scale_byte(amax);
-            if (warp == 0 && c < a.cols) a.scales_t[(uint64_t)row_tile * a.scales_t_stride + c] = (uint8_t)byte;
-            turn_in(turned, lane * 4 + j, warp, v, j, inverse_scale(byte));
+            if (c < a.cols) a.scales_t[(uint64_t)row_tile * a.scales_t_stride + c] = (uint8_t)byte;
+            col_inv[threadIdx.x] = inverse_scale(byte);
         }
+        __syncthreads();
+        const float4 inv4 = *reinterpret_cast<const float4*>(&col_inv[lane * 4]);
+        const float inv[4] = {inv4.x, inv4.y, inv4.z, inv4.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            turn_in(turned, lane, j, warp, to_e4m3x4(v[0][j], v[1][j], v[2][j], v[3][j], inv[j]), to_e4m3x4(v[4][j], v[5][j], v[6][j], v[7][j], inv[j]));
         __syncthreads();
         turn_out(turned, a.qt, a.qt_stride, col0, a.cols, row0, rows);
     }
@@ -276,7 +296,7 @@ struct BlocksArgs {
 template <int DT, bool T, bool WIDE>
 __global__ void __launch_bounds__(kTileThreads, 2) quantize_blocks_kernel(const BlocksArgs a, const value_t<DT>* __restrict__ x) {
     __shared__ uint32_t warp_max[kTileThreads / 32];
-    __shared__ uint4 turned[T ? 128 * 8 : 1];
+    __shared__ __align__(16) uint2 turned[T ? 128 * 16 : 2];
     pdl_wait();
     const uint32_t row = blockIdx.x / a.col_blocks, cb = blockIdx.x - row * a.col_blocks;
     const uint32_t matrix = row / a.row_blocks, rb = row - matrix * a.row_blocks;
@@ -309,13 +329,18 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_blocks_kernel(const 
         if (T) a.scales_t[matrix * a.scales_t_matrix_stride + cb * a.scales_t_stride + rb] = (uint8_t)byte;
     }
     uint8_t* q = a.q + matrix * a.q_matrix_stride + c0;
+    uint32_t four[kTileRows];
 #pragma unroll
-    for (int i = 0; i < kTileRows; ++i)
-        if (first + i < a.rows && c0 < a.cols)
-            put_four(q + (first + i) * a.q_stride, to_e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3], inv), c0, a.cols);
-    if constexpr (T) {
+    for (int i = 0; i < kTileRows; ++i) {
+        four[i] = to_e4m3x4(v[i][0], v[i][1], v[i][2], v[i][3], inv);
+        if (first + i < a.rows && c0 < a.cols) put_four(q + (first + i) * a.q_stride, four[i], c0, a.cols);
+    }
+    if constexpr (T) {  // (the same bytes)
+        uint32_t lo[4], hi[4];
+        turn_bytes(four[0], four[1], four[2], four[3], lo);
+        turn_bytes(four[4], four[5], four[6], four[7], hi);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) turn_in(turned, lane * 4 + j, warp, v, j, inv);
+        for (int j = 0; j < 4; ++j) turn_in(turned, lane, j, warp, lo[j], hi[j]);
         __syncthreads();
         turn_out(turned, a.qt + matrix * a.qt_matrix_stride, a.qt_stride, col0, a.cols, row0, a.rows);
     }
