@@ -283,6 +283,111 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const Ro
     }
 }
 
+// The 16-bit precisions as they are: a word of two values is halved into magnitudes and compared as it stands (their order is
+// that of the bits), and a tile takes 16 registers a thread.  (As fp32 in the kernel above: dispatch of 4096 x 8 rows of 2048
+// in 81 us, 26 instructions a value.)
+constexpr uint32_t kMagnitudes = 0x7fff7fffu;
+
+// the bits of the fp32 value that these magnitude bits stand for
+template <int DT>
+__device__ __forceinline__ uint32_t widen(uint32_t half) {
+    if constexpr (DT == CIERA_BF16) return half << 16;
+    else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)half)));
+}
+template <int DT>
+__device__ __forceinline__ float2 two_values(uint32_t w) {
+    if constexpr (DT == CIERA_BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    else return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+template <int DT>
+__device__ __forceinline__ uint32_t round_four(uint2 w, float inv) {
+    const float2 a = two_values<DT>(w.x), b = two_values<DT>(w.y);
+    return to_e4m3x4(a.x, a.y, b.x, b.y, inv);
+}
+
+template <int DT, bool T>
+__global__ void __launch_bounds__(kTileThreads, T ? 2 : 3) quantize_words_kernel(const RowsArgs a, const value_t<DT>* __restrict__ x) {
+    __shared__ uint2 col_max[T ? kTileThreads / 32 : 1][32];
+    __shared__ __align__(16) float col_inv[128];
+    __shared__ __align__(16) uint2 turned[T ? 128 * 16 : 2];
+    pdl_wait();
+    const uint32_t row_tile = blockIdx.x / a.col_tiles, col_tile = blockIdx.x - row_tile * a.col_tiles;
+    const uint32_t row0 = row_tile * 128u, col0 = col_tile * 128u;
+    const uint32_t rows = a.starts ? min((uint32_t)max(a.starts[a.n_experts], 0), a.rows) : a.rows;
+    if (row0 >= rows) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t c0 = col0 + lane * 4, first = row0 + warp * kTileRows;
+    uint32_t from = first + lane;  // lane i: where row i of the warp comes from
+    bool some = lane < kTileRows && from < rows;
+    if (a.slot_of_row) {
+        const int32_t slot = some ? a.slot_of_row[from] : -1;
+        some = slot >= 0 && (uint64_t)slot < a.x_rows * a.top_k;
+        from = (uint32_t)max(slot, 0) / a.top_k;
+    } else {
+        some = some && from < a.x_rows;
+    }
+    const uint32_t live = __ballot_sync(~0u, some);
+    const bool inside = c0 < a.cols;  // (cols is a multiple of four)
+    uint2 w[kTileRows];
+#pragma unroll
+    for (int i = 0; i < kTileRows; ++i) {
+        const uint32_t r = __shfl_sync(~0u, from, i);
+        w[i] = make_uint2(0, 0);
+        if (inside && live >> i & 1) w[i] = *reinterpret_cast<const uint2*>(x + r * a.x_stride + c0);
+    }
+    uint32_t row_max = 0;  // lane i: the largest magnitude of row i
+#pragma unroll
+    for (int i = 0; i < kTileRows; ++i) {
+        const uint32_t two = __vmaxu2(w[i].x & kMagnitudes, w[i].y & kMagnitudes);
+        const uint32_t amax = __reduce_max_sync(~0u, max(two >> 16, two & 0xffffu));
+        if (lane == i) row_max = amax;
+    }
+    const uint32_t row_byte = scale_byte(widen<DT>(row_max));
+    const float row_inv = inverse_scale(row_byte);
+    if (lane < kTileRows && first + lane < rows) a.scales[(uint64_t)col_tile * a.scales_stride + first + lane] = (uint8_t)row_byte;
+    uint8_t* q = a.q + (uint64_t)first * a.q_stride + c0;
+#pragma unroll
+    for (int i = 0; i < kTileRows; ++i) {
+        const uint32_t four = round_four<DT>(w[i], __shfl_sync(~0u, row_inv, i));
+        if (first + i < rows && inside) *reinterpret_cast<uint32_t*>(q + i * a.q_stride) = four;
+    }
+    if constexpr (T) {
+        uint2 m = make_uint2(0, 0);
+#pragma unroll
+        for (int i = 0; i < kTileRows; ++i) m = make_uint2(__vmaxu2(m.x, w[i].x & kMagnitudes), __vmaxu2(m.y, w[i].y & kMagnitudes));
+        col_max[warp][lane] = m;
+        __syncthreads();
+        if (threadIdx.x < 64) {  // a thread for two columns
+            const uint32_t c = col0 + 2 * threadIdx.x;
+            uint32_t two = 0;
+#pragma unroll
+            for (int i = 0; i < kTileThreads / 32; ++i) two = __vmaxu2(two, reinterpret_cast<const uint32_t*>(col_max[i])[threadIdx.x]);
+            const uint32_t lo = scale_byte(widen<DT>(two & 0xffffu)), hi = scale_byte(widen<DT>(two >> 16));
+            if (c < a.cols) {
+                a.scales_t[(uint64_t)row_tile * a.scales_t_stride + c] = (uint8_t)lo;
+                a.scales_t[(uint64_t)row_tile * a.scales_t_stride + c + 1] = (uint8_t)hi;
+            }
+            *reinterpret_cast<float2*>(&col_inv[2 * threadIdx.x]) = make_float2(inverse_scale(lo), inverse_scale(hi));
+        }
+        __syncthreads();
+        const float4 inv = *reinterpret_cast<const float4*>(&col_inv[lane * 4]);
+        // scaled by column, rounded by row, and the bytes turned
+        uint32_t four[kTileRows];
+#pragma unroll
+        for (int i = 0; i < kTileRows; ++i) {
+            const float2 ab = two_values<DT>(w[i].x), cd = two_values<DT>(w[i].y);
+            four[i] = to_e4m3x4(ab.x * inv.x, ab.y * inv.y, cd.x * inv.z, cd.y * inv.w, 1.f);
+        }
+        uint32_t lo[4], hi[4];
+        turn_bytes(four[0], four[1], four[2], four[3], lo);
+        turn_bytes(four[4], four[5], four[6], four[7], hi);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) turn_in(turned, lane, j, warp, lo[j], hi[j]);
+        __syncthreads();
+        turn_out(turned, a.qt, a.qt_stride, col0, a.cols, row0, rows);
+    }
+}
+
 struct BlocksArgs {
     uint64_t x_stride, x_matrix_stride, q_stride, q_matrix_stride, scales_stride, scales_matrix_stride;
     uint64_t qt_stride, qt_matrix_stride, scales_t_stride, scales_t_matrix_stride;
@@ -346,6 +451,55 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_blocks_kernel(const 
     }
 }
 
+template <int DT, bool T>
+__global__ void __launch_bounds__(kTileThreads, 3) quantize_word_blocks_kernel(const BlocksArgs a, const value_t<DT>* __restrict__ x) {
+    __shared__ uint32_t warp_max[kTileThreads / 32];
+    __shared__ __align__(16) uint2 turned[T ? 128 * 16 : 2];
+    pdl_wait();
+    const uint32_t row = blockIdx.x / a.col_blocks, cb = blockIdx.x - row * a.col_blocks;
+    const uint32_t matrix = row / a.row_blocks, rb = row - matrix * a.row_blocks;
+    const uint32_t row0 = rb * 128u, col0 = cb * 128u;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t c0 = col0 + lane * 4, first = row0 + warp * kTileRows;
+    const value_t<DT>* xr = x + matrix * a.x_matrix_stride + first * a.x_stride + c0;
+    const bool inside = c0 < a.cols;  // (cols is a multiple of four)
+    uint2 w[kTileRows];
+#pragma unroll
+    for (int i = 0; i < kTileRows; ++i) {
+        w[i] = make_uint2(0, 0);
+        if (inside && first + i < a.rows) w[i] = *reinterpret_cast<const uint2*>(xr + i * a.x_stride);
+    }
+    uint32_t two = 0;
+#pragma unroll
+    for (int i = 0; i < kTileRows; ++i) two = __vmaxu2(two, __vmaxu2(w[i].x & kMagnitudes, w[i].y & kMagnitudes));
+    uint32_t amax = __reduce_max_sync(~0u, max(two >> 16, two & 0xffffu));
+    if (lane == 0) warp_max[warp] = amax;
+    __syncthreads();
+    amax = __reduce_max_sync(~0u, warp_max[lane & 15]);
+    const uint32_t byte = scale_byte(widen<DT>(amax));
+    const float inv = inverse_scale(byte);
+    if (threadIdx.x == 0) {
+        a.scales[matrix * a.scales_matrix_stride + rb * a.scales_stride + cb] = (uint8_t)byte;
+        if (T) a.scales_t[matrix * a.scales_t_matrix_stride + cb * a.scales_t_stride + rb] = (uint8_t)byte;
+    }
+    uint8_t* q = a.q + matrix * a.q_matrix_stride + first * a.q_stride + c0;
+    uint32_t four[kTileRows];
+#pragma unroll
+    for (int i = 0; i < kTileRows; ++i) {
+        four[i] = round_four<DT>(w[i], inv);
+        if (inside && first + i < a.rows) *reinterpret_cast<uint32_t*>(q + i * a.q_stride) = four[i];
+    }
+    if constexpr (T) {
+        uint32_t lo[4], hi[4];
+        turn_bytes(four[0], four[1], four[2], four[3], lo);
+        turn_bytes(four[4], four[5], four[6], four[7], hi);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) turn_in(turned, lane, j, warp, lo[j], hi[j]);
+        __syncthreads();
+        turn_out(turned, a.qt + matrix * a.qt_matrix_stride, a.qt_stride, col0, a.cols, row0, a.rows);
+    }
+}
+
 // (the stride of a single row counts for nothing)
 static bool fp8_tensor_ok(const void* p, uint64_t rows, uint64_t stride) { return aligned_to(p, 16) && (rows <= 1 || !(stride & 15)); }
 
@@ -390,6 +544,13 @@ extern "C" int ciera_fp8_quantize_rows(const ciera_fp8_rows* p, void* stream) {
             e = launch_after(quantize_rows_kernel<DT, decltype(source)::value, decltype(both)::value, decltype(four_wide)::value>, dim3((uint32_t)tiles),
                              kTileThreads, 0, (cudaStream_t)stream, a, (const value_t<DT>*)p->x, (const value_t<DT>*)p->grad);
         };
+        if constexpr (DT != CIERA_FP32) {
+            if (wide && src == CIERA_SOURCE_ROWS && !p->row_weights) {
+                e = launch_after(turned ? quantize_words_kernel<DT, true> : quantize_words_kernel<DT, false>, dim3((uint32_t)tiles), kTileThreads, 0,
+                                 (cudaStream_t)stream, a, (const value_t<DT>*)p->x);
+                return;
+            }
+        }
         const auto pick = [&](auto source) {
             const std::true_type yes;
             const std::false_type no;
@@ -435,8 +596,17 @@ extern "C" int ciera_fp8_quantize_blocks(const ciera_fp8_blocks* p, void* stream
         };
         const std::true_type yes;
         const std::false_type no;
-        if (turned) wide ? go(yes, yes) : go(yes, no);
-        else wide ? go(no, yes) : go(no, no);
+        if constexpr (DT != CIERA_FP32) {
+            if (wide) {
+                e = launch_after(turned ? quantize_word_blocks_kernel<DT, true> : quantize_word_blocks_kernel<DT, false>,
+                                 dim3((uint32_t)(rb * p->matrices * cb)), kTileThreads, 0, (cudaStream_t)stream, a, (const value_t<DT>*)p->x);
+            } else {
+                turned ? go(yes, no) : go(no, no);
+            }
+        } else {
+            if (turned) wide ? go(yes, yes) : go(yes, no);
+            else wide ? go(no, yes) : go(no, no);
+        }
     });
     if (e != cudaSuccess) return record_cuda_error(e);
     count_launch();
