@@ -1,4 +1,14 @@
-// Routing of tokens to experts, and its gradient.  A warp per token; expert e of a row is value e / 32 of lane e % 32.
+// Routing of tokens to experts, and its gradient.
+//
+// The choice is that of 64-bit arithmetic.  It is made in 32 bits (route_kernel) and looked over: where two values in the
+// order of choice, or the groups on either side of the last one kept, are nearer to each other than 32 bits can tell, and do not
+// come from the same logit and bias, the token is done again in 64 bits (route_exact).
+//
+// A warp takes up to 32 / L tokens, one after the other at first, a lane with EPL neighbouring experts, for what needs the whole
+// row (the softmax's sums, the scores); the values go to shared memory.  Then L lanes go through a token's values, each with a
+// sorted list of the largest in registers, as single words that hold the place beside the value.  The lists are merged, and the
+// few that are left are compared as they are.  Instructions bound it.  (The k largest picked one by one by the whole warp:
+// 16384 tokens of 256 experts in 8 groups 43 us, 1600 instructions a token.)
 #include <math.h>
 
 #include <type_traits>
@@ -34,115 +44,573 @@ __device__ __forceinline__ float warp_max(float v) {
 // a logit as it counts: closed (-inf) or finite
 __device__ __forceinline__ float open_logit(float x) { return isnan(x) ? -INFINITY : fminf(x, 3.402823466e38f); }
 
-// One token's choice in 64 bits.  x: the lane's logits (-inf: closed).  c: E doubles of the warp's own in shared memory.
-template <int EPL>
-__device__ void route_exact(const float (&x)[EPL], const RouteArgs& a, const float* __restrict__ bias, double* c, int lane,
-                            int32_t* __restrict__ experts, float* __restrict__ weights) {
-    const int E = (int)a.n_experts;
+// The lane's EPL logits; whole: one access for up to 16 bytes of them.
+template <int DT, int EPL>
+__device__ __forceinline__ void load_logits(const value_t<DT>* row, uint32_t E, bool whole, int lane, float (&x)[EPL]) {
+    const uint32_t e0 = lane * EPL;
+    if (whole && e0 + EPL <= E) {
+        load_values<DT, EPL>(row + e0, x);
+    } else {
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) x[j] = e0 + j < E ? ValueOf<DT>::get(row[e0 + j]) : -INFINITY;
+    }
+}
+
+// 64-bit numbers as unsigned integers of the same order, which compare in a fraction of the time; 0 for -inf and NaN
+__device__ __forceinline__ unsigned long long ordered64(double v) {
+    const unsigned long long u = (unsigned long long)__double_as_longlong(v == 0.0 ? 0.0 : v);
+    return v > -INFINITY ? (u >> 63 ? ~u : u | 1ull << 63) : 0ull;
+}
+__device__ __forceinline__ double unordered64(unsigned long long u) {
+    return u ? __longlong_as_double((long long)(u >> 63 ? u & ~(1ull << 63) : ~u)) : -INFINITY;
+}
+
+// One token's choice in 64 bits.  c: n_experts words of 64 bits of the warp's own in shared memory.  What a batch waits for when
+// it has such a token, so with all the parallelism there is: a lane's experts side by side, several lanes to a group.
+template <int DT, int EPL>
+__device__ __noinline__ void route_exact(const value_t<DT>* row, const RouteArgs& a, const float* __restrict__ bias, unsigned long long* c,
+                                         int32_t* __restrict__ experts, float* __restrict__ weights) {
+    const uint32_t E = a.n_experts, lane = threadIdx.x & 31, e0 = lane * EPL;
+    float x[EPL];
+    load_logits<DT, EPL>(row, E, false, (int)lane, x);
     float m = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < EPL; ++j) m = fmaxf(m, x[j]);
+    for (int j = 0; j < EPL; ++j) {
+        x[j] = open_logit(x[j]);
+        m = fmaxf(m, x[j]);
+    }
     m = warp_max(m);
-    double s[EPL], v[EPL];
-    double total = 0.0;
+    double s[EPL], total = 0.0;
 #pragma unroll
     for (int j = 0; j < EPL; ++j) {
-        if (x[j] == -INFINITY) s[j] = 0.0;
-        else if (a.sigmoid) s[j] = 1.0 / (1.0 + exp(-(double)x[j]));
-        else total += s[j] = exp((double)x[j] - (double)m);
+        s[j] = 0.0;
+        if (x[j] == -INFINITY) continue;
+        s[j] = exp(a.sigmoid ? -(double)x[j] : (double)x[j] - (double)m);
+        total += s[j];
     }
-    if (!a.sigmoid) {
-        total = warp_sum(total);
-#pragma unroll
-        for (int j = 0; j < EPL; ++j) s[j] = total > 0.0 ? s[j] / total : 0.0;
-    }
+    if (!a.sigmoid) total = warp_sum(total);
+    unsigned long long key[EPL];
 #pragma unroll
     for (int j = 0; j < EPL; ++j) {
-        const int e = j * 32 + lane;
-        v[j] = s[j] + (bias && e < E ? (double)bias[e] : 0.0);
-        if (x[j] == -INFINITY || isnan(v[j])) v[j] = -INFINITY;
+        key[j] = 0ull;
+        if (x[j] == -INFINITY) continue;
+        s[j] = a.sigmoid ? 1.0 / (1.0 + s[j]) : s[j] / total;
+        key[j] = ordered64(s[j] + (bias ? (double)bias[e0 + j] : 0.0));
     }
     if (a.top_groups < a.n_groups) {
 #pragma unroll
         for (int j = 0; j < EPL; ++j)
-            if (j * 32 + lane < E) c[j * 32 + lane] = v[j];
+            if (e0 + j < E) c[e0 + j] = key[j];
         __syncwarp();
-        double g = -INFINITY;  // lane i: value of group i
-        if (lane < (int)a.n_groups) {
-            double first = -INFINITY, second = -INFINITY;
-            for (uint32_t i = 0; i < a.group_size; ++i) {
-                const double y = c[lane * a.group_size + i];
-                if (y > first) second = first, first = y;
-                else if (y > second) second = y;
-            }
-            g = first;
-            if (a.group_best > 1 && second > -INFINITY) g += second;
+        uint32_t per = 32;  // lanes of a group
+        while (per * a.n_groups > 32) per /= 2;
+        const uint32_t g = lane / per;
+        unsigned long long most = 0ull, second = 0ull;
+        const auto see = [&](unsigned long long y) {
+            second = max(second, min(most, y));
+            most = max(most, y);
+        };
+        if (g < a.n_groups)
+            for (uint32_t i = lane % per; i < a.group_size; i += per) see(c[g * a.group_size + i]);
+        for (uint32_t d = 1; d < per; d *= 2) {
+            const unsigned long long om = __shfl_xor_sync(~0u, most, d), os = __shfl_xor_sync(~0u, second, d);
+            see(om);
+            second = max(second, os);
         }
+        const unsigned long long value = a.group_best > 1 && second ? ordered64(unordered64(most) + unordered64(second)) : most;
+        uint32_t rank = 0;
+        for (uint32_t i = 0; i < a.n_groups; ++i) {
+            const unsigned long long o = __shfl_sync(~0u, value, i * per);
+            rank += o > value || (o == value && i < g);
+        }
+        const uint32_t keep = __ballot_sync(~0u, value && rank < a.top_groups);
+#pragma unroll
+        for (int j = 0; j < EPL; ++j)
+            if (e0 + j < E && !(keep >> ((e0 + j) / a.group_size * per) & 1u)) key[j] = 0ull;
         __syncwarp();
-        uint32_t keep = 0;
-        bool mine = g > -INFINITY;
-        for (uint32_t r = 0; r < a.top_groups; ++r) {
-            double best = mine ? g : -INFINITY;
-#pragma unroll
-            for (int d = 16; d; d >>= 1) best = fmax(best, __shfl_xor_sync(~0u, best, d));
-            const uint32_t at = __ballot_sync(~0u, mine && g == best);
-            if (!at) break;
-            const int w = __ffs(at) - 1;
-            keep |= 1u << w;
-            if (lane == w) mine = false;
-        }
-#pragma unroll
-        for (int j = 0; j < EPL; ++j) {
-            const uint32_t e = j * 32 + lane;
-            if (e < a.n_experts && !((keep >> (e / a.group_size)) & 1u)) v[j] = -INFINITY;
-        }
     }
-    // lane i ends up with choice i
+    // lane i ends up with choice i: the largest, by the upper half first
     int chosen = -1;
     double ws = 0.0, sum = 0.0;
     for (uint32_t r = 0; r < a.top_k; ++r) {
-        double best = -INFINITY, bs = 0.0;
-        int be = 1 << 30;
+        unsigned long long best = 0ull;
+        double bs = 0.0;
+        int be = 0;
 #pragma unroll
         for (int j = 0; j < EPL; ++j)
-            if (v[j] > best) best = v[j], be = j * 32 + lane, bs = s[j];
-#pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            const double ob = __shfl_xor_sync(~0u, best, d), os = __shfl_xor_sync(~0u, bs, d);
-            const int oe = __shfl_xor_sync(~0u, be, d);
-            if (ob > best || (ob == best && oe < be)) best = ob, be = oe, bs = os;
-        }
-        if (be == 1 << 30) break;
-        if (lane == (int)r) chosen = be, ws = bs;
-        sum += bs;
+            if (key[j] > best) best = key[j], be = (int)e0 + j, bs = s[j];
+        const uint32_t up = __reduce_max_sync(~0u, (uint32_t)(best >> 32));
+        if (!up) break;
+        const uint32_t down = __reduce_max_sync(~0u, (uint32_t)(best >> 32) == up ? (uint32_t)best : 0u);
+        const int w = __ffs(__ballot_sync(~0u, (uint32_t)(best >> 32) == up && (uint32_t)best == down)) - 1;  // (the lowest of equal ones)
+        const double taken = __shfl_sync(~0u, bs, w);
+        const int e = __shfl_sync(~0u, be, w);
+        if (lane == r) chosen = e, ws = taken;
+        sum += taken;
 #pragma unroll
         for (int j = 0; j < EPL; ++j)
-            if (j * 32 + lane == be) v[j] = -INFINITY;
+            if ((int)e0 + j == e) key[j] = 0ull;
     }
-    if (lane < (int)a.top_k) {
+    if (lane < a.top_k) {
         if (a.renormalise) ws = sum > 0.0 ? ws / sum : 0.0;
         experts[lane] = chosen;
         weights[lane] = (float)(ws * (double)a.scale);
     }
+    __syncwarp();
 }
 
+// a float as an unsigned integer of the same order; every number is above 0
+__device__ __forceinline__ uint32_t ordered(float f) {
+    const uint32_t b = __float_as_uint(f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+
+__device__ __forceinline__ float sigmoid_of(float x) { return __fdividef(1.f, 1.f + expf(-x)); }
+
+// Scores in 32 bits are off by less than this part of themselves: sigmoid by an exponential, a sum and a reciprocal of a step or
+// two each; softmax also by what all its scores share, a sum of up to 1024 terms in a tree over 32 lanes.
+constexpr float kUnsureSigmoid = 1e-6f, kUnsureSoftmax = 4e-6f;
+
+constexpr uint32_t kClosed = 0x007fffffu;  // ordered(-inf): words up to here are of closed experts
+
+// The lane's words in falling order.
+template <int EPL>
+__device__ __forceinline__ void sort_words(uint32_t (&key)[EPL]) {
+#pragma unroll
+    for (int run = 2; run <= EPL; run *= 2)
+#pragma unroll
+        for (int step = run / 2; step; step /= 2)
+#pragma unroll
+            for (int i = 0; i < EPL; ++i)
+                if (!(i & step)) {
+                    const uint32_t hi = max(key[i], key[i + step]), lo = min(key[i], key[i + step]);
+                    const bool falling = !(i & run) || run == EPL;
+                    key[i] = falling ? hi : lo;
+                    key[i + step] = falling ? lo : hi;
+                }
+}
+
+// Few tokens: a warp for each, which picks the largest one by one.
 template <int DT, int EPL>
-__global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs a, const value_t<DT>* __restrict__ logits,
-                                                                uint64_t n_tokens, uint64_t stride,
-                                                                const float* __restrict__ bias, int32_t* __restrict__ experts,
-                                                                float* __restrict__ weights) {
-    extern __shared__ double route_smem[];
+__global__ void __launch_bounds__(kRouteWarps * 32)
+    route_few_kernel(const RouteArgs a, const value_t<DT>* __restrict__ logits, uint64_t n_tokens, uint64_t stride, int whole,
+                     const float* __restrict__ bias, int32_t* __restrict__ experts, float* __restrict__ weights) {
+    extern __shared__ __align__(16) float route_smem[];
+    __shared__ int chosen[kRouteWarps][32];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    double* c = route_smem + (size_t)warp * a.n_experts;
-    for (uint64_t t = (uint64_t)blockIdx.x * kRouteWarps + warp; t < n_tokens; t += (uint64_t)gridDim.x * kRouteWarps) {
-        float x[EPL];
+    const uint32_t E = a.n_experts, e0 = lane * EPL;
+    float* scratch = route_smem + warp * 2 * E;
+    const uint64_t t = (uint64_t)blockIdx.x * kRouteWarps + warp;
+    if (t >= n_tokens) return;
+    const bool grouped = a.top_groups < a.n_groups, scored = bias || grouped;
+    const float unsure = a.sigmoid ? kUnsureSigmoid : kUnsureSoftmax;
+    const value_t<DT>* row = logits + t * stride;
+    float x[EPL], c[EPL], m = 0.f, inv = 1.f;
+    load_logits<DT, EPL>(row, E, whole, lane, x);
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) x[j] = open_logit(x[j]);
+    if (!a.sigmoid) {
+        m = x[0];
+#pragma unroll
+        for (int j = 1; j < EPL; ++j) m = fmaxf(m, x[j]);
+        m = unordered(__reduce_max_sync(~0u, ordered(m)));
+        if (m == -INFINITY) m = 0.f;  // nothing is open
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) sum += c[j] = expf(x[j] - m);
+        sum = warp_sum(sum);
+        inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
+    }
+    // what the choice goes by: the logits where there is no bias (scores rise with them), else s + b
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) {
+        if (!scored || x[j] == -INFINITY) c[j] = x[j];
+        else c[j] = (a.sigmoid ? sigmoid_of(x[j]) : c[j] * inv) + (bias ? bias[e0 + j] : 0.f);
+        if (isnan(c[j])) c[j] = -INFINITY;
+    }
+    bool sure = a.top_k < 32;  // (there is no lane for the first that is not chosen)
+    if (grouped) {
+#pragma unroll
+        for (int j = 0; j < EPL; ++j)
+            if (e0 + j < E) scratch[e0 + j] = c[j];
+        __syncwarp();
+        uint32_t per = 32;  // lanes of a group
+        while (per * a.n_groups > 32) per /= 2;
+        const uint32_t g = lane / per;
+        float most = -INFINITY, second = -INFINITY;
+        if (g < a.n_groups)
+            for (uint32_t i = lane % per; i < a.group_size; i += per) {
+                const float y = scratch[g * a.group_size + i];
+                second = fmaxf(second, fminf(most, y));
+                most = fmaxf(most, y);
+            }
+        for (uint32_t d = 1; d < per; d *= 2) {
+            const float om = __shfl_xor_sync(~0u, most, d), os = __shfl_xor_sync(~0u, second, d);
+            second = fmaxf(fmaxf(second, os), fminf(most, om));
+            most = fmaxf(most, om);
+        }
+        const float value = a.group_best > 1 && second > -INFINITY ? most + second : most;
+        uint32_t rank = 0;
+        for (uint32_t i = 0; i < a.n_groups; ++i) {
+            const float o = __shfl_sync(~0u, value, i * per);
+            rank += o > value || (o == value && i < g);
+        }
+        const bool open = g < a.n_groups && value > -INFINITY, stays = open && rank < a.top_groups;
+        const uint32_t keep = __ballot_sync(~0u, stays);
+        const float last = -unordered(__reduce_max_sync(~0u, ordered(stays ? -value : -INFINITY)));
+        const float next = unordered(__reduce_max_sync(~0u, ordered(open && !stays ? value : -INFINITY)));
+        if (next > -INFINITY) sure = sure && last - next > unsure * (fabsf(last) + fabsf(next) + (bias ? 4.f : 0.f));
+#pragma unroll
+        for (int j = 0; j < EPL; ++j)
+            if (e0 + j < E && !(keep >> ((e0 + j) / a.group_size * per) & 1u)) c[j] = -INFINITY;
+        __syncwarp();
+    }
+    // order of the value, the last bits its place in the lane, lower places higher
+    uint32_t key[EPL];
+    constexpr uint32_t kPlace = EPL - 1;
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) key[j] = (ordered(c[j]) & ~kPlace) | (kPlace - j);
+    sort_words<EPL>(key);
+    // One more than asked for, to see how near it came.  The lane that has the choice says so itself: where two have the same,
+    // the lower one.
+    chosen[warp][lane] = -1;
+    __syncwarp();
+    for (uint32_t r = 0; r <= a.top_k; ++r) {
+        const uint32_t best = key[0] | kPlace, top = __reduce_max_sync(~0u, best);
+        if (top <= (kClosed | kPlace)) break;
+        const uint32_t same = __ballot_sync(~0u, best == top);
+        const bool won = best == top && !(same & ((1u << lane) - 1));
+        if (won && r < 32) chosen[warp][r] = (int)(e0 + kPlace - (key[0] & kPlace));
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) key[j] = won ? (j + 1 < EPL ? key[j + 1] : 0u) : key[j];
+    }
+    __syncwarp();
+    const int mine = chosen[warp][lane];  // lane r: choice r
+    float xm = 0.f, sm = 0.f, bm = 0.f;
+    if (mine >= 0) {
+        xm = open_logit(ValueOf<DT>::get(row[mine]));
+        sm = a.sigmoid ? sigmoid_of(xm) : expf(xm - m) * inv;
+        bm = bias ? bias[mine] : 0.f;
+    }
+    const float y = scored ? sm + bm : xm;
+    const float xn = __shfl_down_sync(~0u, xm, 1), bn = __shfl_down_sync(~0u, bm, 1), yn = __shfl_down_sync(~0u, y, 1);
+    const int other = __shfl_down_sync(~0u, mine, 1);
+    // where 64 bits no longer tell scores of different logits apart
+    if (mine >= 0 && !scored) sure = sure && (a.sigmoid ? xm < 16.f && xm > -600.f : xm - m > -600.f);
+    // (two values that share a word's bits are out of order at most by what those bits are worth)
+    if (lane < 31 && mine >= 0 && other >= 0 && !(xm == xn && bm == bn))
+        sure = sure && y - yn > (scored ? unsure * (sm + fabsf(y)) : 1e-8f) + (DT == CIERA_FP32 || scored ? 1e-5f * fabsf(y) : 0.f);
+    if (!__all_sync(~0u, sure)) {
+        route_exact<DT, EPL>(row, a, bias, reinterpret_cast<unsigned long long*>(scratch), experts + t * a.top_k, weights + t * a.top_k);
+        return;
+    }
+    if (lane >= (int)a.top_k || mine < 0) sm = 0.f;
+    if (a.renormalise) {
+        const float sum = warp_sum(sm);
+        sm = sum > 0.f ? sm / sum : 0.f;
+    }
+    if (lane < (int)a.top_k) {
+        experts[t * a.top_k + lane] = mine;
+        weights[t * a.top_k + lane] = sm * a.scale;
+    }
+}
+
+// `lanes` lists of `KL` words in falling order, one in each of that many neighbouring lanes: all get the KL largest of all.
+template <int KL, int L>
+__device__ __forceinline__ void merge_lists(uint32_t (&list)[KL]) {
+    constexpr int N = KL <= 16 ? 16 : KL <= 32 ? 32 : 64;
+#pragma unroll
+    for (int d = 1; d < L; d *= 2) {
+        uint32_t t[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) t[i] = i < KL ? list[i] : 0u;
+#pragma unroll
+        for (int i = 0; i < KL; ++i) {
+            const uint32_t o = __shfl_xor_sync(~0u, list[i], d);
+            t[N - 1 - i] = max(t[N - 1 - i], o);  // the N largest, falling and then rising
+        }
+#pragma unroll
+        for (int step = N / 2; step; step /= 2)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (!(i & step)) {
+                    const uint32_t hi = max(t[i], t[i + step]), lo = min(t[i], t[i + step]);
+                    t[i] = hi;
+                    t[i + step] = lo;
+                }
+#pragma unroll
+        for (int i = 0; i < KL; ++i) list[i] = t[i];
+    }
+}
+
+template <int KL>
+__device__ __forceinline__ void put_in_list(uint32_t (&list)[KL], uint32_t v) {
+#pragma unroll
+    for (int i = KL - 1; i > 0; --i) list[i] = max(list[i], min(list[i - 1], v));
+    list[0] = max(list[0], v);
+}
+
+template <int EPL>
+constexpr int kTokenLanes = EPL <= 8 ? 4 : 16;  // L
+
+// floats between the tokens' rows in shared memory: lanes that read 16 bytes together find them in banks of their own
+template <int EPL>
+__host__ __device__ inline uint32_t row_floats(uint32_t n_experts) {
+    return (n_experts + 31) / 32 * 32 + 16;
+}
+// of a warp: its tokens' rows, two floats a token of the softmax, 32 group values a token
+template <int EPL>
+__host__ __device__ inline uint32_t warp_floats(uint32_t n_experts) {
+    return 32 / kTokenLanes<EPL> * (row_floats<EPL>(n_experts) + 2 + 32);
+}
+
+// KL: at least top_k + 2 (one more than asked for, to see how near it came, and one for values that share a word's bits)
+template <int DT, int EPL, int KL>
+__global__ void __launch_bounds__(kRouteWarps * 32)
+    route_kernel(const RouteArgs a, const value_t<DT>* __restrict__ logits, uint64_t n_tokens, uint32_t tokens_each, uint64_t stride,
+                 int whole, const float* __restrict__ bias, int32_t* __restrict__ experts, float* __restrict__ weights) {
+    constexpr int L = kTokenLanes<EPL>, Q = (KL + L - 1) / L;
+    extern __shared__ __align__(16) float route_smem[];
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t E = a.n_experts, e0 = lane * EPL, pitch = row_floats<EPL>(E);
+    float* rows = route_smem + warp * warp_floats<EPL>(E);
+    float* stats = rows + 32 / L * pitch;
+    float* group_values = stats + 32 / L * 2;
+    const bool grouped = a.top_groups < a.n_groups, scored = bias || grouped;
+    const uint32_t place_mask = E > 1 ? ~0u >> __clz(E - 1) : 0u;  // a word's last bits: its place, lower places higher
+    const uint64_t first = ((uint64_t)blockIdx.x * kRouteWarps + warp) * tokens_each;
+    if (first >= n_tokens) return;
+    const uint32_t here = (uint32_t)min((uint64_t)tokens_each, n_tokens - first);
+
+    // the whole rows
+    {
+        constexpr int U = EPL <= 2 ? 4 : EPL <= 8 ? 2 : 1;  // tokens side by side
+        float b[EPL], next[U][EPL];
 #pragma unroll
         for (int j = 0; j < EPL; ++j) {
-            const uint32_t e = j * 32 + lane;
-            x[j] = e < a.n_experts ? open_logit(ValueOf<DT>::get(logits[t * stride + e])) : -INFINITY;
+            b[j] = bias && e0 + j < E ? bias[e0 + j] : 0.f;
+            if (isnan(b[j])) b[j] = -INFINITY;
         }
-        route_exact<EPL>(x, a, bias, c, lane, experts + t * a.top_k, weights + t * a.top_k);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (u < (int)here) load_logits<DT, EPL>(logits + (first + u) * stride, E, whole, lane, next[u]);
+        for (uint32_t i = 0; i < here; i += U) {
+            float x[U][EPL], c[U][EPL], m[U], inv[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int j = 0; j < EPL; ++j) x[u][j] = open_logit(next[u][j]);
+                if (i + U + u < here) load_logits<DT, EPL>(logits + (first + i + U + u) * stride, E, whole, lane, next[u]);
+                inv[u] = 1.f;
+            }
+            if (!a.sigmoid) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    m[u] = x[u][0];
+#pragma unroll
+                    for (int j = 1; j < EPL; ++j) m[u] = fmaxf(m[u], x[u][j]);
+                    m[u] = unordered(__reduce_max_sync(~0u, ordered(m[u])));
+                    if (m[u] == -INFINITY) m[u] = 0.f;  // nothing is open
+                    inv[u] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < EPL; ++j) inv[u] += c[u][j] = expf(x[u][j] - m[u]);
+                }
+#pragma unroll
+                for (int d = 16; d; d >>= 1)
+#pragma unroll
+                    for (int u = 0; u < U; ++u) inv[u] += __shfl_xor_sync(~0u, inv[u], d);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    inv[u] = inv[u] > 0.f ? __fdividef(1.f, inv[u]) : 0.f;
+                    if (lane == 0 && i + u < here) stats[2 * (i + u)] = m[u], stats[2 * (i + u) + 1] = inv[u];
+                }
+            }
+            // what the choice goes by: the logits where there is no bias (scores rise with them), else s + b
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i + u >= here || e0 + EPL > pitch) continue;  // (a multiple of the piece)
+                Pack<float, EPL> v;
+#pragma unroll
+                for (int j = 0; j < EPL; ++j) {
+                    float y = x[u][j];
+                    if (scored && y > -INFINITY) y = (a.sigmoid ? __fdividef(1.f, 1.f + __expf(-y)) : c[u][j] * inv[u]) + b[j];
+                    v.v[j] = e0 + j < E ? y : -INFINITY;
+                }
+                *reinterpret_cast<Pack<float, EPL>*>(rows + (i + u) * pitch + e0) = v;
+            }
+        }
+    }
+    __syncwarp();
+
+    // L lanes a token
+    const uint32_t l = lane % L, mine = lane / L;
+    const bool busy = mine < here;
+    const uint64_t t = first + (busy ? mine : 0);
+    const float* row = rows + (busy ? mine : 0) * pitch;
+    const value_t<DT>* row_logits = logits + t * stride;
+    bool sure = true;
+    uint32_t list[KL];
+#pragma unroll
+    for (int i = 0; i < KL; ++i) list[i] = 0;
+    const float unsure = a.sigmoid ? kUnsureSigmoid : kUnsureSoftmax;
+    const auto put = [&](float y, uint32_t e) { put_in_list<KL>(list, (ordered(y) & ~place_mask) | ((place_mask - e) & place_mask)); };
+    if (grouped) {
+        float* values = group_values + (busy ? mine : 0) * 32;
+        const bool fours = !(a.group_size & 3);
+        for (uint32_t g = l; g < a.n_groups; g += L) {
+            float most = -INFINITY, second = -INFINITY;
+            const auto see = [&](float y) {
+                second = fmaxf(second, fminf(most, y));
+                most = fmaxf(most, y);
+            };
+            if (fours) {
+                const uint32_t n = a.group_size / 4;
+                uint32_t e = l < n ? l : 0;  // (each lane begins elsewhere in its group: banks)
+                for (uint32_t i = 0; i < n; ++i) {
+                    const float4 y = *reinterpret_cast<const float4*>(row + g * a.group_size + 4 * e);
+                    see(y.x);
+                    see(y.y);
+                    see(y.z);
+                    see(y.w);
+                    if (++e == n) e = 0;
+                }
+            } else {
+                for (uint32_t i = 0; i < a.group_size; ++i) see(row[g * a.group_size + i]);
+            }
+            values[g] = a.group_best > 1 && second > -INFINITY ? most + second : most;
+        }
+        __syncwarp();
+        // the groups that stay, and how far the first that goes is from the last of them
+        uint32_t keep = 0;
+        float last = INFINITY, next = -INFINITY;
+        for (uint32_t g = l; g < a.n_groups; g += L) {
+            const float v = values[g];
+            uint32_t rank = 0;
+            for (uint32_t i = 0; i < a.n_groups; ++i) {
+                const float o = values[i];
+                rank += o > v || (o == v && i < g);
+            }
+            if (v > -INFINITY && rank < a.top_groups) keep |= 1u << g, last = fminf(last, v);
+            else next = fmaxf(next, v);
+        }
+#pragma unroll
+        for (int d = 1; d < L; d *= 2) {
+            last = fminf(last, __shfl_xor_sync(~0u, last, d));
+            next = fmaxf(next, __shfl_xor_sync(~0u, next, d));
+            keep |= __shfl_xor_sync(~0u, keep, d);
+        }
+        // (a bias of the other sign makes a sum small; the scores in it are still up to 1 each)
+        if (next > -INFINITY) sure = last - next > unsure * (fabsf(last) + fabsf(next) + (bias ? 4.f : 0.f));
+        for (uint32_t left = keep; left; left &= left - 1) {
+            const uint32_t at = (__ffs(left) - 1) * a.group_size;
+            if (fours) {
+                for (uint32_t e = at + 4 * l; e < at + a.group_size; e += 4 * L) {
+                    const float4 y = *reinterpret_cast<const float4*>(row + e);
+                    put(y.x, e);
+                    put(y.y, e + 1);
+                    put(y.z, e + 2);
+                    put(y.w, e + 3);
+                }
+            } else {
+                for (uint32_t e = at + l; e < at + a.group_size; e += L) put(row[e], e);
+            }
+        }
+        __syncwarp();
+    } else {
+        for (uint32_t e = 4 * l; e < E; e += 4 * L) {  // (behind the last expert: closed ones)
+            const float4 y = *reinterpret_cast<const float4*>(row + e);
+            put(y.x, e);
+            put(y.y, e + 1);
+            put(y.z, e + 2);
+            put(y.w, e + 3);
+        }
+    }
+    __syncwarp();
+    merge_lists<KL, L>(list);
+
+    // what is left, compared as it is: candidate i is with lane i % L
+    uint32_t w[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) w[q] = 0;
+#pragma unroll
+    for (int i = 0; i < KL; ++i)
+        if (l == i % L) w[i / L] = list[i];
+    float x[Q], s[Q], y[Q], b[Q];
+    uint32_t rank[Q];
+    int at[Q];
+    const float m = a.sigmoid ? 0.f : stats[2 * (busy ? mine : 0)], inv = a.sigmoid ? 1.f : stats[2 * (busy ? mine : 0) + 1];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const bool open = w[q] > (kClosed | place_mask);
+        at[q] = open ? (int)(place_mask - (w[q] & place_mask)) : -1;
+        x[q] = open ? open_logit(ValueOf<DT>::get(row_logits[at[q]])) : -INFINITY;
+        b[q] = open && bias ? bias[at[q]] : 0.f;
+        s[q] = !open ? 0.f : a.sigmoid ? sigmoid_of(x[q]) : expf(x[q] - m) * inv;
+        y[q] = !open ? -INFINITY : scored ? s[q] + b[q] : x[q];
+        rank[q] = 0;
+        // where 64 bits no longer tell scores of different logits apart
+        if (open && !scored) sure = sure && (a.sigmoid ? x[q] < 16.f && x[q] > -600.f : x[q] - m > -600.f);
+    }
+    bool near[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) near[q] = false;
+#pragma unroll
+    for (int i = 0; i < KL; ++i) {
+        const int from = lane / L * L + i % L;
+        const float yi = __shfl_sync(~0u, y[i / L], from), xi = __shfl_sync(~0u, x[i / L], from), bi = __shfl_sync(~0u, b[i / L], from);
+        const int ei = __shfl_sync(~0u, at[i / L], from);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            rank[q] += yi > y[q] || (yi == y[q] && ei < at[q]);
+            const float margin = scored ? unsure * (s[q] + fabsf(y[q])) : 1e-8f;  // (logits below 16 this far apart: 64 bits tell)
+            if (ei >= 0 && at[q] >= 0 && !(xi == x[q] && bi == b[q])) near[q] |= !(fabsf(yi - y[q]) > margin);
+        }
+    }
+    // what is not on the list is at most what the last word of it may stand for
+    const uint32_t last = list[KL - 1];
+    const float beyond = last > (kClosed | place_mask) ? unordered(last | place_mask) : -INFINITY;
+    const bool exact_words = DT != CIERA_FP32 && !scored && !(place_mask >> 13);  // (13 bits and more of such a logit are zero)
+    float sum = 0.f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        if (at[q] < 0 || rank[q] >= a.top_k) {
+            if (q * L + (int)l < KL && at[q] >= 0 && rank[q] == a.top_k) sure = sure && !near[q];
+            s[q] = 0.f;
+            continue;
+        }
+        sure = sure && !near[q] && (exact_words || beyond == -INFINITY || y[q] - beyond > 2.f * unsure * (s[q] + fabsf(y[q])));
+        sum += s[q];
+    }
+    if (a.renormalise) {
+#pragma unroll
+        for (int d = 1; d < L; d *= 2) sum += __shfl_xor_sync(~0u, sum, d);
+    }
+    int found = 0;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) found += at[q] >= 0;
+#pragma unroll
+    for (int d = 1; d < L; d *= 2) found += __shfl_xor_sync(~0u, found, d);
+    if (busy) {
+        int32_t* to = experts + t * a.top_k;
+        float* tw = weights + t * a.top_k;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            if (at[q] < 0 || rank[q] >= a.top_k) continue;
+            to[rank[q]] = at[q];
+            tw[rank[q]] = (a.renormalise ? (sum > 0.f ? s[q] / sum : 0.f) : s[q]) * a.scale;
+        }
+        for (uint32_t r = found + l; r < a.top_k; r += L) to[r] = -1, tw[r] = 0.f;
+    }
+    uint32_t again = __ballot_sync(~0u, busy && !sure);
+    while (again) {
+        const uint32_t which = (__ffs(again) - 1) / L;
+        again &= ~((L == 32 ? ~0u : (1u << L) - 1) << (which * L));
+        __syncwarp();  // (the rows are its scratch; what was written above is written over)
+        route_exact<DT, EPL>(logits + (first + which) * stride, a, bias, reinterpret_cast<unsigned long long*>(rows), experts + (first + which) * a.top_k,
+                             weights + (first + which) * a.top_k);
     }
 }
 
@@ -151,72 +619,87 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs
 // sigmoid: dl = s * (1 - s) * ds.
 template <int DT, int EPL>
 __global__ void __launch_bounds__(kRouteWarps * 32)
-    route_backward_kernel(const RouteArgs a, const value_t<DT>* __restrict__ logits, uint64_t n_tokens, uint64_t stride,
+    route_backward_kernel(const RouteArgs a, const value_t<DT>* __restrict__ logits, uint64_t n_tokens, uint64_t stride, int whole,
                           const int32_t* __restrict__ experts, const float* __restrict__ dweights,
                           value_t<DT>* __restrict__ dlogits, uint64_t dstride) {
+    __shared__ __align__(16) float spread[kRouteWarps][32 * EPL];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t E = a.n_experts, e0 = lane * EPL;
+    float* all = spread[warp];
     for (uint64_t t = (uint64_t)blockIdx.x * kRouteWarps + warp; t < n_tokens; t += (uint64_t)gridDim.x * kRouteWarps) {
         const value_t<DT>* row = logits + t * stride;
-        float x[EPL], s[EPL];
         int id = -1;
         float dw = 0.f, xk = -INFINITY;
         if (lane < (int)a.top_k) {
             id = experts[t * a.top_k + lane];
-            if ((uint32_t)id >= a.n_experts) id = -1;
-            if (id >= 0) {
-                dw = dweights[t * a.top_k + lane];
-                xk = open_logit(ValueOf<DT>::get(row[id]));
-            }
+            if ((uint32_t)id >= E) id = -1;
+            dw = dweights[t * a.top_k + lane];
         }
-        float m = -INFINITY;
+        float x[EPL], s[EPL];
+        load_logits<DT, EPL>(row, E, whole, lane, x);
 #pragma unroll
-        for (int j = 0; j < EPL; ++j) {
-            const uint32_t e = j * 32 + lane;
-            x[j] = e < a.n_experts ? open_logit(ValueOf<DT>::get(row[e])) : -INFINITY;
-            m = fmaxf(m, x[j]);
-        }
-        float inv = 1.f, sk;
+        for (int j = 0; j < EPL; ++j) x[j] = open_logit(x[j]);
+        if (id < 0) dw = 0.f;
+        else xk = open_logit(ValueOf<DT>::get(row[id]));
+        float sk;
         if (a.sigmoid) {
 #pragma unroll
-            for (int j = 0; j < EPL; ++j) s[j] = 1.f / (1.f + expf(-x[j]));
-            sk = 1.f / (1.f + expf(-xk));
+            for (int j = 0; j < EPL; ++j) s[j] = sigmoid_of(x[j]);
+            sk = sigmoid_of(xk);
         } else {
-            m = warp_max(m);
+            float m = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < EPL; ++j) m = fmaxf(m, x[j]);
+            m = unordered(__reduce_max_sync(~0u, ordered(m)));
+            if (m == -INFINITY) m = 0.f;
             float sum = 0.f;
 #pragma unroll
-            for (int j = 0; j < EPL; ++j) sum += s[j] = x[j] == -INFINITY ? 0.f : expf(x[j] - m);
+            for (int j = 0; j < EPL; ++j) sum += s[j] = expf(x[j] - m);
             sum = warp_sum(sum);
-            inv = sum > 0.f ? 1.f / sum : 0.f;
+            const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
 #pragma unroll
             for (int j = 0; j < EPL; ++j) s[j] *= inv;
-            sk = xk == -INFINITY ? 0.f : expf(xk - m) * inv;
+            sk = expf(xk - m) * inv;
         }
         float d = dw * a.scale, dot = 0.f;
         if (a.renormalise) {
             const float total = warp_sum(sk);
-            const float it = total > 0.f ? 1.f / total : 0.f;
+            const float it = total > 0.f ? __fdividef(1.f, total) : 0.f;
             d = (d - warp_sum(d * sk) * it) * it;
         } else if (!a.sigmoid) {
             dot = warp_sum(d * sk);
         }
-        float ds[EPL];
-#pragma unroll
-        for (int j = 0; j < EPL; ++j) ds[j] = 0.f;
-        for (uint32_t r = 0; r < a.top_k; ++r) {
-            const int e = __shfl_sync(~0u, id, (int)r);
-            const float dr = __shfl_sync(~0u, d, (int)r);
-#pragma unroll
-            for (int j = 0; j < EPL; ++j)
-                if (e == j * 32 + lane) ds[j] += dr;
+        // an expert that is named more than once gets the sum, in the order of the choices
+        const uint32_t same = __match_any_sync(~0u, id);
+        if (__any_sync(~0u, id >= 0 && __popc(same) > 1)) {
+            float sum = 0.f;
+            for (uint32_t r = 0; r < a.top_k; ++r) {
+                const float dr = __shfl_sync(~0u, d, (int)r);
+                if (same >> r & 1u) sum += dr;
+            }
+            d = sum;
         }
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) all[j * 32 + lane] = 0.f;
+        __syncwarp();
+        if (id >= 0) all[id] = d;  // (the same sum from each of the same)
+        __syncwarp();
+        float ds[EPL];
+        const Pack<float, EPL> mine = *reinterpret_cast<const Pack<float, EPL>*>(all + e0);
 #pragma unroll
         for (int j = 0; j < EPL; ++j) {
-            const uint32_t e = j * 32 + lane;
-            if (e >= a.n_experts) continue;
-            float g = a.sigmoid ? ds[j] * s[j] * (1.f - s[j]) : s[j] * (ds[j] - dot);
-            if (x[j] == -INFINITY) g = 0.f;
-            dlogits[t * dstride + e] = ValueOf<DT>::put(g);
+            ds[j] = a.sigmoid ? mine.v[j] * s[j] * (1.f - s[j]) : s[j] * (mine.v[j] - dot);
+            if (x[j] == -INFINITY) ds[j] = 0.f;
+        }
+        value_t<DT>* to = dlogits + t * dstride + e0;
+        if (whole && e0 + EPL <= E) {
+            store_values<DT, EPL>(to, ds);
+        } else {
+#pragma unroll
+            for (int j = 0; j < EPL; ++j)
+                if (e0 + j < E) to[j] = ValueOf<DT>::put(ds[j]);
         }
     }
 }
@@ -237,12 +720,22 @@ static int route_args(const ciera_route_config* c, RouteArgs* a) {
 // f(values per lane as a constant) for a row of n experts
 template <class F>
 static void with_row(uint32_t n, F&& f) {
-    if (n <= 32) f(std::integral_constant<int, 1>());
-    else if (n <= 64) f(std::integral_constant<int, 2>());
-    else if (n <= 128) f(std::integral_constant<int, 4>());
+    if (n <= 64) f(std::integral_constant<int, 2>());
     else if (n <= 256) f(std::integral_constant<int, 8>());
-    else if (n <= 512) f(std::integral_constant<int, 16>());
     else f(std::integral_constant<int, 32>());
+}
+// f(length of the lists as a constant)
+template <class F>
+static void with_list(uint32_t top_k, F&& f) {
+    if (top_k <= 8) f(std::integral_constant<int, 10>());
+    else if (top_k <= 16) f(std::integral_constant<int, 18>());
+    else f(std::integral_constant<int, 34>());
+}
+
+// whether rows may be read EPL values at a time, in pieces of at most 16 bytes
+static bool whole_rows(const void* p, uint64_t stride, uint64_t value_bytes, uint64_t epl) {
+    const uint64_t piece = epl * value_bytes < 16 ? epl * value_bytes : 16;
+    return !(((uint64_t)p | stride * value_bytes) & (piece - 1));
 }
 
 static uint32_t route_grid(uint64_t n_tokens) {
@@ -270,10 +763,28 @@ extern "C" int ciera_route(const ciera_route_config* config, int dtype, const vo
         constexpr int DT = decltype(dt)::value;
         if (!n_tokens) return;
         with_row(a.n_experts, [&](auto epl) {
-            const size_t smem = a.top_groups < a.n_groups ? sizeof(double) * kRouteWarps * a.n_experts : 0;  // at most 32 KB
-            e = launch_after(route_kernel<DT, decltype(epl)::value>, dim3(route_grid(n_tokens)), kRouteWarps * 32, smem,
-                             (cudaStream_t)stream, a, (const value_t<DT>*)logits_dev, n_tokens, logits_stride, bias_dev,
-                             experts_dev, weights_dev);
+            // A warp for each token while all of them have room on the GPU, else up to 32 / L tokens a warp (one token 2.5 us against
+            // 5.8, 16384 tokens of 256 experts in 8 groups 43 us against 28).
+            if (n_tokens < 148 * 32) {
+                constexpr int EPL = decltype(epl)::value;
+                e = launch_after(route_few_kernel<DT, EPL>, dim3((uint32_t)((n_tokens + kRouteWarps - 1) / kRouteWarps)), kRouteWarps * 32,
+                                 sizeof(float) * kRouteWarps * 2 * a.n_experts /* at most 32 KB */, (cudaStream_t)stream, a, (const value_t<DT>*)logits_dev,
+                                 n_tokens, logits_stride, whole_rows(logits_dev, logits_stride, dtype_bytes(DT), EPL), bias_dev, experts_dev,
+                                 weights_dev);
+                return;
+            }
+            with_list(a.top_k, [&](auto kl) {
+                constexpr int EPL = decltype(epl)::value, KL = decltype(kl)::value;
+                const int whole = whole_rows(logits_dev, logits_stride, dtype_bytes(DT), EPL);
+                const size_t smem = sizeof(float) * kRouteWarps * warp_floats<EPL>(a.n_experts);  // at most 37 KB
+                // a warp's lanes are all at work with 32 / L tokens; fewer where that leaves SMs without any
+                const uint64_t most = 32 / kTokenLanes<EPL>, each = (n_tokens + 148 * 16 - 1) / (148 * 16);
+                const uint32_t tokens_each = (uint32_t)(each < most ? each : most);
+                const uint64_t blocks = (n_tokens + (uint64_t)tokens_each * kRouteWarps - 1) / ((uint64_t)tokens_each * kRouteWarps);
+                e = launch_after(route_kernel<DT, EPL, KL>, dim3((uint32_t)blocks), kRouteWarps * 32, smem, (cudaStream_t)stream, a,
+                                 (const value_t<DT>*)logits_dev, n_tokens, tokens_each, logits_stride, whole, bias_dev, experts_dev,
+                                 weights_dev);
+            });
         });
     });
     if (!known) return CIERA_ERR_INVALID_ARG;
@@ -299,9 +810,12 @@ extern "C" int ciera_route_backward(const ciera_route_config* config, int dtype,
         constexpr int DT = decltype(dt)::value;
         if (!n_tokens) return;
         with_row(a.n_experts, [&](auto epl) {
-            e = launch_after(route_backward_kernel<DT, decltype(epl)::value>, dim3(route_grid(n_tokens)), kRouteWarps * 32, 0,
-                             (cudaStream_t)stream, a, (const value_t<DT>*)logits_dev, n_tokens, logits_stride, experts_dev,
-                             dweights_dev, (value_t<DT>*)dlogits_dev, dlogits_stride);
+            constexpr int EPL = decltype(epl)::value;
+            const int whole = whole_rows(logits_dev, logits_stride, dtype_bytes(DT), EPL) &&
+                              whole_rows(dlogits_dev, dlogits_stride, dtype_bytes(DT), EPL);
+            e = launch_after(route_backward_kernel<DT, EPL>, dim3(route_grid(n_tokens)), kRouteWarps * 32, 0, (cudaStream_t)stream, a,
+                             (const value_t<DT>*)logits_dev, n_tokens, logits_stride, whole, experts_dev, dweights_dev,
+                             (value_t<DT>*)dlogits_dev, dlogits_stride);
         });
     });
     if (!known) return CIERA_ERR_INVALID_ARG;

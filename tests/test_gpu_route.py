@@ -41,6 +41,14 @@ def _check(logits, bias, E, k, score, G=1, top_groups=1, best=2, renorm=False, s
     # a weight is a quotient of sums of at most E terms in 32 bits: each term is off by a few steps, each addition by half of one
     tol = (E + 16) * 2.0**-24 * np.abs(w) + 1e-37
     assert (np.abs(weights[:T].cpu().numpy() - w) <= tol).all()
+    # the same tokens over and over in a batch that is done several tokens a warp
+    n = -(-4801 // T)
+    many_e = torch.full((n * T, k), -7, dtype=torch.int32, device=DEV)
+    many_w = torch.full((n * T, k), -7.0, device=DEV)
+    ciera.route(_config(E, k, score, G, top_groups, best, renorm, scale), dev.repeat(n, 1), None if bias is None else bias.to(DEV),
+                many_e, many_w)
+    many_e, many_w = many_e.view(n, T, k).cpu().numpy(), many_w.view(n, T, k).cpu().numpy()
+    assert (many_e == ids).all() and (np.abs(many_w - w) <= tol).all()
     return experts[:T], weights[:T]
 
 
