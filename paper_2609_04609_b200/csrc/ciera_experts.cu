@@ -136,33 +136,38 @@ __global__ void __launch_bounds__(kLayoutWarps * 32)
 }
 
 // ------------------------------------------------------------------------------------------ weighted sum
-// A thread has N neighbouring columns of one token and adds its rows' up in fp32; a row is read once, so the kernel is bound by memory.
+// A thread has N neighbouring columns of one token and adds its rows' up in fp32; a row is
+// read once, so the kernel is bound by memory.  (Index: uint32_t wherever it holds every thread's number: a division of 64 bits
+// costs as much as all the rest.)
 
 constexpr int kCombineThreads = 256;
 
-template <int DT, int N>
+template <int DT, int N, class Index>
 __global__ void __launch_bounds__(kCombineThreads)
     combine_kernel(const value_t<DT>* __restrict__ rows, uint32_t n_rows, uint64_t rows_stride,
-                   const int32_t* __restrict__ row_of_slot, const float* __restrict__ weights, uint64_t n_tokens,
-                   uint32_t top_k, uint32_t cols, value_t<DT>* __restrict__ out, uint64_t out_stride) {
+                   const int32_t* __restrict__ row_of_slot, const float* __restrict__ weights, Index n, uint32_t per,
+                   uint32_t top_k, value_t<DT>* __restrict__ out, uint64_t out_stride) {
     pdl_wait();
-    const uint32_t per = (cols + N - 1) / N;
-    const uint64_t n = n_tokens * per, step = (uint64_t)gridDim.x * blockDim.x;
-    for (uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += step) {
-        const uint64_t t = i / per;
+    const Index step = (Index)gridDim.x * blockDim.x;
+    for (Index i = (Index)blockIdx.x * blockDim.x + threadIdx.x; i < n;) {
+        const Index t = i / per;
         const uint32_t c = (uint32_t)(i - t * per) * N;
+        const int32_t* at = row_of_slot + (uint64_t)t * top_k;
+        const float* w = weights ? weights + (uint64_t)t * top_k : nullptr;
         float sum[N] = {};
 #pragma unroll 4
         for (uint32_t j = 0; j < top_k; ++j) {
-            const uint32_t row = (uint32_t)row_of_slot[t * top_k + j];
+            const uint32_t row = (uint32_t)at[j];
             if (row >= n_rows) continue;
-            const float w = weights ? weights[t * top_k + j] : 1.f;
+            const float scale = w ? w[j] : 1.f;
             float v[N];
             load_values<DT, N>(rows + row * rows_stride + c, v);
 #pragma unroll
-            for (int q = 0; q < N; ++q) sum[q] = fmaf(w, v[q], sum[q]);
+            for (int q = 0; q < N; ++q) sum[q] = fmaf(scale, v[q], sum[q]);
         }
         store_values<DT, N>(out + t * out_stride + c, sum);
+        if (n - i <= step) break;  // (i + step may not fit)
+        i += step;
     }
 }
 
@@ -292,10 +297,15 @@ extern "C" int ciera_expert_combine(int dtype, const void* rows_dev, uint64_t n_
         const uint64_t bits = (uint64_t)rows_dev | (uint64_t)out_dev | rows_stride * v | out_stride * v | cols * v;
         with_width<DT>(bits, [&](auto width) {
             constexpr int N = decltype(width)::value;
-            e = launch_after(combine_kernel<DT, N>, dim3(blocks_for(n_tokens * ((cols + N - 1) / N), kCombineThreads)),
-                             kCombineThreads, 0, (cudaStream_t)stream, (const value_t<DT>*)rows_dev, (uint32_t)n_rows,
-                             rows_stride, row_of_slot_dev, weights_dev, n_tokens, top_k, (uint32_t)cols,
-                             (value_t<DT>*)out_dev, out_stride);
+            const uint32_t per = (uint32_t)((cols + N - 1) / N);
+            const uint64_t n = n_tokens * per;
+            const auto go = [&](auto index) {
+                using Index = decltype(index);
+                e = launch_after(combine_kernel<DT, N, Index>, dim3(blocks_for(n, kCombineThreads)), kCombineThreads, 0, (cudaStream_t)stream,
+                                 (const value_t<DT>*)rows_dev, (uint32_t)n_rows, rows_stride, row_of_slot_dev, weights_dev, (Index)n, per,
+                                 top_k, (value_t<DT>*)out_dev, out_stride);
+            };
+            n >> 32 ? go(uint64_t()) : go(uint32_t());
         });
     });
     if (e != cudaSuccess) return record_cuda_error(e);
