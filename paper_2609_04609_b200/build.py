@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -38,13 +40,19 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB
     tmp = f"{LIB}.{os.getpid()}.tmp"  # built beside its place and moved there whole: nobody loads half a library
-    cmd = [_nvcc(), "-shared", "-o", tmp, "-I", os.path.join(ROOT, "include"), "-I", CSRC] + NVCC_FLAGS
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode != 0:
-        print(res.stdout)
-        print(res.stderr)
-    if res.returncode != 0:
+    with tempfile.TemporaryDirectory() as work:
+        objects = [os.path.join(work, s + ".o") for s in SOURCES]
+        include = ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
+        steps = [[_nvcc(), "-c", "-o", o] + include + NVCC_FLAGS + [os.path.join(CSRC, s)] for s, o in zip(SOURCES, objects)]
+        with ThreadPoolExecutor(min(len(steps), os.cpu_count() or 1)) as pool:  # the files side by side
+            done = list(pool.map(lambda cmd: subprocess.run(cmd, capture_output=True, text=True), steps))
+        if all(r.returncode == 0 for r in done):
+            done.append(subprocess.run([_nvcc(), "-shared", "-o", tmp] + NVCC_FLAGS + objects, capture_output=True, text=True))
+    for r in done:
+        if verbose or r.returncode != 0:
+            print(r.stdout)
+            print(r.stderr)
+    if any(r.returncode != 0 for r in done):
         if os.path.exists(tmp):
             os.remove(tmp)
         raise RuntimeError("nvcc failed building libciera.so")

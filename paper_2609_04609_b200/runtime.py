@@ -111,6 +111,12 @@ class LayerCodec:
         ciera.step(self.plan, weights, self.sender_cache, self.msg_send, self.msg_recv, self.receiver_cache, out,
                    self.wire_bytes, self.changed_blocks, self.workspace, self.status, stream)
 
+    def expert_layer(self, n_experts: int, d_model: int, d_ff: int, top_k: int, max_tokens: int, **kw):
+        """The MoE layer whose gate, up and down matrices this codec reconstructs (see ``experts.ExpertLayer``)."""
+        from .experts import ExpertLayer
+
+        return ExpertLayer(self, n_experts, d_model, d_ff, top_k, max_tokens, **kw)
+
     def device_buffers(self, weights_dev: torch.Tensor) -> "ciera.DeviceBuffers":
         b = ciera.DeviceBuffers()
         b.weights_dev = weights_dev.data_ptr()
