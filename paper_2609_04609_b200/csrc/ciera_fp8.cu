@@ -47,7 +47,24 @@ __device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d
     return lo | hi << 16;
 }
 
-__device__ __forceinline__ float sigmoid32(float g) { return 1.f / (1.f + expf(-g)); }
+// sigmoid(g) = 1 / (1 + e) and 1 - sigmoid(g) = e / (1 + e) with e = 2^(-g log2 e): the exponent in two parts, so that the power
+// is off by a step or two however large g is, and both results by less than 2^-21 of themselves.  (expf and a division: silu(g) *
+// u of 32768 x 1024 in 93 us.)
+__device__ __forceinline__ float2 sigmoid32(float g) {
+    const float x = fminf(fmaxf(g, -87.f), 87.f), t = x * -1.44269504f;
+    const float rest = fmaf(x, -1.44269504f, -t) + x * -1.92596299e-8f;  // -x log2 e = t + rest
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+    e = fmaf(e, rest * 0.693147181f, e);
+    const float s = isnan(g) ? g : __fdividef(1.f, 1.f + e);
+    return make_float2(s, e * s);
+}
+__device__ __forceinline__ float swiglu32(float g, float u) { return g * sigmoid32(g).x * u; }
+__device__ __forceinline__ float swiglu_gate32(float g, float u, float d) {
+    const float2 s = sigmoid32(g);
+    return d * u * s.x * fmaf(g, s.y, 1.f);
+}
+__device__ __forceinline__ float swiglu_up32(float g, float d) { return d * g * sigmoid32(g).x; }
 
 // Four neighbouring values of a row: x's, silu(g) * u, or one of their gradients.  WIDE: one access for each four of an input.
 template <int DT, int SRC, bool WIDE>
@@ -68,7 +85,7 @@ __device__ __forceinline__ void source_values(const value_t<DT>* __restrict__ x,
         get(x + c, c, g);
         get(x + cols + c, c, u);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = g[j] * sigmoid32(g[j]) * u[j];
+        for (int j = 0; j < 4; ++j) v[j] = swiglu32(g[j], u[j]);
     } else if constexpr (WIDE) {  // (the four are on one side)
         const uint32_t f = cols / 2, at = c < f ? c : c - f;
         float g[4], u[4], d[4];
@@ -77,13 +94,10 @@ __device__ __forceinline__ void source_values(const value_t<DT>* __restrict__ x,
         if (c < f) {
             get(x + f + at, c, u);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float s = sigmoid32(g[j]);
-                v[j] = d[j] * u[j] * s * (1.f + g[j] * (1.f - s));
-            }
+            for (int j = 0; j < 4; ++j) v[j] = swiglu_gate32(g[j], u[j], d[j]);
         } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = d[j] * g[j] * sigmoid32(g[j]);
+            for (int j = 0; j < 4; ++j) v[j] = swiglu_up32(g[j], d[j]);
         }
     } else {
         const uint32_t f = cols / 2;
@@ -93,8 +107,7 @@ __device__ __forceinline__ void source_values(const value_t<DT>* __restrict__ x,
             if (c + j >= cols) continue;
             const uint32_t at = c + j < f ? c + j : c + j - f;
             const float g = ValueOf<DT>::get(x[at]), u = ValueOf<DT>::get(x[f + at]), d = ValueOf<DT>::get(grad[at]);
-            const float s = sigmoid32(g);
-            v[j] = c + j < f ? d * u * s * (1.f + g * (1.f - s)) : d * g * s;
+            v[j] = c + j < f ? swiglu_gate32(g, u, d) : swiglu_up32(g, d);
         }
     }
 }
@@ -113,16 +126,14 @@ __device__ double source_magnitude(const value_t<DT>* __restrict__ x, const valu
     }
 }
 
-// A largest magnitude so close above or below 1.75 * 2^n that 32 bits do not say on which side it is: the values behind
-// an exponential are off by less than 2^-20 of themselves.
+// A largest magnitude that 32 bits do not settle: so close above or below 1.75 * 2^n that they do not say on which side it is
+// (values behind an exponential are off by less than 2^-20 of themselves; 64 steps are 2^-18, for the sum in the gate's gradient,
+// of which some may cancel), or where a sigmoid has left their range.
 __device__ __forceinline__ bool at_border(uint32_t amax) {
-    return amax < 0x7f800000u && amax > 0u && (uint32_t)((amax & 0x7fffffu) - 0x600000u + 16u) <= 32u;
+    return amax < 0x7f800000u && (amax < (32u << 23) || (uint32_t)((amax & 0x7fffffu) - 0x600000u + 64u) <= 128u);
 }
-// amax by its value in 64 bits: on the side of the border on which that is
-__device__ __forceinline__ uint32_t settle(uint32_t amax, double exact) {
-    const uint32_t border = (amax & 0x7f800000u) | 0x600000u;
-    return exact > (double)__uint_as_float(border) ? border + 1u : border;
-}
+// the same from 64 bits, rounded up: on the side of the border on which that is
+__device__ __forceinline__ uint32_t settle(double exact) { return __float_as_uint(__double2float_ru(exact)); }
 
 // The tile's four values of each row, rounded with a scale for each row, to q.
 __device__ __forceinline__ void put_four(uint8_t* to, uint32_t q, uint32_t c0, uint32_t cols) {
@@ -132,6 +143,16 @@ __device__ __forceinline__ void put_four(uint8_t* to, uint32_t q, uint32_t c0, u
 #pragma unroll
         for (int j = 0; j < 3; ++j)
             if (c0 + j < cols) to[j] = (uint8_t)(q >> (8 * j));
+    }
+}
+
+// The bytes of rows r ... r + 15 of a transposed line, as far as there are rows.
+__device__ __forceinline__ void put_sixteen(uint8_t* to, uint4 q, uint32_t r, uint32_t rows) {
+    if (r + 15 < rows) {
+        *reinterpret_cast<uint4*>(to) = q;
+    } else {
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        for (uint32_t i = 0; r + i < rows; ++i) to[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
     }
 }
 
@@ -157,13 +178,7 @@ __device__ __forceinline__ void turn_out(const uint2* turned, uint8_t* qt, uint6
         if (col0 + c >= cols || r >= rows) continue;
         uint4 q = *reinterpret_cast<const uint4*>(turned + c * 16 + ((unit ^ (of & 7)) << 1));
         if (of >> 3 & 1) q = make_uint4(q.z, q.w, q.x, q.y);
-        uint8_t* to = qt + (uint64_t)(col0 + c) * stride + r;
-        if (r + 15 < rows) {
-            *reinterpret_cast<uint4*>(to) = q;
-        } else {
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-            for (uint32_t i = 0; r + i < rows; ++i) to[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
-        }
+        put_sixteen(qt + (uint64_t)(col0 + c) * stride + r, q, r, rows);
     }
 }
 
@@ -217,7 +232,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const Ro
         uint32_t amax = max(max(magnitude(v[i][0]), magnitude(v[i][1])), max(magnitude(v[i][2]), magnitude(v[i][3])));
         amax = __reduce_max_sync(~0u, amax);
         if constexpr (SRC != CIERA_SOURCE_ROWS) {
-            if (at_border(amax)) {
+            if (live >> i & 1 && at_border(amax)) {
                 const uint64_t r = first + i;
                 double m = 0.0;
                 for (int j = 0; j < 4; ++j)
@@ -225,7 +240,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const Ro
                         m = fmax(m, source_magnitude<DT, SRC>(x + r * a.x_stride, SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + r * a.grad_stride : nullptr, c0 + j, a.cols));
 #pragma unroll
                 for (int d = 16; d; d >>= 1) m = fmax(m, __shfl_xor_sync(~0u, m, d));
-                amax = settle(amax, m);
+                amax = settle(m);
             }
         }
         if (lane == i) row_max = amax;
@@ -255,17 +270,24 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const Ro
 #pragma unroll
             for (int w = 0; w < kTileThreads / 32; ++w) amax = max(amax, col_max[w][threadIdx.x]);
             if constexpr (SRC != CIERA_SOURCE_ROWS) {
-                if (at_border(amax)) {
+                // the whole warp goes over such a column, four rows a lane
+                for (uint32_t left = __ballot_sync(~0u, c < a.cols && at_border(amax)); left; left &= left - 1) {
+                    const int which = __ffs(left) - 1;
+                    const uint32_t col = __shfl_sync(~0u, c, which);
                     double most = 0.0;
-                    for (uint32_t r = row0; r < min(row0 + 128u, rows) && c < a.cols; ++r) {
+#pragma unroll 1
+                    for (uint32_t r = row0 + lane; r < min(row0 + 128u, rows); r += 32) {
                         if (a.slot_of_row) {
                             const int32_t slot = a.slot_of_row[r];
                             if (slot < 0 || (uint64_t)slot >= a.x_rows * a.top_k) continue;
                         } else if (r >= a.x_rows) continue;
                         most = fmax(most, source_magnitude<DT, SRC>(x + (uint64_t)r * a.x_stride,
-                                                                    SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + (uint64_t)r * a.grad_stride : nullptr, c, a.cols));
+                                                                    SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + (uint64_t)r * a.grad_stride : nullptr, col, a.cols));
                     }
-                    amax = settle(amax, most);
+                    __syncwarp();
+#pragma unroll
+                    for (int d = 16; d; d >>= 1) most = fmax(most, __shfl_xor_sync(~0u, most, d));
+                    if (lane == which) amax = settle(most);
                 }
             }
             const uint32_t byte = scale_byte(amax);
@@ -284,8 +306,9 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const Ro
 }
 
 // The 16-bit precisions as they are: a word of two values is halved into magnitudes and compared as it stands (their order is
-// that of the bits), and a tile takes 16 registers a thread.  (As fp32 in the kernel above: dispatch of 4096 x 8 rows of 2048
-// in 81 us, 26 instructions a value.)
+// that of the bits), and a tile takes 16 registers a thread.  Half a warp has 4 rows, a lane 8 neighbouring columns of each: one
+// access of 16 bytes, one of 8, and half the steps for each row that 4 columns a lane take (dispatch of 4096 x 8 rows of 2048
+// as fp32 in the kernel above 81 us and 26 instructions a value, 4 columns of 16 bits a lane 74 us and 24).
 constexpr uint32_t kMagnitudes = 0x7fff7fffu;
 
 // the bits of the fp32 value that these magnitude bits stand for
@@ -305,86 +328,134 @@ __device__ __forceinline__ uint32_t round_four(uint2 w, float inv) {
     return to_e4m3x4(a.x, a.y, b.x, b.y, inv);
 }
 
+__device__ __forceinline__ uint32_t most_of(uint4 w) {
+    return __vmaxu2(__vmaxu2(w.x & kMagnitudes, w.y & kMagnitudes), __vmaxu2(w.z & kMagnitudes, w.w & kMagnitudes));
+}
+__device__ __forceinline__ uint4 most_of(uint4 a, uint4 b) {
+    return make_uint4(__vmaxu2(a.x, b.x), __vmaxu2(a.y, b.y), __vmaxu2(a.z, b.z), __vmaxu2(a.w, b.w));
+}
+__device__ __forceinline__ uint4 magnitudes(uint4 w) {
+    return make_uint4(w.x & kMagnitudes, w.y & kMagnitudes, w.z & kMagnitudes, w.w & kMagnitudes);
+}
+
+// Blocks stay and take neighbouring tiles one behind the other, with the next tile's values on their way.
 template <int DT, bool T>
-__global__ void __launch_bounds__(kTileThreads, T ? 2 : 3) quantize_words_kernel(const RowsArgs a, const value_t<DT>* __restrict__ x) {
-    __shared__ uint2 col_max[T ? kTileThreads / 32 : 1][32];
+__global__ void __launch_bounds__(kTileThreads, 2) quantize_words_kernel(const RowsArgs a, const value_t<DT>* __restrict__ x) {
+    __shared__ uint4 col_max[T ? kTileThreads / 32 : 1][16];
     __shared__ __align__(16) float col_inv[128];
-    __shared__ __align__(16) uint2 turned[T ? 128 * 16 : 2];
+    __shared__ __align__(16) uint32_t turned[T ? 128 * 32 : 4];
     pdl_wait();
-    const uint32_t row_tile = blockIdx.x / a.col_tiles, col_tile = blockIdx.x - row_tile * a.col_tiles;
-    const uint32_t row0 = row_tile * 128u, col0 = col_tile * 128u;
     const uint32_t rows = a.starts ? min((uint32_t)max(a.starts[a.n_experts], 0), a.rows) : a.rows;
-    if (row0 >= rows) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t c0 = col0 + lane * 4, first = row0 + warp * kTileRows;
-    uint32_t from = first + lane;  // lane i: where row i of the warp comes from
-    bool some = lane < kTileRows && from < rows;
-    if (a.slot_of_row) {
-        const int32_t slot = some ? a.slot_of_row[from] : -1;
-        some = slot >= 0 && (uint64_t)slot < a.x_rows * a.top_k;
-        from = (uint32_t)max(slot, 0) / a.top_k;
-    } else {
-        some = some && from < a.x_rows;
-    }
-    const uint32_t live = __ballot_sync(~0u, some);
-    const bool inside = c0 < a.cols;  // (cols is a multiple of four)
-    uint2 w[kTileRows];
+    const uint32_t tiles = (rows + 127) / 128 * a.col_tiles, each = (tiles + gridDim.x - 1) / gridDim.x;
+    const uint32_t begin = min(tiles, blockIdx.x * each), end = min(tiles, begin + each);
+    if (begin == end) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, half = lane >> 4, l16 = lane & 15;
+    uint32_t row_tile = begin / a.col_tiles, col_tile = begin - row_tile * a.col_tiles;
+    uint32_t from = 0, live = 0;
+    const auto find_rows = [&](uint32_t tile) {  // lane i: where row i of the warp comes from
+        from = tile * 128u + warp * kTileRows + lane;
+        bool some = lane < kTileRows && from < rows;
+        if (a.slot_of_row) {
+            const int32_t slot = some ? a.slot_of_row[from] : -1;
+            some = slot >= 0 && (uint64_t)slot < a.x_rows * a.top_k;
+            from = (uint32_t)max(slot, 0) / a.top_k;
+        } else {
+            some = some && from < a.x_rows;
+        }
+        live = __ballot_sync(~0u, some) >> (4 * half);
+    };
+    uint4 coming[4];
+    const auto fetch = [&](uint32_t tile) {
+        const uint32_t c = tile * 128u + l16 * 8;
 #pragma unroll
-    for (int i = 0; i < kTileRows; ++i) {
-        const uint32_t r = __shfl_sync(~0u, from, i);
-        w[i] = make_uint2(0, 0);
-        if (inside && live >> i & 1) w[i] = *reinterpret_cast<const uint2*>(x + r * a.x_stride + c0);
-    }
-    uint32_t row_max = 0;  // lane i: the largest magnitude of row i
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t r = __shfl_sync(~0u, from, 4 * half + i);
+            coming[i] = make_uint4(0, 0, 0, 0);
+            if (c < a.cols && live >> i & 1) coming[i] = *reinterpret_cast<const uint4*>(x + r * a.x_stride + c);  // (cols: a multiple of 8)
+        }
+    };
+    find_rows(row_tile);
+    fetch(col_tile);
+    for (uint32_t tile = begin; tile < end; ++tile) {
+        const uint32_t row0 = row_tile * 128u, col0 = col_tile * 128u, row_t = row_tile, col_t = col_tile;
+        const uint32_t c0 = col0 + l16 * 8, first = row0 + warp * kTileRows;
+        const bool inside = c0 < a.cols;
+        uint4 w[4];
 #pragma unroll
-    for (int i = 0; i < kTileRows; ++i) {
-        const uint32_t two = __vmaxu2(w[i].x & kMagnitudes, w[i].y & kMagnitudes);
-        const uint32_t amax = __reduce_max_sync(~0u, max(two >> 16, two & 0xffffu));
-        if (lane == i) row_max = amax;
-    }
-    const uint32_t row_byte = scale_byte(widen<DT>(row_max));
-    const float row_inv = inverse_scale(row_byte);
-    if (lane < kTileRows && first + lane < rows) a.scales[(uint64_t)col_tile * a.scales_stride + first + lane] = (uint8_t)row_byte;
-    uint8_t* q = a.q + (uint64_t)first * a.q_stride + c0;
+        for (int i = 0; i < 4; ++i) w[i] = coming[i];
+        if (++col_tile == a.col_tiles) {
+            col_tile = 0;
+            ++row_tile;
+            if (tile + 1 < end) find_rows(row_tile);
+        }
+        if (tile + 1 < end) fetch(col_tile);
+        // the rows' largest magnitudes, two rows to a word
+        uint32_t m[4];
 #pragma unroll
-    for (int i = 0; i < kTileRows; ++i) {
-        const uint32_t four = round_four<DT>(w[i], __shfl_sync(~0u, row_inv, i));
-        if (first + i < rows && inside) *reinterpret_cast<uint32_t*>(q + i * a.q_stride) = four;
-    }
-    if constexpr (T) {
-        uint2 m = make_uint2(0, 0);
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t two = most_of(w[i]);
+            m[i] = max(two >> 16, two & 0xffffu);
+        }
+        uint32_t m01 = m[0] | m[1] << 16, m23 = m[2] | m[3] << 16;
 #pragma unroll
-        for (int i = 0; i < kTileRows; ++i) m = make_uint2(__vmaxu2(m.x, w[i].x & kMagnitudes), __vmaxu2(m.y, w[i].y & kMagnitudes));
-        col_max[warp][lane] = m;
-        __syncthreads();
-        if (threadIdx.x < 64) {  // a thread for two columns
-            const uint32_t c = col0 + 2 * threadIdx.x;
-            uint32_t two = 0;
+        for (int d = 8; d; d >>= 1) {
+            m01 = __vmaxu2(m01, __shfl_xor_sync(~0u, m01, d));
+            m23 = __vmaxu2(m23, __shfl_xor_sync(~0u, m23, d));
+        }
+        const uint32_t pair = l16 & 2 ? m23 : m01;  // lane i of a half: row i & 3
+        const uint32_t row_byte = scale_byte(widen<DT>(l16 & 1 ? pair >> 16 : pair & 0xffffu));
+        const float row_inv = inverse_scale(row_byte);
+        const uint32_t mine = first + 4 * half;  // the half's first row
+        if (l16 < 4 && mine + l16 < rows) a.scales[(uint64_t)col_t * a.scales_stride + mine + l16] = (uint8_t)row_byte;
+        uint8_t* q = a.q + (uint64_t)mine * a.q_stride + c0;
 #pragma unroll
-            for (int i = 0; i < kTileThreads / 32; ++i) two = __vmaxu2(two, reinterpret_cast<const uint32_t*>(col_max[i])[threadIdx.x]);
-            const uint32_t lo = scale_byte(widen<DT>(two & 0xffffu)), hi = scale_byte(widen<DT>(two >> 16));
-            if (c < a.cols) {
-                a.scales_t[(uint64_t)row_tile * a.scales_t_stride + c] = (uint8_t)lo;
-                a.scales_t[(uint64_t)row_tile * a.scales_t_stride + c + 1] = (uint8_t)hi;
+        for (int i = 0; i < 4; ++i) {
+            const float inv = __shfl_sync(~0u, row_inv, i, 16);
+            const uint2 eight = make_uint2(round_four<DT>(make_uint2(w[i].x, w[i].y), inv), round_four<DT>(make_uint2(w[i].z, w[i].w), inv));
+            if (mine + i < rows && inside) *reinterpret_cast<uint2*>(q + i * a.q_stride) = eight;
+        }
+        if constexpr (T) {
+            uint4 cm = most_of(most_of(magnitudes(w[0]), magnitudes(w[1])), most_of(magnitudes(w[2]), magnitudes(w[3])));
+            cm = most_of(cm, make_uint4(__shfl_xor_sync(~0u, cm.x, 16), __shfl_xor_sync(~0u, cm.y, 16), __shfl_xor_sync(~0u, cm.z, 16),
+                                        __shfl_xor_sync(~0u, cm.w, 16)));
+            if (!half) col_max[warp][l16] = cm;
+            __syncthreads();
+            if (threadIdx.x < 64) {  // a thread for two columns
+                const uint32_t c = col0 + 2 * threadIdx.x;
+                uint32_t two = 0;
+#pragma unroll
+                for (int i = 0; i < kTileThreads / 32; ++i) two = __vmaxu2(two, reinterpret_cast<const uint32_t*>(col_max[i])[threadIdx.x]);
+                const uint32_t lo = scale_byte(widen<DT>(two & 0xffffu)), hi = scale_byte(widen<DT>(two >> 16));
+                if (c < a.cols) {
+                    a.scales_t[(uint64_t)row_t * a.scales_t_stride + c] = (uint8_t)lo;
+                    a.scales_t[(uint64_t)row_t * a.scales_t_stride + c + 1] = (uint8_t)hi;
+                }
+                *reinterpret_cast<float2*>(&col_inv[2 * threadIdx.x]) = make_float2(inverse_scale(lo), inverse_scale(hi));
             }
-            *reinterpret_cast<float2*>(&col_inv[2 * threadIdx.x]) = make_float2(inverse_scale(lo), inverse_scale(hi));
-        }
-        __syncthreads();
-        const float4 inv = *reinterpret_cast<const float4*>(&col_inv[lane * 4]);
-        // scaled by column, rounded by row, and the bytes turned
-        uint32_t four[kTileRows];
+            __syncthreads();
+            // scaled by column, and the bytes turned: the four rows of a column are a word, at a place of its line that is mixed by the lane
 #pragma unroll
-        for (int i = 0; i < kTileRows; ++i) {
-            const float2 ab = two_values<DT>(w[i].x), cd = two_values<DT>(w[i].y);
-            four[i] = to_e4m3x4(ab.x * inv.x, ab.y * inv.y, cd.x * inv.z, cd.y * inv.w, 1.f);
-        }
-        uint32_t lo[4], hi[4];
-        turn_bytes(four[0], four[1], four[2], four[3], lo);
-        turn_bytes(four[4], four[5], four[6], four[7], hi);
+            for (int h = 0; h < 2; ++h) {
+                const float4 inv = *reinterpret_cast<const float4*>(&col_inv[l16 * 8 + 4 * h]);
+                uint32_t four[4], t[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) turn_in(turned, lane, j, warp, lo[j], hi[j]);
-        __syncthreads();
-        turn_out(turned, a.qt, a.qt_stride, col0, a.cols, row0, rows);
+                for (int i = 0; i < 4; ++i) {
+                    const float2 ab = two_values<DT>(h ? w[i].z : w[i].x), cd = two_values<DT>(h ? w[i].w : w[i].y);
+                    four[i] = to_e4m3x4(ab.x * inv.x, ab.y * inv.y, cd.x * inv.z, cd.y * inv.w, 1.f);
+                }
+                turn_bytes(four[0], four[1], four[2], four[3], t);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) turned[(l16 * 8 + 4 * h + j) * 32 + ((warp * 2 + half) ^ (l16 << 1))] = t[j];
+            }
+            __syncthreads();
+            for (int k = threadIdx.x; k < 128 * 8; k += kTileThreads) {
+                const uint32_t c = k >> 3, unit = k & 7, r = row0 + unit * 16, of = c >> 3;  // (the lane that put it there)
+                if (col0 + c >= a.cols || r >= rows) continue;
+                uint4 v = *reinterpret_cast<const uint4*>(turned + c * 32 + ((unit ^ (of >> 1)) << 2));
+                if (of & 1) v = make_uint4(v.z, v.w, v.x, v.y);
+                put_sixteen(a.qt + (uint64_t)(col0 + c) * a.qt_stride + r, v, r, rows);
+            }
+        }
     }
 }
 
@@ -545,8 +616,10 @@ extern "C" int ciera_fp8_quantize_rows(const ciera_fp8_rows* p, void* stream) {
                              kTileThreads, 0, (cudaStream_t)stream, a, (const value_t<DT>*)p->x, (const value_t<DT>*)p->grad);
         };
         if constexpr (DT != CIERA_FP32) {
-            if (wide && src == CIERA_SOURCE_ROWS && !p->row_weights) {
-                e = launch_after(turned ? quantize_words_kernel<DT, true> : quantize_words_kernel<DT, false>, dim3((uint32_t)tiles), kTileThreads, 0,
+            const bool eight = !(((uint64_t)p->x | p->x_stride * 2) & 15) && !(p->cols & 7);
+            if (eight && src == CIERA_SOURCE_ROWS && !p->row_weights) {
+                e = launch_after(turned ? quantize_words_kernel<DT, true> : quantize_words_kernel<DT, false>,
+                                 dim3((uint32_t)(tiles < 2 * 148 ? tiles : 2 * 148)), kTileThreads, 0,
                                  (cudaStream_t)stream, a, (const value_t<DT>*)p->x);
                 return;
             }
