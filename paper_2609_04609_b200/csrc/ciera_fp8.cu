@@ -311,6 +311,12 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const Ro
 // as fp32 in the kernel above 81 us and 26 instructions a value, 4 columns of 16 bits a lane 74 us and 24).
 constexpr uint32_t kMagnitudes = 0x7fff7fffu;
 
+__device__ __forceinline__ uint32_t max_two(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
 // the bits of the fp32 value that these magnitude bits stand for
 template <int DT>
 __device__ __forceinline__ uint32_t widen(uint32_t half) {
@@ -329,10 +335,10 @@ __device__ __forceinline__ uint32_t round_four(uint2 w, float inv) {
 }
 
 __device__ __forceinline__ uint32_t most_of(uint4 w) {
-    return __vmaxu2(__vmaxu2(w.x & kMagnitudes, w.y & kMagnitudes), __vmaxu2(w.z & kMagnitudes, w.w & kMagnitudes));
+    return max_two(max_two(w.x & kMagnitudes, w.y & kMagnitudes), max_two(w.z & kMagnitudes, w.w & kMagnitudes));
 }
 __device__ __forceinline__ uint4 most_of(uint4 a, uint4 b) {
-    return make_uint4(__vmaxu2(a.x, b.x), __vmaxu2(a.y, b.y), __vmaxu2(a.z, b.z), __vmaxu2(a.w, b.w));
+    return make_uint4(max_two(a.x, b.x), max_two(a.y, b.y), max_two(a.z, b.z), max_two(a.w, b.w));
 }
 __device__ __forceinline__ uint4 magnitudes(uint4 w) {
     return make_uint4(w.x & kMagnitudes, w.y & kMagnitudes, w.z & kMagnitudes, w.w & kMagnitudes);
@@ -399,8 +405,8 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_words_kernel(const R
         uint32_t m01 = m[0] | m[1] << 16, m23 = m[2] | m[3] << 16;
 #pragma unroll
         for (int d = 8; d; d >>= 1) {
-            m01 = __vmaxu2(m01, __shfl_xor_sync(~0u, m01, d));
-            m23 = __vmaxu2(m23, __shfl_xor_sync(~0u, m23, d));
+            m01 = max_two(m01, __shfl_xor_sync(~0u, m01, d));
+            m23 = max_two(m23, __shfl_xor_sync(~0u, m23, d));
         }
         const uint32_t pair = l16 & 2 ? m23 : m01;  // lane i of a half: row i & 3
         const uint32_t row_byte = scale_byte(widen<DT>(l16 & 1 ? pair >> 16 : pair & 0xffffu));
@@ -424,7 +430,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_words_kernel(const R
                 const uint32_t c = col0 + 2 * threadIdx.x;
                 uint32_t two = 0;
 #pragma unroll
-                for (int i = 0; i < kTileThreads / 32; ++i) two = __vmaxu2(two, reinterpret_cast<const uint32_t*>(col_max[i])[threadIdx.x]);
+                for (int i = 0; i < kTileThreads / 32; ++i) two = max_two(two, reinterpret_cast<const uint32_t*>(col_max[i])[threadIdx.x]);
                 const uint32_t lo = scale_byte(widen<DT>(two & 0xffffu)), hi = scale_byte(widen<DT>(two >> 16));
                 if (c < a.cols) {
                     a.scales_t[(uint64_t)row_t * a.scales_t_stride + c] = (uint8_t)lo;
@@ -542,7 +548,7 @@ __global__ void __launch_bounds__(kTileThreads, 3) quantize_word_blocks_kernel(c
     }
     uint32_t two = 0;
 #pragma unroll
-    for (int i = 0; i < kTileRows; ++i) two = __vmaxu2(two, __vmaxu2(w[i].x & kMagnitudes, w[i].y & kMagnitudes));
+    for (int i = 0; i < kTileRows; ++i) two = max_two(two, max_two(w[i].x & kMagnitudes, w[i].y & kMagnitudes));
     uint32_t amax = __reduce_max_sync(~0u, max(two >> 16, two & 0xffffu));
     if (lane == 0) warp_max[warp] = amax;
     __syncthreads();
