@@ -105,14 +105,19 @@ struct Walk {
     __device__ uint32_t height() const { return m1 - m0 > 128 && p.tile_m == 256 ? 256u : 128u; }
 };
 
-// 128 scale bytes of a block, four rows a lane: rows row0 + 4 * lane ...; rows from `rows` on count as 1
+// 128 scale bytes of a block, four rows a lane: rows row0 + 4 * lane ...; the bytes of rows from `rows` on do not matter.  words:
+// lines start at multiples of four (the rest of a word that holds a row's byte is read with it).  Nothing is done with what
+// is read, so that all of a group's loads are on their way together.
 __device__ __forceinline__ uint32_t row_scales(const uint8_t* line, uint32_t row0, uint32_t rows, bool words, int lane) {
     const uint32_t r = row0 + 4 * lane;
-    if (words && r + 3 < rows) return __ldg(reinterpret_cast<const uint32_t*>(line + r));
     uint32_t v = 0x7f7f7f7fu;
+    if (words) {
+        if (r < rows) v = __ldg(reinterpret_cast<const uint32_t*>(line + r));
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (r + i < rows) v = (v & ~(255u << (8 * i))) | (uint32_t)__ldg(line + r + i) << (8 * i);
+        for (int i = 0; i < 4; ++i)
+            if (r + i < rows) v = (v & ~(255u << (8 * i))) | (uint32_t)__ldg(line + r + i) << (8 * i);
+    }
     return v;
 }
 // Scale bytes of four blocks, four rows a lane in each, to words of a row's four bytes: row r in word r / 32 of line r % 32.
@@ -329,7 +334,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         }
         __syncwarp();
     } else if (warp < 4) {
-        // this warp's groups are every other one; the bytes of its next are fetched before it lays out the last
+        // this warp's groups are every other one; the next one's bytes are on their way while it waits for room
         uint32_t kb = 0, group = 0;
         bool more = w.next();
         auto settle = [&]() {  // to the next block of the contraction that there is
@@ -348,17 +353,16 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             some = more;
             if (!more) return;
             const uint32_t n0 = w.n0 + 128 * rank;
+            const uint8_t* block = p.b_scales + (MODE == CIERA_PRODUCT_ROWS ? w.e : 0) * p.b_scales_matrix_stride + (uint64_t)(n0 / 128) * p.b_scales_stride;
 #pragma unroll
             for (int j = 0; j < kGroup; ++j) {
-                vb[j] = va0[j] = va1[j] = 0x7f7f7f7fu;
-                if (kb + j >= w.kb1) continue;
-                if (!p.b_blocks)
-                    vb[j] = row_scales(p.b_scales + (kb + j) * p.b_scales_stride, n0, p.n, p.b_words, lane);
-                else if (n0 < p.n)
-                    vb[j] = __ldg(p.b_scales + (MODE == CIERA_PRODUCT_ROWS ? w.e : 0) * p.b_scales_matrix_stride +
-                                  (uint64_t)(n0 / 128) * p.b_scales_stride + kb + j) * 0x01010101u;
-                va0[j] = row_scales(p.a_scales + (kb + j) * p.a_scales_stride, w.m0, w.m1, p.a_words, lane);
-                va1[j] = row_scales(p.a_scales + (kb + j) * p.a_scales_stride, w.m0 + 128, w.m1, p.a_words, lane);
+                vb[j] = va0[j] = va1[j] = 127u;
+                const uint32_t k = kb + j;
+                if (k >= w.kb1) continue;
+                if (!p.b_blocks) vb[j] = row_scales(p.b_scales + k * p.b_scales_stride, n0, p.n, p.b_words, lane);
+                else if (n0 < p.n) vb[j] = __ldg(block + k);
+                va0[j] = row_scales(p.a_scales + k * p.a_scales_stride, w.m0, w.m1, p.a_words, lane);
+                va1[j] = row_scales(p.a_scales + k * p.a_scales_stride, w.m0 + 128, w.m1, p.a_words, lane);
             }
             skip();
         };
@@ -369,22 +373,22 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             group = 1;
         }
         fetch();
-        skip();
         while (some) {
-            uint32_t b_now[kGroup], a0_now[kGroup], a1_now[kGroup];
-#pragma unroll
-            for (int j = 0; j < kGroup; ++j) b_now[j] = vb[j], a0_now[j] = va0[j], a1_now[j] = va1[j];
-            fetch();
-            skip();
             const uint32_t g = group % kGroups;
             if (!mbar_wait_soon(&sm.scales_empty[g], ((group / kGroups) & 1) ^ 1, abort, p.status)) break;
-            lay_out_scales(sm.b_scales[g], b_now, lane);
-            lay_out_scales(sm.a_scales[g][0], a0_now, lane);
-            lay_out_scales(sm.a_scales[g][1], a1_now, lane);
+            if (p.b_blocks) {
+#pragma unroll
+                for (int j = 0; j < kGroup; ++j) vb[j] *= 0x01010101u;
+            }
+            lay_out_scales(sm.b_scales[g], vb, lane);
+            lay_out_scales(sm.a_scales[g][0], va0, lane);
+            lay_out_scales(sm.a_scales[g][1], va1, lane);
             fence_async_shared();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(in_first_block(&sm.scales_full[g]));
             group += 2;
+            skip();
+            fetch();
         }
         __syncwarp();
     } else {
