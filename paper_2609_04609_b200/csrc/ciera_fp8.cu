@@ -41,10 +41,21 @@ __device__ __forceinline__ float inverse_scale(uint32_t byte) {
 }
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// two products by one instruction
+__device__ __forceinline__ float2 times(float a, float b, float x, float y) {
+    unsigned long long r;
+    asm("{\n\t.reg .b64 u, v;\n\tmov.b64 u, {%1, %2};\n\tmov.b64 v, {%3, %4};\n\tmul.rn.f32x2 %0, u, v;\n\t}" : "=l"(r) : "f"(a), "f"(b), "f"(x), "f"(y));
+    float2 p;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(p.x), "=f"(p.y) : "l"(r));
+    return p;
+}
+__device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d, float4 inv) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(times(a, b, inv.x, inv.y), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(times(c, d, inv.z, inv.w), __NV_SATFINITE, __NV_E4M3);
+    return __byte_perm(lo, hi, 0x5410);
+}
 __device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d, float inv) {
-    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a * inv, b * inv), __NV_SATFINITE, __NV_E4M3);
-    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c * inv, d * inv), __NV_SATFINITE, __NV_E4M3);
-    return lo | hi << 16;
+    return to_e4m3x4(a, b, c, d, make_float4(inv, inv, inv, inv));
 }
 
 // sigmoid(g) = 1 / (1 + e) and 1 - sigmoid(g) = e / (1 + e) with e = 2^(-g log2 e): the exponent in two parts, so that the power
@@ -447,7 +458,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_words_kernel(const R
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float2 ab = two_values<DT>(h ? w[i].z : w[i].x), cd = two_values<DT>(h ? w[i].w : w[i].y);
-                    four[i] = to_e4m3x4(ab.x * inv.x, ab.y * inv.y, cd.x * inv.z, cd.y * inv.w, 1.f);
+                    four[i] = to_e4m3x4(ab.x, ab.y, cd.x, cd.y, inv);
                 }
                 turn_bytes(four[0], four[1], four[2], four[3], t);
 #pragma unroll

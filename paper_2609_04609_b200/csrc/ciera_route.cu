@@ -368,7 +368,7 @@ __host__ __device__ inline uint32_t warp_floats(uint32_t n_experts) {
 
 // KL: at least top_k + 2 (one more than asked for, to see how near it came, and one for values that share a word's bits)
 template <int DT, int EPL, int KL>
-__global__ void __launch_bounds__(kRouteWarps * 32)
+__global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
     route_kernel(const RouteArgs a, const value_t<DT>* __restrict__ logits, uint64_t n_tokens, uint32_t tokens_each, uint64_t stride,
                  int whole, const float* __restrict__ bias, int32_t* __restrict__ experts, float* __restrict__ weights) {
     constexpr int L = kTokenLanes<EPL>, Q = (KL + L - 1) / L;
