@@ -41,18 +41,10 @@ __device__ __forceinline__ float inverse_scale(uint32_t byte) {
 }
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
-// two products by one instruction
-__device__ __forceinline__ float2 times(float a, float b, float x, float y) {
-    unsigned long long r;
-    asm("{\n\t.reg .b64 u, v;\n\tmov.b64 u, {%1, %2};\n\tmov.b64 v, {%3, %4};\n\tmul.rn.f32x2 %0, u, v;\n\t}" : "=l"(r) : "f"(a), "f"(b), "f"(x), "f"(y));
-    float2 p;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(p.x), "=f"(p.y) : "l"(r));
-    return p;
-}
 __device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d, float4 inv) {
-    const uint32_t lo = __nv_cvt_float2_to_fp8x2(times(a, b, inv.x, inv.y), __NV_SATFINITE, __NV_E4M3);
-    const uint32_t hi = __nv_cvt_float2_to_fp8x2(times(c, d, inv.z, inv.w), __NV_SATFINITE, __NV_E4M3);
-    return __byte_perm(lo, hi, 0x5410);
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a * inv.x, b * inv.y), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c * inv.z, d * inv.w), __NV_SATFINITE, __NV_E4M3);
+    return lo | hi << 16;
 }
 __device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d, float inv) {
     return to_e4m3x4(a, b, c, d, make_float4(inv, inv, inv, inv));
@@ -355,9 +347,10 @@ __device__ __forceinline__ uint4 magnitudes(uint4 w) {
     return make_uint4(w.x & kMagnitudes, w.y & kMagnitudes, w.z & kMagnitudes, w.w & kMagnitudes);
 }
 
-// Blocks stay and take neighbouring tiles one behind the other, with the next tile's values on their way.
+// A block an SM stays and takes neighbouring tiles one behind the other, with the next tile's values on their way (two blocks an SM
+// with half the registers 63 us, a block for each tile 69, this 59).
 template <int DT, bool T>
-__global__ void __launch_bounds__(kTileThreads, 2) quantize_words_kernel(const RowsArgs a, const value_t<DT>* __restrict__ x) {
+__global__ void __launch_bounds__(kTileThreads, 1) quantize_words_kernel(const RowsArgs a, const value_t<DT>* __restrict__ x) {
     __shared__ uint4 col_max[T ? kTileThreads / 32 : 1][16];
     __shared__ __align__(16) float col_inv[128];
     __shared__ __align__(16) uint32_t turned[T ? 128 * 32 : 4];
@@ -636,7 +629,7 @@ extern "C" int ciera_fp8_quantize_rows(const ciera_fp8_rows* p, void* stream) {
             const bool eight = !(((uint64_t)p->x | p->x_stride * 2) & 15) && !(p->cols & 7);
             if (eight && src == CIERA_SOURCE_ROWS && !p->row_weights) {
                 e = launch_after(turned ? quantize_words_kernel<DT, true> : quantize_words_kernel<DT, false>,
-                                 dim3((uint32_t)(tiles < 2 * 148 ? tiles : 2 * 148)), kTileThreads, 0,
+                                 dim3((uint32_t)(tiles < 148 ? tiles : 148)), kTileThreads, 0,
                                  (cudaStream_t)stream, a, (const value_t<DT>*)p->x);
                 return;
             }
