@@ -617,72 +617,95 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
 // dl = J_s^T ds: with p the chosen s over their sum, ds of choice j is scale * dw_j, or scale / sum * (dw_j - sum of p dw) when
 // the weights are renormalised; softmax: dl = s * (ds - sum of ds s), where that sum is zero after renormalisation;
 // sigmoid: dl = s * (1 - s) * ds.
-template <int DT, int EPL>
+// LT lanes a token: half a warp for short rows (32768 tokens of 64 experts with a warp for each 8.9 us).
+template <int LT>
+__device__ __forceinline__ float token_sum(float v) {
+#pragma unroll
+    for (int d = LT / 2; d; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
+    return v;
+}
+
+template <int DT, int EPL, int LT>
 __global__ void __launch_bounds__(kRouteWarps * 32)
     route_backward_kernel(const RouteArgs a, const value_t<DT>* __restrict__ logits, uint64_t n_tokens, uint64_t stride, int whole,
                           const int32_t* __restrict__ experts, const float* __restrict__ dweights,
                           value_t<DT>* __restrict__ dlogits, uint64_t dstride) {
     __shared__ __align__(16) float spread[kRouteWarps][32 * EPL];
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int full_lane = threadIdx.x & 31, warp = threadIdx.x >> 5, base = full_lane / LT * LT, lane = full_lane - base;
     const uint32_t E = a.n_experts, e0 = lane * EPL;
-    float* all = spread[warp];
-    for (uint64_t t = (uint64_t)blockIdx.x * kRouteWarps + warp; t < n_tokens; t += (uint64_t)gridDim.x * kRouteWarps) {
-        const value_t<DT>* row = logits + t * stride;
-        int id = -1;
-        float dw = 0.f, xk = -INFINITY;
-        if (lane < (int)a.top_k) {
-            id = experts[t * a.top_k + lane];
-            if ((uint32_t)id >= E) id = -1;
-            dw = dweights[t * a.top_k + lane];
-        }
+    float* all = spread[warp] + base * EPL;
+    // a token's choice, its weights' gradients and its logits are on their way while the one before is done
+    constexpr int kTokens = kRouteWarps * 32 / LT;  // of a block
+    const uint64_t step = (uint64_t)gridDim.x * kTokens;
+    uint64_t t = (uint64_t)blockIdx.x * kTokens + threadIdx.x / LT;
+    float next_x[EPL], next_dw = 0.f;
+    int next_id = -1;
+    const auto fetch = [&](uint64_t of) {
+        load_logits<DT, EPL>(logits + of * stride, E, whole, lane, next_x);
+        if (lane < (int)a.top_k) next_id = experts[of * a.top_k + lane], next_dw = dweights[of * a.top_k + lane];
+    };
+    if (t < n_tokens) fetch(t);
+    for (uint64_t first = (uint64_t)blockIdx.x * kTokens + warp * (32 / LT); first < n_tokens; first += step, t += step) {
+        const bool here = t < n_tokens;  // (the warp's last token may have none beside it)
+        const int id = here && (uint32_t)next_id < E ? next_id : -1;
+        const float dw = id < 0 ? 0.f : next_dw;
         float x[EPL], s[EPL];
-        load_logits<DT, EPL>(row, E, whole, lane, x);
 #pragma unroll
-        for (int j = 0; j < EPL; ++j) x[j] = open_logit(x[j]);
-        if (id < 0) dw = 0.f;
-        else xk = open_logit(ValueOf<DT>::get(row[id]));
-        float sk;
+        for (int j = 0; j < EPL; ++j) x[j] = here ? open_logit(next_x[j]) : -INFINITY;
+        if (t + step < n_tokens) fetch(t + step);
         if (a.sigmoid) {
 #pragma unroll
             for (int j = 0; j < EPL; ++j) s[j] = sigmoid_of(x[j]);
-            sk = sigmoid_of(xk);
         } else {
             float m = -INFINITY;
 #pragma unroll
             for (int j = 0; j < EPL; ++j) m = fmaxf(m, x[j]);
-            m = unordered(__reduce_max_sync(~0u, ordered(m)));
+            if constexpr (LT == 32) {
+                m = unordered(__reduce_max_sync(~0u, ordered(m)));
+            } else {
+#pragma unroll
+                for (int d = LT / 2; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+            }
             if (m == -INFINITY) m = 0.f;
             float sum = 0.f;
 #pragma unroll
             for (int j = 0; j < EPL; ++j) sum += s[j] = expf(x[j] - m);
-            sum = warp_sum(sum);
+            sum = token_sum<LT>(sum);
             const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
 #pragma unroll
             for (int j = 0; j < EPL; ++j) s[j] *= inv;
-            sk = expf(xk - m) * inv;
         }
+        // the chosen scores
+        Pack<float, EPL> put;
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) put.v[j] = s[j];
+        __syncwarp();
+        *reinterpret_cast<Pack<float, EPL>*>(all + e0) = put;
+        __syncwarp();
+        const float sk = id < 0 ? 0.f : all[id];
         float d = dw * a.scale, dot = 0.f;
         if (a.renormalise) {
-            const float total = warp_sum(sk);
+            const float total = token_sum<LT>(sk);
             const float it = total > 0.f ? __fdividef(1.f, total) : 0.f;
-            d = (d - warp_sum(d * sk) * it) * it;
+            d = (d - token_sum<LT>(d * sk) * it) * it;
         } else if (!a.sigmoid) {
-            dot = warp_sum(d * sk);
+            dot = token_sum<LT>(d * sk);
         }
         // an expert that is named more than once gets the sum, in the order of the choices
-        const uint32_t same = __match_any_sync(~0u, id);
+        const uint32_t same = __match_any_sync(~0u, id < 0 ? -1 : id + base * 1024);
         if (__any_sync(~0u, id >= 0 && __popc(same) > 1)) {
             float sum = 0.f;
             for (uint32_t r = 0; r < a.top_k; ++r) {
-                const float dr = __shfl_sync(~0u, d, (int)r);
-                if (same >> r & 1u) sum += dr;
+                const float dr = __shfl_sync(~0u, d, base + (int)r);
+                if (same >> (base + r) & 1u) sum += dr;
             }
             d = sum;
         }
-        __syncwarp();
 #pragma unroll
-        for (int j = 0; j < EPL; ++j) all[j * 32 + lane] = 0.f;
+        for (int j = 0; j < EPL; ++j) put.v[j] = 0.f;
+        __syncwarp();
+        *reinterpret_cast<Pack<float, EPL>*>(all + e0) = put;
         __syncwarp();
         if (id >= 0) all[id] = d;  // (the same sum from each of the same)
         __syncwarp();
@@ -693,6 +716,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
             ds[j] = a.sigmoid ? mine.v[j] * s[j] * (1.f - s[j]) : s[j] * (mine.v[j] - dot);
             if (x[j] == -INFINITY) ds[j] = 0.f;
         }
+        if (!here) continue;
         value_t<DT>* to = dlogits + t * dstride + e0;
         if (whole && e0 + EPL <= E) {
             store_values<DT, EPL>(to, ds);
@@ -810,12 +834,22 @@ extern "C" int ciera_route_backward(const ciera_route_config* config, int dtype,
         constexpr int DT = decltype(dt)::value;
         if (!n_tokens) return;
         with_row(a.n_experts, [&](auto epl) {
+            const auto go = [&](auto each, auto lanes) {
+                constexpr int EPL = decltype(each)::value, LT = decltype(lanes)::value;
+                const int whole = whole_rows(logits_dev, logits_stride, dtype_bytes(DT), EPL) &&
+                                  whole_rows(dlogits_dev, dlogits_stride, dtype_bytes(DT), EPL);
+                e = launch_after(route_backward_kernel<DT, EPL, LT>, dim3(route_grid((n_tokens + 32 / LT - 1) / (32 / LT))), kRouteWarps * 32, 0,
+                                 (cudaStream_t)stream, a, (const value_t<DT>*)logits_dev, n_tokens, logits_stride, whole, experts_dev,
+                                 dweights_dev, (value_t<DT>*)dlogits_dev, dlogits_stride);
+            };
             constexpr int EPL = decltype(epl)::value;
-            const int whole = whole_rows(logits_dev, logits_stride, dtype_bytes(DT), EPL) &&
-                              whole_rows(dlogits_dev, dlogits_stride, dtype_bytes(DT), EPL);
-            e = launch_after(route_backward_kernel<DT, EPL>, dim3(route_grid(n_tokens)), kRouteWarps * 32, 0, (cudaStream_t)stream, a,
-                             (const value_t<DT>*)logits_dev, n_tokens, logits_stride, whole, experts_dev, dweights_dev,
-                             (value_t<DT>*)dlogits_dev, dlogits_stride);
+            if constexpr (EPL == 2) {
+                if (a.top_k <= 16) {
+                    go(std::integral_constant<int, 4>(), std::integral_constant<int, 16>());
+                    return;
+                }
+            }
+            go(epl, std::integral_constant<int, 32>());
         });
     });
     if (!known) return CIERA_ERR_INVALID_ARG;
