@@ -4,10 +4,9 @@
 // order of choice, or the groups on either side of the last one kept, are nearer to each other than 32 bits can tell, and do not
 // come from the same logit and bias, the token is done again in 64 bits (route_exact).
 //
-// A warp takes up to 32 / L tokens, one after the other at first, a lane with EPL neighbouring experts, for what needs the whole
-// row (the softmax's sums, the scores); the values go to shared memory.  Then L lanes go through a token's values, each with a
-// sorted list of the largest in registers, as single words that hold the place beside the value.  The lists are merged, and the
-// few that are left are compared as they are.  Instructions bound it.  (The k largest picked one by one by the whole warp:
+// L lanes take a token and go through its row, each with a sorted list of the largest values in registers, as single words that
+// hold the place beside the value (with groups, through shared memory, for their values come first).  The lists are merged,
+// and the few that are left are compared as they are.  Instructions bound it.  (The k largest picked one by one by the whole warp:
 // 16384 tokens of 256 experts in 8 groups 43 us, 1600 instructions a token.)
 #include <math.h>
 
@@ -356,14 +355,11 @@ template <int EPL>
 constexpr int kTokenLanes = EPL <= 8 ? 4 : 16;  // L
 
 // floats between the tokens' rows in shared memory: lanes that read 16 bytes together find them in banks of their own
-template <int EPL>
-__host__ __device__ inline uint32_t row_floats(uint32_t n_experts) {
-    return (n_experts + 31) / 32 * 32 + 16;
-}
-// of a warp: its tokens' rows, two floats a token of the softmax, 32 group values a token
+__host__ __device__ inline uint32_t row_floats(uint32_t n_experts) { return (n_experts + 31) / 32 * 32 + 16; }
+// of a warp: its tokens' rows and 32 group values a token
 template <int EPL>
 __host__ __device__ inline uint32_t warp_floats(uint32_t n_experts) {
-    return 32 / kTokenLanes<EPL> * (row_floats<EPL>(n_experts) + 2 + 32);
+    return 32 / kTokenLanes<EPL> * (row_floats(n_experts) + 32);
 }
 
 // KL: at least top_k + 2 (one more than asked for, to see how near it came, and one for values that share a word's bits)
@@ -371,85 +367,25 @@ template <int DT, int EPL, int KL>
 __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
     route_kernel(const RouteArgs a, const value_t<DT>* __restrict__ logits, uint64_t n_tokens, uint32_t tokens_each, uint64_t stride,
                  int whole, const float* __restrict__ bias, int32_t* __restrict__ experts, float* __restrict__ weights) {
-    constexpr int L = kTokenLanes<EPL>, Q = (KL + L - 1) / L;
+    constexpr int L = kTokenLanes<EPL>, Q = (KL + L - 1) / L, V = 16 / sizeof(value_t<DT>);
     extern __shared__ __align__(16) float route_smem[];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t E = a.n_experts, e0 = lane * EPL, pitch = row_floats<EPL>(E);
+    const uint32_t E = a.n_experts, pitch = row_floats(E);
     float* rows = route_smem + warp * warp_floats<EPL>(E);
-    float* stats = rows + 32 / L * pitch;
-    float* group_values = stats + 32 / L * 2;
+    float* group_values = rows + 32 / L * pitch;
     const bool grouped = a.top_groups < a.n_groups, scored = bias || grouped;
     const uint32_t place_mask = E > 1 ? ~0u >> __clz(E - 1) : 0u;  // a word's last bits: its place, lower places higher
+    float* shifts = route_smem + kRouteWarps * warp_floats<EPL>(E);  // the bias, for the whole block
+    for (uint32_t e = threadIdx.x; e < row_floats(E); e += kRouteWarps * 32) shifts[e] = bias && e < E ? (isnan(bias[e]) ? -INFINITY : bias[e]) : 0.f;
+    __syncthreads();
     const uint64_t first = ((uint64_t)blockIdx.x * kRouteWarps + warp) * tokens_each;
     if (first >= n_tokens) return;
     const uint32_t here = (uint32_t)min((uint64_t)tokens_each, n_tokens - first);
-
-    // the whole rows
-    {
-        constexpr int U = EPL <= 2 ? 4 : EPL <= 8 ? 2 : 1;  // tokens side by side
-        float b[EPL], next[U][EPL];
-#pragma unroll
-        for (int j = 0; j < EPL; ++j) {
-            b[j] = bias && e0 + j < E ? bias[e0 + j] : 0.f;
-            if (isnan(b[j])) b[j] = -INFINITY;
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u < (int)here) load_logits<DT, EPL>(logits + (first + u) * stride, E, whole, lane, next[u]);
-        for (uint32_t i = 0; i < here; i += U) {
-            float x[U][EPL], c[U][EPL], m[U], inv[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-#pragma unroll
-                for (int j = 0; j < EPL; ++j) x[u][j] = open_logit(next[u][j]);
-                if (i + U + u < here) load_logits<DT, EPL>(logits + (first + i + U + u) * stride, E, whole, lane, next[u]);
-                inv[u] = 1.f;
-            }
-            if (!a.sigmoid) {
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    m[u] = x[u][0];
-#pragma unroll
-                    for (int j = 1; j < EPL; ++j) m[u] = fmaxf(m[u], x[u][j]);
-                    m[u] = unordered(__reduce_max_sync(~0u, ordered(m[u])));
-                    if (m[u] == -INFINITY) m[u] = 0.f;  // nothing is open
-                    inv[u] = 0.f;
-#pragma unroll
-                    for (int j = 0; j < EPL; ++j) inv[u] += c[u][j] = expf(x[u][j] - m[u]);
-                }
-#pragma unroll
-                for (int d = 16; d; d >>= 1)
-#pragma unroll
-                    for (int u = 0; u < U; ++u) inv[u] += __shfl_xor_sync(~0u, inv[u], d);
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    inv[u] = inv[u] > 0.f ? __fdividef(1.f, inv[u]) : 0.f;
-                    if (lane == 0 && i + u < here) stats[2 * (i + u)] = m[u], stats[2 * (i + u) + 1] = inv[u];
-                }
-            }
-            // what the choice goes by: the logits where there is no bias (scores rise with them), else s + b
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (i + u >= here || e0 + EPL > pitch) continue;  // (a multiple of the piece)
-                Pack<float, EPL> v;
-#pragma unroll
-                for (int j = 0; j < EPL; ++j) {
-                    float y = x[u][j];
-                    if (scored && y > -INFINITY) y = (a.sigmoid ? __fdividef(1.f, 1.f + __expf(-y)) : c[u][j] * inv[u]) + b[j];
-                    v.v[j] = e0 + j < E ? y : -INFINITY;
-                }
-                *reinterpret_cast<Pack<float, EPL>*>(rows + (i + u) * pitch + e0) = v;
-            }
-        }
-    }
-    __syncwarp();
-
-    // L lanes a token
     const uint32_t l = lane % L, mine = lane / L;
     const bool busy = mine < here;
     const uint64_t t = first + (busy ? mine : 0);
-    const float* row = rows + (busy ? mine : 0) * pitch;
+    float* row = rows + (busy ? mine : 0) * pitch;
     const value_t<DT>* row_logits = logits + t * stride;
     bool sure = true;
     uint32_t list[KL];
@@ -457,6 +393,66 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
     for (int i = 0; i < KL; ++i) list[i] = 0;
     const float unsure = a.sigmoid ? kUnsureSigmoid : kUnsureSoftmax;
     const auto put = [&](float y, uint32_t e) { put_in_list<KL>(list, (ordered(y) & ~place_mask) | ((place_mask - e) & place_mask)); };
+    // Goes through the row, 16 bytes a lane at a time; f(values, the first one's place).  What is behind the row is closed.
+    const auto each_piece = [&](auto&& f) {
+#pragma unroll 2
+        for (uint32_t e = l * V; e < E; e += L * V) {
+            float x[V];
+            if (whole && e + V <= E) {
+                load_values<DT, V>(row_logits + e, x);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) x[j] = e + j < E ? ValueOf<DT>::get(row_logits[e + j]) : -INFINITY;
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[j] = open_logit(x[j]);
+            f(x, e);
+        }
+    };
+    float m = 0.f, inv = 1.f;
+    if (!a.sigmoid) {
+        m = -INFINITY;
+        each_piece([&](const float(&x)[V], uint32_t) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) m = fmaxf(m, x[j]);
+        });
+#pragma unroll
+        for (int d = 1; d < L; d *= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+        if (m == -INFINITY) m = 0.f;  // nothing is open
+        float sum = 0.f;
+        each_piece([&](const float(&x)[V], uint32_t) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum += expf(x[j] - m);
+        });
+#pragma unroll
+        for (int d = 1; d < L; d *= 2) sum += __shfl_xor_sync(~0u, sum, d);
+        inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
+    }
+    // what the choice goes by: the logits where there is no bias (scores rise with them), else s + b
+    each_piece([&](const float(&x)[V], uint32_t e) {
+        float y[V];
+        if (scored) {
+            const Pack<float, V> b = *reinterpret_cast<const Pack<float, V>*>(shifts + e);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float s = a.sigmoid ? __fdividef(1.f, 1.f + __expf(-x[j])) : expf(x[j] - m) * inv;
+                y[j] = x[j] > -INFINITY ? s + b.v[j] : -INFINITY;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) y[j] = x[j];
+        }
+        if (grouped) {
+            if (busy) {
+#pragma unroll
+                for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(row + e + j) = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) put(y[j], e + j);
+        }
+    });
+    __syncwarp();
     if (grouped) {
         float* values = group_values + (busy ? mine : 0) * 32;
         const bool fours = !(a.group_size & 3);
@@ -519,14 +515,6 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
             }
         }
         __syncwarp();
-    } else {
-        for (uint32_t e = 4 * l; e < E; e += 4 * L) {  // (behind the last expert: closed ones)
-            const float4 y = *reinterpret_cast<const float4*>(row + e);
-            put(y.x, e);
-            put(y.y, e + 1);
-            put(y.z, e + 2);
-            put(y.w, e + 3);
-        }
     }
     __syncwarp();
     merge_lists<KL, L>(list);
@@ -541,7 +529,6 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
     float x[Q], s[Q], y[Q], b[Q];
     uint32_t rank[Q];
     int at[Q];
-    const float m = a.sigmoid ? 0.f : stats[2 * (busy ? mine : 0)], inv = a.sigmoid ? 1.f : stats[2 * (busy ? mine : 0) + 1];
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
         const bool open = w[q] > (kClosed | place_mask);
@@ -799,8 +786,9 @@ extern "C" int ciera_route(const ciera_route_config* config, int dtype, const vo
             }
             with_list(a.top_k, [&](auto kl) {
                 constexpr int EPL = decltype(epl)::value, KL = decltype(kl)::value;
-                const int whole = whole_rows(logits_dev, logits_stride, dtype_bytes(DT), EPL);
-                const size_t smem = sizeof(float) * kRouteWarps * warp_floats<EPL>(a.n_experts);  // at most 37 KB
+                const int whole = whole_rows(logits_dev, logits_stride, dtype_bytes(DT), 16 / dtype_bytes(DT));
+                // (also what a token that is done again takes) at most 42 KB
+                const size_t smem = sizeof(float) * (kRouteWarps * warp_floats<EPL>(a.n_experts) + row_floats(a.n_experts));
                 // a warp's lanes are all at work with 32 / L tokens; fewer where that leaves SMs without any
                 const uint64_t most = 32 / kTokenLanes<EPL>, each = (n_tokens + 148 * 16 - 1) / (148 * 16);
                 const uint32_t tokens_each = (uint32_t)(each < most ? each : most);
