@@ -64,10 +64,19 @@ __device__ __forceinline__ double unordered64(unsigned long long u) {
     return u ? __longlong_as_double((long long)(u >> 63 ? u & ~(1ull << 63) : ~u)) : -INFINITY;
 }
 
+// 1 / d for d from 1 to infinity, by Newton's iteration r <- r + r (1 - d r) from 24 bits: 48, then all 53 but the last.  (A
+// division of 64 bits is a call, and as many calls as a lane has experts are done one behind the other.)
+__device__ __forceinline__ double reciprocal64(double d) {
+    double r = (double)__fdividef(1.f, (float)d);
+    r = fma(r, fma(-d, r, 1.0), r);
+    r = fma(r, fma(-d, r, 1.0), r);
+    return d < 1e30 ? r : 1.0 / d;
+}
+
 // One token's choice in 64 bits.  c: n_experts words of 64 bits of the warp's own in shared memory.  What a batch waits for when
 // it has such a token, so with all the parallelism there is: a lane's experts side by side, several lanes to a group.
 template <int DT, int EPL>
-__device__ __noinline__ void route_exact(const value_t<DT>* row, const RouteArgs& a, const float* __restrict__ bias, unsigned long long* c,
+__device__ __noinline__ void route_exact(const value_t<DT>* row, const RouteArgs a, const float* __restrict__ bias, unsigned long long* c,
                                          int32_t* __restrict__ experts, float* __restrict__ weights) {
     const uint32_t E = a.n_experts, lane = threadIdx.x & 31, e0 = lane * EPL;
     float x[EPL];
@@ -88,12 +97,13 @@ __device__ __noinline__ void route_exact(const value_t<DT>* row, const RouteArgs
         total += s[j];
     }
     if (!a.sigmoid) total = warp_sum(total);
+    const double per_total = 1.0 / total;
     unsigned long long key[EPL];
 #pragma unroll
     for (int j = 0; j < EPL; ++j) {
         key[j] = 0ull;
         if (x[j] == -INFINITY) continue;
-        s[j] = a.sigmoid ? 1.0 / (1.0 + s[j]) : s[j] / total;
+        s[j] = a.sigmoid ? reciprocal64(1.0 + s[j]) : s[j] * per_total;
         key[j] = ordered64(s[j] + (bias ? (double)bias[e0 + j] : 0.0));
     }
     if (a.top_groups < a.n_groups) {
@@ -123,9 +133,12 @@ __device__ __noinline__ void route_exact(const value_t<DT>* row, const RouteArgs
             rank += o > value || (o == value && i < g);
         }
         const uint32_t keep = __ballot_sync(~0u, value && rank < a.top_groups);
+        const float per_size = __fdividef(1.f, (float)a.group_size);
 #pragma unroll
-        for (int j = 0; j < EPL; ++j)
-            if (e0 + j < E && !(keep >> ((e0 + j) / a.group_size * per) & 1u)) key[j] = 0ull;
+        for (int j = 0; j < EPL; ++j) {  // (of places below 1024 the quotient is exact: a half is further from a whole than 2^-12)
+            const uint32_t g_of = (uint32_t)(((float)(e0 + j) + 0.5f) * per_size);
+            if (e0 + j < E && !(keep >> (g_of * per) & 1u)) key[j] = 0ull;
+        }
         __syncwarp();
     }
     // lane i ends up with choice i: the largest, by the upper half first
@@ -167,9 +180,19 @@ __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(
 
 __device__ __forceinline__ float sigmoid_of(float x) { return __fdividef(1.f, 1.f + expf(-x)); }
 
-// Scores in 32 bits are off by less than this part of themselves: sigmoid by an exponential, a sum and a reciprocal of a step or
-// two each; softmax also by what all its scores share, a sum of up to 1024 terms in a tree over 32 lanes.
-constexpr float kUnsureSigmoid = 1e-6f, kUnsureSoftmax = 4e-6f;
+// How far two values have to be apart for 32 bits to tell them.  A score by sigmoid is off by less than 3e-7: the exponential by two
+// steps of itself (times s (1 - s), at most a quarter), the sum by half a step, the reciprocal by two, and c by half a step of
+// itself.  Softmax's by less than 4e-6 of itself, with what all its scores share, a sum of up to 1024 terms over 4 to 32 lanes.
+constexpr float kUnsureSigmoid = 4e-7f, kUnsureSoftmax = 4e-6f;
+// two values c whose scores are at most s
+__device__ __forceinline__ float unsure_values(bool sigmoid, float s, float c) {
+    return sigmoid ? 2.f * kUnsureSigmoid + 2e-7f * fabsf(c) : kUnsureSoftmax * (s + fabsf(c));
+}
+// two groups' values, of up to two scores each
+__device__ __forceinline__ float unsure_groups(bool sigmoid, bool bias, float a, float b) {
+    const float size = fabsf(a) + fabsf(b);
+    return sigmoid ? 4.f * kUnsureSigmoid + 3e-7f * size : kUnsureSoftmax * (size + (bias ? 4.f : 0.f));
+}
 
 constexpr uint32_t kClosed = 0x007fffffu;  // ordered(-inf): words up to here are of closed experts
 
@@ -204,7 +227,6 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
     const uint64_t t = (uint64_t)blockIdx.x * kRouteWarps + warp;
     if (t >= n_tokens) return;
     const bool grouped = a.top_groups < a.n_groups, scored = bias || grouped;
-    const float unsure = a.sigmoid ? kUnsureSigmoid : kUnsureSoftmax;
     const value_t<DT>* row = logits + t * stride;
     float x[EPL], c[EPL], m = 0.f, inv = 1.f;
     load_logits<DT, EPL>(row, E, whole, lane, x);
@@ -260,7 +282,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
         const uint32_t keep = __ballot_sync(~0u, stays);
         const float last = -unordered(__reduce_max_sync(~0u, ordered(stays ? -value : -INFINITY)));
         const float next = unordered(__reduce_max_sync(~0u, ordered(open && !stays ? value : -INFINITY)));
-        if (next > -INFINITY) sure = sure && last - next > unsure * (fabsf(last) + fabsf(next) + (bias ? 4.f : 0.f));
+        if (next > -INFINITY) sure = sure && last - next > unsure_groups(a.sigmoid, bias, last, next);
 #pragma unroll
         for (int j = 0; j < EPL; ++j)
             if (e0 + j < E && !(keep >> ((e0 + j) / a.group_size * per) & 1u)) c[j] = -INFINITY;
@@ -300,7 +322,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
     if (mine >= 0 && !scored) sure = sure && (a.sigmoid ? xm < 16.f && xm > -600.f : xm - m > -600.f);
     // (two values that share a word's bits are out of order at most by what those bits are worth)
     if (lane < 31 && mine >= 0 && other >= 0 && !(xm == xn && bm == bn))
-        sure = sure && y - yn > (scored ? unsure * (sm + fabsf(y)) : 1e-8f) + (DT == CIERA_FP32 || scored ? 1e-5f * fabsf(y) : 0.f);
+        sure = sure && y - yn > (scored ? unsure_values(a.sigmoid, sm, y) : 1e-8f) + (DT == CIERA_FP32 || scored ? 1e-5f * fabsf(y) : 0.f);
     if (!__all_sync(~0u, sure)) {
         route_exact<DT, EPL>(row, a, bias, reinterpret_cast<unsigned long long*>(scratch), experts + t * a.top_k, weights + t * a.top_k);
         return;
@@ -391,7 +413,6 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
     uint32_t list[KL];
 #pragma unroll
     for (int i = 0; i < KL; ++i) list[i] = 0;
-    const float unsure = a.sigmoid ? kUnsureSigmoid : kUnsureSoftmax;
     const auto put = [&](float y, uint32_t e) { put_in_list<KL>(list, (ordered(y) & ~place_mask) | ((place_mask - e) & place_mask)); };
     // Goes through the row, 16 bytes a lane at a time; f(values, the first one's place).  What is behind the row is closed.
     const auto each_piece = [&](auto&& f) {
@@ -499,7 +520,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
             keep |= __shfl_xor_sync(~0u, keep, d);
         }
         // (a bias of the other sign makes a sum small; the scores in it are still up to 1 each)
-        if (next > -INFINITY) sure = last - next > unsure * (fabsf(last) + fabsf(next) + (bias ? 4.f : 0.f));
+        if (next > -INFINITY) sure = last - next > unsure_groups(a.sigmoid, bias, last, next);
         for (uint32_t left = keep; left; left &= left - 1) {
             const uint32_t at = (__ffs(left) - 1) * a.group_size;
             if (fours) {
@@ -552,7 +573,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             rank[q] += yi > y[q] || (yi == y[q] && ei < at[q]);
-            const float margin = scored ? unsure * (s[q] + fabsf(y[q])) : 1e-8f;  // (logits below 16 this far apart: 64 bits tell)
+            const float margin = scored ? unsure_values(a.sigmoid, s[q], y[q]) : 1e-8f;  // (logits below 16 this far apart: 64 bits tell)
             if (ei >= 0 && at[q] >= 0 && !(xi == x[q] && bi == b[q])) near[q] |= !(fabsf(yi - y[q]) > margin);
         }
     }
@@ -568,7 +589,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
             s[q] = 0.f;
             continue;
         }
-        sure = sure && !near[q] && (exact_words || beyond == -INFINITY || y[q] - beyond > 2.f * unsure * (s[q] + fabsf(y[q])));
+        sure = sure && !near[q] && (exact_words || beyond == -INFINITY || y[q] - beyond > unsure_values(a.sigmoid, s[q], y[q]));
         sum += s[q];
     }
     if (a.renormalise) {
