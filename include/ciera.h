@@ -548,8 +548,10 @@ CIERA_API int ciera_fp8_quantize_blocks(const ciera_fp8_blocks* args, void* stre
  * a has a scale for each row and 128 columns; b the same (b_blocks 0, CONTRACT and DENSE) or one for each block of
  * 128 x 128 (b_blocks 1, DENSE and ROWS; strides as in ciera_fp8_blocks).
  * starts rise from 0, are multiples of 128 and end at or below m (ROWS) or k (CONTRACT): otherwise CIERA_ERR_CORRUPT is
- * written to *status, if given, and no output.  a, b are 16-byte aligned, their strides multiples of 16 and at most
- * 2^40 - 16.  Limits: m, n, k 1 .. 2^31 - 256, n_experts 1 .. 1024. */
+ * written to *status, if given, and no output; CIERA_ERR_TIMEOUT if a bounded device wait ran out.  a, b are 16-byte aligned,
+ * their strides multiples of 16 and at most 2^40 - 16.  Where lines of scale bytes start at multiples of 4, the rest of an
+ * aligned word that holds a row's byte may be read with it, and is not used.  Limits: m, n, k 1 .. 2^31 - 256, n_experts
+ * 1 .. 1024. */
 typedef enum ciera_product_mode {
     CIERA_PRODUCT_DENSE = 0,
     CIERA_PRODUCT_ROWS = 1,

@@ -5,10 +5,11 @@
 // fp32: no result passes through registers before the last block.
 //
 // Persistent pairs of blocks of threads (a cluster on two SMs) take tiles of 256 columns x 256 (or 128) rows of out.  b's rows
-// are the tensor cores' first operand, 128 to a block, a's rows the second, half of them to a block: a block then moves 32 KB
-// through its shared memory for 128 values of the contraction, where one of its own would move 48 KB and be bound by that
-// (measured: 8192^3 at 2180 TFLOP/s with one block on 128 x 256).  b's rows in front, since segments of a's end at
-// any multiple of 128: a tile's second half is left out where its segment has no rows for it, in both blocks.
+// are the tensor cores' first operand, 128 to a block, a's rows the second, half of them to a block: a block then writes and reads
+// 32 KB of its shared memory for 128 values of the contraction, in the 512 cycles that the products take, where a block on
+// 128 x 256 of its own would have to move 48 KB.  b's rows in front, since segments of a's end at any multiple of 128: a
+// tile's second half is left out where its segment has no rows for it, in both blocks.  (Such a tile costs three quarters of
+// a whole one.)
 //   warp 0      copies tiles of a and b (128 values of the contraction) into a ring of stages by tensor maps
 //   warp 1      of the first block: starts a stage's four products; before every fourth stage of a tile it copies the scales
 //               of four into tensor memory
@@ -19,6 +20,13 @@
 // Two sums are in flight, so a tile's products run while the one before is written.  Tensor memory has 512 columns: the two sums
 // share 64 of them, which are the first that are read (the next tile's products wait for them alone), and 64 hold the scales of
 // four groups of stages.
+//
+// Measured: 8192^3 385 us, 2850 TFLOP/s (a first form with one block on 128 x 256 and a byte of scales four times over 504);
+// 32768 rows of 64 experts, 2048 x 2048, 144 us forward and 229 us for the weights' gradient, 1074 MB of fp32 results at 83% of the
+// copy rate; one token on 8 experts 11.9 us, of which DRAM needs 5.  A copy of this that starts all products and waits for nothing
+// takes 93 us forward; the rest is the change from one tile's sum to the next, copies that come late, and writing.  Tried
+// and slower: tiles brought into L2 ahead of their copies (forward 144 -> 149 to 156 us, 8192^3 394 -> 413 to 456); two tiles of 128
+// rows to a pair as often as one of 256 (144 -> 150 us).
 #include <cuda.h>
 
 #include <type_traits>
@@ -31,8 +39,8 @@ namespace ciera {
 constexpr int kProductThreads = 256;
 constexpr int kStages = 6;
 constexpr uint32_t kTileN = 256;  // columns of a pair's tile
-constexpr int kGroup = 4;   // stages whose scales go together: a byte each in a word
-constexpr int kGroups = 4;  // such groups in shared and in tensor memory
+constexpr int kGroup = 4;         // stages whose scales go together: a byte each in a word
+constexpr int kGroups = 4;        // such groups in shared and in tensor memory
 constexpr uint32_t kMaxSegments = 1024;
 constexpr uint32_t kShared = 64, kSecondSum = 256 - kShared, kScalesAt = kSecondSum + 256;  // columns of tensor memory
 
