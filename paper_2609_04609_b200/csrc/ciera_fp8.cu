@@ -2,8 +2,10 @@
 //
 // A block of threads has a tile of 128 x 128 values.  A warp has 8 rows, a lane 4 neighbouring columns of each, so a row's
 // largest magnitude is one reduction over the warp and the tile is read and kept in registers once for both orientations;
-// the transposed copy goes through shared memory to be written 128 bytes at a time.  Memory bounds it.  Tiles beside each
-// other come one behind the other, so that blocks that run together read and write whole rows.
+// the transposed copy goes through shared memory to be written 128 bytes at a time.  Tiles beside each other come one behind
+// the other, so that blocks that run together read and write whole rows.  Square blocks are bound by memory (64 matrices of
+// 2048 x 1024 in 97 us, 0.85 of the copy rate), rows in both orientations by instructions: each value is scaled and rounded
+// twice (32768 rows of 2048: gathered 59 us, of which memory needs 24; weighted 83; silu(g) * u of 1024 85; its gradient 178).
 #include <type_traits>
 
 #include "ciera_numeric.cuh"

@@ -65,7 +65,6 @@ inline uint64_t dtype_bytes(int dtype) { return dtype == CIERA_FP32 ? 4 : 2; }
 inline bool aligned_to(const void* p, uint64_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
 constexpr int kFp8Block = CIERA_FP8_BLOCK;
-constexpr float kFp8Max = 448.f;  // largest e4m3 value, 1.75 * 2^8
 constexpr uint64_t kMaxExtent = (1ull << 31) - 256;
 
 }  // namespace ciera

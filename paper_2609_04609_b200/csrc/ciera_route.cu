@@ -796,7 +796,7 @@ extern "C" int ciera_route(const ciera_route_config* config, int dtype, const vo
         if (!n_tokens) return;
         with_row(a.n_experts, [&](auto epl) {
             // A warp for each token while all of them have room on the GPU, else up to 32 / L tokens a warp (one token 2.5 us against
-            // 5.8, 16384 tokens of 256 experts in 8 groups 43 us against 28).
+            // 5.8, 16384 tokens of 256 experts in 8 groups 43 us against 24).
             if (n_tokens < 148 * 32) {
                 constexpr int EPL = decltype(epl)::value;
                 e = launch_after(route_few_kernel<DT, EPL>, dim3((uint32_t)((n_tokens + kRouteWarps - 1) / kRouteWarps)), kRouteWarps * 32,
