@@ -5,7 +5,7 @@
 // the transposed copy goes through shared memory to be written 128 bytes at a time.  Tiles beside each other come one behind
 // the other, so that blocks that run together read and write whole rows.  Square blocks are bound by memory (64 matrices of
 // 2048 x 1024 in 97 us, 0.85 of the copy rate), rows in both orientations by instructions: each value is scaled and rounded
-// twice (32768 rows of 2048: gathered 59 us, of which memory needs 24; weighted 83; silu(g) * u of 1024 85; its gradient 178).
+// twice (32768 rows of 2048: gathered 59 us, of which memory needs 24; weighted 80; silu(g) * u of 1024 66; its gradient 159).
 #include <type_traits>
 
 #include "ciera_numeric.cuh"
@@ -61,8 +61,9 @@ __device__ __forceinline__ float2 sigmoid32(float g) {
     float e;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
     e = fmaf(e, rest * 0.693147181f, e);
-    const float s = isnan(g) ? g : __fdividef(1.f, 1.f + e);
-    return make_float2(s, e * s);
+    float s;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + e));
+    return make_float2(s, e * s);  // (a NaN is not seen here; g itself is a factor of all that this goes into)
 }
 __device__ __forceinline__ float swiglu32(float g, float u) { return g * sigmoid32(g).x * u; }
 __device__ __forceinline__ float swiglu_gate32(float g, float u, float d) {
@@ -71,46 +72,53 @@ __device__ __forceinline__ float swiglu_gate32(float g, float u, float d) {
 }
 __device__ __forceinline__ float swiglu_up32(float g, float d) { return d * g * sigmoid32(g).x; }
 
-// Four neighbouring values of a row: x's, silu(g) * u, or one of their gradients.  WIDE: one access for each four of an input.
-template <int DT, int SRC, bool WIDE>
+// Four neighbouring values of each input that four values of a row are made from, as they are read.
+template <int DT>
+struct RawFour {
+    Pack<value_t<DT>, 4> x, up, grad;
+};
+template <int DT, int SRC>
+__device__ __forceinline__ void read_four(const value_t<DT>* __restrict__ x, const value_t<DT>* __restrict__ grad, uint32_t c, uint32_t cols,
+                                          RawFour<DT>& raw) {
+    const auto get = [](const value_t<DT>* p) { return *reinterpret_cast<const Pack<value_t<DT>, 4>*>(p); };
+    if constexpr (SRC == CIERA_SOURCE_ROWS) {
+        raw.x = get(x + c);
+    } else if constexpr (SRC == CIERA_SOURCE_SWIGLU) {
+        raw.x = get(x + c);
+        raw.up = get(x + cols + c);
+    } else {  // (the four are on one side)
+        const uint32_t f = cols / 2, at = c < f ? c : c - f;
+        raw.x = get(x + at);
+        raw.grad = get(grad + at);
+        raw.up = raw.x;
+        if (c < f) raw.up = get(x + f + at);
+    }
+}
+// x's, silu(g) * u, or one of their gradients
+template <int DT, int SRC>
+__device__ __forceinline__ void make_four(const RawFour<DT>& raw, uint32_t c, uint32_t cols, float (&v)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float x = ValueOf<DT>::get(raw.x.v[j]);
+        if constexpr (SRC == CIERA_SOURCE_ROWS) v[j] = x;
+        else if constexpr (SRC == CIERA_SOURCE_SWIGLU) v[j] = swiglu32(x, ValueOf<DT>::get(raw.up.v[j]));
+        else v[j] = c < cols / 2 ? swiglu_gate32(x, ValueOf<DT>::get(raw.up.v[j]), ValueOf<DT>::get(raw.grad.v[j])) : swiglu_up32(x, ValueOf<DT>::get(raw.grad.v[j]));
+    }
+}
+// The same value by value, for rows and widths of any kind; 0 behind the row.
+template <int DT, int SRC>
 __device__ __forceinline__ void source_values(const value_t<DT>* __restrict__ x, const value_t<DT>* __restrict__ grad, uint32_t c,
                                               uint32_t cols, float (&v)[4]) {
-    const auto get = [&](const value_t<DT>* p, uint32_t c0, float(&to)[4]) {
-        if constexpr (WIDE) {
-            load_values<DT, 4>(p, to);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[j] = 0.f;
+        if (c + j >= cols) continue;
+        if constexpr (SRC == CIERA_SOURCE_ROWS) {
+            v[j] = ValueOf<DT>::get(x[c + j]);
+        } else if constexpr (SRC == CIERA_SOURCE_SWIGLU) {
+            v[j] = swiglu32(ValueOf<DT>::get(x[c + j]), ValueOf<DT>::get(x[cols + c + j]));
         } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) to[j] = c0 + j < cols ? ValueOf<DT>::get(p[j]) : 0.f;
-        }
-    };
-    if constexpr (SRC == CIERA_SOURCE_ROWS) {
-        get(x + c, c, v);
-    } else if constexpr (SRC == CIERA_SOURCE_SWIGLU) {
-        float g[4], u[4];
-        get(x + c, c, g);
-        get(x + cols + c, c, u);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = swiglu32(g[j], u[j]);
-    } else if constexpr (WIDE) {  // (the four are on one side)
-        const uint32_t f = cols / 2, at = c < f ? c : c - f;
-        float g[4], u[4], d[4];
-        get(x + at, c, g);
-        get(grad + at, c, d);
-        if (c < f) {
-            get(x + f + at, c, u);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = swiglu_gate32(g[j], u[j], d[j]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = swiglu_up32(g[j], d[j]);
-        }
-    } else {
-        const uint32_t f = cols / 2;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[j] = 0.f;
-            if (c + j >= cols) continue;
-            const uint32_t at = c + j < f ? c + j : c + j - f;
+            const uint32_t f = cols / 2, at = c + j < f ? c + j : c + j - f;
             const float g = ValueOf<DT>::get(x[at]), u = ValueOf<DT>::get(x[f + at]), d = ValueOf<DT>::get(grad[at]);
             v[j] = c + j < f ? swiglu_gate32(g, u, d) : swiglu_up32(g, d);
         }
@@ -213,15 +221,38 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const Ro
         some = some && from < a.x_rows;
     }
     const uint32_t live = __ballot_sync(~0u, some);
-    const bool whole = c0 + 3 < a.cols;
+    if (!some) from = 0;
     float v[kTileRows][4];
+    if constexpr (WIDE) {
+        // Rows without a slot and columns behind the row read the first of either, and are put to zero afterwards: what is read
+        // stands under no condition, so that several rows' values are on their way together (one by one: silu(g) * u of
+        // 32768 x 1024 in 85 us, its gradient in 178).
+        constexpr int kAtOnce = SRC == CIERA_SOURCE_ROWS ? kTileRows : sizeof(value_t<DT>) == 2 ? 4 : 2;
+        const bool whole = c0 < a.cols;  // (cols is a multiple of four)
+        const uint32_t c = whole ? c0 : 0;
 #pragma unroll
-    for (int i = 0; i < kTileRows; ++i) {
-        const uint32_t r = __shfl_sync(~0u, from, i);
+        for (int i0 = 0; i0 < kTileRows; i0 += kAtOnce) {
+            RawFour<DT> raw[kAtOnce];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[i][j] = 0.f;
-        if (live >> i & 1 && (WIDE ? whole : c0 < a.cols))
-            source_values<DT, SRC, WIDE>(x + r * a.x_stride, SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + r * a.grad_stride : nullptr, c0, a.cols, v[i]);
+            for (int i = 0; i < kAtOnce; ++i) {
+                const uint32_t r = __shfl_sync(~0u, from, i0 + i);
+                if (a.x_rows) read_four<DT, SRC>(x + r * a.x_stride, SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + r * a.grad_stride : nullptr, c, a.cols, raw[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                make_four<DT, SRC>(raw[i], c, a.cols, v[i0 + i]);
+                if (!(live >> (i0 + i) & 1 && whole)) v[i0 + i][0] = v[i0 + i][1] = v[i0 + i][2] = v[i0 + i][3] = 0.f;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kTileRows; ++i) {
+            const uint32_t r = __shfl_sync(~0u, from, i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i][j] = 0.f;
+            if (live >> i & 1 && c0 < a.cols)
+                source_values<DT, SRC>(x + r * a.x_stride, SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + r * a.grad_stride : nullptr, c0, a.cols, v[i]);
+        }
     }
     if (SRC == CIERA_SOURCE_ROWS && a.row_weights) {
 #pragma unroll
@@ -498,8 +529,10 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_blocks_kernel(const 
     for (int i = 0; i < kTileRows; ++i) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[i][j] = 0.f;
-        if (first + i < a.rows && (WIDE ? c0 + 3 < a.cols : c0 < a.cols))
-            source_values<DT, CIERA_SOURCE_ROWS, WIDE>(xm + (first + i) * a.x_stride, nullptr, c0, a.cols, v[i]);
+        if (first + i < a.rows && c0 < a.cols) {
+            if constexpr (WIDE) load_values<DT, 4>(xm + (first + i) * a.x_stride + c0, v[i]);
+            else source_values<DT, CIERA_SOURCE_ROWS>(xm + (first + i) * a.x_stride, nullptr, c0, a.cols, v[i]);
+        }
     }
 #pragma unroll
     for (int i = 0; i < kTileRows; ++i)
