@@ -15,7 +15,7 @@
  *   - Every function returns a ciera_status (0 = CIERA_OK, negative = error).  Nothing throws,
  *     nothing is printed, and no codec state lives in the library: caches, messages and scratch
  *     are the caller's buffers.  What the library does keep per process: the launch counter, the
- *     thread's last CUDA error, per device the grid sizes it has worked out for its kernels, and up to
+ *     thread's last CUDA error, per device the grid sizes and attributes it has worked out for its kernels, and up to
  *     eight pairs of copy streams with their events, made by ciera_roundtrip_host when it first needs
  *     them (all but one pair are given up when the last plan is destroyed).
  *   - "dev" pointers are CUDA device pointers, "host" pointers are ordinary host pointers.
