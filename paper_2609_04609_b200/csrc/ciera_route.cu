@@ -810,9 +810,11 @@ extern "C" int ciera_route(const ciera_route_config* config, int dtype, const vo
                 const int whole = whole_rows(logits_dev, logits_stride, dtype_bytes(DT), 16 / dtype_bytes(DT));
                 // (also what a token that is done again takes) at most 42 KB
                 const size_t smem = sizeof(float) * (kRouteWarps * warp_floats<EPL>(a.n_experts) + row_floats(a.n_experts));
-                // a warp's lanes are all at work with 32 / L tokens; fewer where that leaves SMs without any
+                // A warp's lanes are all at work with 32 / L tokens. Spreading the tokens over more warps than that gains nothing once
+                // there are three for each of 16 warps an SM (6000 of 256 experts 22.8 us spread, 18.2 with full warps; 9000 23.5
+                // and 18.4; 12000 of 64 8.9 and 7.8).
                 const uint64_t most = 32 / kTokenLanes<EPL>, each = (n_tokens + 148 * 16 - 1) / (148 * 16);
-                const uint32_t tokens_each = (uint32_t)(each < most ? each : most);
+                const uint32_t tokens_each = (uint32_t)(each < 3 ? each : most);
                 const uint64_t blocks = (n_tokens + (uint64_t)tokens_each * kRouteWarps - 1) / ((uint64_t)tokens_each * kRouteWarps);
                 e = launch_after(route_kernel<DT, EPL, KL>, dim3((uint32_t)blocks), kRouteWarps * 32, smem, (cudaStream_t)stream, a,
                                  (const value_t<DT>*)logits_dev, n_tokens, tokens_each, logits_stride, whole, bias_dev, experts_dev,
