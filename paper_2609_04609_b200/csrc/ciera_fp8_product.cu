@@ -283,12 +283,23 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 if (++s == kStages) s = 0, odd ^= 1;
             }
         }
-        // given up: the copies in flight (they report to the first block) end before the cluster does
-        if (!ok && rank == 0 && lane == 0)
-            for (uint32_t i = it < kStages ? 0 : it - kStages; i < it; ++i) {
+        // No block leaves while an arrival is on its way to one of its barriers: those that nobody else waits for are waited for
+        // here, and with them all products that read the stages.
+        const uint32_t since = it < kStages ? 0 : it - kStages;
+        if (ok) {
+            for (uint32_t i = since; i < it; ++i) mbar_wait_soon(&sm.empty[i % kStages], (i / kStages) & 1, abort, p.status);
+        } else if (rank == 0 && lane == 0) {  // given up: the copies in flight (they report to the first block) end before the cluster does
+            for (uint32_t i = since; i < it; ++i) {
                 int none = 0;
                 mbar_wait(&sm.full[i % kStages], (i / kStages) & 1, &none, p.status, 1024);
             }
+        }
+        __syncwarp();
+        // (the first block's warp 1 waits for its own; it gives up at most one bound later than this block's warps)
+        if (rank == 1) {
+            int none = 0;
+            mbar_wait(&sm.done, 0, &none, p.status, 3 * kMaxBarrierPolls);
+        }
         __syncwarp();
     } else if (warp == 1) {
         if (rank == 0) {
@@ -381,9 +392,13 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             group = 1;
         }
         fetch();
+        bool ok = true;
         while (some) {
             const uint32_t g = group % kGroups;
-            if (!mbar_wait_soon(&sm.scales_empty[g], ((group / kGroups) & 1) ^ 1, abort, p.status)) break;
+            if (!mbar_wait_soon(&sm.scales_empty[g], ((group / kGroups) & 1) ^ 1, abort, p.status)) {
+                ok = false;
+                break;
+            }
             if (p.b_blocks) {
 #pragma unroll
                 for (int j = 0; j < kGroup; ++j) vb[j] *= 0x01010101u;
@@ -398,6 +413,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             skip();
             fetch();
         }
+        // (as in warp 0: the last groups' arrivals)
+        for (uint32_t back = 4; ok && back; back -= 2)
+            if (group >= back) ok = mbar_wait_soon(&sm.scales_empty[(group - back) % kGroups], ((group - back) / kGroups) & 1, abort, p.status);
         __syncwarp();
     } else {
         const int quarter = warp & 3;
