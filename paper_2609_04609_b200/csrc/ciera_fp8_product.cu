@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         // (the first block's warp 1 waits for its own; it gives up at most one bound later than this block's warps)
         if (rank == 1) {
             int none = 0;
-            mbar_wait(&sm.done, 0, &none, p.status, 3 * kMaxBarrierPolls);
+            mbar_wait_soon(&sm.done, 0, &none, p.status, 3 * kMaxBarrierPolls);
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             while (ok && w.next()) {
                 if (w.kb0 == w.kb1) continue;
                 if (tile) {  // the columns shared with the sum before have been read
-                    if (!mbar_wait_soon(&sm.sums_free[(tile - 1) & 1], ((tile - 1) >> 1) & 1, abort, p.status)) break;
+                    if (!mbar_wait_cluster(&sm.sums_free[(tile - 1) & 1], ((tile - 1) >> 1) & 1, abort, p.status)) break;
                     tensor_fence_after();
                 }
                 const uint32_t first = mx_instruction(256, w.height(), 0), d = tmem + (tile & 1) * kSecondSum;
@@ -317,10 +317,11 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 for (uint32_t kb = w.kb0; kb < w.kb1; ++kb) {
                     const uint32_t sc = tmem + kScalesAt + 16 * g;
                     if (!mbar_wait_soon(&sm.full[s], odd, abort, p.status) ||
-                        (j == 0 && !mbar_wait_soon(&sm.scales_full[g], g_odd, abort, p.status))) {
+                        (j == 0 && !mbar_wait_cluster(&sm.scales_full[g], g_odd, abort, p.status))) {
                         ok = false;
                         break;
                     }
+                    if (j == 0) fence_acquire_shared();
                     tensor_fence_after();
                     const bool last = kb + 1 == w.kb1;
                     if (elect_one()) {
@@ -349,7 +350,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             // nothing that this warp started is in flight when the tensor memory is given back
             if (elect_one()) tensor_commit(&sm.done);
             int none = 0;
-            mbar_wait(&sm.done, 0, &none, p.status);
+            mbar_wait_soon(&sm.done, 0, &none, p.status);
         }
         __syncwarp();
     } else if (warp < 4) {
@@ -445,7 +446,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             tmem_wait_load();
             tensor_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(in_first_block(&sm.sums_free[which]));
+            if (lane == 0) mbar_arrive_cluster_read(in_first_block(&sm.sums_free[which]));
 #pragma unroll
             for (int i = 0; i < 2; ++i) write(r[i], first + i);
             for (uint32_t i = 2; i < parts; ++i) {

@@ -22,12 +22,20 @@ __device__ __forceinline__ uint32_t in_first_block(const void* p) {
     asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(p)));
     return a;
 }
-// An arrival on a barrier of either block.  What it hands over is tensor memory that has been read (behind a tensor_fence_before)
-// or shared memory that only tensor copies read (behind a fence_async_shared): nothing that a wider release would have to wait
-// for.  (With .release.cluster here and .acquire.cluster in the waits: 8192^3 516 us, 507 without.)
+// Arrivals on a barrier of either block, for work that the other block starts, so both sides have the cluster's scope.  With what
+// the warp has written to its own shared memory (behind a fence_async_shared), which is all that the release is for: a full one waits
+// for results on their way to memory too (weights' gradient of 32768 rows 270 us with it) ...
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("fence.release.sync_restrict::shared::cta.cluster;\n\t"
+                 "mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
+                 : "memory");
 }
+// ... and with tensor memory that has been read, which a tensor_fence_before orders
+__device__ __forceinline__ void mbar_arrive_cluster_read(uint32_t bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// behind a mbar_wait_cluster: what the other block's warps have written to shared memory
+__device__ __forceinline__ void fence_acquire_shared() { asm volatile("fence.acquire.sync_restrict::shared::cluster.cluster;" ::: "memory"); }
 // true in one lane of the warp, the same one every time.  Tensor work and tensor-map copies are started under this, by a warp that
 // otherwise runs as one: under `lane == 0` the compiler does not see that one thread is left, and starting a stage's products
 // took longer than the products (8192^3 507 us, 403 with this).
@@ -52,6 +60,34 @@ __device__ __forceinline__ bool mbar_wait_soon(uint64_t* bar, uint32_t parity, v
         if (ok) return true;
     }
     return mbar_wait(bar, parity, abort, status, max_polls);
+}
+
+// mbar_wait_soon for a barrier on which the other block's threads arrive
+__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort, int32_t* status) {
+    for (uint32_t i = 0; i < 256 + kMaxBarrierPolls; ++i) {
+        uint32_t ok;
+        if (i < 256)
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                "selp.u32 %0, 1, 0, p;\n\t}"
+                : "=r"(ok)
+                : "r"(smem_u32(bar)), "r"(parity)
+                : "memory");
+        else
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+                "selp.u32 %0, 1, 0, p;\n\t}"
+                : "=r"(ok)
+                : "r"(smem_u32(bar)), "r"(parity), "r"(kSuspendNs)
+                : "memory");
+        if (ok) return true;
+        if (i >= 256 && *abort) return false;
+    }
+    *abort = 1;
+    if (status) atomicCAS(status, 0, (int32_t)CIERA_ERR_TIMEOUT);
+    return false;
 }
 
 // ---- tensor memory: 128 lanes x 512 columns of 32 bits in each block; an address is lane << 16 | column
