@@ -250,10 +250,11 @@ extern "C" int ciera_expert_layout(const int32_t* experts_dev, uint64_t n_slots,
     const uint64_t chunks = layout_chunks(n_slots);
     const cudaStream_t s = (cudaStream_t)stream;
     const uint32_t* hist = nullptr;
-    const size_t smem = sizeof(uint32_t) * ((kLayoutWarps + 3) * n_experts + 1);  // up to 78 KB
+    const auto place_bytes = [](uint32_t experts) { return sizeof(uint32_t) * ((kLayoutWarps + 3) * experts + 1); };  // up to 78 KB
+    const size_t smem = place_bytes(n_experts);
     cudaError_t e = cudaSuccess;
-    if (smem > 48 * 1024) {
-        e = cudaFuncSetAttribute(layout_place, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (smem > 48 * 1024) {  // (always the same limit: another host thread's call must not lower it before this launch)
+        e = cudaFuncSetAttribute(layout_place, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)place_bytes(kMaxExperts));
         if (e != cudaSuccess) return record_cuda_error(e);
     }
     if (chunks > 1) {
