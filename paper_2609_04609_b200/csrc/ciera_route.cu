@@ -40,8 +40,8 @@ __device__ __forceinline__ float warp_max(float v) {
     return v;
 }
 
-// a logit as it counts: closed (-inf) or finite
-__device__ __forceinline__ float open_logit(float x) { return isnan(x) ? -INFINITY : fminf(x, 3.402823466e38f); }
+// a logit as it counts: closed (-inf) or finite, and one zero (its bits are compared)
+__device__ __forceinline__ float open_logit(float x) { return isnan(x) ? -INFINITY : fminf(x, 3.402823466e38f) + 0.f; }
 
 // The lane's EPL logits; whole: one access for up to 16 bytes of them.
 template <int DT, int EPL>
