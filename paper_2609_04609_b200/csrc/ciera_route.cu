@@ -323,6 +323,18 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
     // (two values that share a word's bits are out of order at most by what those bits are worth)
     if (lane < 31 && mine >= 0 && other >= 0 && !(xm == xn && bm == bn))
         sure = sure && y - yn > (scored ? unsure_values(a.sigmoid, sm, y) : 1e-8f) + (DT == CIERA_FP32 || scored ? 1e-5f * fabsf(y) : 0.f);
+    // The first that is not chosen is the same as the last that is: what shares their words' bits has not been seen.  Whatever is
+    // near them without being the same is looked for in the whole row (closed groups too, for which 64 bits are no mistake).
+    if ((DT == CIERA_FP32 || scored) && __any_sync(~0u, lane + 1 == (int)a.top_k && mine >= 0 && other >= 0 && xm == xn && bm == bn)) {
+        const int from = (int)a.top_k - 1;
+        const float xl = __shfl_sync(~0u, xm, from), bl = __shfl_sync(~0u, bm, from), yl = __shfl_sync(~0u, y, from), sl = __shfl_sync(~0u, sm, from);
+        const float margin = (scored ? unsure_values(a.sigmoid, sl, yl) : 1e-8f) + 1e-5f * fabsf(yl);
+        for (uint32_t e = lane; e < E; e += 32) {
+            const float xe = open_logit(ValueOf<DT>::get(row[e])), be = bias ? bias[e] : 0.f;
+            const float ye = !scored ? xe : (a.sigmoid ? sigmoid_of(xe) : expf(xe - m) * inv) + be;
+            if (xe > -INFINITY && ye > -INFINITY && !(xe == xl && be == bl)) sure = sure && fabsf(ye - yl) > margin;
+        }
+    }
     if (!__all_sync(~0u, sure)) {
         route_exact<DT, EPL>(row, a, bias, reinterpret_cast<unsigned long long*>(scratch), experts + t * a.top_k, weights + t * a.top_k);
         return;

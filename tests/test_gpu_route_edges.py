@@ -20,3 +20,23 @@ def test_zeros_of_either_sign_are_equal(score, dtype):
         assert bool(torch.signbit(x[:50]).any()) and not bool(torch.signbit(x[:50]).all())
         _check(x, None, E, k, score)
         _check(x, torch.zeros(E), E, k, score, 2, 1)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E", [64, 256, 1000])
+def test_equal_scores_hide_no_larger_one(score, E):
+    """k + 1 and more equal logits at low places, and one that is larger by a step or a few of 32 bits at a high one."""
+    g = torch.Generator().manual_seed(E)
+    for k in (1, 3, 8):
+        x = torch.randn(60, E, generator=g)
+        for t in range(60):
+            low = torch.randperm(E // 2, generator=g)[: k + 1 + t % 3]
+            x[t, low] = 6.0
+            y = np.float32(6.0)
+            for _ in range(1 + t % 31):
+                y = np.nextafter(y, np.float32(9))
+            x[t, E // 2 + t % (E // 2)] = float(y)
+        ids, _ = _check(x, None, E, k, score)
+        assert (ids[:, 0].cpu() == E // 2 + torch.arange(60) % (E // 2)).all()
+        _check(x, torch.zeros(E), E, k, score)
+        _check(x, torch.zeros(E), E, k, score, 2, 2)
