@@ -182,16 +182,17 @@ __device__ __forceinline__ float sigmoid_of(float x) { return __fdividef(1.f, 1.
 
 // How far two values have to be apart for 32 bits to tell them.  A score by sigmoid is off by less than 3e-7: the exponential by two
 // steps of itself (times s (1 - s), at most a quarter), the sum by half a step, the reciprocal by two, and c by half a step of
-// itself.  Softmax's by less than 4e-6 of itself, with what all its scores share, a sum of up to 1024 terms over 4 to 32 lanes.
-constexpr float kUnsureSigmoid = 4e-7f, kUnsureSoftmax = 4e-6f;
-// two values c whose scores are at most s
+// itself.  Softmax's by less than 5e-6 of itself, with what all its scores share, a sum of up to 1024 terms over 4 to 32 lanes: up to
+// 64 additions in a lane, half a step each (3.8e-6), and what a term is off by; two of them by 5e-6 of the larger and a step of each.
+constexpr float kUnsureSigmoid = 4e-7f, kUnsureSoftmax = 6e-6f;
+// two values c whose scores are at most s: of both, for a bias may put a large score beside a small one
 __device__ __forceinline__ float unsure_values(bool sigmoid, float s, float c) {
     return sigmoid ? 2.f * kUnsureSigmoid + 2e-7f * fabsf(c) : kUnsureSoftmax * (s + fabsf(c));
 }
-// two groups' values, of up to two scores each
-__device__ __forceinline__ float unsure_groups(bool sigmoid, bool bias, float a, float b) {
+// two groups' values, of up to two scores each, which are at most s where there is a bias
+__device__ __forceinline__ float unsure_groups(bool sigmoid, bool bias, float s, float a, float b) {
     const float size = fabsf(a) + fabsf(b);
-    return sigmoid ? 4.f * kUnsureSigmoid + 3e-7f * size : kUnsureSoftmax * (size + (bias ? 4.f : 0.f));
+    return sigmoid ? 4.f * kUnsureSigmoid + 3e-7f * size : kUnsureSoftmax * (size + (bias ? 4.f * s : 0.f));
 }
 
 constexpr uint32_t kClosed = 0x007fffffu;  // ordered(-inf): words up to here are of closed experts
@@ -282,7 +283,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
         const uint32_t keep = __ballot_sync(~0u, stays);
         const float last = -unordered(__reduce_max_sync(~0u, ordered(stays ? -value : -INFINITY)));
         const float next = unordered(__reduce_max_sync(~0u, ordered(open && !stays ? value : -INFINITY)));
-        if (next > -INFINITY) sure = sure && last - next > unsure_groups(a.sigmoid, bias, last, next);
+        if (next > -INFINITY) sure = sure && last - next > unsure_groups(a.sigmoid, bias, inv, last, next);
 #pragma unroll
         for (int j = 0; j < EPL; ++j)
             if (e0 + j < E && !(keep >> ((e0 + j) / a.group_size * per) & 1u)) c[j] = -INFINITY;
@@ -317,17 +318,20 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
     }
     const float y = scored ? sm + bm : xm;
     const float xn = __shfl_down_sync(~0u, xm, 1), bn = __shfl_down_sync(~0u, bm, 1), yn = __shfl_down_sync(~0u, y, 1);
+    const float sn = __shfl_down_sync(~0u, sm, 1);
     const int other = __shfl_down_sync(~0u, mine, 1);
+    // the larger score of the two; behind the last that is chosen there may be any (the largest of softmax is inv)
+    const float top_score = !bias ? sm : lane + 1 == (int)a.top_k ? inv : fmaxf(sm, sn);
     // where 64 bits no longer tell scores of different logits apart
     if (mine >= 0 && !scored) sure = sure && (a.sigmoid ? xm < 16.f && xm > -600.f : xm - m > -600.f);
     // (two values that share a word's bits are out of order at most by what those bits are worth)
     if (lane < 31 && mine >= 0 && other >= 0 && !(xm == xn && bm == bn))
-        sure = sure && y - yn > (scored ? unsure_values(a.sigmoid, sm, y) : 1e-8f) + (DT == CIERA_FP32 || scored ? 1e-5f * fabsf(y) : 0.f);
+        sure = sure && y - yn > (scored ? unsure_values(a.sigmoid, top_score, y) : 1e-8f) + (DT == CIERA_FP32 || scored ? 1e-5f * fabsf(y) : 0.f);
     // The first that is not chosen is the same as the last that is: what shares their words' bits has not been seen.  Whatever is
     // near them without being the same is looked for in the whole row (closed groups too, for which 64 bits are no mistake).
     if ((DT == CIERA_FP32 || scored) && __any_sync(~0u, lane + 1 == (int)a.top_k && mine >= 0 && other >= 0 && xm == xn && bm == bn)) {
         const int from = (int)a.top_k - 1;
-        const float xl = __shfl_sync(~0u, xm, from), bl = __shfl_sync(~0u, bm, from), yl = __shfl_sync(~0u, y, from), sl = __shfl_sync(~0u, sm, from);
+        const float xl = __shfl_sync(~0u, xm, from), bl = __shfl_sync(~0u, bm, from), yl = __shfl_sync(~0u, y, from), sl = __shfl_sync(~0u, top_score, from);
         const float margin = (scored ? unsure_values(a.sigmoid, sl, yl) : 1e-8f) + 1e-5f * fabsf(yl);
         for (uint32_t e = lane; e < E; e += 32) {
             const float xe = open_logit(ValueOf<DT>::get(row[e])), be = bias ? bias[e] : 0.f;
@@ -532,7 +536,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
             keep |= __shfl_xor_sync(~0u, keep, d);
         }
         // (a bias of the other sign makes a sum small; the scores in it are still up to 1 each)
-        if (next > -INFINITY) sure = last - next > unsure_groups(a.sigmoid, bias, last, next);
+        if (next > -INFINITY) sure = last - next > unsure_groups(a.sigmoid, bias, inv, last, next);
         for (uint32_t left = keep; left; left &= left - 1) {
             const uint32_t at = (__ffs(left) - 1) * a.group_size;
             if (fours) {
@@ -581,15 +585,16 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
     for (int i = 0; i < KL; ++i) {
         const int from = lane / L * L + i % L;
         const float yi = __shfl_sync(~0u, y[i / L], from), xi = __shfl_sync(~0u, x[i / L], from), bi = __shfl_sync(~0u, b[i / L], from);
+        const float si = bias ? __shfl_sync(~0u, s[i / L], from) : 0.f;  // (a bias may put a large score beside a small one)
         const int ei = __shfl_sync(~0u, at[i / L], from);
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             rank[q] += yi > y[q] || (yi == y[q] && ei < at[q]);
-            const float margin = scored ? unsure_values(a.sigmoid, s[q], y[q]) : 1e-8f;  // (logits below 16 this far apart: 64 bits tell)
+            const float margin = scored ? unsure_values(a.sigmoid, fmaxf(s[q], si), y[q]) : 1e-8f;  // (logits below 16 this far apart: 64 bits tell)
             if (ei >= 0 && at[q] >= 0 && !(xi == x[q] && bi == b[q])) near[q] |= !(fabsf(yi - y[q]) > margin);
         }
     }
-    // what is not on the list is at most what the last word of it may stand for
+    // what is not on the list is at most what the last word of it may stand for (its score, where there is a bias, at most inv)
     const uint32_t last = list[KL - 1];
     const float beyond = last > (kClosed | place_mask) ? unordered(last | place_mask) : -INFINITY;
     const bool exact_words = DT != CIERA_FP32 && !scored && !(place_mask >> 13);  // (13 bits and more of such a logit are zero)
@@ -601,7 +606,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
             s[q] = 0.f;
             continue;
         }
-        sure = sure && !near[q] && (exact_words || beyond == -INFINITY || y[q] - beyond > unsure_values(a.sigmoid, s[q], y[q]));
+        sure = sure && !near[q] && (exact_words || beyond == -INFINITY || y[q] - beyond > unsure_values(a.sigmoid, bias ? inv : s[q], y[q]));
         sum += s[q];
     }
     if (a.renormalise) {

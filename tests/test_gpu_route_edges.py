@@ -40,3 +40,29 @@ def test_equal_scores_hide_no_larger_one(score, E):
         assert (ids[:, 0].cpu() == E // 2 + torch.arange(60) % (E // 2)).all()
         _check(x, torch.zeros(E), E, k, score)
         _check(x, torch.zeros(E), E, k, score, 2, 2)
+
+
+@pytest.mark.parametrize("E", [8, 64, 100])
+@pytest.mark.parametrize("G,top_groups", [(1, 1), (4, 3)])
+def test_a_large_score_with_a_bias_against_it(E, G, top_groups):
+    """c of a large score and a large negative bias beside c of a small score: the error of the large one counts."""
+    rng = np.random.default_rng(E)
+    T = 500
+    x = rng.standard_normal((T, E)).astype(np.float32)
+    bias = torch.zeros(E)
+    b0 = float(np.float32(-0.98))
+    bias[0] = b0
+    x[:, 1] = np.abs(x[:, 1]) + 2.0
+    for t in range(T):  # s0 + b0 = s1, solved for the first logit, and a few steps to either side
+        e = np.exp(x[t].astype(np.float64))
+        rest = e[1:].sum()
+        y = np.float32(np.log((-b0 * rest + e[1]) / (1 + b0)))
+        for _ in range(t % 4):
+            y = np.nextafter(y, np.float32(90.0 if t % 8 < 4 else -90.0))
+        x[t, 0] = y
+    logits = torch.from_numpy(x)
+    s, _ = ref.scores(logits, "softmax")
+    assert (np.abs(s[:, 0] + b0 - s[:, 1]) < 1e-7).all()
+    for k in (1, 2, 5):
+        if k <= top_groups * (E // G):
+            _check(logits, bias, E, k, "softmax", G, top_groups, 2)
