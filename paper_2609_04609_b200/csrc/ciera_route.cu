@@ -279,7 +279,8 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
             const float o = __shfl_sync(~0u, value, i * per);
             rank += o > value || (o == value && i < g);
         }
-        const bool open = g < a.n_groups && value > -INFINITY, stays = open && rank < a.top_groups;
+        const bool open = g < a.n_groups && most > -INFINITY, stays = open && rank < a.top_groups;
+        if (open && value == -INFINITY) sure = false;  // (two open experts whose sum is too low for 32 bits)
         const uint32_t keep = __ballot_sync(~0u, stays);
         const float last = -unordered(__reduce_max_sync(~0u, ordered(stays ? -value : -INFINITY)));
         const float next = unordered(__reduce_max_sync(~0u, ordered(open && !stays ? value : -INFINITY)));
@@ -513,7 +514,9 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
             } else {
                 for (uint32_t i = 0; i < a.group_size; ++i) see(row[g * a.group_size + i]);
             }
-            values[g] = a.group_best > 1 && second > -INFINITY ? most + second : most;
+            const float value = a.group_best > 1 && second > -INFINITY ? most + second : most;
+            if (most > -INFINITY && value == -INFINITY) sure = false;  // (two open experts whose sum is too low for 32 bits)
+            values[g] = value;
         }
         __syncwarp();
         // the groups that stay, and how far the first that goes is from the last of them
@@ -536,7 +539,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
             keep |= __shfl_xor_sync(~0u, keep, d);
         }
         // (a bias of the other sign makes a sum small; the scores in it are still up to 1 each)
-        if (next > -INFINITY) sure = last - next > unsure_groups(a.sigmoid, bias, inv, last, next);
+        if (next > -INFINITY) sure = sure && last - next > unsure_groups(a.sigmoid, bias, inv, last, next);
         for (uint32_t left = keep; left; left &= left - 1) {
             const uint32_t at = (__ffs(left) - 1) * a.group_size;
             if (fours) {

@@ -66,3 +66,18 @@ def test_a_large_score_with_a_bias_against_it(E, G, top_groups):
     for k in (1, 2, 5):
         if k <= top_groups * (E // G):
             _check(logits, bias, E, k, "softmax", G, top_groups, 2)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("best", [1, 2])
+def test_a_bias_of_the_lowest_value_closes_nothing(score, best):
+    E, G = 16, 4
+    x = _logits(80, E, "fp32", 3)
+    x[5, 4:8] = float("-inf")
+    bias = torch.full((E,), torch.finfo(torch.float32).min)
+    bias[8:12] = 0.0
+    for k, top_groups in ((6, 2), (4, 1), (12, 3)):
+        ids, _ = _check(x, bias, E, k, score, G, top_groups, best, True)
+        assert (ids >= 0).all()
+    bias[8:12] = torch.finfo(torch.float32).min
+    _check(x, bias, E, 6, score, G, 2, best)
