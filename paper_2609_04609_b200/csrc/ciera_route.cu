@@ -195,6 +195,10 @@ __device__ __forceinline__ float unsure_groups(bool sigmoid, bool bias, float s,
     return sigmoid ? 4.f * kUnsureSigmoid + 3e-7f * size : kUnsureSoftmax * (size + (bias ? 4.f * s : 0.f));
 }
 
+// Chosen scores whose sum is below this are divided by it in 64 bits: their quotients are ordinary numbers, but some of them, or all,
+// are no normal 32-bit ones.
+constexpr float kSmallSum = 1e-10f;
+
 constexpr uint32_t kClosed = 0x007fffffu;  // ordered(-inf): words up to here are of closed experts
 
 // The lane's words in falling order.
@@ -340,15 +344,14 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
             if (xe > -INFINITY && ye > -INFINITY && !(xe == xl && be == bl)) sure = sure && fabsf(ye - yl) > margin;
         }
     }
+    if (lane >= (int)a.top_k || mine < 0) sm = 0.f;
+    const float sum = a.renormalise ? warp_sum(sm) : 1.f;
+    if (mine >= 0 && sum < kSmallSum) sure = false;
     if (!__all_sync(~0u, sure)) {
         route_exact<DT, EPL>(row, a, bias, reinterpret_cast<unsigned long long*>(scratch), experts + t * a.top_k, weights + t * a.top_k);
         return;
     }
-    if (lane >= (int)a.top_k || mine < 0) sm = 0.f;
-    if (a.renormalise) {
-        const float sum = warp_sum(sm);
-        sm = sum > 0.f ? sm / sum : 0.f;
-    }
+    if (a.renormalise) sm = sum > 0.f ? sm / sum : 0.f;
     if (lane < (int)a.top_k) {
         experts[t * a.top_k + lane] = mine;
         weights[t * a.top_k + lane] = sm * a.scale;
@@ -621,6 +624,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
     for (int q = 0; q < Q; ++q) found += at[q] >= 0;
 #pragma unroll
     for (int d = 1; d < L; d *= 2) found += __shfl_xor_sync(~0u, found, d);
+    if (a.renormalise && found && sum < kSmallSum) sure = false;
     if (busy) {
         int32_t* to = experts + t * a.top_k;
         float* tw = weights + t * a.top_k;

@@ -81,3 +81,31 @@ def test_a_bias_of_the_lowest_value_closes_nothing(score, best):
         assert (ids >= 0).all()
     bias[8:12] = torch.finfo(torch.float32).min
     _check(x, bias, E, 6, score, G, 2, best)
+
+
+def _small_scores(score, T=120, E=32):
+    """Logits, a bias under which only small scores are chosen, and how many bits below 1 those lie."""
+    g = torch.Generator().manual_seed(9)
+    x = _logits(T, E, "fp32", 31)
+    depth = torch.linspace(60.0, 690.0, T)[:, None]
+    if score == "sigmoid":
+        return x - depth, None
+    x[:, 1:] -= depth  # the first takes all of the softmax, and the bias keeps it from being chosen
+    x[:, 0] = 0.0
+    bias = torch.zeros(E)
+    bias[0] = -5.0
+    bias[1:] = torch.rand(E - 1, generator=g)
+    return x, bias
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_weights_of_scores_that_vanish_in_32_bits_are_quotients(score):
+    x, bias = _small_scores(score)
+    _, w = _check(x, bias, 32, 4, score, renorm=True, scale=2.5)
+    total = w.sum(1).cpu()
+    assert ((total - 2.5).abs() < 1e-5).all()
+    _check(x, bias, 32, 4, score, 4, 2, 2, renorm=True)
+    far = x.clone()
+    far[:60, 1:] -= 1e6  # vanish in 64 bits as well: the sum is 0
+    far[:60, 0] -= 1e6 if score == "sigmoid" else 0.0
+    _check(far, bias, 32, 4, score, renorm=True)
