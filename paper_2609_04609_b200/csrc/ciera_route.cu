@@ -648,13 +648,28 @@ __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
 
 // dl = J_s^T ds: with p the chosen s over their sum, ds of choice j is scale * dw_j, or scale / sum * (dw_j - sum of p dw) when
 // the weights are renormalised; softmax: dl = s * (ds - sum of ds s), where that sum is zero after renormalisation;
-// sigmoid: dl = s * (1 - s) * ds.
+// sigmoid: dl = s * (1 - s) * ds.  A sum that 32 bits do not hold well: dl = p * (dw_j - sum of p dw) with p from 64 bits, since
+// 1 / sum and s leave their range, and 1 - s is 1.
 // LT lanes a token: half a warp for short rows (32768 tokens of 64 experts with a warp for each 8.9 us).
-template <int LT>
-__device__ __forceinline__ float token_sum(float v) {
+template <int LT, class T>
+__device__ __forceinline__ T token_sum(T v) {
 #pragma unroll
     for (int d = LT / 2; d; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
     return v;
+}
+
+// p * (d - sum of p d) over the token's choices, p the score of logit *at over their sum; for the whole warp
+template <int DT, int LT>
+__device__ __noinline__ float quotient_gradient(const value_t<DT>* at, bool some, int32_t sigmoid, float m, float d) {
+    double p = 0.0;
+    if (some) {
+        const double x = open_logit(ValueOf<DT>::get(*at));
+        p = exp(sigmoid ? -x : x - (double)m);
+        if (sigmoid) p = 1.0 / (1.0 + p);
+    }
+    const double total = token_sum<LT>(p);
+    p = total > 0.0 ? p / total : 0.0;
+    return (float)(((double)d - token_sum<LT>((double)d * p)) * p);
 }
 
 template <int DT, int EPL, int LT>
@@ -686,11 +701,12 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
 #pragma unroll
         for (int j = 0; j < EPL; ++j) x[j] = here ? open_logit(next_x[j]) : -INFINITY;
         if (t + step < n_tokens) fetch(t + step);
+        float m = 0.f;
         if (a.sigmoid) {
 #pragma unroll
             for (int j = 0; j < EPL; ++j) s[j] = sigmoid_of(x[j]);
         } else {
-            float m = -INFINITY;
+            m = -INFINITY;
 #pragma unroll
             for (int j = 0; j < EPL; ++j) m = fmaxf(m, x[j]);
             if constexpr (LT == 32) {
@@ -720,7 +736,18 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
         if (a.renormalise) {
             const float total = token_sum<LT>(sk);
             const float it = total > 0.f ? __fdividef(1.f, total) : 0.f;
-            d = (d - token_sum<LT>(d * sk) * it) * it;
+            const float of32 = (d - token_sum<LT>(d * sk) * it) * it;
+            if (__any_sync(~0u, total < kSmallSum && id >= 0)) {
+                const float of64 = quotient_gradient<DT, LT>(logits + (id >= 0 ? t * stride + id : 0), id >= 0, a.sigmoid, m, d);
+                d = of32;
+                if (total < kSmallSum) {  // (such that what follows leaves it as it is)
+                    d = a.sigmoid ? 4.f * of64 : of64;
+#pragma unroll
+                    for (int j = 0; j < EPL; ++j) s[j] = a.sigmoid ? 0.5f : 1.f;
+                }
+            } else {
+                d = of32;
+            }
         } else if (!a.sigmoid) {
             dot = token_sum<LT>(d * sk);
         }

@@ -109,3 +109,28 @@ def test_weights_of_scores_that_vanish_in_32_bits_are_quotients(score):
     far[:60, 1:] -= 1e6  # vanish in 64 bits as well: the sum is 0
     far[:60, 0] -= 1e6 if score == "sigmoid" else 0.0
     _check(far, bias, 32, 4, score, renorm=True)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E", [32, 200])
+def test_gradients_through_scores_that_vanish_in_32_bits(score, E):
+    from paper_2609_04609_b200 import ciera
+
+    x, bias = _small_scores(score, 110, E)
+    x = torch.cat([x[:100], x[:100] - 1e6])
+    if score == "softmax":
+        x[100:, 0] = 0.0
+    k = 4
+    ids, w = ref.route(x, bias, k, score, renormalise=True)
+    dw = torch.randn(200, k, generator=torch.Generator().manual_seed(4))
+    ids[7, 1] = ids[7, 0]  # the same index twice
+    ids[8, 2] = -1
+    experts = torch.from_numpy(ids).to(torch.int32)
+    want = ref.route_backward(x, experts, dw, score, True, 2.0)
+    assert np.isfinite(want).all() and (want[100:] == 0).all() and (np.abs(want[:100]).max(1) > 0).all() and np.abs(want).max() > 0.1
+    out = torch.full((200, E), 7.0, device=DEV)
+    ciera.route_backward(_config(E, k, score, renorm=True, scale=2.0), x.to(DEV), experts.to(DEV), dw.to(DEV), out)
+    # dl = p (d - sum of p d) for p, d of the chosen: a product and a difference of numbers up to 2 max |d|, each off by a few steps
+    # (quotients, at most k terms), beside a factor 1 - s
+    tol = (k + 24) * 2.0**-24 * 4.0 * 2 * dw.abs().max().item() + 1e-37
+    assert (np.abs(out.double().cpu().numpy() - want) <= tol).all()
