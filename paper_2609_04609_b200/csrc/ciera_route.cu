@@ -407,9 +407,10 @@ __host__ __device__ inline uint32_t warp_floats(uint32_t n_experts) {
 // KL: at least top_k + 2 (one more than asked for, to see how near it came, and one for values that share a word's bits)
 template <int DT, int EPL, int KL>
 __global__ void __launch_bounds__(kRouteWarps * 32, EPL <= 8 ? 4 : 2)
-    route_kernel(const RouteArgs a, const value_t<DT>* __restrict__ logits, uint64_t n_tokens, uint32_t tokens_each, uint64_t stride,
+    route_kernel(const RouteArgs a, const value_t<DT>* __restrict__ logits, uint64_t n_tokens, uint64_t stride,
                  int whole, const float* __restrict__ bias, int32_t* __restrict__ experts, float* __restrict__ weights) {
     constexpr int L = kTokenLanes<EPL>, Q = (KL + L - 1) / L, V = 16 / sizeof(value_t<DT>);
+    constexpr uint32_t tokens_each = 32 / L;
     extern __shared__ __align__(16) float route_smem[];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -846,8 +847,8 @@ extern "C" int ciera_route(const ciera_route_config* config, int dtype, const vo
         constexpr int DT = decltype(dt)::value;
         if (!n_tokens) return;
         with_row(a.n_experts, [&](auto epl) {
-            // A warp for each token while all of them have room on the GPU, else up to 32 / L tokens a warp (one token 2.5 us against
-            // 5.8, 16384 tokens of 256 experts in 8 groups 43 us against 24).
+            // A warp for each token while all of them have room on the GPU, else 32 / L tokens a warp (one token 2.5 us against
+            // 5.8, 16384 tokens of 256 experts in 8 groups 43 us against 24; spread over more warps, 6000 of 256 22.8 us against 18.2).
             if (n_tokens < 148 * 32) {
                 constexpr int EPL = decltype(epl)::value;
                 e = launch_after(route_few_kernel<DT, EPL>, dim3((uint32_t)((n_tokens + kRouteWarps - 1) / kRouteWarps)), kRouteWarps * 32,
@@ -861,14 +862,10 @@ extern "C" int ciera_route(const ciera_route_config* config, int dtype, const vo
                 const int whole = whole_rows(logits_dev, logits_stride, dtype_bytes(DT), 16 / dtype_bytes(DT));
                 // (also what a token that is done again takes) at most 42 KB
                 const size_t smem = sizeof(float) * (kRouteWarps * warp_floats<EPL>(a.n_experts) + row_floats(a.n_experts));
-                // A warp's lanes are all at work with 32 / L tokens. Spreading the tokens over more warps than that gains nothing once
-                // there are three for each of 16 warps an SM (6000 of 256 experts 22.8 us spread, 18.2 with full warps; 9000 23.5
-                // and 18.4; 12000 of 64 8.9 and 7.8).
-                const uint64_t most = 32 / kTokenLanes<EPL>, each = (n_tokens + 148 * 16 - 1) / (148 * 16);
-                const uint32_t tokens_each = (uint32_t)(each < 3 ? each : most);
+                constexpr uint32_t tokens_each = 32 / kTokenLanes<EPL>;  // of a warp
                 const uint64_t blocks = (n_tokens + (uint64_t)tokens_each * kRouteWarps - 1) / ((uint64_t)tokens_each * kRouteWarps);
                 e = launch_after(route_kernel<DT, EPL, KL>, dim3((uint32_t)blocks), kRouteWarps * 32, smem, (cudaStream_t)stream, a,
-                                 (const value_t<DT>*)logits_dev, n_tokens, tokens_each, logits_stride, whole, bias_dev, experts_dev,
+                                 (const value_t<DT>*)logits_dev, n_tokens, logits_stride, whole, bias_dev, experts_dev,
                                  weights_dev);
             });
         });

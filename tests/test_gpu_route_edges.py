@@ -134,3 +134,20 @@ def test_gradients_through_scores_that_vanish_in_32_bits(score, E):
     # (quotients, at most k terms), beside a factor 1 - s
     tol = (k + 24) * 2.0**-24 * 4.0 * 2 * dw.abs().max().item() + 1e-37
     assert (np.abs(out.double().cpu().numpy() - want) <= tol).all()
+
+
+def test_every_number_of_tokens_around_the_change_of_kernels():
+    """From one warp a token to several tokens a warp: the last of them alone in its warp, and in its block."""
+    E, k = 64, 4
+    from paper_2609_04609_b200 import ciera
+
+    x = _logits(4800, E, "bf16", 2)
+    ids, w = ref.route(x, None, k, "softmax")
+    dev = x.to(DEV)
+    for T in (4735, 4736, 4737, 4743, 4744, 4745, 4767, 4768, 4769):
+        experts = torch.full((T + 1, k), -7, dtype=torch.int32, device=DEV)
+        weights = torch.full((T + 1, k), -7.0, device=DEV)
+        ciera.route(_config(E, k, "softmax"), dev[:T], None, experts[:T], weights[:T])
+        assert np.array_equal(experts[:T].cpu().numpy(), ids[:T])
+        assert np.allclose(weights[:T].cpu().numpy(), w[:T], rtol=(E + 16) * 2.0**-24, atol=0)
+        assert (experts[T] == -7).all() and (weights[T] == -7).all()
