@@ -52,11 +52,13 @@ __device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d
     return to_e4m3x4(a, b, c, d, make_float4(inv, inv, inv, inv));
 }
 
-// sigmoid(g) = 1 / (1 + e) and 1 - sigmoid(g) = e / (1 + e) with e = 2^(-g log2 e): the exponent in two parts, so that the power
-// is off by a step or two however large g is, and both results by less than 2^-21 of themselves.  (expf and a division: silu(g) *
-// u of 32768 x 1024 in 93 us.)
+// sigmoid(g) = 1 / (1 + e) and 1 - sigmoid(g) = e / (1 + e) with e = 2^(-g log2 e): the exponent in two parts (log2 e as the nearest
+// 32-bit number and what is left of it), so that the power is off by a step or two however large the exponent is, and both
+// results by less than 2^-21 of themselves; for g above 87 e and 1 - sigmoid(g) are 0.  Gates below kLowestGate, where e leaves 32
+// bits, are not for this.  (expf and a division: silu(g) * u of 32768 x 1024 in 93 us.)
+constexpr float kLowestGate = -87.f;
 __device__ __forceinline__ float2 sigmoid32(float g) {
-    const float x = fminf(fmaxf(g, -87.f), 87.f), t = x * -1.44269504f;
+    const float x = fminf(fmaxf(g, kLowestGate), 127.f), t = x * -1.44269504f;
     const float rest = fmaf(x, -1.44269504f, -t) + x * -1.92596299e-8f;  // -x log2 e = t + rest
     float e;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
@@ -94,9 +96,39 @@ __device__ __forceinline__ void read_four(const value_t<DT>* __restrict__ x, con
         if (c < f) raw.up = get(x + f + at);
     }
 }
-// x's, silu(g) * u, or one of their gradients
+__device__ __forceinline__ uint32_t max_two(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// The largest bits of gates: of the lowest one if any is negative (or of a NaN); 16-bit types two at a time.
+template <int DT>
+__device__ __forceinline__ void see_gates(const Pack<value_t<DT>, 4>& g, uint32_t& lowest) {
+    if constexpr (DT == CIERA_FP32) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) lowest = max(lowest, __float_as_uint(g.v[j]));
+    } else {
+        const uint2 w = *reinterpret_cast<const uint2*>(&g);
+        lowest = max_two(lowest, max_two(w.x, w.y));
+    }
+}
+template <int DT>
+__device__ __forceinline__ void see_gate(float g, uint32_t& lowest) {
+    const value_t<DT> v = ValueOf<DT>::put(g);
+    if constexpr (DT == CIERA_FP32) lowest = max(lowest, __float_as_uint(g));
+    else lowest = max_two(lowest, *reinterpret_cast<const unsigned short*>(&v));
+}
+// whether one is below kLowestGate (true for some NaN too)
+template <int DT>
+__device__ __forceinline__ bool below_lowest(uint32_t lowest) {
+    if constexpr (DT == CIERA_FP32) return lowest > __float_as_uint(kLowestGate);
+    constexpr uint32_t bits = DT == CIERA_BF16 ? 0xc2aeu : 0xd570u;  // -87
+    return (lowest >> 16) > bits || (lowest & 0xffffu) > bits;
+}
+// x's, silu(g) * u, or one of their gradients; lowest: see_gates of the gates so far
 template <int DT, int SRC>
-__device__ __forceinline__ void make_four(const RawFour<DT>& raw, uint32_t c, uint32_t cols, float (&v)[4]) {
+__device__ __forceinline__ void make_four(const RawFour<DT>& raw, uint32_t c, uint32_t cols, float (&v)[4], uint32_t& lowest) {
+    if constexpr (SRC != CIERA_SOURCE_ROWS) see_gates<DT>(raw.x, lowest);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const float x = ValueOf<DT>::get(raw.x.v[j]);
@@ -108,7 +140,7 @@ __device__ __forceinline__ void make_four(const RawFour<DT>& raw, uint32_t c, ui
 // The same value by value, for rows and widths of any kind; 0 behind the row.
 template <int DT, int SRC>
 __device__ __forceinline__ void source_values(const value_t<DT>* __restrict__ x, const value_t<DT>* __restrict__ grad, uint32_t c,
-                                              uint32_t cols, float (&v)[4]) {
+                                              uint32_t cols, float (&v)[4], uint32_t& lowest) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         v[j] = 0.f;
@@ -116,27 +148,35 @@ __device__ __forceinline__ void source_values(const value_t<DT>* __restrict__ x,
         if constexpr (SRC == CIERA_SOURCE_ROWS) {
             v[j] = ValueOf<DT>::get(x[c + j]);
         } else if constexpr (SRC == CIERA_SOURCE_SWIGLU) {
-            v[j] = swiglu32(ValueOf<DT>::get(x[c + j]), ValueOf<DT>::get(x[cols + c + j]));
+            const float g = ValueOf<DT>::get(x[c + j]);
+            see_gate<DT>(g, lowest);
+            v[j] = swiglu32(g, ValueOf<DT>::get(x[cols + c + j]));
         } else {
             const uint32_t f = cols / 2, at = c + j < f ? c + j : c + j - f;
             const float g = ValueOf<DT>::get(x[at]), u = ValueOf<DT>::get(x[f + at]), d = ValueOf<DT>::get(grad[at]);
+            see_gate<DT>(g, lowest);
             v[j] = c + j < f ? swiglu_gate32(g, u, d) : swiglu_up32(g, d);
         }
     }
 }
 
-// the same in 64 bits, its magnitude
+// The same in 64 bits, one value; lowest: its gate.
 template <int DT, int SRC>
-__device__ double source_magnitude(const value_t<DT>* __restrict__ x, const value_t<DT>* __restrict__ grad, uint32_t c, uint32_t cols) {
+__device__ double source_value64(const value_t<DT>* __restrict__ x, const value_t<DT>* __restrict__ grad, uint32_t c, uint32_t cols, float& lowest) {
     const uint32_t f = SRC == CIERA_SOURCE_SWIGLU ? cols : cols / 2, j = c < f ? c : c - f;
-    const double g = ValueOf<DT>::get(x[j]), u = ValueOf<DT>::get(x[f + j]);
+    const double g = lowest = ValueOf<DT>::get(x[j]), u = ValueOf<DT>::get(x[f + j]);
     const double s = 1.0 / (1.0 + exp(-g));
     if constexpr (SRC == CIERA_SOURCE_SWIGLU) {
-        return fabs(g * s * u);
+        return g * s * u;
     } else {
         const double d = ValueOf<DT>::get(grad[j]);
-        return fabs(c < f ? d * u * s * (1.0 + g * (1.0 - s)) : d * g * s);
+        return c < f ? d * u * s * (1.0 + g * (1.0 - s)) : d * g * s;
     }
+}
+template <int DT, int SRC>
+__device__ __forceinline__ double source_magnitude(const value_t<DT>* __restrict__ x, const value_t<DT>* __restrict__ grad, uint32_t c, uint32_t cols) {
+    float gate;
+    return fabs(source_value64<DT, SRC>(x, grad, c, cols, gate));
 }
 
 // A largest magnitude that 32 bits do not settle: so close above or below 1.75 * 2^n that they do not say on which side it is
@@ -223,6 +263,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const Ro
     const uint32_t live = __ballot_sync(~0u, some);
     if (!some) from = 0;
     float v[kTileRows][4];
+    uint32_t lowest = 0;
     if constexpr (WIDE) {
         // Rows without a slot and columns behind the row read the first of either, and are put to zero afterwards: what is read
         // stands under no condition, so that several rows' values are on their way together (one by one: silu(g) * u of
@@ -240,7 +281,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const Ro
             }
 #pragma unroll
             for (int i = 0; i < kAtOnce; ++i) {
-                make_four<DT, SRC>(raw[i], c, a.cols, v[i0 + i]);
+                make_four<DT, SRC>(raw[i], c, a.cols, v[i0 + i], lowest);
                 if (!(live >> (i0 + i) & 1 && whole)) v[i0 + i][0] = v[i0 + i][1] = v[i0 + i][2] = v[i0 + i][3] = 0.f;
             }
         }
@@ -251,7 +292,24 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const Ro
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[i][j] = 0.f;
             if (live >> i & 1 && c0 < a.cols)
-                source_values<DT, SRC>(x + r * a.x_stride, SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + r * a.grad_stride : nullptr, c0, a.cols, v[i]);
+                source_values<DT, SRC>(x + r * a.x_stride, SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + r * a.grad_stride : nullptr, c0, a.cols, v[i], lowest);
+        }
+    }
+    if constexpr (SRC != CIERA_SOURCE_ROWS) {
+        if (__any_sync(~0u, below_lowest<DT>(lowest))) {  // such values in 64 bits
+#pragma unroll 1
+            for (uint32_t n = 0; n < kTileRows * 4; ++n) {
+                const uint64_t r = first + n / 4;
+                const uint32_t c = c0 + n % 4;
+                float gate = 0.f, value = 0.f;
+                if (live >> (n / 4) & 1 && c < a.cols)
+                    value = (float)source_value64<DT, SRC>(x + r * a.x_stride, SRC == CIERA_SOURCE_SWIGLU_BACKWARD ? grad + r * a.grad_stride : nullptr, c, a.cols, gate);
+#pragma unroll
+                for (int i = 0; i < kTileRows; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (n == (uint32_t)(i * 4 + j) && gate < kLowestGate) v[i][j] = value;
+            }
         }
     }
     if (SRC == CIERA_SOURCE_ROWS && a.row_weights) {
@@ -346,12 +404,6 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_rows_kernel(const Ro
 // access of 16 bytes, one of 8, and half the steps for each row that 4 columns a lane take (dispatch of 4096 x 8 rows of 2048
 // as fp32 in the kernel above 81 us and 26 instructions a value, 4 columns of 16 bits a lane 74 us and 24).
 constexpr uint32_t kMagnitudes = 0x7fff7fffu;
-
-__device__ __forceinline__ uint32_t max_two(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
 
 // the bits of the fp32 value that these magnitude bits stand for
 template <int DT>
@@ -524,14 +576,14 @@ __global__ void __launch_bounds__(kTileThreads, 2) quantize_blocks_kernel(const 
     const uint32_t c0 = col0 + lane * 4, first = row0 + warp * kTileRows;
     const value_t<DT>* xm = x + matrix * a.x_matrix_stride;
     float v[kTileRows][4];
-    uint32_t amax = 0;
+    uint32_t amax = 0, none = 0;
 #pragma unroll
     for (int i = 0; i < kTileRows; ++i) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[i][j] = 0.f;
         if (first + i < a.rows && c0 < a.cols) {
             if constexpr (WIDE) load_values<DT, 4>(xm + (first + i) * a.x_stride + c0, v[i]);
-            else source_values<DT, CIERA_SOURCE_ROWS>(xm + (first + i) * a.x_stride, nullptr, c0, a.cols, v[i]);
+            else source_values<DT, CIERA_SOURCE_ROWS>(xm + (first + i) * a.x_stride, nullptr, c0, a.cols, v[i], none);
         }
     }
 #pragma unroll

@@ -1,0 +1,82 @@
+"""silu(g) * u and its gradient where 32 bits and 64 part: gates far from zero, and the gate at which the gradient vanishes."""
+import numpy as np
+import pytest
+import torch
+
+from tests import moe_reference as ref
+from tests.test_gpu_fp8 import DEV, DTYPES, _bytes, _up
+
+pytestmark = pytest.mark.gpu
+
+
+def _rows(x, cols, kind, grad=None, layout=None):
+    """Values and scale bytes of both orientations; layout: (slot_of_row, starts)"""
+    from paper_2609_04609_b200 import ciera
+
+    rows = x.shape[0]
+    _, q = _bytes(rows, cols)
+    _, qt = _bytes(cols, rows)
+    s = torch.zeros(_up(cols, 128) // 128, rows, dtype=torch.uint8, device=DEV)
+    st = torch.zeros(_up(rows, 128) // 128, cols, dtype=torch.uint8, device=DEV)
+    kw = {}
+    if layout:
+        kw = dict(slot_of_row=layout[0].to(DEV), top_k=1, starts=layout[1].to(DEV))
+    ciera.fp8_quantize_rows(x.to(DEV), q, s, qt, st, kind=kind, grad=None if grad is None else grad.to(DEV), **kw)
+    torch.cuda.synchronize()
+    return q, s, qt, st
+
+
+def _agree(got, y, cancel=0.0):
+    """Scale bytes of y (64 bits) in both orientations, values within half a step of e4m3 and 16 steps of 32 bits of the result and
+    of the terms that cancel in it."""
+    q, s, qt, st = got
+    for q_, s_, rows in ((q, s, y), (qt, st, y.T.copy())):
+        _, want = ref.quantize_rows(rows)
+        assert np.array_equal(s_.cpu().numpy(), want)
+        have = ref.operand_values(q_, s_).cpu().numpy()
+        f = 2.0 ** (want.T.repeat(128, 1)[:, : rows.shape[1]] - 127.0)
+        size = np.abs(rows) + (cancel if rows is y else np.transpose(cancel))
+        off = 16 * 2.0**-24 * size
+        assert (np.abs(have - rows) <= 2.0**-4 * (np.abs(rows) + off) + 2.0**-10 * f + off).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("f", [128, 130, 34])
+def test_gates_far_below_zero(dtype, f):
+    """silu(g) falls to e^g far beyond the smallest 32-bit number; a large u brings the product back."""
+    from paper_2609_04609_b200 import ciera
+
+    rng = np.random.default_rng(f)
+    rows, dt = 130, DTYPES[dtype]
+    g = rng.uniform(-190.0, -60.0, (rows, f))
+    top = 4.0 if dtype == "fp16" else 37.0
+    u = 10.0 ** rng.uniform(-3.0, top, (rows, f)) * rng.choice([-1.0, 1.0], (rows, f))
+    g[:40] = -60.0 - 130.0 * rng.random((40, 1))  # whole rows of one gate
+    g[40, :] = -87.0
+    g[41, :] = -87.5
+    g[42, 1:] = -300.0
+    u[43, :] = 0.0
+    x = torch.from_numpy(np.concatenate([g, u], 1)).to(dt)
+    assert torch.isfinite(x).all()
+    _agree(_rows(x, f, ciera.SOURCE_SWIGLU), ref.swiglu(x.double().numpy()))
+    # gradients: the same gates, d of an ordinary size
+    d = torch.from_numpy(rng.standard_normal((rows, f))).to(dt)
+    if f % 2 == 0:
+        y = ref.swiglu_backward(x.double().numpy(), d.double().numpy())
+        _agree(_rows(x, 2 * f, ciera.SOURCE_SWIGLU_BACKWARD, d), y)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_gates_far_above_zero(dtype):
+    """silu(g) = g and its derivative 1, however large g is."""
+    from paper_2609_04609_b200 import ciera
+
+    rng = np.random.default_rng(4)
+    rows, f = 128, 128
+    g = 10.0 ** rng.uniform(1.0, 38.0, (rows, f))
+    u = 10.0 ** rng.uniform(-38.0, 0.0, (rows, f))
+    x = torch.from_numpy(np.concatenate([g, u], 1)).to(DTYPES[dtype])
+    _agree(_rows(x, f, ciera.SOURCE_SWIGLU), ref.swiglu(x.double().numpy()))
+    d = torch.from_numpy(10.0 ** rng.uniform(-3.0, 0.0, (rows, f))).to(DTYPES[dtype])
+    y = ref.swiglu_backward(x.double().numpy(), d.double().numpy())
+    _agree(_rows(x, 2 * f, ciera.SOURCE_SWIGLU_BACKWARD, d), y)
