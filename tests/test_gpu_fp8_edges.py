@@ -80,3 +80,56 @@ def test_gates_far_above_zero(dtype):
     d = torch.from_numpy(10.0 ** rng.uniform(-3.0, 0.0, (rows, f))).to(DTYPES[dtype])
     y = ref.swiglu_backward(x.double().numpy(), d.double().numpy())
     _agree(_rows(x, 2 * f, ciera.SOURCE_SWIGLU_BACKWARD, d), y)
+
+
+ROOT = -1.2784645427610738  # 1 + g (1 - sigmoid(g)) = 0
+
+
+@pytest.mark.parametrize("width", [1e-4, 1e-3, 1e-2, 0.06, 0.2])
+@pytest.mark.parametrize("live", ["row", "column"])
+def test_gate_gradients_beside_their_root_next_to_a_border(width, live):
+    """The gradient of the gate vanishes at one g: its terms cancel, and its scale is still that of 64 bits.  One value of a block is
+    live, within rounding of 1.75 * 2^n, as an expert's with one token is in a transposed operand."""
+    from paper_2609_04609_b200 import ciera
+
+    rng = np.random.default_rng(int(width * 1e5))
+    rows, f = 256, 128
+    g = (ROOT + rng.uniform(-width, width, (rows, f))).astype(np.float32)
+    g64 = g.astype(np.float64)
+    s = 1 / (1 + np.exp(-g64))
+    factor = s * (1 + g64 * (1 - s))
+    u = (3.5 / np.abs(factor)).astype(np.float32)
+    steps = rng.integers(-2, 3, (rows, f))
+    for k in (1, 2):
+        u = np.where(steps >= k, np.nextafter(u, np.float32(np.inf)), np.where(steps <= -k, np.nextafter(u, np.float32(0)), u))
+    at = np.zeros((rows, f), bool)
+    at[np.arange(rows), np.arange(rows) % f] = True  # one value in each row, and in each column of 128 rows
+    u = np.where(at, u, np.float32(0.0)) if live == "column" else np.where(at, u, u * np.float32(0.3))
+    x = torch.from_numpy(np.concatenate([g, u], 1))
+    d = torch.ones(rows, f)
+    y = ref.swiglu_backward(x.double().numpy(), d.double().numpy())
+    _, want = ref.quantize_rows(y)
+    assert len(np.unique(want[0])) == 2  # both sides of the border occur
+    cancel = np.concatenate([np.abs(u * s), np.zeros((rows, f))], 1)
+    _agree(_rows(x, 2 * f, ciera.SOURCE_SWIGLU_BACKWARD, d), y, cancel)
+
+
+def test_gate_gradients_beside_their_root_in_an_experts_segment():
+    """bf16 gates at the number next to the root, one token in each expert's segment."""
+    from paper_2609_04609_b200 import ciera
+
+    rows, f = 512, 256
+    rng = np.random.default_rng(7)
+    g = torch.full((rows, f), -1.28125, dtype=torch.bfloat16)
+    g[::128, 1::2] = -1.2734375
+    u = torch.from_numpy(10.0 ** rng.uniform(2.0, 5.0, (rows, f))).bfloat16()
+    d = torch.from_numpy(rng.uniform(0.5, 2.0, (rows, f))).bfloat16()
+    x = torch.cat([g, u], 1)
+    slot = torch.full((rows,), -1, dtype=torch.int32)
+    slot[::128] = torch.arange(4, dtype=torch.int32)
+    starts = torch.arange(0, rows + 1, 128, dtype=torch.int32)
+    y = ref.swiglu_backward(x.double().numpy(), d.double().numpy())
+    y[slot < 0] = 0.0
+    s = 1 / (1 + np.exp(1.28125))
+    cancel = np.concatenate([np.abs((u * d).double().numpy() * s), np.zeros((rows, f))], 1)
+    _agree(_rows(x, 2 * f, ciera.SOURCE_SWIGLU_BACKWARD, d, (slot, starts)), y, cancel)
