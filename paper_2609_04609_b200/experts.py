@@ -6,6 +6,7 @@ from one product to the next is kept in the weights' type, gradients of weights 
 """
 from __future__ import annotations
 
+from contextlib import nullcontext
 from typing import Optional
 
 import torch
@@ -30,7 +31,9 @@ class ExpertLayer:
     ``codec`` holds the experts' matrices in the order gate, up (``d_model`` x ``d_ff``), down (``d_ff`` x ``d_model``), expert by
     expert (``workloads.olmoe_layer_shapes``), each in one piece.  ``refresh`` rounds what the codec has reconstructed
     (``step`` does a gather and that); ``forward`` and ``backward`` then work on up to ``max_tokens`` tokens.  The buffers
-    belong to the layer, so one forward pass at a time can be waiting for its backward pass.
+    belong to the layer, so one forward pass at a time can be waiting for its backward pass, and passes on different streams are put
+    in order by the caller.  With ``stream`` a pass runs there whole: its results are allocated there too, and its inputs are kept
+    from reuse until it is done with them.
     """
 
     def __init__(self, codec, n_experts: int, d_model: int, d_ff: int, top_k: int, max_tokens: int,
@@ -89,6 +92,8 @@ class ExpertLayer:
             self.dx_rows = torch.zeros(cap, d, dtype=self.dtype, device=dev)
             self.dweights = torch.zeros(max_tokens, top_k, device=dev)
         self._batch = None
+        if not torch.cuda.is_current_stream_capturing():  # the buffers are zeros before any stream writes them
+            torch.cuda.current_stream(dev).synchronize()
 
     # -- weights ----------------------------------------------------------------------------------
     def refresh(self, stream=None) -> None:
@@ -108,32 +113,44 @@ class ExpertLayer:
     def _rows(self, t: int) -> int:
         return ciera.expert_rows_capacity(t * self.top_k, self.n_experts)
 
+    def _on(self, stream, *inputs):
+        """The stream that a pass runs on and allocates from."""
+        if stream is None:
+            return nullcontext()
+        for t in inputs:
+            if t is not None:
+                t.record_stream(stream)
+        return torch.cuda.stream(stream)
+
     def forward(self, x: torch.Tensor, logits: torch.Tensor, bias: Optional[torch.Tensor] = None,
                 out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """``x`` [T, d_model] in the weights' type, ``logits`` [T, n_experts]: the layer's output [T, d_model]."""
         t = x.shape[0]
         if t > self.max_tokens or tuple(x.shape) != (t, self.d_model) or x.dtype != self.dtype or logits.shape[0] != t:
             raise ValueError("x is [tokens, d_model] in the weights' type, with at most max_tokens tokens")
-        out = torch.empty_like(x) if out is None else out
-        self._batch = (x, logits)
-        if t == 0:
-            return out
-        cap, k, s = self._rows(t), self.top_k, stream
+        with self._on(stream, x, logits, bias, out):
+            out = torch.empty_like(x) if out is None else out
+            self._batch = (x, logits)
+            if t:
+                self._forward(x, logits, bias, out)
+        return out
+
+    def _forward(self, x, logits, bias, out) -> None:
+        t = x.shape[0]
+        cap, k = self._rows(t), self.top_k
         experts, weights, rows = self.experts[:t], self.weights[:t], self.row_of_slot[:t]
         slots = self.slot_of_row[:cap]
-        ciera.route(self.config, logits, bias, experts, weights, s)
-        ciera.expert_layout(experts, self.n_experts, self.starts, self.counts, rows, slots, self.workspace, s)
+        ciera.route(self.config, logits, bias, experts, weights)
+        ciera.expert_layout(experts, self.n_experts, self.starts, self.counts, rows, slots, self.workspace)
         turned = self.training
         ciera.fp8_quantize_rows(x, self.x_q[:cap], self.x_s, self.x_t[:, :cap] if turned else None,
-                                self.x_ts[: cap // BLOCK] if turned else None, slot_of_row=slots, top_k=k, starts=self.starts,
-                                stream=s)
-        ciera.fp8_matmul(self.x_q[:cap], self.x_s, self.w1, self.w1_s, self.h[:cap], self.starts, status=self.status, stream=s)
+                                self.x_ts[: cap // BLOCK] if turned else None, slot_of_row=slots, top_k=k, starts=self.starts)
+        ciera.fp8_matmul(self.x_q[:cap], self.x_s, self.w1, self.w1_s, self.h[:cap], self.starts, status=self.status)
         ciera.fp8_quantize_rows(self.h[:cap], self.a_q[:cap], self.a_s, self.a_t[:, :cap] if turned else None,
                                 self.a_ts[: cap // BLOCK] if turned else None, kind=ciera.SOURCE_SWIGLU, slot_of_row=slots, top_k=k,
-                                starts=self.starts, stream=s)
-        ciera.fp8_matmul(self.a_q[:cap], self.a_s, self.w2, self.w2_s, self.o[:cap], self.starts, status=self.status, stream=s)
-        ciera.expert_combine(self.o[:cap], rows, weights, out, s)
-        return out
+                                starts=self.starts)
+        ciera.fp8_matmul(self.a_q[:cap], self.a_s, self.w2, self.w2_s, self.o[:cap], self.starts, status=self.status)
+        ciera.expert_combine(self.o[:cap], rows, weights, out)
 
     def backward(self, dout: torch.Tensor, stream=None):
         """Gradients of the last ``forward``: ``(dx, dlogits, dgate, dup, ddown)``, the last three in fp32 and the shapes of
@@ -143,7 +160,11 @@ class ExpertLayer:
         x, logits = self._batch
         if dout.shape != x.shape or dout.dtype != self.dtype:
             raise ValueError("dout has the shape and type of x")
-        t, f, s, k = x.shape[0], self.d_ff, stream, self.top_k
+        with self._on(stream, x, logits, dout):
+            return self._backward(x, logits, dout)
+
+    def _backward(self, x, logits, dout):
+        t, f, k = x.shape[0], self.d_ff, self.top_k
         new = lambda *shape: torch.empty(*shape, device=self.device)  # noqa: E731
         dx, dlogits = torch.empty_like(x), torch.empty_like(logits)
         dgate, dup = new(self.n_experts, self.d_model, f), new(self.n_experts, self.d_model, f)
@@ -153,25 +174,27 @@ class ExpertLayer:
         cap, rows, slots = self._rows(t), self.row_of_slot[:t], self.slot_of_row[: self._rows(t)]
         rb = cap // BLOCK
         dweights = self.dweights[:t]
-        ciera.expert_combine_backward(dout, self.o[:cap], rows, self.weights[:t], dweights, stream=s)
-        ciera.route_backward(self.config, logits, self.experts[:t], dweights, dlogits, s)
+        ciera.expert_combine_backward(dout, self.o[:cap], rows, self.weights[:t], dweights)
+        ciera.route_backward(self.config, logits, self.experts[:t], dweights, dlogits)
         ciera.fp8_quantize_rows(dout, self.do_q[:cap], self.do_s, self.do_t[:, :cap], self.do_ts[:rb], slot_of_row=slots, top_k=k,
-                                row_weights=self.weights[:t], starts=self.starts, stream=s)
-        ciera.fp8_matmul(self.do_q[:cap], self.do_s, self.w2_t, self.w2_ts, self.da[:cap], self.starts, status=self.status, stream=s)
+                                row_weights=self.weights[:t], starts=self.starts)
+        ciera.fp8_matmul(self.do_q[:cap], self.do_s, self.w2_t, self.w2_ts, self.da[:cap], self.starts, status=self.status)
         ciera.fp8_quantize_rows(self.h[:cap], self.dh_q[:cap], self.dh_s, self.dh_t[:, :cap], self.dh_ts[:rb],
                                 kind=ciera.SOURCE_SWIGLU_BACKWARD, grad=self.da[:cap], slot_of_row=slots, top_k=k,
-                                starts=self.starts, stream=s)
-        ciera.fp8_matmul(self.dh_q[:cap], self.dh_s, self.w1_t, self.w1_ts, self.dx_rows[:cap], self.starts, status=self.status,
-                         stream=s)
-        ciera.expert_combine(self.dx_rows[:cap], rows, None, dx, s)
+                                starts=self.starts)
+        ciera.fp8_matmul(self.dh_q[:cap], self.dh_s, self.w1_t, self.w1_ts, self.dx_rows[:cap], self.starts, status=self.status)
+        ciera.expert_combine(self.dx_rows[:cap], rows, None, dx)
         for a, a_s, b, b_s, out in ((self.x_t, self.x_ts, self.dh_t[:f], self.dh_ts[:, :f], dgate),
                                     (self.x_t, self.x_ts, self.dh_t[f:], self.dh_ts[:, f:], dup),
                                     (self.a_t, self.a_ts, self.do_t, self.do_ts, ddown)):
-            ciera.fp8_matmul(a[:, :cap], a_s[:rb], b[:, :cap], b_s[:rb], out, self.starts, contract=True, status=self.status, stream=s)
+            ciera.fp8_matmul(a[:, :cap], a_s[:rb], b[:, :cap], b_s[:rb], out, self.starts, contract=True, status=self.status)
         return dx, dlogits, dgate, dup, ddown
 
     def check_status(self) -> None:
+        """Waits for all streams' work and raises if a kernel of the layer reported an error since the last call."""
+        torch.cuda.synchronize(self.device)
         s = int(self.status.item())
         if s != 0:
             self.status.zero_()
+            torch.cuda.synchronize(self.device)
             raise ciera.CieraError("device status", s)
