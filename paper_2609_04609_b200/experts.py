@@ -128,11 +128,12 @@ class ExpertLayer:
         t = x.shape[0]
         if t > self.max_tokens or tuple(x.shape) != (t, self.d_model) or x.dtype != self.dtype or logits.shape[0] != t:
             raise ValueError("x is [tokens, d_model] in the weights' type, with at most max_tokens tokens")
+        self._batch = None  # (until this pass is on its way)
         with self._on(stream, x, logits, bias, out):
             out = torch.empty_like(x) if out is None else out
-            self._batch = (x, logits)
             if t:
                 self._forward(x, logits, bias, out)
+        self._batch = (x, logits)
         return out
 
     def _forward(self, x, logits, bias, out) -> None:

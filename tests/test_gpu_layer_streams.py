@@ -1,4 +1,4 @@
-"""The MoE layer on a stream of its own: where its results and inputs live."""
+"""The MoE layer on a stream of its own: where its results and inputs live, and what a refused call leaves."""
 import pytest
 import torch
 
@@ -90,3 +90,18 @@ def test_status_of_a_side_stream_is_waited_for_and_reported_once():
         layer.check_status()
     assert e.value.status == ciera.ERR_CORRUPT
     layer.check_status()
+
+
+def test_a_refused_forward_leaves_nothing_to_go_back_through():
+    from paper_2609_04609_b200 import ciera
+
+    layer, w = _layer(4, 128, 128, 2, 8)
+    layer.step(w)
+    x, logits, dout = _inputs(layer, 8, 5)
+    y = layer.forward(x, logits)
+    with pytest.raises(ciera.CieraError):
+        layer.forward(x, logits, bias=torch.zeros(3, device=DEV))
+    with pytest.raises(RuntimeError):
+        layer.backward(dout)
+    assert torch.equal(layer.forward(x, logits), y)
+    layer.backward(dout)
