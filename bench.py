@@ -45,15 +45,27 @@ TRAFFIC_FILE = os.path.join(ROOT, "profiles", "ncu_dram_traffic.json")
 CSRC_DIR = os.path.join(ROOT, "paper_2609_04609_b200", "csrc")
 
 
-def csrc_digest() -> str:
-    """sha256 over the kernel sources (names and contents, sorted by name)."""
-    import hashlib
+# the sources that the captured kernels are made of: these and whatever of the folder they include
+CODEC_SOURCES = ("ciera_host.cu", "ciera_encode.cu", "ciera_encode_hashed.cu", "ciera_decode.cu", "ciera_entropy.cu", "ciera_kernels.cu")
 
+
+def csrc_digest() -> str:
+    """sha256 over the codec's kernel sources (names and contents, sorted by name)."""
+    import hashlib
+    import re
+
+    files, left = {}, list(CODEC_SOURCES)
+    while left:
+        name = left.pop()
+        path = os.path.join(CSRC_DIR, name)
+        if name not in files and os.path.exists(path):  # (a header of another folder is none of these)
+            with open(path, "rb") as f:
+                files[name] = f.read()
+            left += re.findall(r'^\s*#\s*include\s+"([^"]+)"', files[name].decode(), re.M)
     h = hashlib.sha256()
-    for name in sorted(os.listdir(CSRC_DIR)):
+    for name in sorted(files):
         h.update(name.encode())
-        with open(os.path.join(CSRC_DIR, name), "rb") as f:
-            h.update(f.read())
+        h.update(files[name])
     return h.hexdigest()
 
 
