@@ -11,11 +11,16 @@ namespace ciera {
 // block each warp owns a stretch of neighbouring slots and a row of counters, so ranks come out in slot order whatever the
 // order in which the counters are added to.  What a block waits for is the table of counts, so chunks are large: 262168 slots
 // over 256 experts in chunks of 2048 took 27 us.
+// That every block reads the counts of all chunks grows with the square of the slots, so from kLayoutScanFrom chunks on a launch
+// in between (layout_scan) adds them up once: 1.2 million slots of 64 experts 19 us with it and 22 without, of 8 experts 20 and 16;
+// 16 million of 256 experts 179 us and 1802.
 
 constexpr int kLayoutWarps = 16;
 constexpr int kLayoutRounds = 8;  // slots per lane
 constexpr int kLayoutChunk = kLayoutWarps * kLayoutRounds * 32;
 constexpr uint32_t kMaxExperts = 1024;
+constexpr uint64_t kLayoutScanFrom = 256;
+constexpr int kScanStretches = 32;
 
 __device__ __forceinline__ void load_ids(const int32_t* __restrict__ experts, uint64_t n_slots, uint64_t base, int lane,
                                          uint32_t n_experts, uint32_t (&ids)[kLayoutRounds]) {
@@ -42,7 +47,40 @@ __global__ void __launch_bounds__(kLayoutWarps * 32) layout_count(const int32_t*
     for (uint32_t e = threadIdx.x; e < n_experts; e += blockDim.x) hist[(uint64_t)blockIdx.x * n_experts + e] = layout_smem[e];
 }
 
-// hist: counts of every chunk, or NULL for a single chunk
+// In place of every chunk's counts those of the chunks before it, and behind the last chunk those of all.  A block has 32 experts, a
+// warp a stretch of the chunks.
+__global__ void __launch_bounds__(kScanStretches * 32) layout_scan(uint32_t* __restrict__ hist, uint32_t chunks, uint32_t n_experts) {
+    __shared__ uint32_t sums[kScanStretches][32];
+    pdl_wait();
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
+    const uint32_t each = (chunks + kScanStretches - 1) / kScanStretches, begin = min(chunks, warp * each), end = min(chunks, begin + each);
+    uint32_t sum = 0;
+    if (e < n_experts) {
+#pragma unroll 8
+        for (uint32_t c = begin; c < end; ++c) sum += hist[(uint64_t)c * n_experts + e];
+    }
+    sums[warp][lane] = sum;
+    __syncthreads();
+    uint32_t run = 0;
+    for (uint32_t w = 0; w < warp; ++w) run += sums[w][lane];
+    if (e >= n_experts) return;
+    for (uint32_t c = begin; c < end;) {
+        uint32_t v[8];
+        const uint32_t n = min(8u, end - c);
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) v[i] = i < n ? hist[(uint64_t)(c + i) * n_experts + e] : 0u;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            if (i < n) hist[(uint64_t)(c + i) * n_experts + e] = run;
+            run += v[i];
+        }
+        c += n;
+    }
+    if (warp == kScanStretches - 1) hist[(uint64_t)chunks * n_experts + e] = run;
+}
+
+// hist: counts of every chunk, or NULL for a single chunk; SCANNED: as layout_scan leaves them
+template <bool SCANNED>
 __global__ void __launch_bounds__(kLayoutWarps * 32)
     layout_place(const int32_t* __restrict__ experts, uint64_t n_slots, uint32_t n_experts, const uint32_t* __restrict__ hist,
                  int32_t* __restrict__ starts, int32_t* __restrict__ counts, int32_t* __restrict__ row_of_slot,
@@ -62,7 +100,12 @@ __global__ void __launch_bounds__(kLayoutWarps * 32)
 #pragma unroll
     for (int r = 0; r < kLayoutRounds; ++r)
         if (ids[r] < n_experts) atomicAdd(&next[ids[r]], 1u);
-    if (hist) {  // a thread for an expert and every so many chunks
+    if constexpr (SCANNED) {
+        for (uint32_t e = threadIdx.x; e < n_experts; e += blockDim.x) {
+            before[e] = hist[(uint64_t)blockIdx.x * n_experts + e];
+            total[e] = hist[(uint64_t)gridDim.x * n_experts + e];
+        }
+    } else if (hist) {  // a thread for an expert and every so many chunks
         const uint32_t side = blockDim.x / n_experts > 1 ? blockDim.x / n_experts : 1;
         for (uint32_t i = threadIdx.x; i < side * n_experts; i += blockDim.x) {
             const uint32_t e = i % n_experts;
@@ -235,7 +278,7 @@ static uint64_t layout_chunks(uint64_t n_slots) { return (n_slots + kLayoutChunk
 
 extern "C" size_t ciera_expert_layout_workspace_bytes(uint64_t n_slots, uint32_t n_experts) {
     const uint64_t chunks = layout_chunks(n_slots);
-    return chunks > 1 ? (size_t)(chunks * n_experts * sizeof(uint32_t)) : 16;
+    return chunks > 1 ? (size_t)((chunks + (chunks >= kLayoutScanFrom)) * n_experts * sizeof(uint32_t)) : 16;
 }
 
 extern "C" int ciera_expert_layout(const int32_t* experts_dev, uint64_t n_slots, uint32_t n_experts, int32_t* starts_dev,
@@ -250,11 +293,13 @@ extern "C" int ciera_expert_layout(const int32_t* experts_dev, uint64_t n_slots,
     const uint64_t chunks = layout_chunks(n_slots);
     const cudaStream_t s = (cudaStream_t)stream;
     const uint32_t* hist = nullptr;
+    const bool scanned = chunks >= kLayoutScanFrom;
+    const auto place = scanned ? layout_place<true> : layout_place<false>;
     const auto place_bytes = [](uint32_t experts) { return sizeof(uint32_t) * ((kLayoutWarps + 3) * experts + 1); };  // up to 78 KB
     const size_t smem = place_bytes(n_experts);
     cudaError_t e = cudaSuccess;
     if (smem > 48 * 1024) {  // (always the same limit: another host thread's call must not lower it before this launch)
-        e = cudaFuncSetAttribute(layout_place, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)place_bytes(kMaxExperts));
+        e = cudaFuncSetAttribute(place, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)place_bytes(kMaxExperts));
         if (e != cudaSuccess) return record_cuda_error(e);
     }
     if (chunks > 1) {
@@ -264,8 +309,13 @@ extern "C" int ciera_expert_layout(const int32_t* experts_dev, uint64_t n_slots,
         count_launch();
         hist = (const uint32_t*)workspace;
     }
-    e = launch_after(layout_place, dim3((uint32_t)(chunks ? chunks : 1)), kLayoutWarps * 32, smem, s, experts_dev, n_slots, n_experts,
-                     hist, starts_dev, counts_dev, row_of_slot_dev, slot_of_row_dev);
+    if (scanned) {
+        e = launch_after(layout_scan, dim3((n_experts + 31) / 32), kScanStretches * 32, 0, s, (uint32_t*)workspace, (uint32_t)chunks, n_experts);
+        if (e != cudaSuccess) return record_cuda_error(e);
+        count_launch();
+    }
+    e = launch_after(place, dim3((uint32_t)(chunks ? chunks : 1)), kLayoutWarps * 32, smem, s, experts_dev, n_slots, n_experts, hist,
+                     starts_dev, counts_dev, row_of_slot_dev, slot_of_row_dev);
     if (e != cudaSuccess) return record_cuda_error(e);
     count_launch();
     return CIERA_OK;
