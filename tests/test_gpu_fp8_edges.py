@@ -133,3 +133,43 @@ def test_gate_gradients_beside_their_root_in_an_experts_segment():
     s = 1 / (1 + np.exp(1.28125))
     cancel = np.concatenate([np.abs((u * d).double().numpy() * s), np.zeros((rows, f))], 1)
     _agree(_rows(x, 2 * f, ciera.SOURCE_SWIGLU_BACKWARD, d, (slot, starts)), y, cancel)
+
+
+@pytest.mark.parametrize("f", [128, 126, 192])
+@pytest.mark.parametrize("kind", ["value", "gradient"])
+def test_rows_and_columns_of_zeros_and_of_what_is_too_small(f, kind):
+    """A block of zeros has byte 127, one of numbers too small for 32 bits byte 1, in both orientations."""
+    from paper_2609_04609_b200 import ciera
+
+    rng = np.random.default_rng(f)
+    rows = 300
+    g = rng.standard_normal((rows, f)).astype(np.float32)
+    u = rng.standard_normal((rows, f)).astype(np.float32)
+    d = rng.standard_normal((rows, f)).astype(np.float32)
+    u[5], d[6], g[7] = 0.0, 0.0, 0.0
+    g[8, ::2] = u[8, 1::2] = d[8] = 0.0
+    tiny = np.float32(1e-25)
+    g[9:12], u[9:12], d[9:12] = tiny, tiny, tiny  # products of 1e-50
+    u[10, 1:] = d[10, 1:] = 0.0  # (one value of a row that is not a zero)
+    u[128:256], d[128:256] = 0.0, 0.0  # a tile of zeros ...
+    u[128:256, 3], g[128:256, 3], d[128:256, 3] = tiny, tiny, tiny  # ... but for one column ...
+    u[130, 4], g[130, 4], d[130, 4] = tiny, tiny, -tiny  # ... and one value
+    u[:, 7] = d[:, 7] = 0.0
+    u[:128, 9], g[:128, 9], d[:128, 9] = tiny, -tiny, tiny
+    u[256:], d[256:] = 0.0, 0.0
+    x = torch.from_numpy(np.concatenate([g, u], 1))
+    slot = torch.arange(rows, dtype=torch.int32)
+    slot[[20, 140, 299]] = -1
+    starts = torch.tensor([0, rows], dtype=torch.int32)
+    if kind == "value":
+        y = ref.swiglu(x.double().numpy())
+        got = lambda layout: _rows(x, f, ciera.SOURCE_SWIGLU, None, layout)  # noqa: E731
+    else:
+        dd = torch.from_numpy(d)
+        y = ref.swiglu_backward(x.double().numpy(), dd.double().numpy())
+        got = lambda layout: _rows(x, 2 * f, ciera.SOURCE_SWIGLU_BACKWARD, dd, layout)  # noqa: E731
+    assert {1, 127} <= set(np.unique(ref.quantize_rows(y)[1])) and {1, 127} <= set(np.unique(ref.quantize_rows(y.T.copy())[1]))
+    _agree(got(None), y)
+    y = y.copy()
+    y[slot.numpy() < 0] = 0.0
+    _agree(got((slot, starts)), y)
