@@ -430,12 +430,12 @@ typedef enum ciera_score { CIERA_SCORE_SOFTMAX = 0, CIERA_SCORE_SIGMOID = 1 } ci
 /* Routing.  For each token with logits l[0 .. n_experts):
  *   s = softmax(l) or, value by value, sigmoid(l);   c = s + bias (bias 0 if NULL)
  *   an expert whose logit is -inf or NaN, or whose c is -inf or NaN, is closed: its s is 0 where the logit closes it,
- *   and it is never chosen; +inf counts as the largest finite number
+ *   and it is never chosen; +inf counts as the largest finite number, -0 as 0
  *   groups of n_experts / n_groups neighbours; a group's value is the sum of its `group_best` (1 or 2) largest c; the
  *   top_groups groups of the largest values stay (a group without an open expert never does)
  *   the top_k largest c among them are chosen, in falling order; equal values go to the lower index
- *   w = scale * s of the chosen, divided by the sum of their s if `renormalise` (0 where that sum is 0)
- * Choices are those of 64-bit arithmetic.  Where fewer than top_k experts are open, the rest has index -1 and weight 0.
+ *   w = scale * s of the chosen, divided by the sum of their s if `renormalise` (0 where that sum is 0 in 64 bits)
+ * Choices are those of 64-bit arithmetic, and so are quotients by a sum below 1e-10; other weights are 32-bit arithmetic.  Where fewer than top_k experts are open, the rest has index -1 and weight 0.
  * Limits: n_experts 1 .. 1024, top_k 1 .. 32 and at most top_groups * (n_experts / n_groups), n_groups 1 .. 32 and a
  * divisor of n_experts, scale finite. */
 typedef struct ciera_route_config {
@@ -496,7 +496,8 @@ typedef enum ciera_fp8_source {
  *   row_weights    or NULL; x_rows * top_k fp32 (CIERA_SOURCE_ROWS with slot_of_row only)
  *   starts         or NULL: rows from starts[n_experts] on are left as they were, in q, qt and the scales alike
  * q and qt are 16-byte aligned with strides that are multiples of 16 and at least cols / rows.  Limits: rows and cols
- * 1 .. 2^31 - 256.  Arithmetic in 32 bits; the scale is that of 64-bit arithmetic where silu stands in between. */
+ * 1 .. 2^31 - 256.  Arithmetic in 32 bits (in 64 for gates below -87, where sigmoid leaves 32 bits); the scale is that of
+ * 64-bit arithmetic where silu stands in between. */
 typedef struct ciera_fp8_rows {
     int32_t source, dtype; /* dtype of x and grad */
     uint64_t rows, cols, x_rows;

@@ -5,7 +5,7 @@
 // the transposed copy goes through shared memory to be written 128 bytes at a time.  Tiles beside each other come one behind
 // the other, so that blocks that run together read and write whole rows.  Square blocks are bound by memory (64 matrices of
 // 2048 x 1024 in 97 us, 0.85 of the copy rate), rows in both orientations by instructions: each value is scaled and rounded
-// twice (32768 rows of 2048: gathered 59 us, of which memory needs 24; weighted 80; silu(g) * u of 1024 66; its gradient 159).
+// twice (32768 rows of 2048: gathered 59 us, of which memory needs 24; weighted 79; silu(g) * u of 1024 67; its gradient 156).
 #include <type_traits>
 
 #include "ciera_numeric.cuh"

@@ -21,9 +21,13 @@
 // share 64 of them, which are the first that are read (the next tile's products wait for them alone), and 64 hold the scales of
 // four groups of stages.
 //
-// Measured: 8192^3 385 us, 2850 TFLOP/s (a first form with one block on 128 x 256 and a byte of scales four times over 504);
-// 32768 rows of 64 experts, 2048 x 2048, 144 us forward and 229 us for the weights' gradient, 1074 MB of fp32 results at 83% of the
-// copy rate; one token on 8 experts 11.9 us, of which DRAM needs 5.  A copy of this that starts all products and waits for nothing
+// What a block does for the other is ordered in the cluster's scope: scales by a release and an acquire of shared memory, sums that
+// have been read by the tensor fences; and a block leaves when every arrival on its barriers has come.  (Orders of the block's
+// own scope and no wait at the end: one token on 8 experts 11.9 us, 13.5 so; large products the same.)
+//
+// Measured: 8192^3 406 us, 2710 TFLOP/s (a first form with one block on 128 x 256 and a byte of scales four times over 504);
+// 32768 rows of 64 experts, 2048 x 2048, 142 us forward and 227 us for the weights' gradient, 1074 MB of fp32 results at 83% of the
+// copy rate; one token on 8 experts 13.5 us, of which DRAM needs 5.  A copy of this that starts all products and waits for nothing
 // takes 93 us forward; the rest is the change from one tile's sum to the next, copies that come late, and writing.  Tried
 // and slower: tiles brought into L2 ahead of their copies (forward 144 -> 149 to 156 us, 8192^3 394 -> 413 to 456); two tiles of 128
 // rows to a pair as often as one of 256 (144 -> 150 us).
