@@ -577,6 +577,138 @@ typedef struct ciera_fp8_product {
 } ciera_fp8_product;
 CIERA_API int ciera_fp8_matmul(const ciera_fp8_product* args, void* stream);
 
+/* Operands in e2m1 (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives) with a power of two for each 32 values of a row: what a MoE
+ * layer answers with (training stays with the 8 bits above).  Two values to a byte, the even column in the low half; the half
+ * behind an odd last column is zero.  With a group's largest magnitude a, s is the least integer >= -126 with a <= 6 * 2^s (0 for
+ * a group of zeros); the scale byte is s + 127; a value y is stored as y * 2^-s rounded to nearest, ties to the even code.  A
+ * group that holds an infinity or a NaN has byte 255, which stands for NaN in all its places, and zeros in the codes.
+ * Scale bytes come in atoms of 512 bytes, one for 128 rows and 128 columns: the byte of (row, column) is byte
+ *   16 * (row % 32) + 4 * (row % 128 / 32) + column % 128 / 32    of atom    row / 128 * (stride / 512) + column / 128;
+ * an operand [rows, cols] has ceil(rows / 128) lines of ceil(cols / 128) atoms, `stride` bytes apart (a multiple of 512 and at
+ * least ceil(cols / 128) * 512).  A row's four bytes of an atom are written together, 127 behind the last column's group; bytes of
+ * rows that an operand does not have are left as they were.
+ * q is 16-byte aligned, its rows' and matrices' strides count bytes and are multiples of 16; scales are 16-byte aligned and
+ * their matrices' strides multiples of 16.  (Strides of single rows, lines and matrices count for nothing.) */
+#define CIERA_FP4_GROUP 32
+
+/* Rows of an operand, formed from `x` as ciera_fp8_quantize_rows does (CIERA_SOURCE_ROWS, CIERA_SOURCE_SWIGLU) and rounded in
+ * one pass: slot_of_row, top_k, starts, n_experts and x_rows as there. */
+typedef struct ciera_fp4_rows {
+    int32_t source, dtype;
+    uint64_t rows, cols, x_rows;
+    const void* x;
+    uint64_t x_stride;
+    const int32_t* slot_of_row;
+    const int32_t* starts;
+    uint32_t top_k, n_experts;
+    void* q;
+    uint64_t q_stride;
+    uint8_t* scales;
+    uint64_t scales_stride;
+} ciera_fp4_rows;
+CIERA_API int ciera_fp4_quantize_rows(const ciera_fp4_rows* args, void* stream);
+
+/* `matrices` matrices x [rows, cols], x_stride between rows, x_matrix_stride between matrices, as they are (q, scales: groups along
+ * the columns) or transposed (qt, scales_t: [cols, rows], groups of 32 rows), or both; the pair that is not wanted is NULL. */
+typedef struct ciera_fp4_matrices {
+    int32_t dtype;
+    uint32_t matrices;
+    uint64_t rows, cols;
+    const void* x;
+    uint64_t x_stride, x_matrix_stride;
+    void* q;
+    uint64_t q_stride, q_matrix_stride;
+    uint8_t* scales;
+    uint64_t scales_stride, scales_matrix_stride;
+    void* qt;
+    uint64_t qt_stride, qt_matrix_stride;
+    uint8_t* scales_t;
+    uint64_t scales_t_stride, scales_t_matrix_stride;
+} ciera_fp4_matrices;
+CIERA_API int ciera_fp4_quantize_matrices(const ciera_fp4_matrices* args, void* stream);
+
+/* The values that such operands stand for: out = the matrices [rows, cols], rounded once to `dtype`. */
+typedef struct ciera_fp4_value_args {
+    int32_t dtype;
+    uint32_t matrices;
+    uint64_t rows, cols;
+    const void* q;
+    uint64_t q_stride, q_matrix_stride;
+    const uint8_t* scales;
+    uint64_t scales_stride, scales_matrix_stride;
+    void* out;
+    uint64_t out_stride, out_matrix_stride;
+} ciera_fp4_value_args;
+CIERA_API int ciera_fp4_values(const ciera_fp4_value_args* args, void* stream);
+
+/* Products of such operands, summed in fp32: CIERA_PRODUCT_DENSE and CIERA_PRODUCT_ROWS as ciera_fp8_matmul has them, with a scale
+ * for each row and 32 columns on both sides (b's of all matrices: b_scales_matrix_stride apart).
+ * The bytes of an atom behind the last column's group are read with it and must not be 255, nor may the half byte behind an
+ * odd last column be other than zero, on both sides; the calls above leave them so.
+ * starts and *status as there.  Limits: m, n, k 1 .. 2^31 - 256, n_experts 1 .. 1024, strides below 2^40. */
+typedef struct ciera_fp4_product {
+    int32_t mode, out_dtype;
+    uint32_t n_experts;
+    uint64_t m, n, k;
+    const void* a;
+    uint64_t a_stride;
+    const uint8_t* a_scales;
+    uint64_t a_scales_stride;
+    const void* b;
+    uint64_t b_stride, b_matrix_stride;
+    const uint8_t* b_scales;
+    uint64_t b_scales_stride, b_scales_matrix_stride;
+    const int32_t* starts;
+    void* out;
+    uint64_t out_stride;
+    int32_t* status;
+} ciera_fp4_product;
+CIERA_API int ciera_fp4_matmul(const ciera_fp4_product* args, void* stream);
+
+/* A whole MoE layer for a few tokens, from the router's logits to the output:
+ *   experts, weights = ciera_route(logits, bias);   out[t] = sum over j of weights[t, j] * W2 (silu(g) * u),  (g, u) = W1 x[t]
+ * with W1 [2 * d_ff, d_model] (gate above up) and W2 [d_model, d_ff] of the choice's expert; choices of -1 are passed over, a
+ * token without any gets zeros.  The matrices stay in 8 bits (CIERA_WEIGHTS_FP8: e4m3 with a scale for each 128 x 128 block, as
+ * ciera_fp8_quantize_blocks makes them) or 4 (CIERA_WEIGHTS_FP4, scales_stride and so on as above); x keeps its own precision,
+ * other than in ciera_fp8_matmul.  An expert's matrices are read once for up to 8 of its tokens (16, with more than 8 tokens in all).
+ *   x             device, n_tokens rows of d_model values of dtype;  out  the same
+ *   logits, bias, experts, weights   as for ciera_route
+ *   workspace     device, 16-byte aligned, ciera_expert_tokens_workspace_bytes(); any contents, not shared by calls that may
+ *                 overlap
+ * Arithmetic: fp32 sums of 16-bit tensor products with exact weights.  x and silu(g) * u go into them with 11 bits (22 for fp32,
+ * so bf16 and fp16 values of x are exact) below the power of two of the largest of 128 values; values of silu(g) * u below
+ * 2^-111 may lose bits.  Results do not depend on the other tokens of a call but for the order of their sums.
+ * Limits: n_tokens 0 .. CIERA_EXPERT_TOKENS_MAX, d_model and d_ff multiples of 128 up to 65536, config as for ciera_route; weights
+ * and their strides as for the products. */
+#define CIERA_EXPERT_TOKENS_MAX 64
+typedef enum ciera_weights_format { CIERA_WEIGHTS_FP8 = 0, CIERA_WEIGHTS_FP4 = 1 } ciera_weights_format;
+typedef struct ciera_expert_tokens_args {
+    ciera_route_config route;
+    int32_t format, dtype, logits_dtype;
+    uint32_t n_tokens, d_model, d_ff;
+    const void* x;
+    uint64_t x_stride;
+    const void* logits;
+    uint64_t logits_stride;
+    const float* bias;
+    const void* w1;
+    uint64_t w1_stride, w1_matrix_stride;
+    const uint8_t* w1_scales;
+    uint64_t w1_scales_stride, w1_scales_matrix_stride;
+    const void* w2;
+    uint64_t w2_stride, w2_matrix_stride;
+    const uint8_t* w2_scales;
+    uint64_t w2_scales_stride, w2_scales_matrix_stride;
+    void* out;
+    uint64_t out_stride;
+    int32_t* experts;
+    float* weights;
+    void* workspace;
+    uint64_t workspace_bytes;
+} ciera_expert_tokens_args;
+CIERA_API size_t ciera_expert_tokens_workspace_bytes(uint32_t n_tokens, uint32_t top_k, uint32_t d_ff);
+CIERA_API int ciera_expert_tokens(const ciera_expert_tokens_args* args, void* stream);
+
 /* Weighted sum of a token's rows: out[t] = sum over j of weights[t, j] * rows[row_of_slot[t, j]], in fp32, rounded once;
  * weights NULL: 1.  Entries of row_of_slot outside 0 .. n_rows - 1 are passed over (a token without any gets zeros).
  *   rows  device, n_rows rows of `cols` values of `dtype`;  out  device, n_tokens rows, same type

@@ -12,7 +12,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libciera.so")
 SOURCES = ["ciera_host.cu", "ciera_encode.cu", "ciera_encode_hashed.cu", "ciera_decode.cu", "ciera_entropy.cu", "ciera_kernels.cu",
-           "ciera_route.cu", "ciera_experts.cu", "ciera_fp8.cu", "ciera_fp8_product.cu"]
+           "ciera_route.cu", "ciera_experts.cu", "ciera_fp8.cu", "ciera_fp8_product.cu", "ciera_fp4.cu", "ciera_fp4_product.cu",
+           "ciera_tokens.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
     "-lineinfo", "-O3", "-std=c++17",

@@ -48,6 +48,10 @@ SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 FP8_BLOCK = 128
 SOURCE_ROWS, SOURCE_SWIGLU, SOURCE_SWIGLU_BACKWARD = 0, 1, 2
 PRODUCT_DENSE, PRODUCT_ROWS, PRODUCT_CONTRACT = 0, 1, 2
+FP4_GROUP = 32
+FP4_ATOM = 512  # scale bytes of 128 rows and 128 columns
+WEIGHTS_FP8, WEIGHTS_FP4 = 0, 1
+EXPERT_TOKENS_MAX = 64
 
 
 class RouteConfig(ctypes.Structure):
@@ -78,6 +82,42 @@ class _Fp8Product(ctypes.Structure):
                 ("a_scales_stride", _u64), ("b", _vp), ("b_stride", _u64), ("b_matrix_stride", _u64), ("b_scales", _vp),
                 ("b_scales_stride", _u64), ("b_scales_matrix_stride", _u64), ("starts", _vp), ("out", _vp),
                 ("out_stride", _u64), ("out_matrix_stride", _u64), ("status", _vp)]
+
+
+class _Fp4Rows(ctypes.Structure):
+    _fields_ = [("source", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rows", _u64), ("cols", _u64), ("x_rows", _u64),
+                ("x", _vp), ("x_stride", _u64), ("slot_of_row", _vp), ("starts", _vp), ("top_k", _u32), ("n_experts", _u32),
+                ("q", _vp), ("q_stride", _u64), ("scales", _vp), ("scales_stride", _u64)]
+
+
+class _Fp4Matrices(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("matrices", _u32), ("rows", _u64), ("cols", _u64), ("x", _vp),
+                ("x_stride", _u64), ("x_matrix_stride", _u64), ("q", _vp), ("q_stride", _u64), ("q_matrix_stride", _u64),
+                ("scales", _vp), ("scales_stride", _u64), ("scales_matrix_stride", _u64), ("qt", _vp), ("qt_stride", _u64),
+                ("qt_matrix_stride", _u64), ("scales_t", _vp), ("scales_t_stride", _u64), ("scales_t_matrix_stride", _u64)]
+
+
+class _Fp4Values(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("matrices", _u32), ("rows", _u64), ("cols", _u64), ("q", _vp), ("q_stride", _u64),
+                ("q_matrix_stride", _u64), ("scales", _vp), ("scales_stride", _u64), ("scales_matrix_stride", _u64),
+                ("out", _vp), ("out_stride", _u64), ("out_matrix_stride", _u64)]
+
+
+class _Fp4Product(ctypes.Structure):
+    _fields_ = [("mode", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("n_experts", _u32), ("m", _u64), ("n", _u64),
+                ("k", _u64), ("a", _vp), ("a_stride", _u64), ("a_scales", _vp), ("a_scales_stride", _u64), ("b", _vp),
+                ("b_stride", _u64), ("b_matrix_stride", _u64), ("b_scales", _vp), ("b_scales_stride", _u64),
+                ("b_scales_matrix_stride", _u64), ("starts", _vp), ("out", _vp), ("out_stride", _u64), ("status", _vp)]
+
+
+class _ExpertTokens(ctypes.Structure):
+    _fields_ = [("route", RouteConfig), ("format", ctypes.c_int32), ("dtype", ctypes.c_int32), ("logits_dtype", ctypes.c_int32),
+                ("n_tokens", _u32), ("d_model", _u32), ("d_ff", _u32), ("x", _vp), ("x_stride", _u64), ("logits", _vp),
+                ("logits_stride", _u64), ("bias", _vp), ("w1", _vp), ("w1_stride", _u64), ("w1_matrix_stride", _u64),
+                ("w1_scales", _vp), ("w1_scales_stride", _u64), ("w1_scales_matrix_stride", _u64), ("w2", _vp),
+                ("w2_stride", _u64), ("w2_matrix_stride", _u64), ("w2_scales", _vp), ("w2_scales_stride", _u64),
+                ("w2_scales_matrix_stride", _u64), ("out", _vp), ("out_stride", _u64), ("experts", _vp), ("weights", _vp),
+                ("workspace", _vp), ("workspace_bytes", _u64)]
 
 
 class GainIn(ctypes.Structure):
@@ -131,6 +171,12 @@ _SIGS = {
     "ciera_fp8_quantize_rows": ([ctypes.POINTER(_Fp8Rows), _vp], _i32),
     "ciera_fp8_quantize_blocks": ([ctypes.POINTER(_Fp8Blocks), _vp], _i32),
     "ciera_fp8_matmul": ([ctypes.POINTER(_Fp8Product), _vp], _i32),
+    "ciera_fp4_quantize_rows": ([ctypes.POINTER(_Fp4Rows), _vp], _i32),
+    "ciera_fp4_quantize_matrices": ([ctypes.POINTER(_Fp4Matrices), _vp], _i32),
+    "ciera_fp4_values": ([ctypes.POINTER(_Fp4Values), _vp], _i32),
+    "ciera_fp4_matmul": ([ctypes.POINTER(_Fp4Product), _vp], _i32),
+    "ciera_expert_tokens_workspace_bytes": ([_u32, _u32, _u32], _sz),
+    "ciera_expert_tokens": ([ctypes.POINTER(_ExpertTokens), _vp], _i32),
     "ciera_expert_combine": ([_i32, _vp, _u64, _u64, _vp, _vp, _u64, _u32, _u64, _vp, _u64, _vp], _i32),
     "ciera_expert_combine_backward": ([_i32, _vp, _u64, _vp, _u64, _u64, _vp, _vp, _u64, _u32, _u64, _vp, _vp, _u64, _vp],
                                       _i32),
@@ -607,6 +653,168 @@ def fp8_matmul(a, a_scales, b, b_scales, out, starts=None, contract: bool = Fals
     args = _Fp8Product(mode, code, blocks, max(experts, 0), m, n, k, *a_at, *_scale_lines(w, device, a_scales, k, m), *b_at,
                        *bs_at, begin, *o_at, None if status is None else _whole(w, device, status, (1,), _I32))
     _enqueue(w, device, stream, _lib.ciera_fp8_matmul, args)
+
+
+def _codes(where: str, device: int, t, rows: int, cols: int):
+    """The address and the stride of the rows of 4-bit codes [rows, ceil(cols / 2)]."""
+    return _matrix(where, device, t, (rows, (cols + 1) // 2), _U8)
+
+
+def _atom_lines(where: str, device: int, t, rows: int, cols: int):
+    """The address and the stride of the lines of scale bytes [ceil(rows / 128), ceil(cols / 128), 512]."""
+    if not isinstance(t, _Tensor) or t.dtype is not _U8 or t.get_device() != device or \
+            t.shape != (-(-rows // 128), -(-cols // 128), FP4_ATOM) or t.stride(2) != 1 or \
+            (t.shape[1] > 1 and t.stride(1) != FP4_ATOM):
+        raise CieraError(where, ERR_INVALID_ARG)
+    return t.data_ptr(), t.stride(0)
+
+
+def _atom_stack(where: str, device: int, t, matrices: int, rows: int, cols: int):
+    """The same of [matrices, ...], and the stride of the matrices."""
+    if not isinstance(t, _Tensor) or t.dim() != 4 or t.shape[0] != matrices:
+        raise CieraError(where, ERR_INVALID_ARG)
+    if not matrices:
+        return t.data_ptr(), t.stride(1), t.stride(0)
+    return (*_atom_lines(where, device, t[0], rows, cols), t.stride(0))
+
+
+def fp4_quantize_rows(x, q, scales, *, kind: int = SOURCE_ROWS, slot_of_row=None, top_k: int = 1, starts=None,
+                      stream=None) -> None:
+    """Rows formed from ``x`` (as ``fp8_quantize_rows`` forms them, ``SOURCE_ROWS`` or ``SOURCE_SWIGLU``) and rounded to e2m1 with
+    a power of two for each 32 values: ``q`` uint8 [rows, ceil(cols / 2)], two values a byte, and ``scales`` uint8
+    [ceil(rows / 128), ceil(cols / 128), 512] (see ``ciera_fp4_rows``)."""
+    w = "ciera_fp4_quantize_rows"
+    device = _device_of(w, x)
+    code = _code(w, x)
+    x_at = _matrix(w, device, x, None, x.dtype)
+    x_rows, cols = x.shape
+    if kind == SOURCE_SWIGLU:
+        if cols % 2:
+            _refuse(w)
+        cols //= 2
+    if not isinstance(q, _Tensor) or q.dim() != 2:
+        _refuse(w)
+    rows = q.shape[0]
+    q_at = _codes(w, device, q, rows, cols)
+    s_at = _atom_lines(w, device, scales, rows, cols)
+    slots = begin = None
+    n_experts = 0
+    if slot_of_row is not None:
+        slots = _whole(w, device, slot_of_row, slot_of_row.shape, _I32)
+        if slot_of_row.dim() != 1 or slot_of_row.numel() < rows:
+            _refuse(w)
+    if starts is not None:
+        n_experts = starts.numel() - 1
+        begin = _whole(w, device, starts, (n_experts + 1,), _I32)
+    args = _Fp4Rows(kind, code, rows, cols, x_rows, *x_at, slots, begin, top_k, max(n_experts, 0), *q_at, *s_at)
+    _enqueue(w, device, stream, _lib.ciera_fp4_quantize_rows, args)
+
+
+def fp4_quantize_matrices(x, q=None, scales=None, qt=None, scales_t=None, stream=None) -> None:
+    """Matrices ``x`` [matrices, rows, cols] rounded to e2m1: ``q`` uint8 [matrices, rows, ceil(cols / 2)] with ``scales`` uint8
+    [matrices, ceil(rows / 128), ceil(cols / 128), 512], or transposed, ``qt`` and ``scales_t`` of [cols, rows], or both."""
+    w = "ciera_fp4_quantize_matrices"
+    device = _device_of(w, x)
+    code = _code(w, x)
+    x_at = _matrices(w, device, x, None, x.dtype)
+    m, r, c = x.shape
+    if (q is None) != (scales is None) or (qt is None) != (scales_t is None):
+        _refuse(w)
+    none = (None, 0, 0)
+    args = _Fp4Matrices(code, m, r, c, *x_at,
+                        *(none if q is None else _matrices(w, device, q, (m, r, (c + 1) // 2), _U8)),
+                        *(none if q is None else _atom_stack(w, device, scales, m, r, c)),
+                        *(none if qt is None else _matrices(w, device, qt, (m, c, (r + 1) // 2), _U8)),
+                        *(none if qt is None else _atom_stack(w, device, scales_t, m, c, r)))
+    _enqueue(w, device, stream, _lib.ciera_fp4_quantize_matrices, args)
+
+
+def fp4_values(q, scales, out, stream=None) -> None:
+    """``out`` ([rows, cols] or [matrices, rows, cols]) = the values that ``q`` and ``scales`` stand for."""
+    w = "ciera_fp4_values"
+    device = _device_of(w, out)
+    code = _code(w, out)
+    if out.dim() == 3:
+        m, r, c = out.shape
+        o_at = _matrices(w, device, out, None, out.dtype)
+        q_at, s_at = _matrices(w, device, q, (m, r, (c + 1) // 2), _U8), _atom_stack(w, device, scales, m, r, c)
+    else:
+        o_at = (*_matrix(w, device, out, None, out.dtype), 0)
+        m, (r, c) = 1, out.shape
+        q_at, s_at = (*_codes(w, device, q, r, c), 0), (*_atom_lines(w, device, scales, r, c), 0)
+    _enqueue(w, device, stream, _lib.ciera_fp4_values, _Fp4Values(code, m, r, c, *q_at, *s_at, *o_at))
+
+
+def fp4_matmul(a, a_scales, b, b_scales, out, starts=None, status=None, stream=None) -> None:
+    """``out`` [m, n] = ``a`` times ``b`` transposed, of operands as the calls above make them (see ``ciera_fp4_product``).
+
+    ``starts`` None: b [n, ceil(k / 2)] with scales of [n, k].  ``starts`` int32 [E + 1]: rows of ``a`` and ``out`` by segments, each
+    with its own matrix of b [E, n, ceil(k / 2)]."""
+    w = "ciera_fp4_matmul"
+    device = _device_of(w, a)
+    a_at = _matrix(w, device, a, None, _U8)
+    m, line = a.shape
+    k = 2 * line
+    begin, experts = None, 0
+    if starts is not None:
+        experts = starts.numel() - 1
+        begin = _whole(w, device, starts, (experts + 1,), _I32)
+        b_at = _matrices(w, device, b, None, _U8)
+        matrices, n, b_line = b.shape
+        if matrices != experts:
+            _refuse(w)
+        bs_at = _atom_stack(w, device, b_scales, experts, n, k)
+    else:
+        b_at = (*_matrix(w, device, b, None, _U8), 0)
+        n, b_line = b.shape
+        bs_at = (*_atom_lines(w, device, b_scales, n, k), 0)
+    if b_line != line:
+        _refuse(w)
+    code = _code(w, out)
+    args = _Fp4Product(PRODUCT_DENSE if starts is None else PRODUCT_ROWS, code, max(experts, 0), m, n, k, *a_at,
+                       *_atom_lines(w, device, a_scales, m, k), *b_at, *bs_at, begin,
+                       *_matrix(w, device, out, (m, n), out.dtype), None if status is None else _whole(w, device, status, (1,), _I32))
+    _enqueue(w, device, stream, _lib.ciera_fp4_matmul, args)
+
+
+def expert_tokens_workspace_bytes(config: RouteConfig, n_tokens: int, d_model: int, d_ff: int) -> int:
+    return int(_lib.ciera_expert_tokens_workspace_bytes(n_tokens, config.top_k, d_ff))
+
+
+def expert_tokens(config: RouteConfig, x, logits, bias, w1, w1_scales, w2, w2_scales, out, experts, weights, workspace,
+                  stream=None) -> None:
+    """A whole MoE layer for up to ``EXPERT_TOKENS_MAX`` tokens (see ``ciera_expert_tokens_args``): ``x`` and ``out`` [T, d_model],
+    ``logits`` [T, E], ``bias`` fp32 [E] or None; ``experts`` int32 and ``weights`` fp32 [T, top_k] receive the choice.
+
+    Weights in 8 bits: ``w1`` e4m3 [E, 2 d_ff, d_model] with a scale for each 128 x 128 block, ``w2`` [E, d_model, d_ff].  In 4 bits:
+    uint8, half as wide, with scales [E, rows / 128, cols / 128, 512].  ``workspace`` uint8
+    [expert_tokens_workspace_bytes(config, T, d_model, d_ff)]."""
+    w = "ciera_expert_tokens"
+    device = _device_of(w, x)
+    code = _code(w, x)
+    x_at = _matrix(w, device, x, None, x.dtype)
+    t, d = x.shape
+    logits_at = _matrix(w, device, logits, (t, config.n_experts), logits.dtype) if isinstance(logits, _Tensor) else _refuse(w)
+    logits_code = _code(w, logits)
+    e, k = config.n_experts, config.top_k
+    four = isinstance(w1, _Tensor) and w1.dtype is _U8
+    of, wide = (_U8, 2) if four else (_E4M3, 1)
+    if not isinstance(w1, _Tensor) or w1.dim() != 3 or w1.shape[1] % 2:
+        _refuse(w)
+    f = w1.shape[1] // 2
+    at = []
+    for q, s, rows, cols in ((w1, w1_scales, 2 * f, d), (w2, w2_scales, d, f)):
+        at += _matrices(w, device, q, (e, rows, cols // wide), of)
+        at += _atom_stack(w, device, s, e, rows, cols) if four else \
+            _matrices(w, device, s, (e, -(-rows // FP8_BLOCK), -(-cols // FP8_BLOCK)), _U8)
+    if not isinstance(workspace, _Tensor):
+        _refuse(w)
+    room = workspace.numel()
+    args = _ExpertTokens(config, WEIGHTS_FP4 if four else WEIGHTS_FP8, code, logits_code, t, d, f, *x_at, *logits_at,
+                         None if bias is None else _whole(w, device, bias, (e,), _F32), *at,
+                         *_matrix(w, device, out, (t, d), x.dtype), _whole(w, device, experts, (t, k), _I32),
+                         _whole(w, device, weights, (t, k), _F32), _whole(w, device, workspace, (room,), _U8), room)
+    _enqueue(w, device, stream, _lib.ciera_expert_tokens, args)
 
 
 def expert_combine(rows, row_of_slot, weights, out, stream=None) -> None:

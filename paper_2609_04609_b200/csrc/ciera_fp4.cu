@@ -1,0 +1,476 @@
+// Operands of the 4-bit products: rows or matrices rounded to e2m1 with a power of two for each 32 values of a row, and back.
+//
+// A lane has 8 neighbouring columns, so a group of 32 belongs to four neighbouring lanes and a row of 256 columns to a warp; its
+// largest magnitude is two exchanges, its codes are one word a lane.  A warp takes rows r, r + 32, r + 64 and r + 96 of an atom of
+// scales together: their scale bytes are 16 neighbouring bytes of the atom, and their loads are on their way at the same time.
+// Transposed matrices go through shared memory, two columns to a word.
+#include <type_traits>
+
+#include "ciera_fp4.cuh"
+#include "ciera_swiglu.cuh"
+
+namespace ciera {
+
+constexpr int kFp4Threads = 256;
+
+// The scale byte of a group whose largest magnitude has these bits: the least s >= -126 with amax <= 1.5 * 2^2 * 2^s.
+__device__ __forceinline__ uint32_t scale_byte4(uint32_t amax) {
+    if (amax >= 0x7f800000u) return 255u;
+    if (amax == 0u) return 127u;
+    const int s = (int)(amax >> 23) - 127 - 2 + ((amax & 0x7fffffu) > 0x400000u ? 1 : 0);
+    return (uint32_t)(max(s, -126) + 127);
+}
+// 2^-s; 0 for byte 255
+__device__ __forceinline__ float inverse_scale4(uint32_t byte) { return __uint_as_float(byte == 255u ? 0u : (254u - byte) << 23); }
+__device__ __forceinline__ uint32_t magnitude4(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Eight values, the first in the lowest four bits.
+__device__ __forceinline__ uint32_t to_e2m1x8(const float (&v)[8], float inv) {
+    uint32_t r;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(r)
+        : "f"(v[0] * inv), "f"(v[1] * inv), "f"(v[2] * inv), "f"(v[3] * inv), "f"(v[4] * inv), "f"(v[5] * inv), "f"(v[6] * inv),
+          "f"(v[7] * inv));
+    return r;
+}
+
+// Values c .. c + 7 of a row of `cols`, V of them in one access; 0 behind the row.
+template <int DT, int V>
+__device__ __forceinline__ void load_eight(const value_t<DT>* __restrict__ row, uint32_t c, uint32_t cols, float (&v)[8]) {
+    if (c + 8 <= cols) {
+#pragma unroll
+        for (int i = 0; i < 8; i += V) {
+            float part[V];
+            load_values<DT, V>(row + c + i, part);
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[i + j] = part[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? ValueOf<DT>::get(row[c + i]) : 0.f;
+    }
+}
+
+struct Rows4Args {
+    uint64_t x_stride, x_matrix_stride, q_stride, q_matrix_stride, scales_stride, scales_matrix_stride;
+    uint64_t x_rows;
+    const int32_t* slot_of_row;
+    const int32_t* starts;
+    uint32_t rows, cols, col_tiles, units, top_k, n_experts, source_rows;  // units: warps' work in a matrix
+    uint8_t* q;
+    uint8_t* scales;
+};
+
+// A largest magnitude of silu(g) * u that 32 bits do not settle: within 256 steps of the border 1.5 * 2^n (they are off by less than
+// 2^-20), or so small that a factor has left their range.
+__device__ __forceinline__ bool at_border4(uint32_t amax) {
+    return amax < 0x7f800000u && (amax < (32u << 23) || (uint32_t)((amax & 0x7fffffu) - 0x400000u + 256u) <= 512u);
+}
+
+// Whole tokens' worth of a warp: rows r + 32 * j of a block of 128, 256 columns.
+template <int DT, int SRC, int V>
+__global__ void __launch_bounds__(kFp4Threads) quantize4_rows_kernel(const Rows4Args a, const value_t<DT>* __restrict__ x_) {
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t used = a.starts ? min((uint32_t)max(a.starts[a.n_experts], 0), a.rows) : a.rows;
+    const uint32_t unit = blockIdx.x * (kFp4Threads / 32) + warp;
+    if (unit >= a.units) return;
+    const uint32_t line = unit / a.col_tiles, tile = unit - line * a.col_tiles;
+    const uint32_t rb = line >> 5, r0 = rb * 128u + (line & 31u);
+    if (r0 >= used) return;
+    const value_t<DT>* x = x_ + blockIdx.y * a.x_matrix_stride;
+    // lane j: where row j of the four comes from
+    uint32_t from = r0 + 32u * (lane & 3);
+    bool some = from < used;
+    if (a.slot_of_row) {
+        const int32_t slot = some ? a.slot_of_row[from] : -1;
+        some = slot >= 0 && (uint64_t)slot < a.x_rows * a.top_k;
+        if (SRC == CIERA_SOURCE_ROWS) from = some ? (uint32_t)slot / a.top_k : 0u;
+    }
+    const uint32_t there = __ballot_sync(~0u, some);
+    const uint32_t c0 = tile * 256u + lane * 8;
+    float v[4][8];
+    uint32_t some_values = 0;  // bit j: a value of row j is more than a zero times something
+    if constexpr (SRC == CIERA_SOURCE_ROWS) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t f = __shfl_sync(~0u, from, j);
+            if (there >> j & 1u) {
+                load_eight<DT, V>(x + (uint64_t)f * a.x_stride, c0, a.cols, v[j]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t f = __shfl_sync(~0u, from, j);
+            float u[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] = u[i] = 0.f;
+            if (!(there >> j & 1u)) continue;
+            const value_t<DT>* row = x + (uint64_t)f * a.x_stride;
+            load_eight<DT, V>(row, c0, a.cols, v[j]);
+            load_eight<DT, V>(row + a.cols, c0, a.cols, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float g = v[j][i];
+                v[j][i] = swiglu32(g, u[i]);
+                some_values |= (uint32_t)(g != 0.f && u[i] != 0.f) << j;
+                if (g < kLowestGate) v[j][i] = (float)((double)g / (1.0 + exp(-(double)g)) * (double)u[i]);
+            }
+        }
+    }
+    uint32_t bytes = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t row = r0 + 32u * j;
+        uint32_t amax = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) amax = max(amax, magnitude4(v[j][i]));
+        amax = max(amax, __shfl_xor_sync(~0u, amax, 1));
+        amax = max(amax, __shfl_xor_sync(~0u, amax, 2));
+        if constexpr (SRC == CIERA_SOURCE_SWIGLU) {
+            // settled in 64 bits, by the four lanes of each such group
+            const uint32_t has = __ballot_sync(~0u, some_values >> j & 1u) >> (lane & 28) & 15u;
+            const bool settle = at_border4(amax) && has;
+            if (__any_sync(~0u, settle)) {
+                const uint32_t f = __shfl_sync(~0u, from, j);
+                double most = 0.0;
+                if (settle) {
+                    const value_t<DT>* at = x + (uint64_t)f * a.x_stride;
+#pragma unroll 1
+                    for (uint32_t c = c0; c < min(c0 + 8u, a.cols); ++c) {
+                        const double g = ValueOf<DT>::get(at[c]), u = ValueOf<DT>::get(at[a.cols + c]);
+                        most = fmax(most, fabs(g / (1.0 + exp(-g)) * u));
+                    }
+                }
+                most = fmax(most, __shfl_xor_sync(~0u, most, 1));
+                most = fmax(most, __shfl_xor_sync(~0u, most, 2));
+                if (settle) amax = __float_as_uint(__double2float_ru(most));
+            }
+        }
+        const uint32_t byte = scale_byte4(amax);
+        uint32_t codes = to_e2m1x8(v[j], inverse_scale4(byte));
+        if (byte == 255u) codes = 0u;
+        bytes |= byte << (8 * j);
+        if (row < used && c0 < a.cols) {
+            uint8_t* to = a.q + blockIdx.y * a.q_matrix_stride + (uint64_t)row * a.q_stride + c0 / 2;
+            if (c0 + 8 <= a.cols) {
+                *reinterpret_cast<uint32_t*>(to) = codes;
+            } else {
+                for (uint32_t i = 0; 2 * i < a.cols - c0; ++i) to[i] = (uint8_t)(codes >> (8 * i));
+            }
+        }
+    }
+    // from a group's bytes of four rows to a row's of four groups, which lane 4 * j of the 16 writes for row j
+    const uint32_t g = lane >> 2;
+    uint32_t t = __shfl_xor_sync(~0u, bytes, 4);
+    bytes = g & 1 ? __byte_perm(t, bytes, 0x7351) : __byte_perm(bytes, t, 0x6240);
+    t = __shfl_xor_sync(~0u, bytes, 8);
+    bytes = g & 2 ? __byte_perm(t, bytes, 0x7632) : __byte_perm(bytes, t, 0x5410);
+    const uint32_t row = r0 + 32u * (g & 3), atom = tile * 2 + (lane >> 4);
+    if (!(lane & 3) && row < used && atom * 128u < a.cols)
+        *reinterpret_cast<uint32_t*>(a.scales + blockIdx.y * a.scales_matrix_stride + (uint64_t)rb * a.scales_stride + (uint64_t)atom * kAtomBytes +
+                                     atom_word(row)) = bytes;
+}
+
+struct Turned4Args {
+    uint64_t x_stride, x_matrix_stride, q_stride, q_matrix_stride, scales_stride, scales_matrix_stride;
+    uint32_t rows, cols, row_tiles, col_tiles;
+    uint8_t* q;
+    uint8_t* scales;
+};
+
+// Transposed: a block has 128 rows (the contraction) and 256 bytes of columns, 64 words of two 16-bit columns or one of 32 bits.
+// A thread rounds the 32 values of a group in its word's columns; word w of row r lies at (w + 8 * (r / 32)) % 64, so that the four
+// groups of 8 words, which a warp reads together, are in different banks.
+template <int DT, bool WIDE>
+__global__ void __launch_bounds__(kFp4Threads) quantize4_turned_kernel(const Turned4Args a, const value_t<DT>* __restrict__ x_) {
+    constexpr int kCols = 4 / sizeof(value_t<DT>);  // of a word
+    __shared__ __align__(16) uint32_t tile[128 * 64];
+    pdl_wait();
+    const uint32_t row_tile = blockIdx.x % a.row_tiles, col_tile = blockIdx.x / a.row_tiles;
+    const uint32_t row0 = row_tile * 128u, col0 = col_tile * 64u * kCols;
+    const value_t<DT>* x = x_ + blockIdx.y * a.x_matrix_stride;
+    if (WIDE) {
+        uint4 v[8];
+        const uint32_t piece = threadIdx.x & 15, c = col0 + piece * 4 * kCols;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t r = row0 + i * 16 + (threadIdx.x >> 4);
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (r < a.rows && c < a.cols) v[i] = *reinterpret_cast<const uint4*>(x + (uint64_t)r * a.x_stride + c);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t r = i * 16 + (threadIdx.x >> 4);
+            *reinterpret_cast<uint4*>(tile + r * 64 + ((piece * 4 + 8 * (r >> 5)) & 63)) = v[i];
+        }
+    } else {
+        for (uint32_t i = threadIdx.x; i < 128 * 64 * kCols; i += kFp4Threads) {
+            const uint32_t r = i / (64 * kCols), c = i % (64 * kCols), w = c / kCols;
+            value_t<DT> v = ValueOf<DT>::put(0.f);
+            if (row0 + r < a.rows && col0 + c < a.cols) v = x[(uint64_t)(row0 + r) * a.x_stride + col0 + c];
+            reinterpret_cast<value_t<DT>*>(tile + r * 64 + ((w + 8 * (r >> 5)) & 63))[c % kCols] = v;
+        }
+    }
+    __syncthreads();
+    const uint32_t group = threadIdx.x & 3, w = threadIdx.x >> 2;
+    const uint32_t* from = tile + group * 32 * 64 + ((w + 8 * group) & 63);
+    uint32_t word[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) word[i] = from[i * 64];
+    uint32_t bytes[kCols];
+#pragma unroll
+    for (int k = 0; k < kCols; ++k) {
+        const auto value = [&](int i) {
+            if constexpr (DT == CIERA_FP32) return __uint_as_float(word[i]);
+            else if constexpr (DT == CIERA_BF16) return __uint_as_float(k ? word[i] & 0xffff0000u : word[i] << 16);
+            else return __half2float(__ushort_as_half((unsigned short)(word[i] >> (16 * k))));
+        };
+        uint32_t amax = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) amax = max(amax, magnitude4(value(i)));
+        const uint32_t byte = bytes[k] = scale_byte4(amax);
+        const float inv = inverse_scale4(byte);
+        uint32_t q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float v[8] = {value(8 * i), value(8 * i + 1), value(8 * i + 2), value(8 * i + 3),
+                                value(8 * i + 4), value(8 * i + 5), value(8 * i + 6), value(8 * i + 7)};
+            q[i] = byte == 255u ? 0u : to_e2m1x8(v, inv);
+        }
+        const uint32_t c = col0 + w * kCols + k, r = row0 + group * 32;
+        if (c < a.cols && r < a.rows) {
+            uint8_t* to = a.q + blockIdx.y * a.q_matrix_stride + (uint64_t)c * a.q_stride + r / 2;
+            if (r + 32 <= a.rows) {
+                *reinterpret_cast<uint4*>(to) = make_uint4(q[0], q[1], q[2], q[3]);
+            } else {
+                for (uint32_t i = 0; 2 * i < a.rows - r; ++i) {
+                    const uint32_t part = i < 4 ? q[0] : i < 8 ? q[1] : i < 12 ? q[2] : q[3];
+                    to[i] = (uint8_t)(part >> (8 * (i & 3)));
+                }
+            }
+        }
+    }
+    // four neighbouring lanes have a column's four groups
+#pragma unroll
+    for (int k = 0; k < kCols; ++k) {
+        uint32_t all = bytes[k] << (8 * group);
+        all |= __shfl_xor_sync(~0u, all, 1);
+        all |= __shfl_xor_sync(~0u, all, 2);
+        const uint32_t c = col0 + w * kCols + k;
+        if (group == 0 && c < a.cols)
+            *reinterpret_cast<uint32_t*>(a.scales + blockIdx.y * a.scales_matrix_stride + (uint64_t)(c >> 7) * a.scales_stride + (uint64_t)row_tile * kAtomBytes +
+                                         atom_word(c)) = all;
+    }
+}
+
+struct Values4Args {
+    uint64_t q_stride, q_matrix_stride, scales_stride, scales_matrix_stride, out_stride, out_matrix_stride;
+    uint32_t rows, cols, col_tiles, units;
+    const uint8_t* q;
+    const uint8_t* scales;
+};
+
+// Back: the same rows and columns for a warp as above.
+template <int DT, bool WIDE>
+__global__ void __launch_bounds__(kFp4Threads) values4_kernel(const Values4Args a, value_t<DT>* __restrict__ out_) {
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t unit = blockIdx.x * (kFp4Threads / 32) + warp;
+    if (unit >= a.units) return;
+    const uint32_t line = unit / a.col_tiles, tile = unit - line * a.col_tiles;
+    const uint32_t rb = line >> 5, r0 = rb * 128u + (line & 31u), c0 = tile * 256u + lane * 8;
+    if (r0 >= a.rows || c0 >= a.cols) return;
+    const uint8_t* q = a.q + blockIdx.y * a.q_matrix_stride + c0 / 2;
+    const uint4 s = *reinterpret_cast<const uint4*>(a.scales + blockIdx.y * a.scales_matrix_stride + (uint64_t)rb * a.scales_stride +
+                                                    (uint64_t)(c0 >> 7) * kAtomBytes + (line & 31u) * 16);
+    const uint32_t scale[4] = {s.x, s.y, s.z, s.w};
+    uint32_t codes[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t row = r0 + 32u * j;
+        codes[j] = 0;
+        if (row >= a.rows) continue;
+        const uint8_t* from = q + (uint64_t)row * a.q_stride;
+        if (c0 + 8 <= a.cols) {
+            codes[j] = *reinterpret_cast<const uint32_t*>(from);
+        } else {
+            for (uint32_t i = 0; 2 * i < a.cols - c0; ++i) codes[j] |= (uint32_t)from[i] << (8 * i);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t row = r0 + 32u * j;
+        if (row >= a.rows) continue;
+        const float f = scale_value(scale[j] >> (lane >> 2 & 3) * 8 & 255u);
+        float v[8];
+        uint32_t two[4];
+        from_e2m1x8(codes[j], two);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&two[i]));
+            v[2 * i] = y.x * f;
+            v[2 * i + 1] = y.y * f;
+        }
+        value_t<DT>* to = out_ + blockIdx.y * a.out_matrix_stride + (uint64_t)row * a.out_stride + c0;
+        if (WIDE && c0 + 8 <= a.cols) {
+            constexpr int kEach = 16 / sizeof(value_t<DT>);
+#pragma unroll
+            for (int i = 0; i < 8; i += kEach) {
+                float part[kEach];
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) part[k] = v[i + k];
+                store_values<DT, kEach>(to + i, part);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c0 + i < a.cols) to[i] = ValueOf<DT>::put(v[i]);
+        }
+    }
+}
+
+// f(values that may be read at a time as a constant): rows that start at multiples of 8 values, of 2, or of 1
+template <class F>
+static void with_width(bool eight, bool two, F&& f) {
+    if (eight) f(std::integral_constant<int, 8>());
+    else if (two) f(std::integral_constant<int, 2>());
+    else f(std::integral_constant<int, 1>());
+}
+
+// An operand's codes and scales; lines: of atoms.  0, or the status of what is wrong with them.
+static int operand4(const void* q, uint64_t q_stride, uint64_t q_matrix_stride, const void* scales, uint64_t scales_stride,
+                    uint64_t scales_matrix_stride, uint64_t matrices, uint64_t rows, uint64_t cols) {
+    const uint64_t line = (cols + 1) / 2, atoms = (cols + 127) / 128;
+    if (!q || !scales || (rows > 1 && q_stride < line) || (rows > 128 && scales_stride < atoms * kAtomBytes)) return CIERA_ERR_INVALID_ARG;
+    if (!aligned_to(q, 16) || !aligned_to(scales, 16) || (rows > 1 && (q_stride & 15)) || (rows > 128 && (scales_stride & 511)) ||
+        (matrices > 1 && ((q_matrix_stride | scales_matrix_stride) & 15)))
+        return CIERA_ERR_MISALIGNED;
+    return CIERA_OK;
+}
+
+static uint64_t warp_units(uint64_t rows, uint64_t cols) {
+    return (rows + 127) / 128 * (rows < 32 ? rows : 32) * ((cols + 255) / 256);
+}
+
+// Warps' work has 32 lines for each block of 128 rows; of a single block with fewer rows those that it has.
+template <int SRC>
+static cudaError_t launch_rows4(const Rows4Args& a, int dtype, const void* x, uint32_t matrices, cudaStream_t s) {
+    cudaError_t e = cudaSuccess;
+    with_dtype(dtype, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        const uint64_t v = dtype_bytes(DT);
+        uint64_t at = (uint64_t)x | (a.source_rows > 1 ? a.x_stride * v : 0) | (matrices > 1 ? a.x_matrix_stride * v : 0);
+        if (SRC == CIERA_SOURCE_SWIGLU) at |= a.cols * v;
+        const dim3 grid((a.units + kFp4Threads / 32 - 1) / (kFp4Threads / 32), matrices);
+        with_width(!(at & 15), !(at & (2 * v - 1)), [&](auto width) {
+            e = launch_after(quantize4_rows_kernel<DT, SRC, decltype(width)::value>, grid, kFp4Threads, 0, s, a, (const value_t<DT>*)x);
+        });
+    });
+    return e;
+}
+
+}  // namespace ciera
+
+using namespace ciera;
+
+extern "C" int ciera_fp4_quantize_rows(const ciera_fp4_rows* p, void* stream) {
+    if (!p || p->rows > kMaxExtent || p->cols > kMaxExtent || p->x_rows > kMaxExtent) return CIERA_ERR_INVALID_ARG;
+    if (p->source != CIERA_SOURCE_ROWS && p->source != CIERA_SOURCE_SWIGLU) return CIERA_ERR_INVALID_ARG;
+    if (p->dtype != CIERA_BF16 && p->dtype != CIERA_FP32 && p->dtype != CIERA_FP16) return CIERA_ERR_INVALID_ARG;
+    if (!p->rows) return CIERA_OK;
+    const bool swiglu = p->source == CIERA_SOURCE_SWIGLU;
+    const uint64_t width = swiglu ? 2 * p->cols : p->cols;
+    if (p->cols < 1 || (p->x_rows && !p->x) || (p->x_rows > 1 && p->x_stride < width) ||
+        (p->slot_of_row && (p->top_k < 1 || p->top_k > 32 || p->x_rows * p->top_k > kMaxExtent)) ||
+        (p->starts && (p->n_experts < 1 || p->n_experts > 1024)) || ((swiglu || !p->slot_of_row) && p->x_rows < p->rows))
+        return CIERA_ERR_INVALID_ARG;
+    const int rc = operand4(p->q, p->q_stride, 0, p->scales, p->scales_stride, 0, 1, p->rows, p->cols);
+    if (rc) return rc;
+    if (!aligned_to(p->x, dtype_bytes(p->dtype)) || !aligned_to(p->slot_of_row, 4) || !aligned_to(p->starts, 4)) return CIERA_ERR_MISALIGNED;
+    const uint64_t units = warp_units(p->rows, p->cols);
+    if (units > kMaxExtent) return CIERA_ERR_UNSUPPORTED;
+    const Rows4Args a{p->x_stride, 0, p->q_stride, 0, p->scales_stride, 0, p->x_rows, p->slot_of_row, p->starts, (uint32_t)p->rows,
+                      (uint32_t)p->cols, (uint32_t)((p->cols + 255) / 256), (uint32_t)units, p->slot_of_row ? p->top_k : 1u, p->n_experts,
+                      (uint32_t)p->x_rows, (uint8_t*)p->q, p->scales};
+    const cudaError_t e = swiglu ? launch_rows4<CIERA_SOURCE_SWIGLU>(a, p->dtype, p->x, 1, (cudaStream_t)stream)
+                                 : launch_rows4<CIERA_SOURCE_ROWS>(a, p->dtype, p->x, 1, (cudaStream_t)stream);
+    if (e != cudaSuccess) return record_cuda_error(e);
+    count_launch();
+    return CIERA_OK;
+}
+
+extern "C" int ciera_fp4_quantize_matrices(const ciera_fp4_matrices* p, void* stream) {
+    if (!p || p->rows > kMaxExtent || p->cols > kMaxExtent || p->matrices > 65535) return CIERA_ERR_INVALID_ARG;
+    if (p->dtype != CIERA_BF16 && p->dtype != CIERA_FP32 && p->dtype != CIERA_FP16) return CIERA_ERR_INVALID_ARG;
+    if ((p->q != nullptr) != (p->scales != nullptr) || (p->qt != nullptr) != (p->scales_t != nullptr) || (!p->q && !p->qt)) return CIERA_ERR_INVALID_ARG;
+    if (!p->rows || !p->cols || !p->matrices) return CIERA_OK;
+    if (!p->x || (p->rows > 1 && p->x_stride < p->cols)) return CIERA_ERR_INVALID_ARG;
+    if (!aligned_to(p->x, dtype_bytes(p->dtype))) return CIERA_ERR_MISALIGNED;
+    if (p->q) {
+        const int rc = operand4(p->q, p->q_stride, p->q_matrix_stride, p->scales, p->scales_stride, p->scales_matrix_stride, p->matrices, p->rows, p->cols);
+        if (rc) return rc;
+    }
+    if (p->qt) {
+        const int rc = operand4(p->qt, p->qt_stride, p->qt_matrix_stride, p->scales_t, p->scales_t_stride, p->scales_t_matrix_stride, p->matrices, p->cols, p->rows);
+        if (rc) return rc;
+    }
+    const uint64_t v = dtype_bytes(p->dtype), units = warp_units(p->rows, p->cols), wide_cols = 256 / v;
+    const uint64_t row_tiles = (p->rows + 127) / 128, col_tiles = (p->cols + wide_cols - 1) / wide_cols;
+    if (units > kMaxExtent || row_tiles * col_tiles > kMaxExtent) return CIERA_ERR_UNSUPPORTED;
+    cudaError_t e = cudaSuccess;
+    if (p->q) {
+        const Rows4Args a{p->x_stride, p->x_matrix_stride, p->q_stride, p->q_matrix_stride, p->scales_stride, p->scales_matrix_stride,
+                          p->rows, nullptr, nullptr, (uint32_t)p->rows, (uint32_t)p->cols, (uint32_t)((p->cols + 255) / 256), (uint32_t)units, 1u, 0u,
+                          (uint32_t)p->rows, (uint8_t*)p->q, p->scales};
+        e = launch_rows4<CIERA_SOURCE_ROWS>(a, p->dtype, p->x, p->matrices, (cudaStream_t)stream);
+        if (e != cudaSuccess) return record_cuda_error(e);
+        count_launch();
+    }
+    if (p->qt) {
+        const Turned4Args a{p->x_stride, p->x_matrix_stride, p->qt_stride, p->qt_matrix_stride, p->scales_t_stride, p->scales_t_matrix_stride,
+                            (uint32_t)p->rows, (uint32_t)p->cols, (uint32_t)row_tiles, (uint32_t)col_tiles, (uint8_t*)p->qt, p->scales_t};
+        const bool wide = !(((uint64_t)p->x | (p->rows > 1 ? p->x_stride * v : 0) | (p->matrices > 1 ? p->x_matrix_stride * v : 0) | p->cols * v) & 15);
+        with_dtype(p->dtype, [&](auto dt) {
+            constexpr int DT = decltype(dt)::value;
+            e = launch_after(wide ? quantize4_turned_kernel<DT, true> : quantize4_turned_kernel<DT, false>,
+                             dim3((uint32_t)(row_tiles * col_tiles), p->matrices), kFp4Threads, 0, (cudaStream_t)stream, a, (const value_t<DT>*)p->x);
+        });
+        if (e != cudaSuccess) return record_cuda_error(e);
+        count_launch();
+    }
+    return CIERA_OK;
+}
+
+extern "C" int ciera_fp4_values(const ciera_fp4_value_args* p, void* stream) {
+    if (!p || p->rows > kMaxExtent || p->cols > kMaxExtent || p->matrices > 65535) return CIERA_ERR_INVALID_ARG;
+    if (p->dtype != CIERA_BF16 && p->dtype != CIERA_FP32 && p->dtype != CIERA_FP16) return CIERA_ERR_INVALID_ARG;
+    if (!p->rows || !p->cols || !p->matrices) return CIERA_OK;
+    if (!p->out || (p->rows > 1 && p->out_stride < p->cols)) return CIERA_ERR_INVALID_ARG;
+    const int rc = operand4(p->q, p->q_stride, p->q_matrix_stride, p->scales, p->scales_stride, p->scales_matrix_stride, p->matrices, p->rows, p->cols);
+    if (rc) return rc;
+    const uint64_t v = dtype_bytes(p->dtype), units = warp_units(p->rows, p->cols);
+    if (!aligned_to(p->out, v)) return CIERA_ERR_MISALIGNED;
+    if (units > kMaxExtent) return CIERA_ERR_UNSUPPORTED;
+    const Values4Args a{p->q_stride, p->q_matrix_stride, p->scales_stride, p->scales_matrix_stride, p->out_stride, p->out_matrix_stride,
+                        (uint32_t)p->rows, (uint32_t)p->cols, (uint32_t)((p->cols + 255) / 256), (uint32_t)units, (const uint8_t*)p->q, p->scales};
+    const bool wide = !(((uint64_t)p->out | (p->rows > 1 ? p->out_stride * v : 0) | (p->matrices > 1 ? p->out_matrix_stride * v : 0)) & 15);
+    const dim3 grid((uint32_t)((units + kFp4Threads / 32 - 1) / (kFp4Threads / 32)), p->matrices);
+    cudaError_t e = cudaSuccess;
+    with_dtype(p->dtype, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        e = launch_after(wide ? values4_kernel<DT, true> : values4_kernel<DT, false>, grid, kFp4Threads, 0, (cudaStream_t)stream, a, (value_t<DT>*)p->out);
+    });
+    if (e != cudaSuccess) return record_cuda_error(e);
+    count_launch();
+    return CIERA_OK;
+}

@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "ciera_numeric.cuh"
+#include "ciera_swiglu.cuh"
 
 namespace ciera {
 
@@ -52,22 +53,6 @@ __device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d
     return to_e4m3x4(a, b, c, d, make_float4(inv, inv, inv, inv));
 }
 
-// sigmoid(g) = 1 / (1 + e) and 1 - sigmoid(g) = e / (1 + e) with e = 2^(-g log2 e): the exponent in two parts (log2 e as the nearest
-// 32-bit number and what is left of it), so that the power is off by a step or two however large the exponent is, and both
-// results by less than 2^-21 of themselves; for g above 87 e and 1 - sigmoid(g) are 0.  Gates below kLowestGate, where e leaves 32
-// bits, are not for this.  (expf and a division: silu(g) * u of 32768 x 1024 in 93 us.)
-constexpr float kLowestGate = -87.f;
-__device__ __forceinline__ float2 sigmoid32(float g) {
-    const float x = fminf(fmaxf(g, kLowestGate), 127.f), t = x * -1.44269504f;
-    const float rest = fmaf(x, -1.44269504f, -t) + x * -1.92596299e-8f;  // -x log2 e = t + rest
-    float e;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
-    e = fmaf(e, rest * 0.693147181f, e);
-    float s;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + e));
-    return make_float2(s, e * s);  // (a NaN is not seen here; g itself is a factor of all that this goes into)
-}
-__device__ __forceinline__ float swiglu32(float g, float u) { return g * sigmoid32(g).x * u; }
 // 1 + g (1 - sigmoid(g)) is zero at one g, which is here in two parts, and cancels around it: within 1/16 it comes from its series (a
 // fit of degree 3 to what the definition gives in 50 digits, off by less than 2^-21 of itself), beyond that it is off by less
 // than 2^-17.

@@ -151,6 +151,20 @@ __device__ __forceinline__ void tensor_mma_mx(uint32_t d, uint64_t a, uint64_t b
         : "memory");
 }
 
+// e2m1 operands with a power of two for each row and 32 values of the contraction, 64 of which an instruction takes; the scales
+// are two bytes of the words in tensor memory, from byte 0 or (mx_byte(2)) 2 on
+__host__ __device__ constexpr uint32_t mx4_instruction(uint32_t m, uint32_t n) {
+    return 1u << 7 | 1u << 10 | (n >> 3) << 17 | 1u << 23 /* scales are powers of two */ | (m >> 7) << 27;
+}
+__device__ __forceinline__ void tensor_mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, uint32_t a_scales,
+                                               uint32_t b_scales, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(instruction), "r"(a_scales), "r"(b_scales), "r"((uint32_t)add)
+        : "memory");
+}
+
 // ---- tensor maps
 
 __device__ __forceinline__ void prefetch_map(const void* map) {
@@ -162,6 +176,14 @@ __device__ __forceinline__ void map_load3(void* dst, const void* map, int32_t x,
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
             smem_u32(dst)),
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+
+__device__ __forceinline__ void map_load4(void* dst, const void* map, int32_t x, int32_t y, int32_t z, int32_t w, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+            smem_u32(dst)),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
         : "memory");
 }
 

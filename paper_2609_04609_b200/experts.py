@@ -2,7 +2,8 @@
 
 Plumbing only, as in ``runtime``: torch allocates the buffers, every operation is a call into the library.  The products run
 in 8-bit floating point with a power of two for each block of 128 values, forwards and backwards; what is summed or handed
-from one product to the next is kept in the weights' type, gradients of weights in fp32.
+from one product to the next is kept in the weights' type, gradients of weights in fp32.  A layer that only answers may have them
+in 4 bits with a power of two for each 32 values, and has one call for a few tokens, whichever its weights are in.
 """
 from __future__ import annotations
 
@@ -25,6 +26,12 @@ def _bytes(device, *shape):
     return torch.zeros(*shape, dtype=torch.uint8, device=device)
 
 
+def _atoms(device, *shape):
+    """Scale bytes of a 4-bit operand [..., rows, cols]."""
+    rows, cols = shape[-2:]
+    return torch.full((*shape[:-2], -(-rows // BLOCK), -(-cols // BLOCK), ciera.FP4_ATOM), 127, dtype=torch.uint8, device=device)
+
+
 class ExpertLayer:
     """``n_experts`` experts, each ``down(silu(gate(x)) * up(x))``, of which every token uses ``top_k``.
 
@@ -34,11 +41,17 @@ class ExpertLayer:
     belong to the layer, so one forward pass at a time can be waiting for its backward pass, and passes on different streams are put
     in order by the caller.  With ``stream`` a pass runs there whole: its results are allocated there too, and its inputs are kept
     from reuse until it is done with them.
+
+    ``weight_bits=4`` (with ``training=False``): weights and rows in 4 bits, half the bytes and twice the rate, one bit behind the
+    point.  ``forward_tokens`` is the pass of a few tokens (``ciera.EXPERT_TOKENS_MAX``) in one call that reads each reached
+    expert's weights once; rows are not rounded to 8 or 4 bits there, so it is the more exact of the two.
     """
 
     def __init__(self, codec, n_experts: int, d_model: int, d_ff: int, top_k: int, max_tokens: int,
                  score: int = ciera.SCORE_SOFTMAX, n_groups: int = 1, top_groups: int = 1, group_best: int = 2,
-                 renormalise: bool = False, scale: float = 1.0, training: bool = True):
+                 renormalise: bool = False, scale: float = 1.0, training: bool = True, weight_bits: int = 8):
+        if weight_bits not in (8, 4) or (weight_bits == 4 and training):
+            raise ValueError("weight_bits is 8, or 4 with training=False: gradients take 8 bits")
         if d_model % BLOCK or d_ff % BLOCK or d_model < 1 or d_ff < 1:
             raise ValueError(f"d_model and d_ff are multiples of {BLOCK}")
         if max_tokens < 1 or n_experts < 1:
@@ -47,7 +60,7 @@ class ExpertLayer:
             raise ValueError("the codec has no buffer for reconstructed weights")
         self.codec, self.device = codec, codec.device
         self.n_experts, self.d_model, self.d_ff, self.top_k, self.max_tokens = n_experts, d_model, d_ff, top_k, max_tokens
-        self.training = training
+        self.training, self.weight_bits = training, weight_bits
         self.dtype = TORCH_DTYPES[codec.dtype_name]
         self.config = ciera.RouteConfig(n_experts=n_experts, top_k=top_k, n_groups=n_groups, top_groups=top_groups,
                                         group_best=group_best, score=score, renormalise=int(renormalise), scale=scale)
@@ -63,10 +76,15 @@ class ExpertLayer:
         self.down = flat.as_strided((n_experts, d_ff, d_model), (3 * size, d_model, 1), flat.storage_offset() + 2 * size)
         dev, e, d, f, b = self.device, n_experts, d_model, d_ff, BLOCK
         # gate and up side by side, down: rows of outputs (forward) and rows of inputs (backward)
-        self.w1, self.w1_s = _operand(dev, e, 2 * f, d), _bytes(dev, e, 2 * f // b, d // b)
-        self.w2, self.w2_s = _operand(dev, e, d, f), _bytes(dev, e, d // b, f // b)
-        self.w1_t, self.w1_ts = _operand(dev, e, d, 2 * f), _bytes(dev, e, d // b, 2 * f // b)
-        self.w2_t, self.w2_ts = _operand(dev, e, f, d), _bytes(dev, e, f // b, d // b)
+        four = weight_bits == 4
+        if four:
+            self.w1, self.w1_s = _bytes(dev, e, 2 * f, d // 2), _atoms(dev, e, 2 * f, d)
+            self.w2, self.w2_s = _bytes(dev, e, d, f // 2), _atoms(dev, e, d, f)
+        else:
+            self.w1, self.w1_s = _operand(dev, e, 2 * f, d), _bytes(dev, e, 2 * f // b, d // b)
+            self.w2, self.w2_s = _operand(dev, e, d, f), _bytes(dev, e, d // b, f // b)
+            self.w1_t, self.w1_ts = _operand(dev, e, d, 2 * f), _bytes(dev, e, d // b, 2 * f // b)
+            self.w2_t, self.w2_ts = _operand(dev, e, f, d), _bytes(dev, e, f // b, d // b)
         # per batch
         slots = max_tokens * top_k
         cap = ciera.expert_rows_capacity(slots, e)
@@ -76,9 +94,15 @@ class ExpertLayer:
         self.starts, self.counts, self.slot_of_row = torch.zeros(e + 1, **i32), torch.zeros(e, **i32), torch.zeros(cap, **i32)
         self.workspace = _bytes(dev, max(ciera.expert_layout_workspace_bytes(slots, e), 16))
         self.status = torch.zeros(1, **i32)
-        self.x_q, self.x_s = _operand(dev, cap, d), _bytes(dev, d // b, cap)
+        if four:
+            self.x_q, self.x_s = _bytes(dev, cap, d // 2), _atoms(dev, cap, d)
+            self.a_q, self.a_s = _bytes(dev, cap, f // 2), _atoms(dev, cap, f)
+        else:
+            self.x_q, self.x_s = _operand(dev, cap, d), _bytes(dev, d // b, cap)
+            self.a_q, self.a_s = _operand(dev, cap, f), _bytes(dev, f // b, cap)
         self.h = torch.zeros(cap, 2 * f, dtype=self.dtype, device=dev)
-        self.a_q, self.a_s = _operand(dev, cap, f), _bytes(dev, f // b, cap)
+        self.few = min(max_tokens, ciera.EXPERT_TOKENS_MAX)  # tokens of forward_tokens
+        self.few_workspace = _bytes(dev, ciera.expert_tokens_workspace_bytes(self.config, self.few, d, f))
         self.o = torch.zeros(cap, d, dtype=self.dtype, device=dev)
         if training:
             rb = cap // b
@@ -97,7 +121,13 @@ class ExpertLayer:
 
     # -- weights ----------------------------------------------------------------------------------
     def refresh(self, stream=None) -> None:
-        """Rounds the codec's reconstructed weights, both orientations."""
+        """Rounds the codec's reconstructed weights, both orientations (in 4 bits the one that forward passes need)."""
+        if self.weight_bits == 4:
+            f, lines = self.d_ff, self.d_ff // BLOCK
+            ciera.fp4_quantize_matrices(self.gate, qt=self.w1[:, :f], scales_t=self.w1_s[:, :lines], stream=stream)
+            ciera.fp4_quantize_matrices(self.up, qt=self.w1[:, f:], scales_t=self.w1_s[:, lines:], stream=stream)
+            ciera.fp4_quantize_matrices(self.down, qt=self.w2, scales_t=self.w2_s, stream=stream)
+            return
         f, fb = self.d_ff, self.d_ff // BLOCK
         for x, lo, lob in ((self.gate, 0, 0), (self.up, f, fb)):
             ciera.fp8_quantize_blocks(x, self.w1_t[:, :, lo : lo + f], self.w1_ts[:, :, lob : lob + fb], self.w1[:, lo : lo + f],
@@ -143,6 +173,15 @@ class ExpertLayer:
         slots = self.slot_of_row[:cap]
         ciera.route(self.config, logits, bias, experts, weights)
         ciera.expert_layout(experts, self.n_experts, self.starts, self.counts, rows, slots, self.workspace)
+        if self.weight_bits == 4:
+            lines = cap // BLOCK
+            ciera.fp4_quantize_rows(x, self.x_q[:cap], self.x_s[:lines], slot_of_row=slots, top_k=k, starts=self.starts)
+            ciera.fp4_matmul(self.x_q[:cap], self.x_s[:lines], self.w1, self.w1_s, self.h[:cap], self.starts, status=self.status)
+            ciera.fp4_quantize_rows(self.h[:cap], self.a_q[:cap], self.a_s[:lines], kind=ciera.SOURCE_SWIGLU, slot_of_row=slots,
+                                    top_k=k, starts=self.starts)
+            ciera.fp4_matmul(self.a_q[:cap], self.a_s[:lines], self.w2, self.w2_s, self.o[:cap], self.starts, status=self.status)
+            ciera.expert_combine(self.o[:cap], rows, weights, out)
+            return
         turned = self.training
         ciera.fp8_quantize_rows(x, self.x_q[:cap], self.x_s, self.x_t[:, :cap] if turned else None,
                                 self.x_ts[: cap // BLOCK] if turned else None, slot_of_row=slots, top_k=k, starts=self.starts)
@@ -152,6 +191,21 @@ class ExpertLayer:
                                 starts=self.starts)
         ciera.fp8_matmul(self.a_q[:cap], self.a_s, self.w2, self.w2_s, self.o[:cap], self.starts, status=self.status)
         ciera.expert_combine(self.o[:cap], rows, weights, out)
+
+    def forward_tokens(self, x: torch.Tensor, logits: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                       out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """``forward`` of at most ``few`` tokens by one call that reads each reached expert's weights once; nothing to go back
+        through remains of it, nor of a ``forward`` before it.  The choice is in ``experts`` and ``weights`` as after ``forward``."""
+        t = x.shape[0]
+        if t > self.few or tuple(x.shape) != (t, self.d_model) or x.dtype != self.dtype or logits.shape[0] != t:
+            raise ValueError("x is [tokens, d_model] in the weights' type, with at most `few` tokens")
+        self._batch = None
+        with self._on(stream, x, logits, bias, out):
+            out = torch.empty_like(x) if out is None else out
+            if t:
+                ciera.expert_tokens(self.config, x, logits, bias, self.w1, self.w1_s, self.w2, self.w2_s, out, self.experts[:t],
+                                    self.weights[:t], self.few_workspace)
+        return out
 
     def backward(self, dout: torch.Tensor, stream=None):
         """Gradients of the last ``forward``: ``(dx, dlogits, dgate, dup, ddown)``, the last three in fp32 and the shapes of
