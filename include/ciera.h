@@ -673,8 +673,9 @@ CIERA_API int ciera_fp4_matmul(const ciera_fp4_product* args, void* stream);
  * other than in ciera_fp8_matmul.  An expert's matrices are read once for up to 8 of its tokens (16, with more than 8 tokens in all).
  *   x             device, n_tokens rows of d_model values of dtype;  out  the same
  *   logits, bias, experts, weights   as for ciera_route
- *   workspace     device, 16-byte aligned, ciera_expert_tokens_workspace_bytes(); any contents, not shared by calls that may
- *                 overlap
+ *   workspace     device, 16-byte aligned, ciera_expert_tokens_workspace_bytes() of the largest call: zero-filled once, its first
+ *                 256 bytes are handed back zero by every call (but one that reports an error); not shared by calls that may overlap
+ *   status        device int32 or NULL: CIERA_ERR_TIMEOUT if the blocks' bounded wait for each other ran out
  * Arithmetic: fp32 sums of 16-bit tensor products with exact weights.  x and silu(g) * u go into them with 11 bits (22 for fp32,
  * so bf16 and fp16 values of x are exact) below the power of two of the largest of 128 values; values of silu(g) * u below
  * 2^-111 may lose bits.  Results do not depend on the other tokens of a call but for the order of their sums.
@@ -705,6 +706,7 @@ typedef struct ciera_expert_tokens_args {
     float* weights;
     void* workspace;
     uint64_t workspace_bytes;
+    int32_t* status;
 } ciera_expert_tokens_args;
 CIERA_API size_t ciera_expert_tokens_workspace_bytes(uint32_t n_tokens, uint32_t top_k, uint32_t d_ff);
 CIERA_API int ciera_expert_tokens(const ciera_expert_tokens_args* args, void* stream);

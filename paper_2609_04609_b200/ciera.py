@@ -117,7 +117,7 @@ class _ExpertTokens(ctypes.Structure):
                 ("w1_scales", _vp), ("w1_scales_stride", _u64), ("w1_scales_matrix_stride", _u64), ("w2", _vp),
                 ("w2_stride", _u64), ("w2_matrix_stride", _u64), ("w2_scales", _vp), ("w2_scales_stride", _u64),
                 ("w2_scales_matrix_stride", _u64), ("out", _vp), ("out_stride", _u64), ("experts", _vp), ("weights", _vp),
-                ("workspace", _vp), ("workspace_bytes", _u64)]
+                ("workspace", _vp), ("workspace_bytes", _u64), ("status", _vp)]
 
 
 class GainIn(ctypes.Structure):
@@ -782,13 +782,14 @@ def expert_tokens_workspace_bytes(config: RouteConfig, n_tokens: int, d_model: i
 
 
 def expert_tokens(config: RouteConfig, x, logits, bias, w1, w1_scales, w2, w2_scales, out, experts, weights, workspace,
-                  stream=None) -> None:
+                  status=None, stream=None) -> None:
     """A whole MoE layer for up to ``EXPERT_TOKENS_MAX`` tokens (see ``ciera_expert_tokens_args``): ``x`` and ``out`` [T, d_model],
     ``logits`` [T, E], ``bias`` fp32 [E] or None; ``experts`` int32 and ``weights`` fp32 [T, top_k] receive the choice.
 
     Weights in 8 bits: ``w1`` e4m3 [E, 2 d_ff, d_model] with a scale for each 128 x 128 block, ``w2`` [E, d_model, d_ff].  In 4 bits:
     uint8, half as wide, with scales [E, rows / 128, cols / 128, 512].  ``workspace`` uint8
-    [expert_tokens_workspace_bytes(config, T, d_model, d_ff)]."""
+    [expert_tokens_workspace_bytes(config, T, d_model, d_ff) or more], zeros before the first call; every call leaves it fit for the
+    next."""
     w = "ciera_expert_tokens"
     device = _device_of(w, x)
     code = _code(w, x)
@@ -813,7 +814,8 @@ def expert_tokens(config: RouteConfig, x, logits, bias, w1, w1_scales, w2, w2_sc
     args = _ExpertTokens(config, WEIGHTS_FP4 if four else WEIGHTS_FP8, code, logits_code, t, d, f, *x_at, *logits_at,
                          None if bias is None else _whole(w, device, bias, (e,), _F32), *at,
                          *_matrix(w, device, out, (t, d), x.dtype), _whole(w, device, experts, (t, k), _I32),
-                         _whole(w, device, weights, (t, k), _F32), _whole(w, device, workspace, (room,), _U8), room)
+                         _whole(w, device, weights, (t, k), _F32), _whole(w, device, workspace, (room,), _U8), room,
+                         None if status is None else _whole(w, device, status, (1,), _I32))
     _enqueue(w, device, stream, _lib.ciera_expert_tokens, args)
 
 

@@ -7,12 +7,14 @@
 // are exact in fp16, whose power of two comes after the sum over a block (or group) that shares it.  The tokens' values are made fp16
 // below a power of two of their own for 128 values; fp32 ones in two parts.
 //
-// Two kernels behind the router's:
+// One kernel behind the router's, whose blocks all run at once (a cooperative launch), in two parts with a barrier between them:
 //   up     a block takes tiles of 8 columns of the middle, 8 rows of the gate and 8 of up as the 16 rows of a warp, so that the sums
-//          of both meet in one lane; its warps split the contraction and add up in shared memory.  silu(g) * u goes to the
-//          workspace as fp16 below a power of two for its 8 columns.
+//          of both meet in one lane; its warps split the contraction, and several tiles' sums are added up in shared memory
+//          together.  silu(g) * u goes to the workspace as fp16 below a power of two for its 8 columns.
 //   down   a block takes 16 columns of the output and the warps split what they are summed over, experts and middle alike; a warp
 //          adds each token's part to sums of its own, which are added up at the end in the order of the warps.
+// A warp's copies go on from the one part's units to the other's, so the weights of the second are on their way (for one token nearly
+// all of them) while the blocks wait for each other.
 // Tokens of an expert are taken 8 at a time (16, with more than 8 tokens in all): a group.  Groups come in the order of the experts
 // and of their slots, so a result does not depend on how warps run.
 #include <type_traits>
@@ -24,9 +26,12 @@
 namespace ciera {
 
 constexpr int kTokenThreads = 512, kTokenWarps = kTokenThreads / 32;
-constexpr int kTokenRing = 4;          // units of 16 rows x 128 columns that a warp has on their way
+template <int BITS>
+constexpr int kTokenRing = BITS == 8 ? 4 : 6;  // units of 16 rows x 128 columns that a warp has on their way, and the one it works on
+constexpr uint32_t kTokenHead = 256;   // bytes of the workspace's counters
 constexpr uint32_t kMaxSlots = CIERA_EXPERT_TOKENS_MAX * 32;
 constexpr int kColumnPitch = 20;       // floats between columns of 16 sums: a warp's are in different banks
+constexpr int kTokenPitch = 17;        // the same between tokens, which come in any order
 constexpr uint32_t kLeastExponent = 16;  // of a power of two that values are taken below
 
 struct Matrices {
@@ -35,28 +40,30 @@ struct Matrices {
     uint64_t stride, matrix_stride, scales_stride, scales_matrix_stride;
 };
 struct TokensArgs {
-    Matrices w;  // of the kernel's product
+    Matrices w1, w2;
     const int32_t* experts;
     const float* weights;
     uint64_t x_stride, out_stride;
-    uint8_t* hidden;     // [slots][parts][d_ff] fp16
-    uint8_t* exponents;  // [slots][d_ff / 8]
+    uint32_t* counters;  // blocks at the barrier, blocks that have left it: zero before and after
+    int32_t* status;
+    uint8_t* hidden;     // [places][parts][d_ff] fp16
+    uint8_t* exponents;  // [places][d_ff / 8]
     uint32_t n_tokens, top_k, n_experts, d_model, d_ff;
     uint32_t splits, tiles;  // up: warps that share a tile, tiles of a block at a time
     int32_t x_wide;          // x may be read 16 bytes at a time
 };
 
-// The slots of the reached experts, and groups of up to `columns` of an expert's.
+// The slots of the reached experts in the order of the experts, each at a place, and groups of up to `columns` of an expert's.
 struct TokenLists {
-    uint32_t group[kMaxSlots];  // expert << 16 | slots - 1 << 11 | first place in `slot`
-    uint16_t slot[kMaxSlots];
+    uint32_t group[kMaxSlots];  // expert << 16 | slots - 1 << 11 | first place
+    float weight[kMaxSlots];
+    uint8_t token[kMaxSlots];
     uint32_t warp_total[kTokenWarps];
     uint32_t groups;
 };
 struct ListScratch {
     uint32_t at[1024];  // slots of an expert; then their first place
-    int16_t expert[kMaxSlots];
-    uint16_t rank[kMaxSlots];
+    uint8_t count[kMaxSlots / 32 * 1024];  // [32 slots][expert]; n_experts apart
 };
 __device__ __forceinline__ uint32_t group_expert(uint32_t g) { return g >> 16; }
 __device__ __forceinline__ uint32_t group_slots(uint32_t g) { return (g >> 11 & 31u) + 1; }
@@ -64,28 +71,58 @@ __device__ __forceinline__ uint32_t group_first(uint32_t g) { return g & 2047u; 
 
 // By the whole block; ends with a barrier.
 __device__ __forceinline__ void make_lists(TokenLists& l, ListScratch& s, const TokensArgs& a, uint32_t columns) {
-    const uint32_t n = a.n_tokens * a.top_k, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    for (uint32_t i = tid; i < n; i += kTokenThreads) {
-        const int32_t e = __ldcg(a.experts + i);
-        s.expert[i] = (int16_t)((uint32_t)e < a.n_experts ? e : -1);
-    }
-    for (uint32_t e = tid; e < 1024; e += kTokenThreads) s.at[e] = 0;
-    __syncthreads();
-    if (warp == 0)  // a slot's place among its expert's
-        for (uint32_t i0 = 0; i0 < n; i0 += 32) {
-            const int e = i0 + lane < n ? s.expert[i0 + lane] : -1;
-            const uint32_t same = __match_any_sync(~0u, e);
-            const uint32_t before = e < 0 ? 0 : s.at[e];
-            __syncwarp();
-            if (e >= 0) {
-                s.rank[i0 + lane] = (uint16_t)(before + __popc(same & ((1u << lane) - 1)));
-                if (__ffs(same) - 1 == (int)lane) s.at[e] = before + __popc(same);
+    const uint32_t n = a.n_tokens * a.top_k, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, E = a.n_experts;
+    if (n <= 32) {  // by one warp, a slot a lane
+        if (warp == 0) {
+            const int32_t id = lane < n ? __ldcg(a.experts + lane) : -1;
+            const float w = lane < n ? __ldcg(a.weights + lane) : 0.f;
+            const uint32_t e = (uint32_t)id < E ? (uint32_t)id : 0xffffu;
+            uint32_t place = 0, rank = 0, count = 0, groups = 0;  // places before, before of the same expert, the expert's, groups before
+            for (uint32_t i = 0; i < n; ++i) {
+                const uint32_t o = __shfl_sync(~0u, e, i);
+                place += o < e || (o == e && i < lane);
+                rank += o == e && i < lane;
+                count += o == e;
             }
-            __syncwarp();
+            const bool first = rank % columns == 0 && e != 0xffffu;  // the lane makes a group
+            for (uint32_t i = 0; i < n; ++i) groups += __shfl_sync(~0u, first ? place : ~0u, i) < place;
+            if (e != 0xffffu) l.token[place] = (uint8_t)(lane / a.top_k), l.weight[place] = w;
+            if (first) l.group[groups] = e << 16 | (min(columns, count - rank) - 1) << 11 | place;
+            const uint32_t all = __popc(__ballot_sync(~0u, first));
+            if (lane == 0) l.groups = all;
         }
+        __syncthreads();
+        return;
+    }
+    // slots of an expert are counted for each 32 neighbours, then over those before
+    const uint32_t chunks = (n + 31) / 32;
+    for (uint32_t i = tid; i < (chunks * E + 15) / 16; i += kTokenThreads) reinterpret_cast<uint4*>(s.count)[i] = make_uint4(0, 0, 0, 0);
+    int32_t id[kMaxSlots / kTokenThreads];
+#pragma unroll
+    for (int j = 0; j < (int)(kMaxSlots / kTokenThreads); ++j) {
+        const uint32_t i = j * kTokenThreads + tid;
+        id[j] = i < n ? __ldcg(a.experts + i) : -1;
+        if ((uint32_t)id[j] >= E) id[j] = -1;
+    }
+    __syncthreads();
+    uint32_t rank[kMaxSlots / kTokenThreads];
+#pragma unroll
+    for (int j = 0; j < (int)(kMaxSlots / kTokenThreads); ++j) {
+        const uint32_t chunk = j * kTokenWarps + warp;
+        if (chunk >= chunks) break;
+        const uint32_t same = __match_any_sync(~0u, id[j]);
+        rank[j] = __popc(same & ((1u << lane) - 1));
+        if (id[j] >= 0 && rank[j] == 0) s.count[chunk * E + id[j]] = (uint8_t)__popc(same);
+    }
     __syncthreads();
     // places and groups before each expert, two experts a thread: slots in the low half, groups in the high one
-    const uint32_t c0 = s.at[2 * tid], c1 = s.at[2 * tid + 1];
+    uint32_t c0 = 0, c1 = 0;
+    if (2 * tid < E) {
+        for (uint32_t i = 0; i < chunks; ++i) {
+            c0 += s.count[i * E + 2 * tid];
+            if (2 * tid + 1 < E) c1 += s.count[i * E + 2 * tid + 1];
+        }
+    }
     const uint32_t v0 = c0 | (c0 + columns - 1) / columns << 16, v1 = c1 | (c1 + columns - 1) / columns << 16;
     uint32_t sum = v0 + v1;
 #pragma unroll
@@ -107,8 +144,17 @@ __device__ __forceinline__ void make_lists(TokenLists& l, ListScratch& s, const 
         s.at[e] = at;
     }
     __syncthreads();
-    for (uint32_t i = tid; i < n; i += kTokenThreads)
-        if (s.expert[i] >= 0) l.slot[s.at[s.expert[i]] + s.rank[i]] = (uint16_t)i;
+#pragma unroll
+    for (int j = 0; j < (int)(kMaxSlots / kTokenThreads); ++j) {
+        const uint32_t chunk = j * kTokenWarps + warp;
+        if (chunk >= chunks) break;
+        if (id[j] < 0) continue;
+        uint32_t place = s.at[id[j]] + rank[j];
+        for (uint32_t i = 0; i < chunk; ++i) place += s.count[i * E + id[j]];
+        const uint32_t slot = j * kTokenThreads + tid;
+        l.token[place] = (uint8_t)(slot / a.top_k);
+        l.weight[place] = __ldcg(a.weights + slot);
+    }
     __syncthreads();
 }
 
@@ -147,27 +193,44 @@ __device__ __forceinline__ uint32_t fragment_column(int i, uint32_t t) {  // of 
     return BITS == 8 ? (i >> 4) * 64 + t * 16 + (i & 15) : (i >> 3) * 32 + t * 8 + (i & 7);
 }
 
-// rows lo + g and hi + g of matrix e, columns from 128 * kb on
+// Where a lane's part of a unit comes from: rows lo + g and hi + g of matrix e (lo and hi - lo are multiples of 8), columns from
+// 128 * kb on.
 template <int BITS>
-__device__ __forceinline__ void copy_unit(Unit<BITS>& u, const Matrices& m, uint32_t e, uint32_t lo, uint32_t hi, uint32_t kb, int lane) {
-    const uint32_t g = lane >> 2, t = lane & 3;
-    const uint8_t* q = m.q + e * m.matrix_stride + (uint64_t)kb * (16 * BITS) + t * 16;
-    const uint8_t* a = q + (uint64_t)(lo + g) * m.stride;
-    const uint8_t* b = q + (uint64_t)(hi + g) * m.stride;
-    if constexpr (BITS == 8) {
-        cp_async16(&u.w[0][lane], a);
-        cp_async16(&u.w[1][lane], a + 64);
-        cp_async16(&u.w[2][lane], b);
-        cp_async16(&u.w[3][lane], b + 64);
-    } else {
-        cp_async16(&u.w[0][lane], a);
-        cp_async16(&u.w[1][lane], b);
-        const uint8_t* s = m.scales + e * m.scales_matrix_stride + (uint64_t)kb * kAtomBytes;
-        const uint32_t ra = lo + g, rb = hi + g;
-        cp_async4(&u.s[0][lane], s + (uint64_t)(ra >> 7) * m.scales_stride + atom_word(ra));
-        cp_async4(&u.s[1][lane], s + (uint64_t)(rb >> 7) * m.scales_stride + atom_word(rb));
+struct UnitSource {
+    const uint8_t* a;
+    const uint8_t* b;
+    const uint8_t* sa;  // 4 bits: the scale words of rows g and hi - lo + g ...
+    const uint8_t* sb;
+    uint32_t lo;        // ... from which row lo's are this far
+
+    __device__ __forceinline__ void point(const Matrices& m, uint32_t e, uint32_t row, uint32_t apart, uint32_t kb, int lane) {
+        const uint32_t g = lane >> 2, t = lane & 3;
+        a = m.q + e * m.matrix_stride + (uint64_t)(row + g) * m.stride + kb * (16 * BITS) + t * 16;
+        b = a + (uint64_t)apart * m.stride;
+        if constexpr (BITS == 4) {
+            lo = row;
+            sa = m.scales + e * m.scales_matrix_stride + (uint64_t)kb * kAtomBytes + g * 16;
+            sb = apart == 8 ? sa + 128 : sa + (uint64_t)(apart >> 7) * m.scales_stride;  // (8: the same block of 32 rows)
+        }
     }
-}
+    __device__ __forceinline__ void copy(uint32_t to, const Matrices& m, int lane) const {
+        to += lane * 16;
+        const auto copy16 = [](uint32_t dst, const uint8_t* p) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(p) : "memory");
+        };
+        copy16(to, a);
+        if constexpr (BITS == 8) {
+            copy16(to + 512, a + 64);
+            copy16(to + 1024, b);
+            copy16(to + 1536, b + 64);
+        } else {
+            copy16(to + 512, b);
+            const uint64_t off = (uint64_t)(lo >> 7) * m.scales_stride + atom_word(lo);
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 1024 - lane * 12), "l"(sa + off) : "memory");
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 1152 - lane * 12), "l"(sb + off) : "memory");
+        }
+    }
+};
 // 8 bits: the scale of a row's block
 __device__ __forceinline__ float block_scale(const Matrices& m, uint32_t e, uint32_t row, uint32_t kb) {
     return scale_value(__ldg(m.scales + e * m.scales_matrix_stride + (uint64_t)(row >> 7) * m.scales_stride + kb));
@@ -189,18 +252,32 @@ __device__ __forceinline__ void turn_words(uint32_t (&w)[4], uint32_t t) {
     }
 }
 
+__device__ __forceinline__ uint4 read16(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t read4(uint32_t at) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+
 // sums[nt] = the unit's rows times the columns of x, scales of the rows included: rows g, g + 8 of columns 2 t, 2 t + 1
 template <int BITS, int NT, int P>
-__device__ __forceinline__ void multiply_unit(const Unit<BITS>& u, const uint32_t (&x)[NT][P][16], float s_lo, float s_hi, float (&sums)[NT][4], int lane) {
+__device__ __forceinline__ void multiply_unit(uint32_t unit, const uint32_t (&x)[NT][P][16], float s_lo, float s_hi, float (&sums)[NT][4], int lane) {
+    unit += lane * 16;
     if constexpr (BITS == 8) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) sums[nt][i] = 0.f;
+        uint4 w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = read16(unit + 512 * i);
 #pragma unroll
         for (int piece = 0; piece < 2; ++piece) {
-            const uint4 lo = u.w[piece][lane], hi = u.w[2 + piece][lane];
-            const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, h[4] = {hi.x, hi.y, hi.z, hi.w};
+            const uint32_t l[4] = {w[piece].x, w[piece].y, w[piece].z, w[piece].w}, h[4] = {w[2 + piece].x, w[2 + piece].y, w[2 + piece].z, w[2 + piece].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 uint32_t a0, a1, a2, a3;
@@ -216,11 +293,11 @@ __device__ __forceinline__ void multiply_unit(const Unit<BITS>& u, const uint32_
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) sums[nt][0] *= s_lo, sums[nt][1] *= s_lo, sums[nt][2] *= s_hi, sums[nt][3] *= s_hi;
     } else {
-        const uint4 lo = u.w[0][lane], hi = u.w[1][lane];
+        const uint4 lo = read16(unit), hi = read16(unit + 512);
+        const uint32_t sl = read4(unit + 1024 - lane * 12), sh = read4(unit + 1152 - lane * 12);
         uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, h[4] = {hi.x, hi.y, hi.z, hi.w};
         turn_words(l, lane & 3);
         turn_words(h, lane & 3);
-        const uint32_t sl = u.s[0][lane], sh = u.s[1][lane];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             uint32_t a[4], c[4];
@@ -293,155 +370,14 @@ __device__ __forceinline__ float load_tokens(const value_t<DT>* __restrict__ row
     return from_half_range(e);
 }
 
-template <int BITS, int NT>
-struct UpSmem {
-    Unit<BITS> ring[kTokenWarps][kTokenRing];
-    float sums[2][kTokenWarps][NT * 8 * kColumnPitch];
-    TokenLists lists;
-};
-
-template <int DT, int BITS, int NT>
-__global__ void __launch_bounds__(kTokenThreads, 1) tokens_up_kernel(const TokensArgs a, const value_t<DT>* __restrict__ x_) {
-    constexpr int P = DT == CIERA_FP32 ? 2 : 1;
-    extern __shared__ __align__(16) uint8_t tokens_smem[];
-    UpSmem<BITS, NT>& sm = *reinterpret_cast<UpSmem<BITS, NT>*>(tokens_smem);
-    static_assert(sizeof(ListScratch) <= sizeof(sm.ring), "the lists are made where the ring will be");
-    pdl_wait();
-    make_lists(sm.lists, *reinterpret_cast<ListScratch*>(&sm.ring), a, NT * 8);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t g = lane >> 2, t = lane & 3;
-    const uint32_t kb_all = a.d_model / 128, across = a.d_ff / 8;
-    const uint64_t all = (uint64_t)sm.lists.groups * across;
-    const uint32_t from = (uint32_t)(all * blockIdx.x / gridDim.x), to = (uint32_t)(all * (blockIdx.x + 1) / gridDim.x);
-    const uint32_t mine = warp / a.splits, split = warp % a.splits;  // the warp's tile of those at a time, its part of the contraction
-    const bool busy = mine < a.tiles;
-    const uint32_t rounds = (to - from + a.tiles - 1) / a.tiles, each = (kb_all + a.splits - 1) / a.splits;
-    Unit<BITS>* ring = sm.ring[warp];
-
-    // the next unit to be copied
-    uint32_t c_task = from + mine, c_group = c_task / across, c_tile = c_task % across, c_kb = split, c_at = 0;
-    const auto copy = [&]() {
-        if (busy && c_task < to) {
-            if (c_kb < kb_all) {
-                const uint32_t row = c_tile * 8;
-                copy_unit<BITS>(ring[c_at], a.w, group_expert(sm.lists.group[c_group]), row, a.d_ff + row, c_kb, lane);
-            }
-            c_kb += a.splits;
-            if (c_kb >= each * a.splits) {
-                c_kb = split;
-                c_task += a.tiles;
-                c_tile += a.tiles;
-                if (c_tile >= across) c_tile -= across, ++c_group;
-            }
-        }
-        if (++c_at == kTokenRing) c_at = 0;
-        cp_async_commit();
-    };
-#pragma unroll
-    for (int i = 0; i < kTokenRing - 1; ++i) copy();
-    uint32_t at = 0, task = from + mine, group = task / across, tile = task % across, loaded_group = ~0u, loaded_kb = ~0u;
-    uint32_t xf[NT][P][16];
-    float scale[NT][2];
-    for (uint32_t r = 0; r < rounds; ++r) {
-        float acc[NT][4];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[nt][i] = 0.f;
-        const bool work = busy && task < to;
-        const uint32_t packed = work ? sm.lists.group[group] : 0u, slots = work ? group_slots(packed) : 0u;
-        for (uint32_t i = 0; i < each; ++i) {
-            const uint32_t kb = split + i * a.splits;
-            float s_lo = 1.f, s_hi = 1.f;
-            if (work && kb < kb_all) {
-                if (BITS == 8) {
-                    s_lo = block_scale(a.w, group_expert(packed), tile * 8, kb);
-                    s_hi = block_scale(a.w, group_expert(packed), a.d_ff + tile * 8, kb);
-                }
-                if (group != loaded_group || kb != loaded_kb) {
-                    loaded_group = group, loaded_kb = kb;
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const uint32_t c = nt * 8 + g;
-                        const uint32_t token = c < slots ? sm.lists.slot[group_first(packed) + c] / a.top_k : 0u;
-                        const float f = load_tokens<DT, BITS, P>(x_ + token * a.x_stride + kb * 128, c < slots, a.x_wide, xf[nt], t);
-                        scale[nt][0] = __shfl_sync(~0u, f, 8 * t);
-                        scale[nt][1] = __shfl_sync(~0u, f, 8 * t + 4);
-                    }
-                }
-            }
-            cp_async_wait<kTokenRing - 2>();
-            if (work && kb < kb_all) {
-                float sums[NT][4];
-                multiply_unit<BITS, NT, P>(ring[at], xf, s_lo, s_hi, sums, lane);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[nt][j] = fmaf(sums[nt][j], scale[nt][j & 1], acc[nt][j]);
-            }
-            if (++at == kTokenRing) at = 0;
-            copy();
-        }
-        if (work) {
-            float* put = sm.sums[r & 1][warp] + 2 * t * kColumnPitch + g;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                if (nt * 8 >= (int)slots) break;
-                float* p = put + nt * 8 * kColumnPitch;
-                p[0] = acc[nt][0];
-                p[kColumnPitch] = acc[nt][1];
-                p[8] = acc[nt][2];
-                p[kColumnPitch + 8] = acc[nt][3];
-            }
-        }
-        __syncthreads();
-        // a warp adds up a column of 8 gates and 8 ups, four lanes a sum
-        for (uint32_t c = warp; c < a.tiles * NT * 8; c += kTokenWarps) {
-            const uint32_t which = c / (NT * 8), column = c % (NT * 8), of = from + r * a.tiles + which;
-            if (of >= to) break;
-            const uint32_t p = sm.lists.group[of / across], f0 = of % across * 8;
-            if (column >= group_slots(p)) continue;
-            float gate = 0.f, up = 0.f;
-            for (uint32_t s = lane >> 3; s < a.splits; s += 4) {
-                const float* part = sm.sums[r & 1][which * a.splits + s] + column * kColumnPitch + (lane & 7);
-                gate += part[0];
-                up += part[8];
-            }
-#pragma unroll
-            for (int d = 8; d < 32; d <<= 1) {
-                gate += __shfl_xor_sync(~0u, gate, d);
-                up += __shfl_xor_sync(~0u, up, d);
-            }
-            float v = swiglu32(gate, up);
-            if (gate < kLowestGate) v = (float)((double)gate / (1.0 + exp(-(double)gate)) * (double)up);
-            uint32_t most = __float_as_uint(v) & 0x7fffffffu;
-#pragma unroll
-            for (int d = 1; d < 8; d <<= 1) most = max(most, __shfl_xor_sync(~0u, most, d));
-            const uint32_t e = exponent_of(most), slot = sm.lists.slot[group_first(p) + column];
-            if (lane < 8) {
-                v *= to_half_range(e);
-                __half* h = reinterpret_cast<__half*>(a.hidden) + (uint64_t)slot * P * a.d_ff + f0 + lane;
-                const __half hi = __float2half_rn(v);
-                h[0] = hi;
-                if (P == 2) h[a.d_ff] = __float2half_rn(rest_of(v, hi));
-                if (lane == 0) a.exponents[(uint64_t)slot * across + f0 / 8] = (uint8_t)e;
-            }
-        }
-        task += a.tiles;
-        tile += a.tiles;
-        if (tile >= across) tile -= across, ++group;
-    }
-    cp_async_wait_all();
-}
-
-// The middle's values of a slot, 128 of them, in a lane's order; scaled to the power of two of the largest.
+// The middle's values at a place, 128 of them, in a lane's order; scaled to the power of two of the largest.
 template <int P>
 struct HiddenPiece {
     uint4 v[P][4];
     uint4 e;
 };
 template <int BITS, int P>
-__device__ __forceinline__ void read_hidden(HiddenPiece<P>& h, const TokensArgs& a, uint32_t slot, uint32_t kb, bool there, uint32_t t) {
+__device__ __forceinline__ void read_hidden(HiddenPiece<P>& h, const TokensArgs& a, uint32_t place, uint32_t kb, bool there, uint32_t t) {
     if (!there) {
         h.e = make_uint4(0, 0, 0, 0);
 #pragma unroll
@@ -450,10 +386,10 @@ __device__ __forceinline__ void read_hidden(HiddenPiece<P>& h, const TokensArgs&
             for (int i = 0; i < 4; ++i) h.v[p][i] = make_uint4(0, 0, 0, 0);
         return;
     }
-    h.e = __ldcg(reinterpret_cast<const uint4*>(a.exponents + (uint64_t)slot * (a.d_ff / 8) + kb * 16));
+    h.e = __ldcg(reinterpret_cast<const uint4*>(a.exponents + (uint64_t)place * (a.d_ff / 8) + kb * 16));
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        const __half* from = reinterpret_cast<const __half*>(a.hidden) + ((uint64_t)slot * P + p) * a.d_ff + kb * 128;
+        const __half* from = reinterpret_cast<const __half*>(a.hidden) + ((uint64_t)place * P + p) * a.d_ff + kb * 128;
 #pragma unroll
         for (int i = 0; i < 4; ++i) h.v[p][i] = __ldcg(reinterpret_cast<const uint4*>(from + fragment_column<BITS>(8 * i, t)));
     }
@@ -490,84 +426,285 @@ __device__ __forceinline__ float settle_hidden(const HiddenPiece<P>& h, uint32_t
 }
 
 template <int BITS>
-struct DownSmem {
-    Unit<BITS> ring[kTokenWarps][kTokenRing];
+struct TokensSmem {
+    Unit<BITS> ring[kTokenWarps][kTokenRing<BITS>];
     TokenLists lists;
-    float sums[];  // [warps][tokens][kColumnPitch]
+    int stop;
+    // up: [rounds of a batch][warp][column][kColumnPitch]; down: [warp][token][kTokenPitch]
+    __align__(16) float sums[];
 };
+// rounds of tiles whose sums are added up together, and what they need
+template <int NT>
+constexpr uint32_t kBatch = NT == 1 ? 8 : 4;
+template <int NT>
+constexpr uint32_t kBatchFloats = kBatch<NT> * kTokenWarps * NT * 8 * kColumnPitch;
+
+// All blocks have come here, and what they wrote before can be read (past the first-level cache).  false: the wait ran out.
+__device__ __forceinline__ bool all_blocks(const TokensArgs& a, int& stop) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t seen, polls = 0;
+        __threadfence();
+        atomicAdd(a.counters, 1u);
+        do {
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(a.counters) : "memory");
+        } while (seen < gridDim.x && ++polls < kMaxPolls);
+        stop = seen < gridDim.x;
+        if (stop && a.status) atomicCAS(a.status, 0, (int32_t)CIERA_ERR_TIMEOUT);
+        // the last one to leave sets both counters back
+        if (!stop && atomicAdd(a.counters + 1, 1u) == gridDim.x - 1) {
+            a.counters[0] = 0;
+            a.counters[1] = 0;
+        }
+    }
+    __syncthreads();
+    return !stop;
+}
 
 template <int DT, int BITS, int NT>
-__global__ void __launch_bounds__(kTokenThreads, 1) tokens_down_kernel(const TokensArgs a, value_t<DT>* __restrict__ out) {
-    constexpr int P = DT == CIERA_FP32 ? 2 : 1;
+__global__ void __launch_bounds__(kTokenThreads, 1) tokens_kernel(const TokensArgs a, const value_t<DT>* __restrict__ x_, value_t<DT>* __restrict__ out) {
+    constexpr int P = DT == CIERA_FP32 ? 2 : 1, R = kTokenRing<BITS>;
     extern __shared__ __align__(16) uint8_t tokens_smem[];
-    DownSmem<BITS>& sm = *reinterpret_cast<DownSmem<BITS>*>(tokens_smem);
+    TokensSmem<BITS>& sm = *reinterpret_cast<TokensSmem<BITS>*>(tokens_smem);
     static_assert(sizeof(ListScratch) <= sizeof(sm.ring), "the lists are made where the ring will be");
     pdl_wait();
     make_lists(sm.lists, *reinterpret_cast<ListScratch*>(&sm.ring), a, NT * 8);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t g = lane >> 2, t = lane & 3;
-    const uint32_t kb_all = a.d_ff / 128, units = sm.lists.groups * kb_all, row = blockIdx.x * 16;
-    float* sums = sm.sums + (uint64_t)warp * a.n_tokens * kColumnPitch;
-    for (uint32_t i = lane; i < a.n_tokens * kColumnPitch; i += 32) sums[i] = 0.f;
-    Unit<BITS>* ring = sm.ring[warp];
-    uint32_t c_unit = warp, c_at = 0;
-    const auto copy = [&]() {
-        if (c_unit < units) copy_unit<BITS>(ring[c_at], a.w, group_expert(sm.lists.group[c_unit / kb_all]), row, row + 8, c_unit % kb_all, lane);
-        c_unit += kTokenWarps;
-        if (++c_at == kTokenRing) c_at = 0;
-        cp_async_commit();
+    // the warp's ring: the next unit to be copied and to be worked on
+    const uint32_t ring = smem_u32(sm.ring[warp]), ring_end = ring + sizeof(sm.ring[warp]);
+    uint32_t c_at = ring, at = ring;
+    const auto advance = [&](uint32_t& p) {
+        p += sizeof(Unit<BITS>);
+        if (p == ring_end) p = ring;
     };
-#pragma unroll
-    for (int i = 0; i < kTokenRing - 1; ++i) copy();
-    HiddenPiece<P> piece[NT];
-    const auto read = [&](uint32_t unit) {
-        const uint32_t packed = sm.lists.group[unit / kb_all], slots = group_slots(packed);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const uint32_t c = nt * 8 + g;
-            read_hidden<BITS, P>(piece[nt], a, c < slots ? sm.lists.slot[group_first(packed) + c] : 0u, unit % kb_all, c < slots, t);
+
+    // up: tiles of 8 columns of the middle, in the order of the groups; a block has neighbouring ones, `tiles` at a time
+    const uint32_t kb_up = a.d_model / 128, across = a.d_ff / 8;
+    const uint64_t all = (uint64_t)sm.lists.groups * across;
+    const uint32_t from = (uint32_t)(all * blockIdx.x / gridDim.x), to = (uint32_t)(all * (blockIdx.x + 1) / gridDim.x);
+    const uint32_t mine = warp / a.splits, split = warp - mine * a.splits;  // the warp's tile of those, its part of the contraction
+    const uint32_t rounds = (to - from + a.tiles - 1) / a.tiles;
+    const uint32_t own = mine < a.tiles ? to : 0;  // the warp's tiles end here
+    const uint32_t first_group = from / across, first_tile = from - first_group * across;
+    // down: 16 columns of the output, everything that they are summed over
+    const uint32_t kb_down = a.d_ff / 128, units = sm.lists.groups * kb_down;
+    const uint32_t w_group = warp / kb_down, w_kb = warp - w_group * kb_down;
+
+    // Copies go in runs, in which the source moves on by the same step: the warp's tiles of one group, or, where a warp has more than
+    // one part of a tile's contraction, those; then single units of the second matrices.
+    UnitSource<BITS> src;
+    const bool by_tile = kb_up <= a.splits;
+    uint32_t c_task = from + mine, c_group = first_group, c_tile = first_tile + mine, c_left = 0;
+    uint32_t d_row = blockIdx.x * 16, d_unit = warp, d_group = w_group, d_kb = w_kb;
+    bool up = true;
+    const uint64_t a_step = by_tile ? (uint64_t)a.tiles * 8 * a.w1.stride : a.splits * (16 * BITS);
+    const auto next_run = [&]() {
+        if (up && c_task < own) {
+            while (c_tile >= across) c_tile -= across, ++c_group;
+            src.point(a.w1, group_expert(sm.lists.group[c_group]), c_tile * 8, a.d_ff, split, lane);
+            if (by_tile) {
+                c_left = (min(across - c_tile, own - c_task) + a.tiles - 1) / a.tiles;
+                c_task += c_left * a.tiles;
+                c_tile += c_left * a.tiles;
+            } else {
+                c_left = (kb_up - split + a.splits - 1) / a.splits;
+                c_task += a.tiles;
+                c_tile += a.tiles;
+            }
+            return;
+        }
+        up = false;
+        if (d_unit >= units) {
+            d_unit = warp, d_group = w_group, d_kb = w_kb;
+            d_row += gridDim.x * 16;
+        }
+        if (d_row < a.d_model && d_unit < units) {
+            src.point(a.w2, group_expert(sm.lists.group[d_group]), d_row, 8, d_kb, lane);
+            c_left = 1;
+            d_unit += kTokenWarps;
+            d_kb += kTokenWarps;
+            while (d_kb >= kb_down) d_kb -= kb_down, ++d_group;
         }
     };
-    if ((uint32_t)warp < units) read(warp);
-    __syncwarp();
-    uint32_t at = 0;
-    for (uint32_t unit = warp; unit < units; unit += kTokenWarps) {
-        const uint32_t packed = sm.lists.group[unit / kb_all], slots = group_slots(packed);
-        const float s = BITS == 8 ? block_scale(a.w, group_expert(packed), row, unit % kb_all) : 1.f;
-        uint32_t xf[NT][P][16];
-        float f[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) f[nt] = settle_hidden<BITS, P>(piece[nt], xf[nt], t);
-        if (unit + kTokenWarps < units) read(unit + kTokenWarps);
-        cp_async_wait<kTokenRing - 2>();
-        float part[NT][4];
-        multiply_unit<BITS, NT, P>(ring[at], xf, s, s, part, lane);
-        if (++at == kTokenRing) at = 0;
-        copy();
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t c = nt * 8 + 2 * t + i;
-                const float fc = __shfl_sync(~0u, f[nt], 8 * t + 4 * i);
-                if (c >= slots) continue;
-                const uint32_t slot = sm.lists.slot[group_first(packed) + c];
-                const float w = __ldg(a.weights + slot);
-                float* to = sums + slot / a.top_k * kColumnPitch + g;
-                to[0] = fmaf(part[nt][i] * fc, w, to[0]);
-                to[8] = fmaf(part[nt][2 + i] * fc, w, to[8]);
+    next_run();
+    const auto copy = [&]() {
+        if (c_left) {
+            src.copy(c_at, up ? a.w1 : a.w2, lane);
+            src.a += a_step;
+            src.b += a_step;
+            if (BITS == 4) {
+                if (by_tile) src.lo += a.tiles * 8;
+                else src.sa += a.splits * kAtomBytes, src.sb += a.splits * kAtomBytes;
             }
+            if (--c_left == 0) next_run();
+        }
+        advance(c_at);
+        cp_async_commit();
+    };
+#pragma unroll 1
+    for (int i = 0; i < R - 1; ++i) copy();
+
+    {
+        uint32_t task = from + mine, group = first_group, tile = first_tile + mine, loaded_group = ~0u, loaded_kb = ~0u, scaled = ~0u;
+        uint32_t packed = 0, slots = 0;
+        uint32_t xf[NT][P][16];
+        float scale[NT][2], s_lo = 1.f, s_hi = 1.f;
+        uint32_t b_group = first_group, b_tile = first_tile;  // of the batch
+        for (uint32_t r0 = 0; r0 < rounds; r0 += kBatch<NT>) {
+            const uint32_t batch = min(kBatch<NT>, rounds - r0);
+            float* put = sm.sums + (warp * NT * 8 + 2 * t) * kColumnPitch + g;
+            for (uint32_t r = 0; r < batch && task < own; ++r) {
+                while (tile >= across) tile -= across, ++group;
+                float acc[NT][4];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[nt][i] = 0.f;
+                for (uint32_t kb = split; kb < kb_up; kb += a.splits) {
+                    const bool other = group != loaded_group || kb != loaded_kb;
+                    if (other) {
+                        loaded_group = group, loaded_kb = kb;
+                        packed = sm.lists.group[group];
+                        slots = group_slots(packed);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const uint32_t c = nt * 8 + g;
+                            const uint32_t token = c < slots ? sm.lists.token[group_first(packed) + c] : 0u;
+                            const float f = load_tokens<DT, BITS, P>(x_ + token * a.x_stride + kb * 128, c < slots, a.x_wide, xf[nt], t);
+                            scale[nt][0] = __shfl_sync(~0u, f, 8 * t);
+                            scale[nt][1] = __shfl_sync(~0u, f, 8 * t + 4);
+                        }
+                    }
+                    if (BITS == 8 && (other || tile >> 4 != scaled)) {
+                        scaled = tile >> 4;
+                        s_lo = block_scale(a.w1, group_expert(packed), tile * 8, kb);
+                        s_hi = block_scale(a.w1, group_expert(packed), a.d_ff + tile * 8, kb);
+                    }
+                    cp_async_wait<R - 2>();
+                    float sums[NT][4];
+                    multiply_unit<BITS, NT, P>(at, xf, s_lo, s_hi, sums, lane);
+                    advance(at);
+                    copy();
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[nt][j] = fmaf(sums[nt][j], scale[nt][j & 1], acc[nt][j]);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float* p = put + nt * 8 * kColumnPitch;
+                    if (nt * 8 + 2 * t < slots) p[0] = acc[nt][0], p[8] = acc[nt][2];
+                    if (nt * 8 + 2 * t + 1 < slots) p[kColumnPitch] = acc[nt][1], p[kColumnPitch + 8] = acc[nt][3];
+                }
+                put += kTokenWarps * NT * 8 * kColumnPitch;
+                task += a.tiles;
+                tile += a.tiles;
+            }
+            __syncthreads();
+            // A warp adds up a column of 8 gates and 8 ups, four lanes a sum: column warp % (8 NT) of every (2 / NT)th tile.
+            const uint32_t column = warp % (NT * 8), of_batch = min(batch * a.tiles, to - from - r0 * a.tiles);
+            uint32_t c_in = b_tile + warp / (NT * 8), c_of = b_group;
+            for (uint32_t which = warp / (NT * 8), r = 0, first = 0; which < of_batch; which += 2 / NT, c_in += 2 / NT) {
+                while (c_in >= across) c_in -= across, ++c_of;
+                const uint32_t p = sm.lists.group[c_of];
+                if (column >= group_slots(p)) continue;
+                if (a.tiles == 1) r = which;
+                else r = which / a.tiles, first = (which - r * a.tiles) * a.splits;
+                const float* part = sm.sums + ((r * kTokenWarps + first + (lane >> 3)) * NT * 8 + column) * kColumnPitch + (lane & 7);
+                float gate = 0.f, up_ = 0.f;
+#pragma unroll
+                for (int s = 0; s < kTokenWarps; s += 4)
+                    if (s + (lane >> 3) < a.splits) {
+                        gate += part[s * NT * 8 * kColumnPitch];
+                        up_ += part[s * NT * 8 * kColumnPitch + 8];
+                    }
+#pragma unroll
+                for (int d = 8; d < 32; d <<= 1) {
+                    gate += __shfl_xor_sync(~0u, gate, d);
+                    up_ += __shfl_xor_sync(~0u, up_, d);
+                }
+                float v = swiglu32(gate, up_);
+                if (gate < kLowestGate) v = (float)((double)gate / (1.0 + exp(-(double)gate)) * (double)up_);
+                uint32_t most = __float_as_uint(v) & 0x7fffffffu;
+#pragma unroll
+                for (int d = 1; d < 8; d <<= 1) most = max(most, __shfl_xor_sync(~0u, most, d));
+                const uint32_t e = exponent_of(most), place = group_first(p) + column;
+                if (lane < 8) {
+                    v *= to_half_range(e);
+                    __half* h = reinterpret_cast<__half*>(a.hidden) + (uint64_t)place * P * a.d_ff + c_in * 8 + lane;
+                    const __half hi = __float2half_rn(v);
+                    h[0] = hi;
+                    if (P == 2) h[a.d_ff] = __float2half_rn(rest_of(v, hi));
+                    if (lane == 0) a.exponents[(uint64_t)place * across + c_in] = (uint8_t)e;
+                }
+            }
+            b_tile += batch * a.tiles;
+            while (b_tile >= across) b_tile -= across, ++b_group;
+            if (r0 + batch < rounds) __syncthreads();
+        }
+    }
+    if (!all_blocks(a, sm.stop)) {
+        cp_async_wait_all();
+        return;
+    }
+
+    float* sums = sm.sums + warp * a.n_tokens * kTokenPitch;
+    HiddenPiece<P> piece[NT];
+    float s_next = 1.f;
+    uint32_t group = w_group, kb = w_kb;  // of `unit`
+    const auto read = [&](uint32_t row) {
+        const uint32_t packed = sm.lists.group[group], slots = group_slots(packed);
+        if (BITS == 8) s_next = block_scale(a.w2, group_expert(packed), row, kb);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) read_hidden<BITS, P>(piece[nt], a, group_first(packed) + nt * 8 + g, kb, nt * 8 + g < slots, t);
+    };
+    for (uint32_t row = blockIdx.x * 16; row < a.d_model; row += gridDim.x * 16) {
+        group = w_group, kb = w_kb;
+        if ((uint32_t)warp < units) read(row);
+        for (uint32_t i = lane; i < a.n_tokens * kTokenPitch; i += 32) sums[i] = 0.f;
         __syncwarp();
+        for (uint32_t unit = warp; unit < units; unit += kTokenWarps) {
+            const uint32_t packed = sm.lists.group[group], slots = group_slots(packed);
+            uint32_t xf[NT][P][16];
+            float f[NT];
+            const float s = s_next;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) f[nt] = settle_hidden<BITS, P>(piece[nt], xf[nt], t);
+            kb += kTokenWarps;
+            while (kb >= kb_down) kb -= kb_down, ++group;
+            if (unit + kTokenWarps < units) read(row);
+            cp_async_wait<R - 2>();
+            float part[NT][4];
+            multiply_unit<BITS, NT, P>(at, xf, s, s, part, lane);
+            advance(at);
+            copy();
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t c = nt * 8 + 2 * t + i;
+                    const float fc = __shfl_sync(~0u, f[nt], 8 * t + 4 * i);
+                    if (c >= slots) continue;
+                    const uint32_t place = group_first(packed) + c;
+                    const float w = sm.lists.weight[place];
+                    float* to = sums + sm.lists.token[place] * kTokenPitch + g;
+                    to[0] = fmaf(part[nt][i] * fc, w, to[0]);
+                    to[8] = fmaf(part[nt][2 + i] * fc, w, to[8]);
+                }
+            __syncwarp();
+        }
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < a.n_tokens * 16; i += kTokenThreads) {
+            const uint32_t token = i / 16, r = i % 16;
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < kTokenWarps; ++w) v += sm.sums[((uint32_t)w * a.n_tokens + token) * kTokenPitch + r];
+            out[token * a.out_stride + row + r] = ValueOf<DT>::put(v);
+        }
+        if (row + gridDim.x * 16 < a.d_model) __syncthreads();
     }
     cp_async_wait_all();
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < a.n_tokens * 16; i += kTokenThreads) {
-        const uint32_t token = i / 16, r = i % 16;
-        float v = 0.f;
-#pragma unroll
-        for (int w = 0; w < kTokenWarps; ++w) v += sm.sums[((uint64_t)w * a.n_tokens + token) * kColumnPitch + r];
-        out[token * a.out_stride + row + r] = ValueOf<DT>::put(v);
-    }
 }
 
 template <class K>
@@ -582,21 +719,29 @@ static cudaError_t allow_shared(K kernel, size_t bytes, std::atomic<uint64_t>& a
 }
 
 template <int DT, int BITS, int NT>
-static cudaError_t launch_tokens(TokensArgs a, const Matrices& w1, const Matrices& w2, const void* x, void* out, uint32_t sms, cudaStream_t s) {
-    static std::atomic<uint64_t> allowed_up{0}, allowed_down{0};
-    constexpr size_t up = sizeof(UpSmem<BITS, NT>), most = sizeof(DownSmem<BITS>) + 4ull * kTokenWarps * CIERA_EXPERT_TOKENS_MAX * kColumnPitch;
-    static_assert(up <= 227 * 1024 && most <= 227 * 1024, "more than a block may have");
-    const size_t down = sizeof(DownSmem<BITS>) + 4ull * kTokenWarps * a.n_tokens * kColumnPitch;
-    cudaError_t e = allow_shared(tokens_up_kernel<DT, BITS, NT>, up, allowed_up);
-    if (e == cudaSuccess) e = allow_shared(tokens_down_kernel<DT, BITS, NT>, most, allowed_down);
+static cudaError_t launch_tokens(const TokensArgs& a, const void* x, void* out, uint32_t sms, cudaStream_t s) {
+    static std::atomic<uint64_t> allowed{0};
+    constexpr uint64_t most = 4ull * kTokenWarps * CIERA_EXPERT_TOKENS_MAX * kTokenPitch;
+    static_assert(sizeof(TokensSmem<BITS>) + (most > 4 * kBatchFloats<NT> ? most : 4 * kBatchFloats<NT>) <= 227 * 1024, "more than a block may have");
+    const uint64_t down = 4ull * kTokenWarps * a.n_tokens * kTokenPitch, up = 4 * kBatchFloats<NT>;
+    auto kernel = tokens_kernel<DT, BITS, NT>;
+    cudaError_t e = allow_shared(kernel, sizeof(TokensSmem<BITS>) + (most > up ? most : up), allowed);
     if (e != cudaSuccess) return e;
-    a.w = w1;
-    const uint64_t tasks = (uint64_t)a.n_tokens * a.top_k * (a.d_ff / 8);  // (no fewer than there are)
-    e = launch_after(tokens_up_kernel<DT, BITS, NT>, dim3((uint32_t)(tasks < sms ? tasks : sms)), kTokenThreads, up, s, a, (const value_t<DT>*)x);
-    if (e != cudaSuccess) return e;
-    count_launch();
-    a.w = w2;
-    e = launch_after(tokens_down_kernel<DT, BITS, NT>, dim3(a.d_model / 16), kTokenThreads, down, s, a, (value_t<DT>*)out);
+    // no more blocks than have work in one of the parts
+    const uint64_t tasks = (uint64_t)a.n_tokens * a.top_k * (a.d_ff / 8), rows = a.d_model / 16, work = tasks > rows ? tasks : rows;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeCooperative;
+    at[0].val.cooperative = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((uint32_t)(work < sms ? work : sms));
+    cfg.blockDim = dim3(kTokenThreads);
+    cfg.dynamicSmemBytes = sizeof(TokensSmem<BITS>) + (down > up ? down : up);
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    e = cudaLaunchKernelEx(&cfg, kernel, a, (const value_t<DT>*)x, (value_t<DT>*)out);
     if (e == cudaSuccess) count_launch();
     return e;
 }
@@ -608,7 +753,7 @@ using namespace ciera;
 extern "C" size_t ciera_expert_tokens_workspace_bytes(uint32_t n_tokens, uint32_t top_k, uint32_t d_ff) {
     // silu(g) * u of every slot in at most two parts of fp16, and an exponent for 8 of them
     const uint64_t values = (uint64_t)n_tokens * top_k * d_ff;
-    return 4 * values + (values / 8 + 15) / 16 * 16 + 16;
+    return kTokenHead + 4 * values + (values / 8 + 15) / 16 * 16;
 }
 
 extern "C" int ciera_expert_tokens(const ciera_expert_tokens_args* p, void* stream) {
@@ -633,7 +778,9 @@ extern "C" int ciera_expert_tokens(const ciera_expert_tokens_args* p, void* stre
         int rc = weights(p->w1, p->w1_stride, p->w1_matrix_stride, p->w1_scales, p->w1_scales_stride, p->w1_scales_matrix_stride, 2 * f, d);
         if (!rc) rc = weights(p->w2, p->w2_stride, p->w2_matrix_stride, p->w2_scales, p->w2_scales_stride, p->w2_scales_matrix_stride, d, f);
         if (rc) return rc;
-        if (!aligned_to(p->x, dtype_bytes(p->dtype)) || !aligned_to(p->out, dtype_bytes(p->dtype)) || !aligned_to(p->workspace, 16)) return CIERA_ERR_MISALIGNED;
+        if (!aligned_to(p->x, dtype_bytes(p->dtype)) || !aligned_to(p->out, dtype_bytes(p->dtype)) || !aligned_to(p->workspace, 16) ||
+            !aligned_to(p->status, 4))
+            return CIERA_ERR_MISALIGNED;
         if (p->workspace_bytes < ciera_expert_tokens_workspace_bytes(p->n_tokens, p->route.top_k, p->d_ff)) return CIERA_ERR_CAPACITY;
     }
     const int rc = ciera_route(&p->route, p->logits_dtype, p->logits, t, p->logits_stride, p->bias, p->experts, p->weights, stream);
@@ -646,14 +793,15 @@ extern "C" int ciera_expert_tokens(const ciera_expert_tokens_args* p, void* stre
     const uint32_t kb = (uint32_t)(d / 128), splits = kb < kTokenWarps ? kb : kTokenWarps, tiles = kTokenWarps / splits;
     const uint64_t values = t * p->route.top_k * f, v = dtype_bytes(p->dtype);
     const bool x_wide = !(((uint64_t)p->x | (t > 1 ? p->x_stride * v : 0)) & 15);
-    const TokensArgs a{{}, p->experts, p->weights, p->x_stride, p->out_stride, (uint8_t*)p->workspace, (uint8_t*)p->workspace + 4 * values,
+    uint8_t* room = (uint8_t*)p->workspace + kTokenHead;
+    const TokensArgs a{{(const uint8_t*)p->w1, p->w1_scales, p->w1_stride, p->w1_matrix_stride, p->w1_scales_stride, p->w1_scales_matrix_stride},
+                       {(const uint8_t*)p->w2, p->w2_scales, p->w2_stride, p->w2_matrix_stride, p->w2_scales_stride, p->w2_scales_matrix_stride},
+                       p->experts, p->weights, p->x_stride, p->out_stride, (uint32_t*)p->workspace, p->status, room, room + 4 * values,
                        (uint32_t)t, p->route.top_k, p->route.n_experts, (uint32_t)d, (uint32_t)f, splits, tiles, x_wide};
-    const Matrices w1{(const uint8_t*)p->w1, p->w1_scales, p->w1_stride, p->w1_matrix_stride, p->w1_scales_stride, p->w1_scales_matrix_stride};
-    const Matrices w2{(const uint8_t*)p->w2, p->w2_scales, p->w2_stride, p->w2_matrix_stride, p->w2_scales_stride, p->w2_scales_matrix_stride};
     with_dtype(p->dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         const auto go = [&](auto bits, auto nt) {
-            e = launch_tokens<DT, decltype(bits)::value, decltype(nt)::value>(a, w1, w2, p->x, p->out, (uint32_t)sms, (cudaStream_t)stream);
+            e = launch_tokens<DT, decltype(bits)::value, decltype(nt)::value>(a, p->x, p->out, (uint32_t)sms, (cudaStream_t)stream);
         };
         const std::integral_constant<int, 1> one;
         const std::integral_constant<int, 2> two;

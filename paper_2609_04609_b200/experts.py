@@ -204,7 +204,7 @@ class ExpertLayer:
             out = torch.empty_like(x) if out is None else out
             if t:
                 ciera.expert_tokens(self.config, x, logits, bias, self.w1, self.w1_s, self.w2, self.w2_s, out, self.experts[:t],
-                                    self.weights[:t], self.few_workspace)
+                                    self.weights[:t], self.few_workspace, self.status)
         return out
 
     def backward(self, dout: torch.Tensor, stream=None):

@@ -57,17 +57,22 @@ class Case:
         self.experts = torch.full((t, k), 77, dtype=torch.int32, device=DEV)
         self.weights = torch.full((t, k), 7.0, device=DEV)
         n = ciera.expert_tokens_workspace_bytes(self.config, t, self.d, self.f)
-        self.workspace = torch.full((n,), 255, dtype=torch.uint8, device=DEV)
+        self.workspace = torch.zeros(n, dtype=torch.uint8, device=DEV)
+        self.workspace[256:] = 255  # (only the head has to be zero)
         return self
 
     def run(self, stream=None):
         from paper_2609_04609_b200 import ciera
 
         ciera.expert_tokens(self.config, self.x, self.logits, self.bias, self.w1, self.w1_s, self.w2, self.w2_s, self.out, self.experts,
-                            self.weights, self.workspace, stream)
+                            self.weights, self.workspace, stream=stream)
         return self.out
 
     def check(self, tokens=None):
+        assert not self.workspace[:256].any()
+        self._check(tokens)
+
+    def _check(self, tokens):
         """silu(g) * u goes into the second product with 11 bits (22 for fp32): off by 2^-11 of itself, or for single values of 128 by
         less than 2^-24 of the largest; sums of d and f terms in 32 bits, of which the tensor cores may cut off what is added,
         so two steps a term and 16 more for silu and the scales; the weights of the choice by 2^-20; one rounding at the end."""
