@@ -670,15 +670,17 @@ CIERA_API int ciera_fp4_matmul(const ciera_fp4_product* args, void* stream);
  * with W1 [2 * d_ff, d_model] (gate above up) and W2 [d_model, d_ff] of the choice's expert; choices of -1 are passed over, a
  * token without any gets zeros.  The matrices stay in 8 bits (CIERA_WEIGHTS_FP8: e4m3 with a scale for each 128 x 128 block, as
  * ciera_fp8_quantize_blocks makes them) or 4 (CIERA_WEIGHTS_FP4, scales_stride and so on as above); x keeps its own precision,
- * other than in ciera_fp8_matmul.  An expert's matrices are read once for up to 8 of its tokens (16, with more than 8 tokens in all).
+ * other than in ciera_fp8_matmul.  An expert's matrices are read once for up to 16 of its tokens (11 in fp32 on 4 bits).
  *   x             device, n_tokens rows of d_model values of dtype;  out  the same
  *   logits, bias, experts, weights   as for ciera_route
  *   workspace     device, 16-byte aligned, ciera_expert_tokens_workspace_bytes() of the largest call: zero-filled once, its first
  *                 256 bytes are handed back zero by every call (but one that reports an error); not shared by calls that may overlap
  *   status        device int32 or NULL: CIERA_ERR_TIMEOUT if the blocks' bounded wait for each other ran out
- * Arithmetic: fp32 sums of 16-bit tensor products with exact weights.  x and silu(g) * u go into them with 11 bits (22 for fp32,
- * so bf16 and fp16 values of x are exact) below the power of two of the largest of 128 values; values of silu(g) * u below
- * 2^-111 may lose bits.  Results do not depend on the other tokens of a call but for the order of their sums.
+ * Arithmetic: fp32 sums of 8-bit (4-bit) tensor products.  The weights are what they are; x and silu(g) * u go into the products as
+ * sums of parts in the weights' bits, each below a power of two of its own for 32 values.  8 bits: three parts, of which 2^-12 of a
+ * value is left out at most and 2^-14 on the average (fp32: five, 2^-20 and 2^-24); bf16 and fp16 values of x are exact next to others
+ * within 2^15.  4 bits: six parts, seven for fp16 and ten for fp32: 2^-11.6, 2^-13.6 and 2^-19.6 of the largest of 32 at most.  A
+ * token with an infinity or a NaN gets NaN, and nobody else does.  Results do not depend on the other tokens of a call.
  * Limits: n_tokens 0 .. CIERA_EXPERT_TOKENS_MAX, d_model and d_ff multiples of 128 up to 65536, config as for ciera_route; weights
  * and their strides as for the products. */
 #define CIERA_EXPERT_TOKENS_MAX 64
@@ -708,7 +710,7 @@ typedef struct ciera_expert_tokens_args {
     uint64_t workspace_bytes;
     int32_t* status;
 } ciera_expert_tokens_args;
-CIERA_API size_t ciera_expert_tokens_workspace_bytes(uint32_t n_tokens, uint32_t top_k, uint32_t d_ff);
+CIERA_API size_t ciera_expert_tokens_workspace_bytes(uint32_t n_tokens, uint32_t top_k, uint32_t d_model, uint32_t d_ff);
 CIERA_API int ciera_expert_tokens(const ciera_expert_tokens_args* args, void* stream);
 
 /* Weighted sum of a token's rows: out[t] = sum over j of weights[t, j] * rows[row_of_slot[t, j]], in fp32, rounded once;

@@ -175,7 +175,7 @@ _SIGS = {
     "ciera_fp4_quantize_matrices": ([ctypes.POINTER(_Fp4Matrices), _vp], _i32),
     "ciera_fp4_values": ([ctypes.POINTER(_Fp4Values), _vp], _i32),
     "ciera_fp4_matmul": ([ctypes.POINTER(_Fp4Product), _vp], _i32),
-    "ciera_expert_tokens_workspace_bytes": ([_u32, _u32, _u32], _sz),
+    "ciera_expert_tokens_workspace_bytes": ([_u32] * 4, _sz),
     "ciera_expert_tokens": ([ctypes.POINTER(_ExpertTokens), _vp], _i32),
     "ciera_expert_combine": ([_i32, _vp, _u64, _u64, _vp, _vp, _u64, _u32, _u64, _vp, _u64, _vp], _i32),
     "ciera_expert_combine_backward": ([_i32, _vp, _u64, _vp, _u64, _u64, _vp, _vp, _u64, _u32, _u64, _vp, _vp, _u64, _vp],
@@ -778,7 +778,7 @@ def fp4_matmul(a, a_scales, b, b_scales, out, starts=None, status=None, stream=N
 
 
 def expert_tokens_workspace_bytes(config: RouteConfig, n_tokens: int, d_model: int, d_ff: int) -> int:
-    return int(_lib.ciera_expert_tokens_workspace_bytes(n_tokens, config.top_k, d_ff))
+    return int(_lib.ciera_expert_tokens_workspace_bytes(n_tokens, config.top_k, d_model, d_ff))
 
 
 def expert_tokens(config: RouteConfig, x, logits, bias, w1, w1_scales, w2, w2_scales, out, experts, weights, workspace,

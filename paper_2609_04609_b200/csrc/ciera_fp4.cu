@@ -13,13 +13,6 @@ namespace ciera {
 
 constexpr int kFp4Threads = 256;
 
-// The scale byte of a group whose largest magnitude has these bits: the least s >= -126 with amax <= 1.5 * 2^2 * 2^s.
-__device__ __forceinline__ uint32_t scale_byte4(uint32_t amax) {
-    if (amax >= 0x7f800000u) return 255u;
-    if (amax == 0u) return 127u;
-    const int s = (int)(amax >> 23) - 127 - 2 + ((amax & 0x7fffffu) > 0x400000u ? 1 : 0);
-    return (uint32_t)(max(s, -126) + 127);
-}
 // 2^-s; 0 for byte 255
 __device__ __forceinline__ float inverse_scale4(uint32_t byte) { return __uint_as_float(byte == 255u ? 0u : (254u - byte) << 23); }
 __device__ __forceinline__ uint32_t magnitude4(float v) { return __float_as_uint(v) & 0x7fffffffu; }

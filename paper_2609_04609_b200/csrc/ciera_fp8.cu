@@ -8,7 +8,7 @@
 // twice (32768 rows of 2048: gathered 59 us, of which memory needs 24; weighted 79; silu(g) * u of 1024 67; its gradient 156).
 #include <type_traits>
 
-#include "ciera_numeric.cuh"
+#include "ciera_fp8.cuh"
 #include "ciera_swiglu.cuh"
 
 namespace ciera {
@@ -31,13 +31,6 @@ struct RowsArgs {
     uint8_t* scales_t;
 };
 
-// The scale byte of a block whose largest magnitude has these bits: the least s >= -126 with amax <= 1.75 * 2^8 * 2^s.
-__device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
-    if (amax >= 0x7f800000u) return 255u;
-    if (amax == 0u) return 127u;
-    const int s = (int)(amax >> 23) - 127 - 8 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
-    return (uint32_t)(max(s, -126) + 127);
-}
 // 2^-s; NaN for byte 255, so that every value of the block becomes one
 __device__ __forceinline__ float inverse_scale(uint32_t byte) {
     return __uint_as_float(byte == 255u ? 0x7fc00000u : (254u - byte) << 23);

@@ -829,13 +829,8 @@ static uint32_t route_grid(uint64_t n_tokens) {
     return (uint32_t)(blocks < 148 * 16 ? blocks : 148 * 16);
 }
 
-}  // namespace ciera
-
-using namespace ciera;
-
-extern "C" int ciera_route(const ciera_route_config* config, int dtype, const void* logits_dev, uint64_t n_tokens,
-                           uint64_t logits_stride, const float* bias_dev, int32_t* experts_dev, float* weights_dev,
-                           void* stream) {
+int check_route(const ciera_route_config* config, int dtype, const void* logits_dev, uint64_t n_tokens, uint64_t logits_stride,
+                const float* bias_dev, const int32_t* experts_dev, const float* weights_dev) {
     RouteArgs a;
     const int rc = route_args(config, &a);
     if (rc) return rc;
@@ -844,8 +839,22 @@ extern "C" int ciera_route(const ciera_route_config* config, int dtype, const vo
     if (!aligned_to(logits_dev, dtype_bytes(dtype)) || !aligned_to(bias_dev, 4) || !aligned_to(experts_dev, 4) ||
         !aligned_to(weights_dev, 4))
         return CIERA_ERR_MISALIGNED;
+    return dtype == CIERA_BF16 || dtype == CIERA_FP32 || dtype == CIERA_FP16 ? CIERA_OK : CIERA_ERR_INVALID_ARG;
+}
+
+}  // namespace ciera
+
+using namespace ciera;
+
+extern "C" int ciera_route(const ciera_route_config* config, int dtype, const void* logits_dev, uint64_t n_tokens,
+                           uint64_t logits_stride, const float* bias_dev, int32_t* experts_dev, float* weights_dev,
+                           void* stream) {
+    const int rc = check_route(config, dtype, logits_dev, n_tokens, logits_stride, bias_dev, experts_dev, weights_dev);
+    if (rc) return rc;
+    RouteArgs a;
+    route_args(config, &a);
     cudaError_t e = cudaSuccess;
-    const bool known = with_dtype(dtype, [&](auto dt) {
+    with_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         if (!n_tokens) return;
         with_row(a.n_experts, [&](auto epl) {
@@ -872,7 +881,6 @@ extern "C" int ciera_route(const ciera_route_config* config, int dtype, const vo
             });
         });
     });
-    if (!known) return CIERA_ERR_INVALID_ARG;
     if (e != cudaSuccess) return record_cuda_error(e);
     if (n_tokens) count_launch();
     return CIERA_OK;

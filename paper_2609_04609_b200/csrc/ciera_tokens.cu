@@ -1,68 +1,77 @@
 // A whole MoE layer for a few tokens.
 //
 // What it costs is reading the matrices of the experts that are reached, once: one token of 8 experts of 2048 x 1024 reads 50 MB
-// in 8 bits and multiplies each weight once.  So a warp streams 16 rows of a matrix through 128 columns at a time, by
-// asynchronous copies into a ring of its own (every lane reads what it has copied itself, so a warp waits for nobody), and has the
-// 16-bit tensor cores multiply them, as rows of the first operand, with up to 8 tokens as columns of the second: both formats
-// are exact in fp16, whose power of two comes after the sum over a block (or group) that shares it.  The tokens' values are made fp16
-// below a power of two of their own for 128 values; fp32 ones in two parts.
+// in 8 bits and multiplies each weight once.  So the weights go from memory to the tensor cores without passing through a
+// register: a tile of 128 rows comes by tensor map and is the first operand as it is, in 8 bits (kind::mxf8f6f4) or 4 (kind::mxf4),
+// with its powers of two; the tokens are the second operand, in the same bits.  A token's values keep their own precision there: they
+// come as a sum of parts, each rounded to 8 or 4 bits below a power of two of its own for 32 values, every part a column of the
+// product, whose sums are added in the end.  An e4m3 part leaves 2^-4 of a value at most (bf16 takes two, fp16 three), so three leave
+// 2^-12, on the average 2^-14; an e2m1 part leaves 1/3 of the largest of 32 at most and each further one a quarter of that, so six
+// leave 2^-11.6, on the average 2^-13.
+// (With weights made fp16 in registers and 16-bit tensor products the same took 300 instructions for 2 KB: one token 24 us, 64
+// tokens 164 us.)
 //
-// One kernel behind the router's, whose blocks all run at once (a cooperative launch), in two parts with a barrier between them:
-//   up     a block takes tiles of 8 columns of the middle, 8 rows of the gate and 8 of up as the 16 rows of a warp, so that the sums
-//          of both meet in one lane; its warps split the contraction, and several tiles' sums are added up in shared memory
-//          together.  silu(g) * u goes to the workspace as fp16 below a power of two for its 8 columns.
-//   down   a block takes 16 columns of the output and the warps split what they are summed over, experts and middle alike; a warp
-//          adds each token's part to sums of its own, which are added up at the end in the order of the warps.
-// A warp's copies go on from the one part's units to the other's, so the weights of the second are on their way (for one token nearly
-// all of them) while the blocks wait for each other.
-// Tokens of an expert are taken 8 at a time (16, with more than 8 tokens in all): a group.  Groups come in the order of the experts
-// and of their slots, so a result does not depend on how warps run.
+// One kernel behind the router's, whose blocks all run at once (a cooperative launch):
+//   parts  the tokens' rows as parts, at the places of their slots in the order of the experts
+//   up     tiles of 64 rows of the gate and the same 64 of up; silu(g) * u goes to the workspace as parts again
+//   down   tiles of 128 rows of the output, expert by expert, as fp32 to the workspace
+//   sum    a token's rows, weighted, in the order of its choices
+// with a barrier of all blocks between them, which only the copies of the second operand wait for: those of the weights go on,
+// so that a block's next 100 to 180 KB of them are on their way meanwhile.
+// Tokens of an expert are taken 16 at a time (a group; 11 where there are ten parts): 112 columns.
 #include <type_traits>
 
 #include "ciera_fp4.cuh"
-#include "ciera_pipe.cuh"
+#include "ciera_fp8.cuh"
+#include "ciera_product.cuh"
 #include "ciera_swiglu.cuh"
 
 namespace ciera {
 
-constexpr int kTokenThreads = 512, kTokenWarps = kTokenThreads / 32;
-template <int BITS>
-constexpr int kTokenRing = BITS == 8 ? 4 : 6;  // units of 16 rows x 128 columns that a warp has on their way, and the one it works on
-constexpr uint32_t kTokenHead = 256;   // bytes of the workspace's counters
+constexpr int kTokenThreads = 256, kTokenWarps = kTokenThreads / 32;
+constexpr int kMostStages = 10;
 constexpr uint32_t kMaxSlots = CIERA_EXPERT_TOKENS_MAX * 32;
-constexpr int kColumnPitch = 20;       // floats between columns of 16 sums: a warp's are in different banks
-constexpr int kTokenPitch = 17;        // the same between tokens, which come in any order
-constexpr uint32_t kLeastExponent = 16;  // of a power of two that values are taken below
+constexpr uint32_t kMaxColumns = 112;
+constexpr uint32_t kTokenHead = 256;  // bytes of the workspace's counters
+constexpr uint32_t kTileBytes = 128 * 128;
+constexpr uint32_t kSumColumns = 112, kTokenScalesAt = 2 * kSumColumns, kTokenTmem = 256;  // of tensor memory: two sums, scales
+
+// Parts of a value and slots of a group.
+template <int BITS, int DT>
+constexpr int kParts = BITS == 8 ? (DT == CIERA_FP32 ? 5 : 3) : (DT == CIERA_FP32 ? 10 : DT == CIERA_FP16 ? 7 : 6);
+template <int BITS, int DT>
+constexpr uint32_t kGroupSlots = kMaxColumns / kParts<BITS, DT> < 16 ? kMaxColumns / kParts<BITS, DT> : 16;
 
 struct Matrices {
-    const uint8_t* q;
     const uint8_t* scales;
-    uint64_t stride, matrix_stride, scales_stride, scales_matrix_stride;
+    uint64_t scales_stride, scales_matrix_stride;
 };
 struct TokensArgs {
     Matrices w1, w2;
     const int32_t* experts;
     const float* weights;
     uint64_t x_stride, out_stride;
-    uint32_t* counters;  // blocks at the barrier, blocks that have left it: zero before and after
+    uint32_t* counters;  // blocks that are done with parts, with up, with down, with all: zero before and after
     int32_t* status;
-    uint8_t* hidden;     // [places][parts][d_ff] fp16
-    uint8_t* exponents;  // [places][d_ff / 8]
+    uint8_t* x_parts;        // [slots * parts][d_model], 8 or 4 bits
+    uint32_t* x_scales;      // [d_model / 128][slots * parts]
+    uint8_t* hidden;         // [slots * parts][d_ff]
+    uint32_t* hidden_scales;
+    float* rows;             // [slots][d_model]
     uint32_t n_tokens, top_k, n_experts, d_model, d_ff;
-    uint32_t splits, tiles;  // up: warps that share a tile, tiles of a block at a time
-    int32_t x_wide;          // x may be read 16 bytes at a time
+    uint32_t stages, stage_bytes;
+    int32_t x_wide;  // x may be read four values at a time
 };
 
-// The slots of the reached experts in the order of the experts, each at a place, and groups of up to `columns` of an expert's.
+// The slots of the reached experts in the order of the experts, each at a place, and groups of up to `most` of an expert's.
 struct TokenLists {
-    uint32_t group[kMaxSlots];  // expert << 16 | slots - 1 << 11 | first place
-    float weight[kMaxSlots];
-    uint8_t token[kMaxSlots];
+    uint32_t group[kMaxSlots];   // expert << 16 | slots - 1 << 11 | first place
+    uint16_t place[kMaxSlots];   // of a slot; 0xffff: none
     uint32_t warp_total[kTokenWarps];
     uint32_t groups;
 };
 struct ListScratch {
-    uint32_t at[1024];  // slots of an expert; then their first place
+    uint32_t at[1024];  // first place of an expert
     uint8_t count[kMaxSlots / 32 * 1024];  // [32 slots][expert]; n_experts apart
 };
 __device__ __forceinline__ uint32_t group_expert(uint32_t g) { return g >> 16; }
@@ -70,12 +79,11 @@ __device__ __forceinline__ uint32_t group_slots(uint32_t g) { return (g >> 11 & 
 __device__ __forceinline__ uint32_t group_first(uint32_t g) { return g & 2047u; }
 
 // By the whole block; ends with a barrier.
-__device__ __forceinline__ void make_lists(TokenLists& l, ListScratch& s, const TokensArgs& a, uint32_t columns) {
+__device__ __forceinline__ void make_lists(TokenLists& l, ListScratch& s, const TokensArgs& a, uint32_t most) {
     const uint32_t n = a.n_tokens * a.top_k, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, E = a.n_experts;
     if (n <= 32) {  // by one warp, a slot a lane
         if (warp == 0) {
             const int32_t id = lane < n ? __ldcg(a.experts + lane) : -1;
-            const float w = lane < n ? __ldcg(a.weights + lane) : 0.f;
             const uint32_t e = (uint32_t)id < E ? (uint32_t)id : 0xffffu;
             uint32_t place = 0, rank = 0, count = 0, groups = 0;  // places before, before of the same expert, the expert's, groups before
             for (uint32_t i = 0; i < n; ++i) {
@@ -84,10 +92,10 @@ __device__ __forceinline__ void make_lists(TokenLists& l, ListScratch& s, const 
                 rank += o == e && i < lane;
                 count += o == e;
             }
-            const bool first = rank % columns == 0 && e != 0xffffu;  // the lane makes a group
+            const bool first = rank % most == 0 && e != 0xffffu;  // the lane makes a group
             for (uint32_t i = 0; i < n; ++i) groups += __shfl_sync(~0u, first ? place : ~0u, i) < place;
-            if (e != 0xffffu) l.token[place] = (uint8_t)(lane / a.top_k), l.weight[place] = w;
-            if (first) l.group[groups] = e << 16 | (min(columns, count - rank) - 1) << 11 | place;
+            if (lane < n) l.place[lane] = (uint16_t)(e == 0xffffu ? 0xffffu : place);
+            if (first) l.group[groups] = e << 16 | (min(most, count - rank) - 1) << 11 | place;
             const uint32_t all = __popc(__ballot_sync(~0u, first));
             if (lane == 0) l.groups = all;
         }
@@ -95,19 +103,20 @@ __device__ __forceinline__ void make_lists(TokenLists& l, ListScratch& s, const 
         return;
     }
     // slots of an expert are counted for each 32 neighbours, then over those before
+    constexpr int kEach = kMaxSlots / kTokenThreads;
     const uint32_t chunks = (n + 31) / 32;
     for (uint32_t i = tid; i < (chunks * E + 15) / 16; i += kTokenThreads) reinterpret_cast<uint4*>(s.count)[i] = make_uint4(0, 0, 0, 0);
-    int32_t id[kMaxSlots / kTokenThreads];
+    int32_t id[kEach];
 #pragma unroll
-    for (int j = 0; j < (int)(kMaxSlots / kTokenThreads); ++j) {
+    for (int j = 0; j < kEach; ++j) {
         const uint32_t i = j * kTokenThreads + tid;
         id[j] = i < n ? __ldcg(a.experts + i) : -1;
         if ((uint32_t)id[j] >= E) id[j] = -1;
     }
     __syncthreads();
-    uint32_t rank[kMaxSlots / kTokenThreads];
+    uint32_t rank[kEach];
 #pragma unroll
-    for (int j = 0; j < (int)(kMaxSlots / kTokenThreads); ++j) {
+    for (int j = 0; j < kEach; ++j) {
         const uint32_t chunk = j * kTokenWarps + warp;
         if (chunk >= chunks) break;
         const uint32_t same = __match_any_sync(~0u, id[j]);
@@ -115,16 +124,18 @@ __device__ __forceinline__ void make_lists(TokenLists& l, ListScratch& s, const 
         if (id[j] >= 0 && rank[j] == 0) s.count[chunk * E + id[j]] = (uint8_t)__popc(same);
     }
     __syncthreads();
-    // places and groups before each expert, two experts a thread: slots in the low half, groups in the high one
-    uint32_t c0 = 0, c1 = 0;
-    if (2 * tid < E) {
-        for (uint32_t i = 0; i < chunks; ++i) {
-            c0 += s.count[i * E + 2 * tid];
-            if (2 * tid + 1 < E) c1 += s.count[i * E + 2 * tid + 1];
-        }
+    // places and groups before each expert, four experts a thread: slots in the low half, groups in the high one
+    uint32_t count[4], v[4], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t e = 4 * tid + i;
+        count[i] = 0;
+        if (e < E)
+            for (uint32_t c = 0; c < chunks; ++c) count[i] += s.count[c * E + e];
+        v[i] = count[i] | (count[i] + most - 1) / most << 16;
+        sum += v[i];
     }
-    const uint32_t v0 = c0 | (c0 + columns - 1) / columns << 16, v1 = c1 | (c1 + columns - 1) / columns << 16;
-    uint32_t sum = v0 + v1;
+    const uint32_t own = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         const uint32_t o = __shfl_up_sync(~0u, sum, d);
@@ -135,600 +146,639 @@ __device__ __forceinline__ void make_lists(TokenLists& l, ListScratch& s, const 
     uint32_t base = 0;
     for (uint32_t w = 0; w < warp; ++w) base += l.warp_total[w];
     if (tid == kTokenThreads - 1) l.groups = (base + sum) >> 16;
-    const uint32_t first[2] = {base + sum - v0 - v1, base + sum - v1}, count[2] = {c0, c1};
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t e = 2 * tid + i, at = first[i] & 0xffffu;
-        uint32_t g = first[i] >> 16;
-        for (uint32_t c = 0; c < count[i]; c += columns, ++g) l.group[g] = e << 16 | (min(columns, count[i] - c) - 1) << 11 | (at + c);
-        s.at[e] = at;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < (int)(kMaxSlots / kTokenThreads); ++j) {
-        const uint32_t chunk = j * kTokenWarps + warp;
-        if (chunk >= chunks) break;
-        if (id[j] < 0) continue;
-        uint32_t place = s.at[id[j]] + rank[j];
-        for (uint32_t i = 0; i < chunk; ++i) place += s.count[i * E + id[j]];
-        const uint32_t slot = j * kTokenThreads + tid;
-        l.token[place] = (uint8_t)(slot / a.top_k);
-        l.weight[place] = __ldcg(a.weights + slot);
-    }
-    __syncthreads();
-}
-
-__device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void from_e4m3x4(uint32_t codes, uint32_t& lo, uint32_t& hi) {
-    asm("{\n\t.reg .b16 a, b;\n\t"
-        "mov.b32 {a, b}, %2;\n\t"
-        "cvt.rn.f16x2.e4m3x2 %0, a;\n\t"
-        "cvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
-        : "=r"(lo), "=r"(hi)
-        : "r"(codes));
-}
-
-// A warp's unit: 16 rows of a matrix x 128 columns.  Lane (g, t) = (lane / 4, lane % 4) copies of rows g and g + 8
-//   8 bits  columns 16 t ... and 64 + 16 t ..., 16 bytes each; block scales are read when they are needed
-//   4 bits  columns 32 t ..., 16 bytes, a group; and the row's word of scales
-// and has the tokens' values of its columns in this order, two to a register.  In 4 bits the lanes of a row exchange words first, so
-// that all four have columns of one group at a time: 8 of them from 32 b + 8 t on, for b = 0 .. 3.
-template <int BITS>
-struct alignas(16) Unit;
-template <>
-struct alignas(16) Unit<8> {
-    uint4 w[4][32];  // [row half * 2 + piece][lane]
-};
-template <>
-struct alignas(16) Unit<4> {
-    uint4 w[2][32];  // [row half][lane]
-    uint32_t s[2][32];
-};
-template <int BITS>
-__device__ __forceinline__ uint32_t fragment_column(int i, uint32_t t) {  // of the lane's value i, 0 .. 31
-    return BITS == 8 ? (i >> 4) * 64 + t * 16 + (i & 15) : (i >> 3) * 32 + t * 8 + (i & 7);
-}
-
-// Where a lane's part of a unit comes from: rows lo + g and hi + g of matrix e (lo and hi - lo are multiples of 8), columns from
-// 128 * kb on.
-template <int BITS>
-struct UnitSource {
-    const uint8_t* a;
-    const uint8_t* b;
-    const uint8_t* sa;  // 4 bits: the scale words of rows g and hi - lo + g ...
-    const uint8_t* sb;
-    uint32_t lo;        // ... from which row lo's are this far
-
-    __device__ __forceinline__ void point(const Matrices& m, uint32_t e, uint32_t row, uint32_t apart, uint32_t kb, int lane) {
-        const uint32_t g = lane >> 2, t = lane & 3;
-        a = m.q + e * m.matrix_stride + (uint64_t)(row + g) * m.stride + kb * (16 * BITS) + t * 16;
-        b = a + (uint64_t)apart * m.stride;
-        if constexpr (BITS == 4) {
-            lo = row;
-            sa = m.scales + e * m.scales_matrix_stride + (uint64_t)kb * kAtomBytes + g * 16;
-            sb = apart == 8 ? sa + 128 : sa + (uint64_t)(apart >> 7) * m.scales_stride;  // (8: the same block of 32 rows)
-        }
-    }
-    __device__ __forceinline__ void copy(uint32_t to, const Matrices& m, int lane) const {
-        to += lane * 16;
-        const auto copy16 = [](uint32_t dst, const uint8_t* p) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(p) : "memory");
-        };
-        copy16(to, a);
-        if constexpr (BITS == 8) {
-            copy16(to + 512, a + 64);
-            copy16(to + 1024, b);
-            copy16(to + 1536, b + 64);
-        } else {
-            copy16(to + 512, b);
-            const uint64_t off = (uint64_t)(lo >> 7) * m.scales_stride + atom_word(lo);
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 1024 - lane * 12), "l"(sa + off) : "memory");
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 1152 - lane * 12), "l"(sb + off) : "memory");
-        }
-    }
-};
-// 8 bits: the scale of a row's block
-__device__ __forceinline__ float block_scale(const Matrices& m, uint32_t e, uint32_t row, uint32_t kb) {
-    return scale_value(__ldg(m.scales + e * m.scales_matrix_stride + (uint64_t)(row >> 7) * m.scales_stride + kb));
-}
-
-// The four words of a row's four lanes, turned: word j of lane t to word t of lane j.
-__device__ __forceinline__ void turn_words(uint32_t (&w)[4], uint32_t t) {
-#pragma unroll
-    for (int i = 0; i < 4; i += 2) {
-        const uint32_t o = __shfl_xor_sync(~0u, t & 1 ? w[i] : w[i + 1], 1);
-        if (t & 1) w[i] = o;
-        else w[i + 1] = o;
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t o = __shfl_xor_sync(~0u, t & 2 ? w[i] : w[i + 2], 2);
-        if (t & 2) w[i] = o;
-        else w[i + 2] = o;
-    }
-}
-
-__device__ __forceinline__ uint4 read16(uint32_t at) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint32_t read4(uint32_t at) {
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-    return v;
-}
-
-// sums[nt] = the unit's rows times the columns of x, scales of the rows included: rows g, g + 8 of columns 2 t, 2 t + 1
-template <int BITS, int NT, int P>
-__device__ __forceinline__ void multiply_unit(uint32_t unit, const uint32_t (&x)[NT][P][16], float s_lo, float s_hi, float (&sums)[NT][4], int lane) {
-    unit += lane * 16;
-    if constexpr (BITS == 8) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sums[nt][i] = 0.f;
-        uint4 w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = read16(unit + 512 * i);
-#pragma unroll
-        for (int piece = 0; piece < 2; ++piece) {
-            const uint32_t l[4] = {w[piece].x, w[piece].y, w[piece].z, w[piece].w}, h[4] = {w[2 + piece].x, w[2 + piece].y, w[2 + piece].z, w[2 + piece].w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t a0, a1, a2, a3;
-                from_e4m3x4(l[j], a0, a2);
-                from_e4m3x4(h[j], a1, a3);
-                const int r = piece * 8 + 2 * j;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int p = 0; p < P; ++p) mma_16x8x16(sums[nt], a0, a1, a2, a3, x[nt][p][r], x[nt][p][r + 1]);
-            }
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) sums[nt][0] *= s_lo, sums[nt][1] *= s_lo, sums[nt][2] *= s_hi, sums[nt][3] *= s_hi;
-    } else {
-        const uint4 lo = read16(unit), hi = read16(unit + 512);
-        const uint32_t sl = read4(unit + 1024 - lane * 12), sh = read4(unit + 1152 - lane * 12);
-        uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, h[4] = {hi.x, hi.y, hi.z, hi.w};
-        turn_words(l, lane & 3);
-        turn_words(h, lane & 3);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            uint32_t a[4], c[4];
-            from_e2m1x8(l[b], a);
-            from_e2m1x8(h[b], c);
-            const float fl = scale_value(sl >> (8 * b) & 255u), fh = scale_value(sh >> (8 * b) & 255u);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    mma_16x8x16(part, a[0], c[0], a[1], c[1], x[nt][p][4 * b], x[nt][p][4 * b + 1]);
-                    mma_16x8x16(part, a[2], c[2], a[3], c[3], x[nt][p][4 * b + 2], x[nt][p][4 * b + 3]);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float f = i < 2 ? fl : fh;
-                    sums[nt][i] = b == 0 ? part[i] * f : fmaf(part[i], f, sums[nt][i]);
-                }
-            }
-        }
-    }
-}
-
-// The biased exponent e of the power of two that values of these largest bits lie below (e = 255: not finite), what brings them
-// below 2^15, and what takes it back.
-__device__ __forceinline__ uint32_t exponent_of(uint32_t magnitude) { return max(magnitude >> 23, kLeastExponent); }
-__device__ __forceinline__ float to_half_range(uint32_t e) { return __uint_as_float((268u - e) << 23); }
-__device__ __forceinline__ float from_half_range(uint32_t e) { return __uint_as_float((e - 14u) << 23); }
-// The rest of a value in that range behind its fp16 part.
-__device__ __forceinline__ float rest_of(float v, __half h) {
-    const float r = v - __half2float(h);
-    return isfinite(r) ? r : 0.f;
-}
-
-// 128 values of a token (row) as a lane's column of the second operand, and what their sums are multiplied by.
-template <int DT, int BITS, int P>
-__device__ __forceinline__ float load_tokens(const value_t<DT>* __restrict__ row, bool there, bool wide, uint32_t (&x)[P][16], uint32_t t) {
-    float v[32];
-    if (there && wide) {
-        constexpr int kEach = 16 / sizeof(value_t<DT>);
-#pragma unroll
-        for (int i = 0; i < 32; i += kEach) {
-            float part[kEach];
-            load_values<DT, kEach>(row + fragment_column<BITS>(i, t), part);
-#pragma unroll
-            for (int j = 0; j < kEach; ++j) v[i + j] = part[j];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = there ? ValueOf<DT>::get(row[fragment_column<BITS>(i, t)]) : 0.f;
-    }
-    uint32_t most = 0;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
-    most = max(most, __shfl_xor_sync(~0u, most, 1));
-    most = max(most, __shfl_xor_sync(~0u, most, 2));
-    const uint32_t e = exponent_of(most);
-    const float f = to_half_range(e);
-#pragma unroll
-    for (int i = 0; i < 32; i += 2) {
-        const float lo = v[i] * f, hi = v[i + 1] * f;
-        const __half2 h = __floats2half2_rn(lo, hi);
-        x[0][i / 2] = *reinterpret_cast<const uint32_t*>(&h);
-        if constexpr (P == 2) {
-            const __half2 r = __floats2half2_rn(rest_of(lo, __low2half(h)), rest_of(hi, __high2half(h)));
-            x[1][i / 2] = *reinterpret_cast<const uint32_t*>(&r);
-        }
-    }
-    return from_half_range(e);
-}
-
-// The middle's values at a place, 128 of them, in a lane's order; scaled to the power of two of the largest.
-template <int P>
-struct HiddenPiece {
-    uint4 v[P][4];
-    uint4 e;
-};
-template <int BITS, int P>
-__device__ __forceinline__ void read_hidden(HiddenPiece<P>& h, const TokensArgs& a, uint32_t place, uint32_t kb, bool there, uint32_t t) {
-    if (!there) {
-        h.e = make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) h.v[p][i] = make_uint4(0, 0, 0, 0);
-        return;
-    }
-    h.e = __ldcg(reinterpret_cast<const uint4*>(a.exponents + (uint64_t)place * (a.d_ff / 8) + kb * 16));
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-        const __half* from = reinterpret_cast<const __half*>(a.hidden) + ((uint64_t)place * P + p) * a.d_ff + kb * 128;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h.v[p][i] = __ldcg(reinterpret_cast<const uint4*>(from + fragment_column<BITS>(8 * i, t)));
-    }
-}
-// 2^-n as fp16, twice; 0 where there is none
-__device__ __forceinline__ uint32_t half_power(uint32_t n) {
-    const uint32_t h = n < 15 ? (15 - n) << 10 : n < 25 ? 1u << (24 - n) : 0u;
-    return h | h << 16;
-}
-template <int BITS, int P>
-__device__ __forceinline__ float settle_hidden(const HiddenPiece<P>& h, uint32_t (&x)[P][16], uint32_t t) {
-    uint32_t m = __vmaxu4(__vmaxu4(h.e.x, h.e.y), __vmaxu4(h.e.z, h.e.w));
-    m = __vmaxu4(m, m >> 16);
-    const uint32_t e = max(max(m & 255u, m >> 8 & 255u), kLeastExponent);
-    const uint32_t word[4] = {h.e.x, h.e.y, h.e.z, h.e.w};
+    uint32_t before = base + sum - own;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        uint32_t own;  // the exponent of the lane's values 8 i .. 8 i + 7
-        if (BITS == 8) own = ((t & 2 ? word[(i >> 1) * 2 + 1] : word[(i >> 1) * 2]) >> ((t & 1) * 16 + (i & 1) * 8)) & 255u;
-        else own = word[i] >> (8 * t) & 255u;
-        const uint32_t f = half_power(e - own);
-        const __half2 factor = *reinterpret_cast<const __half2*>(&f);
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const uint32_t v[4] = {h.v[p][i].x, h.v[p][i].y, h.v[p][i].z, h.v[p][i].w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&v[j]), factor);
-                x[p][4 * i + j] = *reinterpret_cast<const uint32_t*>(&y);
-            }
-        }
+        const uint32_t e = 4 * tid + i, at = before & 0xffffu;
+        uint32_t g = before >> 16;
+        for (uint32_t c = 0; c < count[i]; c += most, ++g) l.group[g] = e << 16 | (min(most, count[i] - c) - 1) << 11 | (at + c);
+        s.at[e] = at;
+        before += v[i];
     }
-    return from_half_range(e);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const uint32_t chunk = j * kTokenWarps + warp, slot = j * kTokenThreads + tid;
+        if (chunk >= chunks) break;
+        uint32_t place = 0xffffu;
+        if (id[j] >= 0) {
+            place = s.at[id[j]] + rank[j];
+            for (uint32_t i = 0; i < chunk; ++i) place += s.count[i * E + id[j]];
+        }
+        if (slot < n) l.place[slot] = (uint16_t)place;
+    }
+    __syncthreads();
 }
 
+// ---- parts
+
+// The scale byte of 32 values whose largest magnitude has these bits, and what takes them below it (0 where they are not finite).
 template <int BITS>
-struct TokensSmem {
-    Unit<BITS> ring[kTokenWarps][kTokenRing<BITS>];
-    TokenLists lists;
-    int stop;
-    // up: [rounds of a batch][warp][column][kColumnPitch]; down: [warp][token][kTokenPitch]
-    __align__(16) float sums[];
-};
-// rounds of tiles whose sums are added up together, and what they need
-template <int NT>
-constexpr uint32_t kBatch = NT == 1 ? 8 : 4;
-template <int NT>
-constexpr uint32_t kBatchFloats = kBatch<NT> * kTokenWarps * NT * 8 * kColumnPitch;
+__device__ __forceinline__ uint32_t part_byte(uint32_t amax) {
+    return BITS == 8 ? scale_byte(amax) : scale_byte4(amax);
+}
+__device__ __forceinline__ float part_inverse(uint32_t byte) { return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23); }
 
-// All blocks have come here, and what they wrote before can be read (past the first-level cache).  false: the wait ran out.
-__device__ __forceinline__ bool all_blocks(const TokensArgs& a, int& stop) {
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        uint32_t seen, polls = 0;
-        __threadfence();
-        atomicAdd(a.counters, 1u);
-        do {
-            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(a.counters) : "memory");
-        } while (seen < gridDim.x && ++polls < kMaxPolls);
-        stop = seen < gridDim.x;
-        if (stop && a.status) atomicCAS(a.status, 0, (int32_t)CIERA_ERR_TIMEOUT);
-        // the last one to leave sets both counters back
-        if (!stop && atomicAdd(a.counters + 1, 1u) == gridDim.x - 1) {
-            a.counters[0] = 0;
-            a.counters[1] = 0;
-        }
-    }
-    __syncthreads();
-    return !stop;
+// Four values rounded to e4m3, and what is left of them.
+__device__ __forceinline__ uint32_t take_part8(float (&v)[4], float inv, float unit) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[0] * inv, v[1] * inv), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[2] * inv, v[3] * inv), __NV_SATFINITE, __NV_E4M3);
+    const float2 a = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)lo, __NV_E4M3)));
+    const float2 b = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)hi, __NV_E4M3)));
+    v[0] = fmaf(-a.x, unit, v[0]);
+    v[1] = fmaf(-a.y, unit, v[1]);
+    v[2] = fmaf(-b.x, unit, v[2]);
+    v[3] = fmaf(-b.y, unit, v[3]);
+    return lo | hi << 16;
+}
+// Four values rounded to e2m1 in 16 bits, and what is left of them.
+__device__ __forceinline__ uint32_t take_part4(float (&v)[4], float inv, float unit) {
+    uint32_t r, ab, cd;
+    asm("{\n\t.reg .b8 a, b, n;\n\t.reg .b16 z;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %6, %5;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, a;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, b;\n\t"
+        "mov.b16 z, 0;\n\tcvt.u8.u16 n, z;\n\t"
+        "mov.b32 %0, {a, b, n, n};\n\t}"
+        : "=r"(r), "=r"(ab), "=r"(cd)
+        : "f"(v[0] * inv), "f"(v[1] * inv), "f"(v[2] * inv), "f"(v[3] * inv));
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&ab)), b = __half22float2(*reinterpret_cast<const __half2*>(&cd));
+    v[0] = fmaf(-a.x, unit, v[0]);
+    v[1] = fmaf(-a.y, unit, v[1]);
+    v[2] = fmaf(-b.x, unit, v[2]);
+    v[3] = fmaf(-b.y, unit, v[3]);
+    return r;
 }
 
-template <int DT, int BITS, int NT>
-__global__ void __launch_bounds__(kTokenThreads, 1) tokens_kernel(const TokensArgs a, const value_t<DT>* __restrict__ x_, value_t<DT>* __restrict__ out) {
-    constexpr int P = DT == CIERA_FP32 ? 2 : 1, R = kTokenRing<BITS>;
-    extern __shared__ __align__(16) uint8_t tokens_smem[];
-    TokensSmem<BITS>& sm = *reinterpret_cast<TokensSmem<BITS>*>(tokens_smem);
-    static_assert(sizeof(ListScratch) <= sizeof(sm.ring), "the lists are made where the ring will be");
-    pdl_wait();
-    make_lists(sm.lists, *reinterpret_cast<ListScratch*>(&sm.ring), a, NT * 8);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t g = lane >> 2, t = lane & 3;
-    // the warp's ring: the next unit to be copied and to be worked on
-    const uint32_t ring = smem_u32(sm.ring[warp]), ring_end = ring + sizeof(sm.ring[warp]);
-    uint32_t c_at = ring, at = ring;
-    const auto advance = [&](uint32_t& p) {
-        p += sizeof(Unit<BITS>);
-        if (p == ring_end) p = ring;
-    };
+// 128 values of a token, four a lane, as parts at all its places.
+template <int DT, int BITS>
+__device__ __forceinline__ void make_parts(const TokensArgs& a, const TokenLists& l, const value_t<DT>* __restrict__ x, uint32_t token, uint32_t kb,
+                                           uint32_t lane) {
+    constexpr uint32_t P = kParts<BITS, DT>;
+    float v[4];
+    const value_t<DT>* from = x + token * a.x_stride + kb * 128 + lane * 4;
+    if (a.x_wide) {
+        load_values<DT, 4>(from, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = ValueOf<DT>::get(from[i]);
+    }
+    const uint32_t rows = a.n_tokens * a.top_k * P;
+    uint32_t word[P], bytes[P];
+#pragma unroll
+    for (uint32_t p = 0; p < P; ++p) {
+        uint32_t amax = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) amax = max(amax, __shfl_xor_sync(~0u, amax, d));
+        const uint32_t byte = part_byte<BITS>(amax);
+        const float inv = part_inverse(byte), unit = __uint_as_float(byte << 23);
+        if constexpr (BITS == 8) word[p] = take_part8(v, inv, unit);
+        else word[p] = take_part4(v, inv, unit);
+        if (byte == 255u) {  // NaN by its scale; nothing is left
+            word[p] = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = 0.f;
+        }
+        // the four groups' bytes
+        uint32_t all = byte << (lane >> 3) * 8;
+        all |= __shfl_xor_sync(~0u, all, 8);
+        all |= __shfl_xor_sync(~0u, all, 16);
+        bytes[p] = all;
+    }
+    for (uint32_t j = 0; j < a.top_k; ++j) {
+        const uint32_t place = l.place[token * a.top_k + j];
+        if (place == 0xffffu) continue;
+#pragma unroll
+        for (uint32_t p = 0; p < P; ++p) {
+            const uint32_t row = place * P + p;
+            if constexpr (BITS == 8) *reinterpret_cast<uint32_t*>(a.x_parts + (uint64_t)row * a.d_model + kb * 128 + lane * 4) = word[p];
+            else *reinterpret_cast<uint16_t*>(a.x_parts + (uint64_t)row * (a.d_model / 2) + kb * 64 + lane * 2) = (uint16_t)word[p];
+            if (lane == p) a.x_scales[(uint64_t)kb * rows + row] = bytes[p];
+        }
+    }
+}
 
-    // up: tiles of 8 columns of the middle, in the order of the groups; a block has neighbouring ones, `tiles` at a time
-    const uint32_t kb_up = a.d_model / 128, across = a.d_ff / 8;
-    const uint64_t all = (uint64_t)sm.lists.groups * across;
-    const uint32_t from = (uint32_t)(all * blockIdx.x / gridDim.x), to = (uint32_t)(all * (blockIdx.x + 1) / gridDim.x);
-    const uint32_t mine = warp / a.splits, split = warp - mine * a.splits;  // the warp's tile of those, its part of the contraction
-    const uint32_t rounds = (to - from + a.tiles - 1) / a.tiles;
-    const uint32_t own = mine < a.tiles ? to : 0;  // the warp's tiles end here
-    const uint32_t first_group = from / across, first_tile = from - first_group * across;
-    // down: 16 columns of the output, everything that they are summed over
-    const uint32_t kb_down = a.d_ff / 128, units = sm.lists.groups * kb_down;
-    const uint32_t w_group = warp / kb_down, w_kb = warp - w_group * kb_down;
+// 32 neighbouring values of the middle, one a lane, as parts at one place; columns f ... of d_ff.
+template <int DT, int BITS>
+__device__ __forceinline__ void put_hidden(const TokensArgs& a, float v, uint32_t place, uint32_t f, uint32_t lane) {
+    constexpr uint32_t P = kParts<BITS, DT>;
+    const uint32_t rows = a.n_tokens * a.top_k * P;
+#pragma unroll
+    for (uint32_t p = 0; p < P; ++p) {
+        const uint32_t amax = __reduce_max_sync(~0u, __float_as_uint(v) & 0x7fffffffu), byte = part_byte<BITS>(amax), row = place * P + p;
+        const float inv = part_inverse(byte), unit = __uint_as_float(byte << 23);
+        const bool bad = byte == 255u;
+        if constexpr (BITS == 8) {
+            const uint8_t q = __nv_cvt_float_to_fp8(v * inv, __NV_SATFINITE, __NV_E4M3);
+            v = fmaf(-__half2float(__half(__nv_cvt_fp8_to_halfraw(q, __NV_E4M3))), unit, v);
+            a.hidden[(uint64_t)row * a.d_ff + f + lane] = bad ? 0 : q;
+        } else {
+            const float other = __shfl_xor_sync(~0u, v, 1);
+            uint32_t q, two;
+            asm("{\n\t.reg .b8 a;\n\t.reg .b16 w;\n\t"
+                "cvt.rn.satfinite.e2m1x2.f32 a, %3, %2;\n\t"
+                "cvt.rn.f16x2.e2m1x2 %1, a;\n\t"
+                "cvt.u16.u8 w, a;\n\tcvt.u32.u16 %0, w;\n\t}"
+                : "=r"(q), "=r"(two)
+                : "f"((lane & 1 ? other : v) * inv), "f"((lane & 1 ? v : other) * inv));
+            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&two));
+            v = fmaf(-(lane & 1 ? y.y : y.x), unit, v);
+            if (!(lane & 1)) a.hidden[(uint64_t)row * (a.d_ff / 2) + f / 2 + lane / 2] = bad ? 0 : (uint8_t)q;
+        }
+        if (lane == 0) reinterpret_cast<uint8_t*>(a.hidden_scales + (uint64_t)(f >> 7) * rows + row)[f >> 5 & 3u] = (uint8_t)byte;
+        if (bad) v = 0.f;
+    }
+}
 
-    // Copies go in runs, in which the source moves on by the same step: the warp's tiles of one group, or, where a warp has more than
-    // one part of a tile's contraction, those; then single units of the second matrices.
-    UnitSource<BITS> src;
-    const bool by_tile = kb_up <= a.splits;
-    uint32_t c_task = from + mine, c_group = first_group, c_tile = first_tile + mine, c_left = 0;
-    uint32_t d_row = blockIdx.x * 16, d_unit = warp, d_group = w_group, d_kb = w_kb;
+// ---- tensor cores of one block (ciera_tensor.cuh has the pair's)
+
+__device__ __forceinline__ void tmem_alloc_one(uint32_t* where, uint32_t columns) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free_one(uint32_t at, uint32_t columns) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void tensor_commit_one(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tmem_copy_scales_one(uint32_t to, uint64_t rows) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(rows) : "memory");
+}
+template <int BITS>
+__device__ __forceinline__ void tensor_mma_one(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, uint32_t a_scales, uint32_t b_scales, bool add) {
+    if constexpr (BITS == 8)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(instruction), "r"(a_scales), "r"(b_scales), "r"((uint32_t)add)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(instruction), "r"(a_scales), "r"(b_scales), "r"((uint32_t)add)
+            : "memory");
+}
+__device__ __forceinline__ void map_load3_one(void* dst, const void* map, int32_t x, int32_t y, int32_t z, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                     smem_u32(dst)),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+                 : "memory");
+}
+// 16 columns of the warp's 32 lanes
+__device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(at));
+}
+
+// ---- the kernel
+
+struct alignas(16) TokensSmem {
+    TokenLists lists;
+    float exchange[16][128];  // the sums of a tile, [slot][row]
+    uint64_t full[kMostStages], empty[kMostStages], sums_full[2], sums_free[2], done;
+    uint32_t tmem;
+    int abort;
+};
+constexpr uint32_t kStageScales = 4 * 512;  // a stage's scale bytes: two atoms (8 bits: one) of each operand
+// a stage: the weights' tile, the tokens' columns, the scales of both
+static_assert(sizeof(TokensSmem) + 1024 + sizeof(ListScratch) <= 227 * 1024, "more than a block may have");
+
+// All blocks have added to a counter.  false: the bounded wait ran out, or another of the block's has.
+__device__ __forceinline__ bool wait_for_all(const uint32_t* counter, uint32_t blocks, volatile int* abort, int32_t* status) {
+    for (uint32_t polls = 0; polls < kMaxPolls; ++polls) {
+        uint32_t seen;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(counter) : "memory");
+        if (seen >= blocks) return true;
+        if (*abort) return false;
+    }
+    *abort = 1;
+    if (status) atomicCAS(status, 0, (int32_t)CIERA_ERR_TIMEOUT);
+    return false;
+}
+__device__ __forceinline__ void fence_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
+// The tiles of a block in both parts, in order: all roles walk them alike.
+template <int BITS>
+struct TokenWalk {
+    const TokensArgs& a;
+    const TokenLists& l;
+    uint32_t up_tiles, down_tiles, at;
     bool up = true;
-    const uint64_t a_step = by_tile ? (uint64_t)a.tiles * 8 * a.w1.stride : a.splits * (16 * BITS);
-    const auto next_run = [&]() {
-        if (up && c_task < own) {
-            while (c_tile >= across) c_tile -= across, ++c_group;
-            src.point(a.w1, group_expert(sm.lists.group[c_group]), c_tile * 8, a.d_ff, split, lane);
-            if (by_tile) {
-                c_left = (min(across - c_tile, own - c_task) + a.tiles - 1) / a.tiles;
-                c_task += c_left * a.tiles;
-                c_tile += c_left * a.tiles;
-            } else {
-                c_left = (kb_up - split + a.splits - 1) / a.splits;
-                c_task += a.tiles;
-                c_tile += a.tiles;
-            }
-            return;
-        }
-        up = false;
-        if (d_unit >= units) {
-            d_unit = warp, d_group = w_group, d_kb = w_kb;
-            d_row += gridDim.x * 16;
-        }
-        if (d_row < a.d_model && d_unit < units) {
-            src.point(a.w2, group_expert(sm.lists.group[d_group]), d_row, 8, d_kb, lane);
-            c_left = 1;
-            d_unit += kTokenWarps;
-            d_kb += kTokenWarps;
-            while (d_kb >= kb_down) d_kb -= kb_down, ++d_group;
-        }
-    };
-    next_run();
-    const auto copy = [&]() {
-        if (c_left) {
-            src.copy(c_at, up ? a.w1 : a.w2, lane);
-            src.a += a_step;
-            src.b += a_step;
-            if (BITS == 4) {
-                if (by_tile) src.lo += a.tiles * 8;
-                else src.sa += a.splits * kAtomBytes, src.sb += a.splits * kAtomBytes;
-            }
-            if (--c_left == 0) next_run();
-        }
-        advance(c_at);
-        cp_async_commit();
-    };
-#pragma unroll 1
-    for (int i = 0; i < R - 1; ++i) copy();
+    uint32_t group = 0, tile = 0, stages = 0;
 
-    {
-        uint32_t task = from + mine, group = first_group, tile = first_tile + mine, loaded_group = ~0u, loaded_kb = ~0u, scaled = ~0u;
-        uint32_t packed = 0, slots = 0;
-        uint32_t xf[NT][P][16];
-        float scale[NT][2], s_lo = 1.f, s_hi = 1.f;
-        uint32_t b_group = first_group, b_tile = first_tile;  // of the batch
-        for (uint32_t r0 = 0; r0 < rounds; r0 += kBatch<NT>) {
-            const uint32_t batch = min(kBatch<NT>, rounds - r0);
-            float* put = sm.sums + (warp * NT * 8 + 2 * t) * kColumnPitch + g;
-            for (uint32_t r = 0; r < batch && task < own; ++r) {
-                while (tile >= across) tile -= across, ++group;
-                float acc[NT][4];
+    __device__ TokenWalk(const TokensArgs& a_, const TokenLists& l_) : a(a_), l(l_), up_tiles(a_.d_ff / 64), down_tiles(a_.d_model / 128), at(blockIdx.x) {}
+    __device__ bool next() {  // false behind the last tile
+        if (up) {
+            if (at < l.groups * up_tiles) {
+                group = at / up_tiles;
+                tile = at - group * up_tiles;
+                stages = (a.d_model * BITS / 8 + 127) / 128;
+                at += gridDim.x;
+                return true;
+            }
+            up = false;
+            at = blockIdx.x;
+        }
+        if (at >= l.groups * down_tiles) return false;
+        group = at / down_tiles;
+        tile = at - group * down_tiles;
+        stages = (a.d_ff * BITS / 8 + 127) / 128;
+        at += gridDim.x;
+        return true;
+    }
+    __device__ uint32_t packed() const { return l.group[group]; }
+};
+
+template <int DT, int BITS>
+__global__ void __launch_bounds__(kTokenThreads, 1)
+    tokens_kernel(const TokensArgs a, const __grid_constant__ CUtensorMap w1_map, const __grid_constant__ CUtensorMap w2_map,
+                  const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap hidden_map, const value_t<DT>* __restrict__ x,
+                  value_t<DT>* __restrict__ out) {
+    constexpr uint32_t P = kParts<BITS, DT>;
+    constexpr uint32_t kAtoms = BITS == 8 ? 1 : 2;        // of a stage and operand
+    constexpr uint32_t kBuffers = BITS == 8 ? 4 : 2;      // stages whose scales tensor memory holds
+    extern __shared__ uint8_t tokens_smem[];
+    uint8_t* ring = tokens_smem + (-smem_u32(tokens_smem) & 1023u);
+    TokensSmem& sm = *reinterpret_cast<TokensSmem*>(ring + a.stages * a.stage_bytes);
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(~0u, (int)(threadIdx.x >> 5), 0);
+    const uint32_t columns_bytes = a.stage_bytes - kTileBytes - kStageScales;
+    if (threadIdx.x == 0) {
+        prefetch_map(&w1_map);
+        prefetch_map(&w2_map);
+        prefetch_map(&x_map);
+        prefetch_map(&hidden_map);
+        for (uint32_t s = 0; s < a.stages; ++s) {
+            mbar_init(&sm.full[s], 4);  // the weights' copy, their scales, the columns' copy, theirs
+            mbar_init(&sm.empty[s], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sm.sums_full[i], 1);
+            mbar_init(&sm.sums_free[i], 4);
+        }
+        mbar_init(&sm.done, 1);
+        sm.abort = 0;
+        mbar_fence_init();
+    }
+    if (warp == 3) {
+        tmem_alloc_one(&sm.tmem, kTokenTmem);
+        tensor_fence_before();
+    }
+    pdl_wait();
+    make_lists(sm.lists, *reinterpret_cast<ListScratch*>(ring), a, kGroupSlots<BITS, DT>);
+    tensor_fence_after();
+    fence_async_all();  // (what the lists were made in becomes the ring)
+    __syncthreads();
+    const uint32_t tmem = sm.tmem, blocks = gridDim.x;
+    volatile int* abort = &sm.abort;
+    TokenWalk<BITS> w(a, sm.lists);
+    const auto stage = [&](uint32_t s) { return ring + s * a.stage_bytes; };
+    const auto scales_of = [&](uint32_t s) { return ring + s * a.stage_bytes + kTileBytes + columns_bytes; };  // the weights', then the columns'
+
+    if (warp == 0) {
+        // copies of weights; they wait for nobody but the tensor cores
+        uint32_t it = 0, s = 0, odd = 1;
+        bool ok = true;
+        while (ok && w.next()) {
+            const int32_t e = (int32_t)group_expert(w.packed());
+            for (uint32_t k = 0; k < w.stages; ++k, ++it) {
+                if (!mbar_wait_soon(&sm.empty[s], odd, abort, a.status)) {
+                    ok = false;
+                    break;
+                }
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&sm.full[s], kTileBytes);
+                    const int32_t k0 = (int32_t)(k * 128);
+                    if (w.up) {
+                        map_load3_one(stage(s), &w1_map, k0, (int32_t)(w.tile * 64), e, &sm.full[s]);
+                        map_load3_one(stage(s) + kTileBytes / 2, &w1_map, k0, (int32_t)(a.d_ff + w.tile * 64), e, &sm.full[s]);
+                    } else {
+                        map_load3_one(stage(s), &w2_map, k0, (int32_t)(w.tile * 128), e, &sm.full[s]);
+                        map_load3_one(stage(s) + kTileBytes / 2, &w2_map, k0, (int32_t)(w.tile * 128 + 64), e, &sm.full[s]);
+                    }
+                }
+                __syncwarp();
+                if (++s == a.stages) s = 0, odd ^= 1;
+            }
+        }
+        if (!ok && lane == 0)  // given up: the copies in flight end before the block does
+            for (uint32_t i = it < a.stages ? 0 : it - a.stages; i < it; ++i) {
+                int none = 0;
+                mbar_wait(&sm.full[i % a.stages], (i / a.stages) & 1, &none, a.status, 1024);
+            }
+        __syncwarp();
+    } else if (warp == 1) {
+        // copies of the tokens' columns and their scale words, behind the blocks that make them
+        uint32_t it = 0, s = 0, odd = 1, back = 0, behind = 0;  // behind: stages whose scales have not been reported yet
+        bool ok = true, was_up = true;
+        const uint32_t rows = a.n_tokens * a.top_k * P;
+        ok = wait_for_all(a.counters, blocks, abort, a.status);
+        fence_async_all();
+        const auto report = [&]() {
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.full[back]);
+            if (++back == a.stages) back = 0;
+            --behind;
+        };
+        while (ok && w.next()) {
+            if (was_up && !w.up) {
+                cp_async_wait<0>();  // (up's last stages, which the blocks' barrier stands behind)
+                while (behind) report();
+                was_up = false;
+                ok = wait_for_all(a.counters + 1, blocks, abort, a.status);
+                fence_async_all();
+                if (!ok) break;
+            }
+            const uint32_t packed = w.packed(), first = group_first(packed) * P, boxes = (group_slots(packed) * P + 15) / 16;
+            const uint32_t* words = (w.up ? a.x_scales : a.hidden_scales) + first;
+            const uint32_t atoms = (w.up ? a.d_model : a.d_ff) / 128, there = rows - first;
+            for (uint32_t k = 0; k < w.stages; ++k, ++it) {
+                if (!mbar_wait_soon(&sm.empty[s], odd, abort, a.status)) {
+                    ok = false;
+                    break;
+                }
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&sm.full[s], boxes * 2048);
+                    for (uint32_t b = 0; b < boxes; ++b)
+                        map_load3_one(stage(s) + kTileBytes + b * 2048, w.up ? &x_map : &hidden_map, (int32_t)(k * 128), (int32_t)(first + b * 16), 0,
+                                      &sm.full[s]);
+                }
+                __syncwarp();
+                uint8_t* to = scales_of(s) + kAtoms * 512 + lane * 16;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (uint32_t i = 0; i < kAtoms; ++i)
+                    for (uint32_t j = 0; j < 4; ++j) {
+                        const uint32_t row = j * 32 + lane;
+                        if (j * 32 < boxes * 16 && row < there && k * kAtoms + i < atoms)
+                            cp_async4(to + i * 512 + j * 4, words + (uint64_t)(k * kAtoms + i) * rows + row);
+                    }
+                cp_async_commit();
+                ++behind;
+                if (++s == a.stages) s = 0, odd ^= 1;
+                if (behind > 2) {  // (two stages' words are on their way)
+                    cp_async_wait<2>();
+                    report();
+                }
+            }
+        }
+        cp_async_wait<0>();
+        while (behind) report();
+        if (!ok && lane == 0)
+            for (uint32_t i = it < a.stages ? 0 : it - a.stages; i < it; ++i) {
+                int none = 0;
+                mbar_wait(&sm.full[i % a.stages], (i / a.stages) & 1, &none, a.status, 1024);
+            }
+        __syncwarp();
+    } else if (warp == 2) {
+        // the weights' scales.  8 bits: a byte for 64 or 128 rows, all over an atom's line; 4 bits: the gate's and up's halves of lines
+        uint32_t s = 0, odd = 1, back = 0, behind = 0;
+        bool ok = true;
+        const auto report = [&]() {
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.full[back]);
+            if (++back == a.stages) back = 0;
+            --behind;
+        };
+        while (ok && w.next()) {
+            const Matrices& m = w.up ? a.w1 : a.w2;
+            const uint32_t lo = w.up ? w.tile * 64 : w.tile * 128, hi = w.up ? a.d_ff + lo : lo + 64;
+            const uint8_t* from = m.scales + group_expert(w.packed()) * m.scales_matrix_stride;
+            const uint8_t* a_line = from + (uint64_t)(lo >> 7) * m.scales_stride;
+            const uint8_t* b_line = from + (uint64_t)(hi >> 7) * m.scales_stride;
+            const uint32_t atoms = (w.up ? a.d_model : a.d_ff) / 128;
+            uint32_t a_bytes = 0, b_bytes = 0;  // lane i: of stage k / 32 * 32 + i
+            for (uint32_t k = 0; k < w.stages; ++k) {
+                if (BITS == 8 && (k & 31) == 0) {
+                    if (k + lane < atoms) a_bytes = __ldg(a_line + k + lane), b_bytes = __ldg(b_line + k + lane);
+                }
+                if (!mbar_wait_soon(&sm.empty[s], odd, abort, a.status)) {
+                    ok = false;
+                    break;
+                }
+                uint8_t* to = scales_of(s) + lane * 16;
+                if constexpr (BITS == 8) {
+                    const uint32_t va = __shfl_sync(~0u, a_bytes, k & 31) * 0x01010101u, vb = __shfl_sync(~0u, b_bytes, k & 31) * 0x01010101u;
+                    *reinterpret_cast<uint4*>(to) = make_uint4(va, va, vb, vb);
+                } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[nt][i] = 0.f;
-                for (uint32_t kb = split; kb < kb_up; kb += a.splits) {
-                    const bool other = group != loaded_group || kb != loaded_kb;
-                    if (other) {
-                        loaded_group = group, loaded_kb = kb;
-                        packed = sm.lists.group[group];
-                        slots = group_slots(packed);
+                    for (uint32_t i = 0; i < kAtoms; ++i)
+                        if (k * kAtoms + i < atoms) {
+                            const uint64_t off = (uint64_t)(k * kAtoms + i) * kAtomBytes + lane * 16;
+                            cp_async8(to + i * 512, a_line + off + (lo & 64 ? 8 : 0));
+                            cp_async8(to + i * 512 + 8, b_line + off + (hi & 64 ? 8 : 0));
+                        }
+                    cp_async_commit();
+                }
+                ++behind;
+                if (++s == a.stages) s = 0, odd ^= 1;
+                if (BITS == 8) {
+                    report();
+                } else if (behind > 2) {
+                    cp_async_wait<2>();
+                    report();
+                }
+            }
+        }
+        cp_async_wait<0>();
+        while (behind) report();
+    } else if (warp == 3) {
+        uint32_t it = 0, s = 0, odd = 0, tile = 0, before = 0, before_odd = 0;  // before: the stage kBuffers ago
+        bool ok = true;
+        const uint32_t stage_units = a.stage_bytes / 16;
+        const uint64_t da0 = operand_descriptor(ring), db0 = operand_descriptor(ring + kTileBytes), ds0 = scales_descriptor(scales_of(0));
+        while (ok && w.next()) {
+            const uint32_t which = tile & 1;
+            if (tile >= 2 && !mbar_wait_soon(&sm.sums_free[which], ((tile >> 1) - 1) & 1, abort, a.status)) break;
+            tensor_fence_after();
+            const uint32_t n = (group_slots(w.packed()) * P + 15) / 16 * 16, d = tmem + which * kSumColumns;
+            const uint32_t instruction = BITS == 8 ? mx_instruction(128, n, 0) : mx4_instruction(128, n);
+            for (uint32_t k = 0; k < w.stages; ++k, ++it) {
+                // (the products whose scales these replace have ended)
+                if (!mbar_wait_soon(&sm.full[s], odd, abort, a.status) || (it >= kBuffers && !mbar_wait_soon(&sm.empty[before], before_odd, abort, a.status))) {
+                    ok = false;
+                    break;
+                }
+                if (it >= kBuffers && ++before == a.stages) before = 0, before_odd ^= 1;
+                tensor_fence_after();
+                const uint32_t sc = tmem + kTokenScalesAt + (it % kBuffers) * (8 * kAtoms);
+                const uint32_t left = w.up ? a.d_model - k * 128 * kAtoms : a.d_ff - k * 128 * kAtoms;  // of the contraction
+                if (elect_one()) {
+                    const uint64_t da = da0 + s * stage_units, db = db0 + s * stage_units, ds = ds0 + s * stage_units;
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            const uint32_t c = nt * 8 + g;
-                            const uint32_t token = c < slots ? sm.lists.token[group_first(packed) + c] : 0u;
-                            const float f = load_tokens<DT, BITS, P>(x_ + token * a.x_stride + kb * 128, c < slots, a.x_wide, xf[nt], t);
-                            scale[nt][0] = __shfl_sync(~0u, f, 8 * t);
-                            scale[nt][1] = __shfl_sync(~0u, f, 8 * t + 4);
+                    for (uint32_t i = 0; i < 2 * kAtoms; ++i) tmem_copy_scales_one(sc + 4 * i, ds + 32 * i);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (BITS == 8) {
+                            tensor_mma_one<8>(d, da + 2 * i, db + 2 * i, instruction + i * mx_byte(1), sc, sc + 4, k > 0 || i > 0);
+                        } else {
+                            if (i < 2 || left > 128)
+                                tensor_mma_one<4>(d, da + 2 * i, db + 2 * i, instruction + (i & 1) * mx_byte(2), sc + 4 * (i >> 1), sc + 8 + 4 * (i >> 1),
+                                                  k > 0 || i > 0);
                         }
                     }
-                    if (BITS == 8 && (other || tile >> 4 != scaled)) {
-                        scaled = tile >> 4;
-                        s_lo = block_scale(a.w1, group_expert(packed), tile * 8, kb);
-                        s_hi = block_scale(a.w1, group_expert(packed), a.d_ff + tile * 8, kb);
-                    }
-                    cp_async_wait<R - 2>();
-                    float sums[NT][4];
-                    multiply_unit<BITS, NT, P>(at, xf, s_lo, s_hi, sums, lane);
-                    advance(at);
-                    copy();
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[nt][j] = fmaf(sums[nt][j], scale[nt][j & 1], acc[nt][j]);
+                    tensor_commit_one(&sm.empty[s]);
+                    if (k + 1 == w.stages) tensor_commit_one(&sm.sums_full[which]);
                 }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float* p = put + nt * 8 * kColumnPitch;
-                    if (nt * 8 + 2 * t < slots) p[0] = acc[nt][0], p[8] = acc[nt][2];
-                    if (nt * 8 + 2 * t + 1 < slots) p[kColumnPitch] = acc[nt][1], p[kColumnPitch + 8] = acc[nt][3];
-                }
-                put += kTokenWarps * NT * 8 * kColumnPitch;
-                task += a.tiles;
-                tile += a.tiles;
+                __syncwarp();
+                if (++s == a.stages) s = 0, odd ^= 1;
             }
-            __syncthreads();
-            // A warp adds up a column of 8 gates and 8 ups, four lanes a sum: column warp % (8 NT) of every (2 / NT)th tile.
-            const uint32_t column = warp % (NT * 8), of_batch = min(batch * a.tiles, to - from - r0 * a.tiles);
-            uint32_t c_in = b_tile + warp / (NT * 8), c_of = b_group;
-            for (uint32_t which = warp / (NT * 8), r = 0, first = 0; which < of_batch; which += 2 / NT, c_in += 2 / NT) {
-                while (c_in >= across) c_in -= across, ++c_of;
-                const uint32_t p = sm.lists.group[c_of];
-                if (column >= group_slots(p)) continue;
-                if (a.tiles == 1) r = which;
-                else r = which / a.tiles, first = (which - r * a.tiles) * a.splits;
-                const float* part = sm.sums + ((r * kTokenWarps + first + (lane >> 3)) * NT * 8 + column) * kColumnPitch + (lane & 7);
-                float gate = 0.f, up_ = 0.f;
-#pragma unroll
-                for (int s = 0; s < kTokenWarps; s += 4)
-                    if (s + (lane >> 3) < a.splits) {
-                        gate += part[s * NT * 8 * kColumnPitch];
-                        up_ += part[s * NT * 8 * kColumnPitch + 8];
-                    }
-#pragma unroll
-                for (int d = 8; d < 32; d <<= 1) {
-                    gate += __shfl_xor_sync(~0u, gate, d);
-                    up_ += __shfl_xor_sync(~0u, up_, d);
-                }
-                float v = swiglu32(gate, up_);
-                if (gate < kLowestGate) v = (float)((double)gate / (1.0 + exp(-(double)gate)) * (double)up_);
-                uint32_t most = __float_as_uint(v) & 0x7fffffffu;
-#pragma unroll
-                for (int d = 1; d < 8; d <<= 1) most = max(most, __shfl_xor_sync(~0u, most, d));
-                const uint32_t e = exponent_of(most), place = group_first(p) + column;
-                if (lane < 8) {
-                    v *= to_half_range(e);
-                    __half* h = reinterpret_cast<__half*>(a.hidden) + (uint64_t)place * P * a.d_ff + c_in * 8 + lane;
-                    const __half hi = __float2half_rn(v);
-                    h[0] = hi;
-                    if (P == 2) h[a.d_ff] = __float2half_rn(rest_of(v, hi));
-                    if (lane == 0) a.exponents[(uint64_t)place * across + c_in] = (uint8_t)e;
-                }
-            }
-            b_tile += batch * a.tiles;
-            while (b_tile >= across) b_tile -= across, ++b_group;
-            if (r0 + batch < rounds) __syncthreads();
+            ++tile;
         }
-    }
-    if (!all_blocks(a, sm.stop)) {
-        cp_async_wait_all();
-        return;
-    }
-
-    float* sums = sm.sums + warp * a.n_tokens * kTokenPitch;
-    HiddenPiece<P> piece[NT];
-    float s_next = 1.f;
-    uint32_t group = w_group, kb = w_kb;  // of `unit`
-    const auto read = [&](uint32_t row) {
-        const uint32_t packed = sm.lists.group[group], slots = group_slots(packed);
-        if (BITS == 8) s_next = block_scale(a.w2, group_expert(packed), row, kb);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) read_hidden<BITS, P>(piece[nt], a, group_first(packed) + nt * 8 + g, kb, nt * 8 + g < slots, t);
-    };
-    for (uint32_t row = blockIdx.x * 16; row < a.d_model; row += gridDim.x * 16) {
-        group = w_group, kb = w_kb;
-        if ((uint32_t)warp < units) read(row);
-        for (uint32_t i = lane; i < a.n_tokens * kTokenPitch; i += 32) sums[i] = 0.f;
+        // nothing that this warp started is in flight when the tensor memory is given back
+        if (elect_one()) tensor_commit_one(&sm.done);
+        int none = 0;
+        mbar_wait_soon(&sm.done, 0, &none, a.status);
         __syncwarp();
-        for (uint32_t unit = warp; unit < units; unit += kTokenWarps) {
-            const uint32_t packed = sm.lists.group[group], slots = group_slots(packed);
-            uint32_t xf[NT][P][16];
-            float f[NT];
-            const float s = s_next;
+    } else {
+        // first the tokens' parts, then what the tensor cores have finished
+        const uint32_t quarter = warp & 3, tid = threadIdx.x - 128;
+        const auto all_four = []() { asm volatile("bar.sync 1, 128;" ::: "memory"); };
+        // (they go on or give up together)
+        const auto all_agree = [](bool ok) {
+            uint32_t r;
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                         : "=r"(r)
+                         : "r"((uint32_t)ok)
+                         : "memory");
+            return r != 0;
+        };
+        const auto done_with = [&](uint32_t* counter) {
+            fence_async_all();  // (written by threads, read by copies)
+            __threadfence();
+            all_four();
+            if (tid == 0) {
+                __threadfence();
+                atomicAdd(counter, 1u);
+            }
+        };
+        const uint32_t kbs = a.d_model / 128;
+        for (uint32_t u = blockIdx.x * 4 + quarter; u < a.n_tokens * kbs; u += blocks * 4) make_parts<DT, BITS>(a, sm.lists, x, u / kbs, u % kbs, lane);
+        done_with(a.counters);
+        uint32_t tile = 0;
+        bool ok = true, was_up = true;
+        while (w.next()) {
+            if (was_up && !w.up) {
+                done_with(a.counters + 1);
+                was_up = false;
+            }
+            const uint32_t which = tile & 1, packed = w.packed(), slots = group_slots(packed), first = group_first(packed);
+            ok = all_agree(mbar_wait_soon(&sm.sums_full[which], (tile >> 1) & 1, abort, a.status, kMaxBarrierPolls + w.stages));
+            if (!ok) break;
+            tensor_fence_after();
+            const uint32_t from = tmem + (quarter << 21) + which * kSumColumns;
+            for (uint32_t slot = 0; slot < slots; ++slot) {
+                uint32_t r[16];
+                tmem_load16(from + slot * P, r);
+                tmem_wait_load();
+                float v = __uint_as_float(r[P - 1]);  // small ones first
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) f[nt] = settle_hidden<BITS, P>(piece[nt], xf[nt], t);
-            kb += kTokenWarps;
-            while (kb >= kb_down) kb -= kb_down, ++group;
-            if (unit + kTokenWarps < units) read(row);
-            cp_async_wait<R - 2>();
-            float part[NT][4];
-            multiply_unit<BITS, NT, P>(at, xf, s, s, part, lane);
-            advance(at);
-            copy();
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t c = nt * 8 + 2 * t + i;
-                    const float fc = __shfl_sync(~0u, f[nt], 8 * t + 4 * i);
-                    if (c >= slots) continue;
-                    const uint32_t place = group_first(packed) + c;
-                    const float w = sm.lists.weight[place];
-                    float* to = sums + sm.lists.token[place] * kTokenPitch + g;
-                    to[0] = fmaf(part[nt][i] * fc, w, to[0]);
-                    to[8] = fmaf(part[nt][2 + i] * fc, w, to[8]);
-                }
+                for (int p = (int)P - 2; p >= 0; --p) v += __uint_as_float(r[p]);
+                if (w.up) sm.exchange[slot][quarter * 32 + lane] = v;
+                else a.rows[(uint64_t)(first + slot) * a.d_model + w.tile * 128 + quarter * 32 + lane] = v;
+            }
+            tensor_fence_before();
             __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.sums_free[which]);
+            if (w.up) {
+                all_four();
+                // a warp has 32 columns of the middle, for every other slot
+                for (uint32_t slot = quarter >> 1; slot < slots; slot += 2) {
+                    const float gate = sm.exchange[slot][(quarter & 1) * 32 + lane], up = sm.exchange[slot][64 + (quarter & 1) * 32 + lane];
+                    float v = swiglu32(gate, up);
+                    if (gate < kLowestGate) v = (float)((double)gate / (1.0 + exp(-(double)gate)) * (double)up);
+                    put_hidden<DT, BITS>(a, v, first + slot, w.tile * 64 + (quarter & 1) * 32, lane);
+                }
+                all_four();
+            }
+            ++tile;
         }
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < a.n_tokens * 16; i += kTokenThreads) {
-            const uint32_t token = i / 16, r = i % 16;
-            float v = 0.f;
-#pragma unroll
-            for (int w = 0; w < kTokenWarps; ++w) v += sm.sums[((uint32_t)w * a.n_tokens + token) * kTokenPitch + r];
-            out[token * a.out_stride + row + r] = ValueOf<DT>::put(v);
+        if (ok) {
+            if (was_up) done_with(a.counters + 1);
+            done_with(a.counters + 2);
         }
-        if (row + gridDim.x * 16 < a.d_model) __syncthreads();
     }
-    cp_async_wait_all();
+    __syncthreads();
+    if (warp == 3) {
+        tensor_fence_after();
+        tmem_free_one(tmem, kTokenTmem);
+    }
+    if (threadIdx.x == 0 && !*abort) wait_for_all(a.counters + 2, blocks, abort, a.status);
+    __syncthreads();
+    if (*abort) return;
+    // a token's rows, in the order of its choices; the last block to leave sets the counters back
+    if (threadIdx.x == 0 && atomicAdd(a.counters + 3, 1u) == blocks - 1)
+        for (int i = 0; i < 4; ++i) a.counters[i] = 0;
+    for (uint32_t i = blockIdx.x * kTokenThreads + threadIdx.x; i < a.n_tokens * a.d_model; i += blocks * kTokenThreads) {
+        const uint32_t token = i / a.d_model, c = i - token * a.d_model;
+        float v = 0.f;
+        for (uint32_t j = 0; j < a.top_k; ++j) {
+            const uint32_t place = sm.lists.place[token * a.top_k + j];
+            if (place != 0xffffu) v = fmaf(__ldg(a.weights + token * a.top_k + j), __ldcg(a.rows + (uint64_t)place * a.d_model + c), v);
+        }
+        out[token * a.out_stride + c] = ValueOf<DT>::put(v);
+    }
 }
 
-template <class K>
-static cudaError_t allow_shared(K kernel, size_t bytes, std::atomic<uint64_t>& allowed) {
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev < 64 && (allowed.load(std::memory_order_relaxed) >> dev & 1)) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e == cudaSuccess && dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
-    return e;
+// Tiles of 128 bytes x `box` rows of [matrices][rows, line] bytes.
+static bool rows_map(CUtensorMap* map, const void* p, uint64_t line, uint64_t rows, uint64_t matrices, uint64_t stride, uint64_t matrix_stride, uint32_t box) {
+    return operand_map(map, p, line, rows, matrices, stride, matrix_stride, box);
 }
 
-template <int DT, int BITS, int NT>
-static cudaError_t launch_tokens(const TokensArgs& a, const void* x, void* out, uint32_t sms, cudaStream_t s) {
-    static std::atomic<uint64_t> allowed{0};
-    constexpr uint64_t most = 4ull * kTokenWarps * CIERA_EXPERT_TOKENS_MAX * kTokenPitch;
-    static_assert(sizeof(TokensSmem<BITS>) + (most > 4 * kBatchFloats<NT> ? most : 4 * kBatchFloats<NT>) <= 227 * 1024, "more than a block may have");
-    const uint64_t down = 4ull * kTokenWarps * a.n_tokens * kTokenPitch, up = 4 * kBatchFloats<NT>;
-    auto kernel = tokens_kernel<DT, BITS, NT>;
-    cudaError_t e = allow_shared(kernel, sizeof(TokensSmem<BITS>) + (most > up ? most : up), allowed);
-    if (e != cudaSuccess) return e;
+struct TokensRoom {  // offsets of the workspace's parts
+    uint64_t x_parts, x_scales, hidden, hidden_scales, rows, all;
+};
+// `parts`: ten suffice for every type and format (five of 8 bits take as much room as ten of 4)
+static TokensRoom tokens_room(uint64_t slots, uint64_t d, uint64_t f, uint64_t bits, uint64_t parts) {
+    const auto up = [](uint64_t v) { return (v + 255) / 256 * 256; };
+    TokensRoom r;
+    r.x_parts = kTokenHead;
+    r.x_scales = r.x_parts + up(slots * parts * d * bits / 8);
+    r.hidden = r.x_scales + up(slots * parts * d / 32);
+    r.hidden_scales = r.hidden + up(slots * parts * f * bits / 8);
+    r.rows = r.hidden_scales + up(slots * parts * f / 32);
+    r.all = r.rows + up(slots * d * 4);
+    return r;
+}
+
+template <int DT, int BITS>
+static cudaError_t launch_tokens(TokensArgs a, const ciera_expert_tokens_args* p, int dev, uint32_t sms, cudaStream_t s) {
+    static std::atomic<uint64_t> allowed{0};  // devices on which this instance may have its shared memory
+    constexpr uint32_t P = kParts<BITS, DT>, kMost = 227 * 1024 - 1024 - sizeof(TokensSmem);
+    const uint64_t slots = (uint64_t)a.n_tokens * a.top_k, d = a.d_model, f = a.d_ff;
+    const TokensRoom room = tokens_room(slots, d, f, BITS, P);
+    uint8_t* const base = (uint8_t*)p->workspace;
+    a.x_parts = base + room.x_parts;
+    a.x_scales = (uint32_t*)(base + room.x_scales);
+    a.hidden = base + room.hidden;
+    a.hidden_scales = (uint32_t*)(base + room.hidden_scales);
+    a.rows = (float*)(base + room.rows);
+    // columns of a group at most (no token is there twice), and the stages that there is room for
+    const uint32_t group = a.n_tokens < kGroupSlots<BITS, DT> ? a.n_tokens : kGroupSlots<BITS, DT>;
+    a.stage_bytes = kTileBytes + (group * P + 15) / 16 * 2048 + kStageScales;
+    a.stages = kMost / a.stage_bytes < (uint32_t)kMostStages ? kMost / a.stage_bytes : (uint32_t)kMostStages;
+    CUtensorMap w1, w2, xm, hm;
+    if (!rows_map(&w1, p->w1, d * BITS / 8, 2 * f, a.n_experts, p->w1_stride, p->w1_matrix_stride, 64) ||
+        !rows_map(&w2, p->w2, f * BITS / 8, d, a.n_experts, p->w2_stride, p->w2_matrix_stride, 64) ||
+        !rows_map(&xm, a.x_parts, d * BITS / 8, slots * P, 1, d * BITS / 8, 0, 16) ||
+        !rows_map(&hm, a.hidden, f * BITS / 8, slots * P, 1, f * BITS / 8, 0, 16))
+        return cudaErrorInvalidValue;
+    auto kernel = tokens_kernel<DT, BITS>;
+    if (dev >= 64 || !(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
     // no more blocks than have work in one of the parts
-    const uint64_t tasks = (uint64_t)a.n_tokens * a.top_k * (a.d_ff / 8), rows = a.d_model / 16, work = tasks > rows ? tasks : rows;
+    const uint64_t up = slots * (f / 64), down = slots * (d / 128), work = up > down ? up : down;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeCooperative;
     at[0].val.cooperative = 1;
@@ -737,11 +787,12 @@ static cudaError_t launch_tokens(const TokensArgs& a, const void* x, void* out, 
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((uint32_t)(work < sms ? work : sms));
     cfg.blockDim = dim3(kTokenThreads);
-    cfg.dynamicSmemBytes = sizeof(TokensSmem<BITS>) + (down > up ? down : up);
+    cfg.dynamicSmemBytes = 1024 + a.stages * a.stage_bytes + sizeof(TokensSmem);
+    if (cfg.dynamicSmemBytes < 1024 + sizeof(ListScratch) + sizeof(TokensSmem)) cfg.dynamicSmemBytes = 1024 + sizeof(ListScratch) + sizeof(TokensSmem);
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, kernel, a, (const value_t<DT>*)x, (value_t<DT>*)out);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a, w1, w2, xm, hm, (const value_t<DT>*)p->x, (value_t<DT>*)p->out);
     if (e == cudaSuccess) count_launch();
     return e;
 }
@@ -750,10 +801,8 @@ static cudaError_t launch_tokens(const TokensArgs& a, const void* x, void* out, 
 
 using namespace ciera;
 
-extern "C" size_t ciera_expert_tokens_workspace_bytes(uint32_t n_tokens, uint32_t top_k, uint32_t d_ff) {
-    // silu(g) * u of every slot in at most two parts of fp16, and an exponent for 8 of them
-    const uint64_t values = (uint64_t)n_tokens * top_k * d_ff;
-    return kTokenHead + 4 * values + (values / 8 + 15) / 16 * 16;
+extern "C" size_t ciera_expert_tokens_workspace_bytes(uint32_t n_tokens, uint32_t top_k, uint32_t d_model, uint32_t d_ff) {
+    return tokens_room((uint64_t)n_tokens * top_k, d_model, d_ff, 4, 10).all;
 }
 
 extern "C" int ciera_expert_tokens(const ciera_expert_tokens_args* p, void* stream) {
@@ -772,6 +821,7 @@ extern "C" int ciera_expert_tokens(const ciera_expert_tokens_args* p, void* stre
         if (stride < line || (rows > 128 && scales_stride < scale_line)) return (int)CIERA_ERR_INVALID_ARG;
         if (!aligned_to(q, 16) || (stride & 15) || (E > 1 && (matrix_stride & 15))) return (int)CIERA_ERR_MISALIGNED;
         if (four && (!aligned_to(scales, 16) || (rows > 128 && (scales_stride & 511)) || (E > 1 && (scales_matrix_stride & 15)))) return (int)CIERA_ERR_MISALIGNED;
+        if (stride >= 1ull << 40 || (E > 1 && matrix_stride >= 1ull << 40)) return (int)CIERA_ERR_UNSUPPORTED;
         return (int)CIERA_OK;
     };
     if (t) {
@@ -781,34 +831,36 @@ extern "C" int ciera_expert_tokens(const ciera_expert_tokens_args* p, void* stre
         if (!aligned_to(p->x, dtype_bytes(p->dtype)) || !aligned_to(p->out, dtype_bytes(p->dtype)) || !aligned_to(p->workspace, 16) ||
             !aligned_to(p->status, 4))
             return CIERA_ERR_MISALIGNED;
-        if (p->workspace_bytes < ciera_expert_tokens_workspace_bytes(p->n_tokens, p->route.top_k, p->d_ff)) return CIERA_ERR_CAPACITY;
+        if (p->workspace_bytes < ciera_expert_tokens_workspace_bytes(p->n_tokens, p->route.top_k, p->d_model, p->d_ff)) return CIERA_ERR_CAPACITY;
     }
-    const int rc = ciera_route(&p->route, p->logits_dtype, p->logits, t, p->logits_stride, p->bias, p->experts, p->weights, stream);
+    int rc = check_route(&p->route, p->logits_dtype, p->logits, t, p->logits_stride, p->bias, p->experts, p->weights);
     if (rc || !t) return rc;
     int dev = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess) return record_cuda_error(e);
-    // warps that share a tile's contraction, at most one 128 columns each, and the tiles that a block then has at a time
-    const uint32_t kb = (uint32_t)(d / 128), splits = kb < kTokenWarps ? kb : kTokenWarps, tiles = kTokenWarps / splits;
-    const uint64_t values = t * p->route.top_k * f, v = dtype_bytes(p->dtype);
-    const bool x_wide = !(((uint64_t)p->x | (t > 1 ? p->x_stride * v : 0)) & 15);
-    uint8_t* room = (uint8_t*)p->workspace + kTokenHead;
-    const TokensArgs a{{(const uint8_t*)p->w1, p->w1_scales, p->w1_stride, p->w1_matrix_stride, p->w1_scales_stride, p->w1_scales_matrix_stride},
-                       {(const uint8_t*)p->w2, p->w2_scales, p->w2_stride, p->w2_matrix_stride, p->w2_scales_stride, p->w2_scales_matrix_stride},
-                       p->experts, p->weights, p->x_stride, p->out_stride, (uint32_t*)p->workspace, p->status, room, room + 4 * values,
-                       (uint32_t)t, p->route.top_k, p->route.n_experts, (uint32_t)d, (uint32_t)f, splits, tiles, x_wide};
+    rc = device_and_sms(&dev, &sms);
+    if (rc) return rc;
+    if (!encode_tiled()) return record_cuda_error(cudaErrorNotSupported);
+    rc = ciera_route(&p->route, p->logits_dtype, p->logits, t, p->logits_stride, p->bias, p->experts, p->weights, stream);
+    if (rc) return rc;
+    const uint64_t v = dtype_bytes(p->dtype);
+    TokensArgs a = {};
+    a.w1 = Matrices{p->w1_scales, p->w1_scales_stride, p->w1_scales_matrix_stride};
+    a.w2 = Matrices{p->w2_scales, p->w2_scales_stride, p->w2_scales_matrix_stride};
+    a.experts = p->experts;
+    a.weights = p->weights;
+    a.x_stride = p->x_stride;
+    a.out_stride = p->out_stride;
+    a.counters = (uint32_t*)p->workspace;
+    a.status = p->status;
+    a.n_tokens = (uint32_t)t;
+    a.top_k = p->route.top_k;
+    a.n_experts = p->route.n_experts;
+    a.d_model = (uint32_t)d;
+    a.d_ff = (uint32_t)f;
+    a.x_wide = !(((uint64_t)p->x | (t > 1 ? p->x_stride * v : 0)) & (4 * v - 1));
+    cudaError_t e = cudaSuccess;
     with_dtype(p->dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        const auto go = [&](auto bits, auto nt) {
-            e = launch_tokens<DT, decltype(bits)::value, decltype(nt)::value>(a, p->x, p->out, (uint32_t)sms, (cudaStream_t)stream);
-        };
-        const std::integral_constant<int, 1> one;
-        const std::integral_constant<int, 2> two;
-        const std::integral_constant<int, 8> eight;
-        const std::integral_constant<int, 4> bits4;
-        if (four) t <= 8 ? go(bits4, one) : go(bits4, two);
-        else t <= 8 ? go(eight, one) : go(eight, two);
+        e = four ? launch_tokens<DT, 4>(a, p, dev, (uint32_t)sms, (cudaStream_t)stream) : launch_tokens<DT, 8>(a, p, dev, (uint32_t)sms, (cudaStream_t)stream);
     });
     if (e != cudaSuccess) return record_cuda_error(e);
     return CIERA_OK;
