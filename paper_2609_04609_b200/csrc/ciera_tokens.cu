@@ -12,7 +12,7 @@
 // tokens 164 us.)
 //
 // One kernel behind the router's, whose blocks all run at once (a cooperative launch):
-//   parts  the tokens' rows as parts, at the places of their slots in the order of the experts
+//   parts  the tokens' rows as parts, while the router still runs
 //   up     tiles of 64 rows of the gate and the same 64 of up; silu(g) * u goes to the workspace as parts again
 //   down   tiles of 128 rows of the output, expert by expert, as fp32 to the workspace
 //   sum    a token's rows, weighted, in the order of its choices
@@ -28,8 +28,10 @@
 
 namespace ciera {
 
-constexpr int kTokenThreads = 256, kTokenWarps = kTokenThreads / 32;
+constexpr int kTokenThreads = 384, kTokenWarps = kTokenThreads / 32;
+constexpr uint32_t kColumnWarps = 4;  // that copy the tokens' columns, a stage each in turn
 constexpr int kMostStages = 10;
+constexpr int kBehind = 5;  // stages whose weights' scales are on their way; fewer than there are stages
 constexpr uint32_t kMaxSlots = CIERA_EXPERT_TOKENS_MAX * 32;
 constexpr uint32_t kMaxColumns = 112;
 constexpr uint32_t kTokenHead = 256;  // bytes of the workspace's counters
@@ -53,26 +55,27 @@ struct TokensArgs {
     uint64_t x_stride, out_stride;
     uint32_t* counters;  // blocks that are done with parts, with up, with down, with all: zero before and after
     int32_t* status;
-    uint8_t* x_parts;        // [slots * parts][d_model], 8 or 4 bits
-    uint32_t* x_scales;      // [d_model / 128][slots * parts]
+    uint8_t* x_parts;        // [tokens * parts][d_model], 8 or 4 bits
+    uint32_t* x_scales;      // [d_model / 128][tokens * parts]
     uint8_t* hidden;         // [slots * parts][d_ff]
     uint32_t* hidden_scales;
     float* rows;             // [slots][d_model]
     uint32_t n_tokens, top_k, n_experts, d_model, d_ff;
     uint32_t stages, stage_bytes;
-    int32_t x_wide;  // x may be read four values at a time
+    int32_t x_wide, out_wide;  // four values at a time
 };
 
 // The slots of the reached experts in the order of the experts, each at a place, and groups of up to `most` of an expert's.
 struct TokenLists {
     uint32_t group[kMaxSlots];   // expert << 16 | slots - 1 << 11 | first place
     uint16_t place[kMaxSlots];   // of a slot; 0xffff: none
+    uint8_t token[kMaxSlots];    // at a place
     uint32_t warp_total[kTokenWarps];
     uint32_t groups;
 };
 struct ListScratch {
     uint32_t at[1024];  // first place of an expert
-    uint8_t count[kMaxSlots / 32 * 1024];  // [32 slots][expert]; n_experts apart
+    uint16_t count[kMaxSlots / 32 * 1024];  // [32 slots][expert], n_experts apart: the expert's slots; then those before
 };
 __device__ __forceinline__ uint32_t group_expert(uint32_t g) { return g >> 16; }
 __device__ __forceinline__ uint32_t group_slots(uint32_t g) { return (g >> 11 & 31u) + 1; }
@@ -95,6 +98,7 @@ __device__ __forceinline__ void make_lists(TokenLists& l, ListScratch& s, const 
             const bool first = rank % most == 0 && e != 0xffffu;  // the lane makes a group
             for (uint32_t i = 0; i < n; ++i) groups += __shfl_sync(~0u, first ? place : ~0u, i) < place;
             if (lane < n) l.place[lane] = (uint16_t)(e == 0xffffu ? 0xffffu : place);
+            if (e != 0xffffu) l.token[place] = (uint8_t)(lane / a.top_k);
             if (first) l.group[groups] = e << 16 | (min(most, count - rank) - 1) << 11 | place;
             const uint32_t all = __popc(__ballot_sync(~0u, first));
             if (lane == 0) l.groups = all;
@@ -103,9 +107,9 @@ __device__ __forceinline__ void make_lists(TokenLists& l, ListScratch& s, const 
         return;
     }
     // slots of an expert are counted for each 32 neighbours, then over those before
-    constexpr int kEach = kMaxSlots / kTokenThreads;
+    constexpr int kEach = (kMaxSlots + kTokenThreads - 1) / kTokenThreads;
     const uint32_t chunks = (n + 31) / 32;
-    for (uint32_t i = tid; i < (chunks * E + 15) / 16; i += kTokenThreads) reinterpret_cast<uint4*>(s.count)[i] = make_uint4(0, 0, 0, 0);
+    for (uint32_t i = tid; i < (chunks * E + 7) / 8; i += kTokenThreads) reinterpret_cast<uint4*>(s.count)[i] = make_uint4(0, 0, 0, 0);
     int32_t id[kEach];
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
@@ -121,49 +125,54 @@ __device__ __forceinline__ void make_lists(TokenLists& l, ListScratch& s, const 
         if (chunk >= chunks) break;
         const uint32_t same = __match_any_sync(~0u, id[j]);
         rank[j] = __popc(same & ((1u << lane) - 1));
-        if (id[j] >= 0 && rank[j] == 0) s.count[chunk * E + id[j]] = (uint8_t)__popc(same);
+        if (id[j] >= 0 && rank[j] == 0) s.count[chunk * E + id[j]] = (uint16_t)__popc(same);
     }
     __syncthreads();
-    // places and groups before each expert, four experts a thread: slots in the low half, groups in the high one
-    uint32_t count[4], v[4], sum = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t e = 4 * tid + i;
-        count[i] = 0;
-        if (e < E)
-            for (uint32_t c = 0; c < chunks; ++c) count[i] += s.count[c * E + e];
-        v[i] = count[i] | (count[i] + most - 1) / most << 16;
-        sum += v[i];
-    }
-    const uint32_t own = sum;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t o = __shfl_up_sync(~0u, sum, d);
-        if (lane >= (uint32_t)d) sum += o;
-    }
-    if (lane == 31) l.warp_total[warp] = sum;
-    __syncthreads();
+    // an expert's slots before each 32, then places and groups before each expert, a thread for each (of 256 at a time): slots in the
+    // low half, groups in the high one
     uint32_t base = 0;
-    for (uint32_t w = 0; w < warp; ++w) base += l.warp_total[w];
-    if (tid == kTokenThreads - 1) l.groups = (base + sum) >> 16;
-    uint32_t before = base + sum - own;
+    for (uint32_t e0 = 0; e0 < E; e0 += kTokenThreads) {
+        const uint32_t e = e0 + tid;
+        uint32_t count = 0;
+        if (e < E)
+#pragma unroll 4
+            for (uint32_t c = 0; c < chunks; ++c) {
+                const uint32_t v = s.count[c * E + e];
+                s.count[c * E + e] = (uint16_t)count;
+                count += v;
+            }
+        const uint32_t v = count | (count + most - 1) / most << 16;
+        uint32_t sum = v;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t e = 4 * tid + i, at = before & 0xffffu;
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t o = __shfl_up_sync(~0u, sum, d);
+            if (lane >= (uint32_t)d) sum += o;
+        }
+        if (lane == 31) l.warp_total[warp] = sum;
+        __syncthreads();
+        uint32_t before = base;
+#pragma unroll
+        for (uint32_t w = 0; w < kTokenWarps; ++w) {
+            const uint32_t o = l.warp_total[w];
+            if (w < warp) before += o;
+            base += o;
+        }
+        before += sum - v;
         uint32_t g = before >> 16;
-        for (uint32_t c = 0; c < count[i]; c += most, ++g) l.group[g] = e << 16 | (min(most, count[i] - c) - 1) << 11 | (at + c);
-        s.at[e] = at;
-        before += v[i];
+        const uint32_t at = before & 0xffffu;
+        for (uint32_t c = 0; c < count; c += most, ++g) l.group[g] = e << 16 | (min(most, count - c) - 1) << 11 | (at + c);
+        if (e < E) s.at[e] = at;
+        __syncthreads();
     }
-    __syncthreads();
+    if (tid == 0) l.groups = base >> 16;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
         const uint32_t chunk = j * kTokenWarps + warp, slot = j * kTokenThreads + tid;
         if (chunk >= chunks) break;
         uint32_t place = 0xffffu;
         if (id[j] >= 0) {
-            place = s.at[id[j]] + rank[j];
-            for (uint32_t i = 0; i < chunk; ++i) place += s.count[i * E + id[j]];
+            place = s.at[id[j]] + s.count[chunk * E + id[j]] + rank[j];
+            l.token[place] = (uint8_t)(slot / a.top_k);
         }
         if (slot < n) l.place[slot] = (uint16_t)place;
     }
@@ -211,10 +220,9 @@ __device__ __forceinline__ uint32_t take_part4(float (&v)[4], float inv, float u
     return r;
 }
 
-// 128 values of a token, four a lane, as parts at all its places.
+// 128 values of a token, four a lane, as parts.
 template <int DT, int BITS>
-__device__ __forceinline__ void make_parts(const TokensArgs& a, const TokenLists& l, const value_t<DT>* __restrict__ x, uint32_t token, uint32_t kb,
-                                           uint32_t lane) {
+__device__ __forceinline__ void make_parts(const TokensArgs& a, const value_t<DT>* __restrict__ x, uint32_t token, uint32_t kb, uint32_t lane) {
     constexpr uint32_t P = kParts<BITS, DT>;
     float v[4];
     const value_t<DT>* from = x + token * a.x_stride + kb * 128 + lane * 4;
@@ -224,8 +232,7 @@ __device__ __forceinline__ void make_parts(const TokensArgs& a, const TokenLists
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = ValueOf<DT>::get(from[i]);
     }
-    const uint32_t rows = a.n_tokens * a.top_k * P;
-    uint32_t word[P], bytes[P];
+    const uint32_t rows = a.n_tokens * P;
 #pragma unroll
     for (uint32_t p = 0; p < P; ++p) {
         uint32_t amax = 0;
@@ -233,31 +240,23 @@ __device__ __forceinline__ void make_parts(const TokensArgs& a, const TokenLists
         for (int i = 0; i < 4; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);
 #pragma unroll
         for (int d = 1; d < 8; d <<= 1) amax = max(amax, __shfl_xor_sync(~0u, amax, d));
-        const uint32_t byte = part_byte<BITS>(amax);
+        const uint32_t byte = part_byte<BITS>(amax), row = token * P + p;
         const float inv = part_inverse(byte), unit = __uint_as_float(byte << 23);
-        if constexpr (BITS == 8) word[p] = take_part8(v, inv, unit);
-        else word[p] = take_part4(v, inv, unit);
+        uint32_t word;
+        if constexpr (BITS == 8) word = take_part8(v, inv, unit);
+        else word = take_part4(v, inv, unit);
         if (byte == 255u) {  // NaN by its scale; nothing is left
-            word[p] = 0;
+            word = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = 0.f;
         }
+        if constexpr (BITS == 8) *reinterpret_cast<uint32_t*>(a.x_parts + (uint64_t)row * a.d_model + kb * 128 + lane * 4) = word;
+        else *reinterpret_cast<uint16_t*>(a.x_parts + (uint64_t)row * (a.d_model / 2) + kb * 64 + lane * 2) = (uint16_t)word;
         // the four groups' bytes
         uint32_t all = byte << (lane >> 3) * 8;
         all |= __shfl_xor_sync(~0u, all, 8);
         all |= __shfl_xor_sync(~0u, all, 16);
-        bytes[p] = all;
-    }
-    for (uint32_t j = 0; j < a.top_k; ++j) {
-        const uint32_t place = l.place[token * a.top_k + j];
-        if (place == 0xffffu) continue;
-#pragma unroll
-        for (uint32_t p = 0; p < P; ++p) {
-            const uint32_t row = place * P + p;
-            if constexpr (BITS == 8) *reinterpret_cast<uint32_t*>(a.x_parts + (uint64_t)row * a.d_model + kb * 128 + lane * 4) = word[p];
-            else *reinterpret_cast<uint16_t*>(a.x_parts + (uint64_t)row * (a.d_model / 2) + kb * 64 + lane * 2) = (uint16_t)word[p];
-            if (lane == p) a.x_scales[(uint64_t)kb * rows + row] = bytes[p];
-        }
+        if (lane == 0) a.x_scales[(uint64_t)kb * rows + row] = all;
     }
 }
 
@@ -351,6 +350,14 @@ constexpr uint32_t kStageScales = 4 * 512;  // a stage's scale bytes: two atoms 
 // a stage: the weights' tile, the tokens' columns, the scales of both
 static_assert(sizeof(TokensSmem) + 1024 + sizeof(ListScratch) <= 227 * 1024, "more than a block may have");
 
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok)
+                 : "r"(smem_u32(bar)), "r"(parity)
+                 : "memory");
+    return ok != 0;
+}
 // All blocks have added to a counter.  false: the bounded wait ran out, or another of the block's has.
 __device__ __forceinline__ bool wait_for_all(const uint32_t* counter, uint32_t blocks, volatile int* abort, int32_t* status) {
     for (uint32_t polls = 0; polls < kMaxPolls; ++polls) {
@@ -427,9 +434,24 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         sm.abort = 0;
         mbar_fence_init();
     }
-    if (warp == 3) {
+    const uint32_t tid = threadIdx.x & 127;  // of the last four warps, which compute
+    const auto all_four = []() { asm volatile("bar.sync 1, 128;" ::: "memory"); };
+    const auto done_with = [&](uint32_t* counter) {
+        all_four();
+        if (tid == 0) {
+            __threadfence();
+            atomicAdd(counter, 1u);
+        }
+    };
+    if (warp == 2) {
         tmem_alloc_one(&sm.tmem, kTokenTmem);
         tensor_fence_before();
+    } else if (warp >= 8) {
+        // Before the router has ended: it lets this kernel begin when all that came before it has, the call before this one and whatever
+        // wrote x.
+        const uint32_t kbs = a.d_model / 128;
+        for (uint32_t u = blockIdx.x * 4 + (warp & 3); u < a.n_tokens * kbs; u += gridDim.x * 4) make_parts<DT, BITS>(a, x, u / kbs, u % kbs, lane);
+        done_with(a.counters);
     }
     pdl_wait();
     make_lists(sm.lists, *reinterpret_cast<ListScratch*>(ring), a, kGroupSlots<BITS, DT>);
@@ -475,69 +497,6 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
             }
         __syncwarp();
     } else if (warp == 1) {
-        // copies of the tokens' columns and their scale words, behind the blocks that make them
-        uint32_t it = 0, s = 0, odd = 1, back = 0, behind = 0;  // behind: stages whose scales have not been reported yet
-        bool ok = true, was_up = true;
-        const uint32_t rows = a.n_tokens * a.top_k * P;
-        ok = wait_for_all(a.counters, blocks, abort, a.status);
-        fence_async_all();
-        const auto report = [&]() {
-            fence_async_shared();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.full[back]);
-            if (++back == a.stages) back = 0;
-            --behind;
-        };
-        while (ok && w.next()) {
-            if (was_up && !w.up) {
-                cp_async_wait<0>();  // (up's last stages, which the blocks' barrier stands behind)
-                while (behind) report();
-                was_up = false;
-                ok = wait_for_all(a.counters + 1, blocks, abort, a.status);
-                fence_async_all();
-                if (!ok) break;
-            }
-            const uint32_t packed = w.packed(), first = group_first(packed) * P, boxes = (group_slots(packed) * P + 15) / 16;
-            const uint32_t* words = (w.up ? a.x_scales : a.hidden_scales) + first;
-            const uint32_t atoms = (w.up ? a.d_model : a.d_ff) / 128, there = rows - first;
-            for (uint32_t k = 0; k < w.stages; ++k, ++it) {
-                if (!mbar_wait_soon(&sm.empty[s], odd, abort, a.status)) {
-                    ok = false;
-                    break;
-                }
-                if (elect_one()) {
-                    mbar_arrive_expect_tx(&sm.full[s], boxes * 2048);
-                    for (uint32_t b = 0; b < boxes; ++b)
-                        map_load3_one(stage(s) + kTileBytes + b * 2048, w.up ? &x_map : &hidden_map, (int32_t)(k * 128), (int32_t)(first + b * 16), 0,
-                                      &sm.full[s]);
-                }
-                __syncwarp();
-                uint8_t* to = scales_of(s) + kAtoms * 512 + lane * 16;
-#pragma unroll
-                for (uint32_t i = 0; i < kAtoms; ++i)
-                    for (uint32_t j = 0; j < 4; ++j) {
-                        const uint32_t row = j * 32 + lane;
-                        if (j * 32 < boxes * 16 && row < there && k * kAtoms + i < atoms)
-                            cp_async4(to + i * 512 + j * 4, words + (uint64_t)(k * kAtoms + i) * rows + row);
-                    }
-                cp_async_commit();
-                ++behind;
-                if (++s == a.stages) s = 0, odd ^= 1;
-                if (behind > 2) {  // (two stages' words are on their way)
-                    cp_async_wait<2>();
-                    report();
-                }
-            }
-        }
-        cp_async_wait<0>();
-        while (behind) report();
-        if (!ok && lane == 0)
-            for (uint32_t i = it < a.stages ? 0 : it - a.stages; i < it; ++i) {
-                int none = 0;
-                mbar_wait(&sm.full[i % a.stages], (i / a.stages) & 1, &none, a.status, 1024);
-            }
-        __syncwarp();
-    } else if (warp == 2) {
         // the weights' scales.  8 bits: a byte for 64 or 128 rows, all over an atom's line; 4 bits: the gate's and up's halves of lines
         uint32_t s = 0, odd = 1, back = 0, behind = 0;
         bool ok = true;
@@ -582,15 +541,15 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
                 if (++s == a.stages) s = 0, odd ^= 1;
                 if (BITS == 8) {
                     report();
-                } else if (behind > 2) {
-                    cp_async_wait<2>();
+                } else if (behind > kBehind) {
+                    cp_async_wait<kBehind>();
                     report();
                 }
             }
         }
         cp_async_wait<0>();
         while (behind) report();
-    } else if (warp == 3) {
+    } else if (warp == 2) {
         uint32_t it = 0, s = 0, odd = 0, tile = 0, before = 0, before_odd = 0;  // before: the stage kBuffers ago
         bool ok = true;
         const uint32_t stage_units = a.stage_bytes / 16;
@@ -638,10 +597,90 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         int none = 0;
         mbar_wait_soon(&sm.done, 0, &none, a.status);
         __syncwarp();
-    } else {
-        // first the tokens' parts, then what the tensor cores have finished
-        const uint32_t quarter = warp & 3, tid = threadIdx.x - 128;
-        const auto all_four = []() { asm volatile("bar.sync 1, 128;" ::: "memory"); };
+    } else if (warp >= 4 && warp < 8) {
+        // copies of the tokens' columns and their scale words, behind the blocks that make them; every fourth stage.  (By one warp
+        // 64 tokens took 107 us.)
+        uint32_t it = 0, s = 0, odd = 1, last = 0;  // last: the warp's stage whose words are on their way
+        bool ok, was_up = true, some = false;
+        ok = wait_for_all(a.counters, blocks, abort, a.status);
+        fence_async_all();  // (written by threads, read by copies)
+        const auto report = [&]() {
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.full[last]);
+            some = false;
+        };
+        while (ok && w.next()) {
+            if (was_up && !w.up) {
+                cp_async_wait<0>();  // (up's last stages, which the blocks' barrier stands behind)
+                if (some) report();
+                was_up = false;
+                ok = wait_for_all(a.counters + 1, blocks, abort, a.status);
+                fence_async_all();
+                if (!ok) break;
+            }
+            const uint32_t packed = w.packed(), first = group_first(packed), slots = group_slots(packed);
+            const uint32_t atoms = (w.up ? a.d_model : a.d_ff) / 128, rows = a.n_tokens * (w.up ? 1 : a.top_k) * P;
+            const uint32_t boxes = (slots * P + 15) / 16, there = min(boxes * 16, rows - (w.up ? 0 : first * P));
+            const uint32_t* words = w.up ? a.x_scales : a.hidden_scales;
+            uint32_t row[4];  // of the lane's columns lane + 32 * j; none: rows
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                const uint32_t n = j * 32 + lane, slot = n / P;
+                row[j] = rows;
+                if (w.up) {
+                    if (slot < slots) row[j] = sm.lists.token[first + slot] * P + n - slot * P;
+                } else if (n < there) {
+                    row[j] = first * P + n;
+                }
+            }
+            for (uint32_t k = 0; k < w.stages; ++k, ++it) {
+                const uint32_t s_now = s, odd_now = odd;
+                if (++s == a.stages) s = 0, odd ^= 1;
+                if ((it & (kColumnWarps - 1)) != (uint32_t)(warp & 3)) continue;
+                if (some && !__all_sync(~0u, mbar_test(&sm.empty[s_now], odd_now))) {  // no room yet
+                    cp_async_wait<0>();
+                    report();
+                }
+                if (!mbar_wait_soon(&sm.empty[s_now], odd_now, abort, a.status)) {
+                    ok = false;
+                    break;
+                }
+                // up: a token's parts at a time; down: they lie one behind the other
+                if (elect_one()) {
+                    uint8_t* to = stage(s_now) + kTileBytes;
+                    if (w.up) {
+                        mbar_arrive_expect_tx(&sm.full[s_now], slots * P * 128);
+                        for (uint32_t i = 0; i < slots; ++i)
+                            map_load3_one(to + i * P * 128, &x_map, (int32_t)(k * 128), (int32_t)(sm.lists.token[first + i] * P), 0, &sm.full[s_now]);
+                    } else {
+                        mbar_arrive_expect_tx(&sm.full[s_now], boxes * 2048);
+                        for (uint32_t i = 0; i < boxes; ++i)
+                            map_load3_one(to + i * 2048, &hidden_map, (int32_t)(k * 128), (int32_t)(first * P + i * 16), 0, &sm.full[s_now]);
+                    }
+                }
+                __syncwarp();
+                uint8_t* to = scales_of(s_now) + kAtoms * 512 + lane * 16;
+#pragma unroll
+                for (uint32_t i = 0; i < kAtoms; ++i)
+#pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j)
+                        if (row[j] < rows && k * kAtoms + i < atoms) cp_async4(to + i * 512 + j * 4, words + (uint64_t)(k * kAtoms + i) * rows + row[j]);
+                cp_async_commit();
+                if (some) {
+                    cp_async_wait<1>();
+                    report();
+                }
+                last = s_now;
+                some = true;
+            }
+        }
+        cp_async_wait<0>();
+        if (some) report();
+        __syncwarp();
+    } else if (warp >= 8) {
+        // what the tensor cores have finished
+        const uint32_t quarter = warp & 3;
         // (they go on or give up together)
         const auto all_agree = [](bool ok) {
             uint32_t r;
@@ -651,18 +690,6 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
                          : "memory");
             return r != 0;
         };
-        const auto done_with = [&](uint32_t* counter) {
-            fence_async_all();  // (written by threads, read by copies)
-            __threadfence();
-            all_four();
-            if (tid == 0) {
-                __threadfence();
-                atomicAdd(counter, 1u);
-            }
-        };
-        const uint32_t kbs = a.d_model / 128;
-        for (uint32_t u = blockIdx.x * 4 + quarter; u < a.n_tokens * kbs; u += blocks * 4) make_parts<DT, BITS>(a, sm.lists, x, u / kbs, u % kbs, lane);
-        done_with(a.counters);
         uint32_t tile = 0;
         bool ok = true, was_up = true;
         while (w.next()) {
@@ -707,7 +734,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         }
     }
     __syncthreads();
-    if (warp == 3) {
+    if (warp == 2) {
         tensor_fence_after();
         tmem_free_one(tmem, kTokenTmem);
     }
@@ -717,32 +744,52 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
     // a token's rows, in the order of its choices; the last block to leave sets the counters back
     if (threadIdx.x == 0 && atomicAdd(a.counters + 3, 1u) == blocks - 1)
         for (int i = 0; i < 4; ++i) a.counters[i] = 0;
-    for (uint32_t i = blockIdx.x * kTokenThreads + threadIdx.x; i < a.n_tokens * a.d_model; i += blocks * kTokenThreads) {
-        const uint32_t token = i / a.d_model, c = i - token * a.d_model;
-        float v = 0.f;
-        for (uint32_t j = 0; j < a.top_k; ++j) {
-            const uint32_t place = sm.lists.place[token * a.top_k + j];
-            if (place != 0xffffu) v = fmaf(__ldg(a.weights + token * a.top_k + j), __ldcg(a.rows + (uint64_t)place * a.d_model + c), v);
+    const uint32_t quads = a.d_model / 4;
+    for (uint32_t i = blockIdx.x * kTokenThreads + threadIdx.x; i < a.n_tokens * quads; i += blocks * kTokenThreads) {
+        const uint32_t token = i / quads, c = (i - token * quads) * 4;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (uint32_t j0 = 0; j0 < a.top_k; j0 += 8) {
+            float4 r[8];
+            float wt[8];
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) {
+                const uint32_t place = j0 + j < a.top_k ? sm.lists.place[token * a.top_k + j0 + j] : 0xffffu;
+                r[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                wt[j] = 0.f;
+                if (place != 0xffffu) {
+                    r[j] = __ldcg(reinterpret_cast<const float4*>(a.rows + (uint64_t)place * a.d_model + c));
+                    wt[j] = __ldg(a.weights + token * a.top_k + j0 + j);
+                }
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) {
+                v[0] = fmaf(wt[j], r[j].x, v[0]);
+                v[1] = fmaf(wt[j], r[j].y, v[1]);
+                v[2] = fmaf(wt[j], r[j].z, v[2]);
+                v[3] = fmaf(wt[j], r[j].w, v[3]);
+            }
         }
-        out[token * a.out_stride + c] = ValueOf<DT>::put(v);
+        value_t<DT>* to = out + token * a.out_stride + c;
+        if (a.out_wide) {
+            store_values<DT, 4>(to, v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to[j] = ValueOf<DT>::put(v[j]);
+        }
     }
-}
-
-// Tiles of 128 bytes x `box` rows of [matrices][rows, line] bytes.
-static bool rows_map(CUtensorMap* map, const void* p, uint64_t line, uint64_t rows, uint64_t matrices, uint64_t stride, uint64_t matrix_stride, uint32_t box) {
-    return operand_map(map, p, line, rows, matrices, stride, matrix_stride, box);
 }
 
 struct TokensRoom {  // offsets of the workspace's parts
     uint64_t x_parts, x_scales, hidden, hidden_scales, rows, all;
 };
 // `parts`: ten suffice for every type and format (five of 8 bits take as much room as ten of 4)
-static TokensRoom tokens_room(uint64_t slots, uint64_t d, uint64_t f, uint64_t bits, uint64_t parts) {
+static TokensRoom tokens_room(uint64_t tokens, uint64_t top_k, uint64_t d, uint64_t f, uint64_t bits, uint64_t parts) {
+    const uint64_t slots = tokens * top_k;
     const auto up = [](uint64_t v) { return (v + 255) / 256 * 256; };
     TokensRoom r;
     r.x_parts = kTokenHead;
-    r.x_scales = r.x_parts + up(slots * parts * d * bits / 8);
-    r.hidden = r.x_scales + up(slots * parts * d / 32);
+    r.x_scales = r.x_parts + up(tokens * parts * d * bits / 8);
+    r.hidden = r.x_scales + up(tokens * parts * d / 32);
     r.hidden_scales = r.hidden + up(slots * parts * f * bits / 8);
     r.rows = r.hidden_scales + up(slots * parts * f / 32);
     r.all = r.rows + up(slots * d * 4);
@@ -754,7 +801,7 @@ static cudaError_t launch_tokens(TokensArgs a, const ciera_expert_tokens_args* p
     static std::atomic<uint64_t> allowed{0};  // devices on which this instance may have its shared memory
     constexpr uint32_t P = kParts<BITS, DT>, kMost = 227 * 1024 - 1024 - sizeof(TokensSmem);
     const uint64_t slots = (uint64_t)a.n_tokens * a.top_k, d = a.d_model, f = a.d_ff;
-    const TokensRoom room = tokens_room(slots, d, f, BITS, P);
+    const TokensRoom room = tokens_room(a.n_tokens, a.top_k, d, f, BITS, P);
     uint8_t* const base = (uint8_t*)p->workspace;
     a.x_parts = base + room.x_parts;
     a.x_scales = (uint32_t*)(base + room.x_scales);
@@ -766,10 +813,10 @@ static cudaError_t launch_tokens(TokensArgs a, const ciera_expert_tokens_args* p
     a.stage_bytes = kTileBytes + (group * P + 15) / 16 * 2048 + kStageScales;
     a.stages = kMost / a.stage_bytes < (uint32_t)kMostStages ? kMost / a.stage_bytes : (uint32_t)kMostStages;
     CUtensorMap w1, w2, xm, hm;
-    if (!rows_map(&w1, p->w1, d * BITS / 8, 2 * f, a.n_experts, p->w1_stride, p->w1_matrix_stride, 64) ||
-        !rows_map(&w2, p->w2, f * BITS / 8, d, a.n_experts, p->w2_stride, p->w2_matrix_stride, 64) ||
-        !rows_map(&xm, a.x_parts, d * BITS / 8, slots * P, 1, d * BITS / 8, 0, 16) ||
-        !rows_map(&hm, a.hidden, f * BITS / 8, slots * P, 1, f * BITS / 8, 0, 16))
+    if (!operand_map(&w1, p->w1, d * BITS / 8, 2 * f, a.n_experts, p->w1_stride, p->w1_matrix_stride, 64) ||
+        !operand_map(&w2, p->w2, f * BITS / 8, d, a.n_experts, p->w2_stride, p->w2_matrix_stride, 64) ||
+        !operand_map(&xm, a.x_parts, d * BITS / 8, (uint64_t)a.n_tokens * P, 1, d * BITS / 8, 0, P) ||
+        !operand_map(&hm, a.hidden, f * BITS / 8, slots * P, 1, f * BITS / 8, 0, 16))
         return cudaErrorInvalidValue;
     auto kernel = tokens_kernel<DT, BITS>;
     if (dev >= 64 || !(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
@@ -802,7 +849,7 @@ static cudaError_t launch_tokens(TokensArgs a, const ciera_expert_tokens_args* p
 using namespace ciera;
 
 extern "C" size_t ciera_expert_tokens_workspace_bytes(uint32_t n_tokens, uint32_t top_k, uint32_t d_model, uint32_t d_ff) {
-    return tokens_room((uint64_t)n_tokens * top_k, d_model, d_ff, 4, 10).all;
+    return tokens_room(n_tokens, top_k, d_model, d_ff, 4, 10).all;
 }
 
 extern "C" int ciera_expert_tokens(const ciera_expert_tokens_args* p, void* stream) {
@@ -857,6 +904,7 @@ extern "C" int ciera_expert_tokens(const ciera_expert_tokens_args* p, void* stre
     a.d_model = (uint32_t)d;
     a.d_ff = (uint32_t)f;
     a.x_wide = !(((uint64_t)p->x | (t > 1 ? p->x_stride * v : 0)) & (4 * v - 1));
+    a.out_wide = !(((uint64_t)p->out | (t > 1 ? p->out_stride * v : 0)) & (4 * v - 1));
     cudaError_t e = cudaSuccess;
     with_dtype(p->dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
