@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -190,6 +191,13 @@ for _name, (_args, _res) in _SIGS.items():
     _f.argtypes, _f.restype = _args, _res
 
 EXPORTS = tuple(_SIGS)
+
+# ``ciera_expert_tokens`` with its many arguments packed in one go: a few microseconds less than a structure takes, of a call whose
+# kernels take sixteen.
+_TOKENS = struct.Struct("=32s6i24Q")
+assert _TOKENS.size == ctypes.sizeof(_ExpertTokens)
+_tokens = _lib["ciera_expert_tokens"]
+_tokens.argtypes, _tokens.restype = [ctypes.c_char_p, _vp], _i32
 
 
 class CieraError(RuntimeError):
@@ -662,20 +670,25 @@ def _codes(where: str, device: int, t, rows: int, cols: int):
 
 def _atom_lines(where: str, device: int, t, rows: int, cols: int):
     """The address and the stride of the lines of scale bytes [ceil(rows / 128), ceil(cols / 128), 512]."""
-    if not isinstance(t, _Tensor) or t.dtype is not _U8 or t.get_device() != device or \
-            t.shape != (-(-rows // 128), -(-cols // 128), FP4_ATOM) or t.stride(2) != 1 or \
-            (t.shape[1] > 1 and t.stride(1) != FP4_ATOM):
+    atoms = -(-cols // 128)
+    if not isinstance(t, _Tensor) or t.dtype is not _U8 or t.shape != (-(-rows // 128), atoms, FP4_ATOM) or t.get_device() != device:
         raise CieraError(where, ERR_INVALID_ARG)
-    return t.data_ptr(), t.stride(0)
+    stride = t.stride()
+    if stride[2] != 1 or (stride[1] != FP4_ATOM and atoms > 1):
+        raise CieraError(where, ERR_INVALID_ARG)
+    return t.data_ptr(), stride[0]
 
 
 def _atom_stack(where: str, device: int, t, matrices: int, rows: int, cols: int):
     """The same of [matrices, ...], and the stride of the matrices."""
-    if not isinstance(t, _Tensor) or t.dim() != 4 or t.shape[0] != matrices:
+    atoms = -(-cols // 128)
+    if not isinstance(t, _Tensor) or t.dtype is not _U8 or t.shape != (matrices, -(-rows // 128), atoms, FP4_ATOM) or \
+            t.get_device() != device:
         raise CieraError(where, ERR_INVALID_ARG)
-    if not matrices:
-        return t.data_ptr(), t.stride(1), t.stride(0)
-    return (*_atom_lines(where, device, t[0], rows, cols), t.stride(0))
+    stride = t.stride()
+    if stride[3] != 1 or (stride[2] != FP4_ATOM and atoms > 1):
+        raise CieraError(where, ERR_INVALID_ARG)
+    return t.data_ptr(), stride[1], stride[0]
 
 
 def fp4_quantize_rows(x, q, scales, *, kind: int = SOURCE_ROWS, slot_of_row=None, top_k: int = 1, starts=None,
@@ -792,31 +805,33 @@ def expert_tokens(config: RouteConfig, x, logits, bias, w1, w1_scales, w2, w2_sc
     next."""
     w = "ciera_expert_tokens"
     device = _device_of(w, x)
+    dtype = x.dtype
     code = _code(w, x)
-    x_at = _matrix(w, device, x, None, x.dtype)
-    t, d = x.shape
-    logits_at = _matrix(w, device, logits, (t, config.n_experts), logits.dtype) if isinstance(logits, _Tensor) else _refuse(w)
-    logits_code = _code(w, logits)
+    x_at = _matrix(w, device, x, None, dtype)
+    t, d = shape = x.shape
     e, k = config.n_experts, config.top_k
-    four = isinstance(w1, _Tensor) and w1.dtype is _U8
-    of, wide = (_U8, 2) if four else (_E4M3, 1)
-    if not isinstance(w1, _Tensor) or w1.dim() != 3 or w1.shape[1] % 2:
+    if not isinstance(logits, _Tensor) or not isinstance(w1, _Tensor) or w1.dim() != 3 or w1.shape[1] % 2 or not isinstance(workspace, _Tensor):
         _refuse(w)
+    logits_code = _code(w, logits)
     f = w1.shape[1] // 2
-    at = []
-    for q, s, rows, cols in ((w1, w1_scales, 2 * f, d), (w2, w2_scales, d, f)):
-        at += _matrices(w, device, q, (e, rows, cols // wide), of)
-        at += _atom_stack(w, device, s, e, rows, cols) if four else \
-            _matrices(w, device, s, (e, -(-rows // FP8_BLOCK), -(-cols // FP8_BLOCK)), _U8)
-    if not isinstance(workspace, _Tensor):
-        _refuse(w)
+    if w1.dtype is _U8:
+        form = WEIGHTS_FP4
+        at = (*_matrices(w, device, w1, (e, 2 * f, d // 2), _U8), *_atom_stack(w, device, w1_scales, e, 2 * f, d),
+              *_matrices(w, device, w2, (e, d, f // 2), _U8), *_atom_stack(w, device, w2_scales, e, d, f))
+    else:
+        form = WEIGHTS_FP8
+        fb, db = -(-f // FP8_BLOCK), -(-d // FP8_BLOCK)
+        at = (*_matrices(w, device, w1, (e, 2 * f, d), _E4M3),
+              *_matrices(w, device, w1_scales, (e, -(-2 * f // FP8_BLOCK), db), _U8),
+              *_matrices(w, device, w2, (e, d, f), _E4M3), *_matrices(w, device, w2_scales, (e, db, fb), _U8))
+    choice = (t, k)
     room = workspace.numel()
-    args = _ExpertTokens(config, WEIGHTS_FP4 if four else WEIGHTS_FP8, code, logits_code, t, d, f, *x_at, *logits_at,
-                         None if bias is None else _whole(w, device, bias, (e,), _F32), *at,
-                         *_matrix(w, device, out, (t, d), x.dtype), _whole(w, device, experts, (t, k), _I32),
-                         _whole(w, device, weights, (t, k), _F32), _whole(w, device, workspace, (room,), _U8), room,
-                         None if status is None else _whole(w, device, status, (1,), _I32))
-    _enqueue(w, device, stream, _lib.ciera_expert_tokens, args)
+    args = _TOKENS.pack(bytes(config), form, code, logits_code, t, d, f, *x_at, *_matrix(w, device, logits, (t, e), logits.dtype),
+                        0 if bias is None else _whole(w, device, bias, (e,), _F32), *at, *_matrix(w, device, out, shape, dtype),
+                        _whole(w, device, experts, choice, _I32), _whole(w, device, weights, choice, _F32),
+                        _whole(w, device, workspace, (room,), _U8), room,
+                        0 if status is None else _whole(w, device, status, (1,), _I32))
+    _enqueue(w, device, stream, _tokens, args)
 
 
 def expert_combine(rows, row_of_slot, weights, out, stream=None) -> None:
