@@ -32,29 +32,107 @@ __device__ __forceinline__ uint32_t to_e2m1x8(const float (&v)[8], float inv) {
     return r;
 }
 
-// Values c .. c + 7 of a row of `cols`, V of them in one access; 0 behind the row.
-template <int DT, int V>
-__device__ __forceinline__ void load_eight(const value_t<DT>* __restrict__ row, uint32_t c, uint32_t cols, float (&v)[8]) {
-    if (c + 8 <= cols) {
+// ---- 256 values of a row, eight neighbouring ones a lane, as they are in memory
+
+// Rows that start at multiples of 16 bytes and are multiples of 8 wide: the lane's own.  Others: words of 4 bytes, neighbouring ones
+// by neighbouring lanes, that go through the warp's shared memory.  (Eight accesses of 2 bytes a lane: silu(g) * u of 8008 rows of
+// 1001 35 us, their values back 50 us; so 14 and 15.)
+template <int DT>
+constexpr int kWords = 8 * sizeof(value_t<DT>) / 4;  // of a lane
+template <int DT>
+struct Staging {
+    uint32_t w[kWords<DT> * 32 + 4];
+};
+
+template <int DT, bool WIDE>
+struct RawEight {
+    uint32_t w[kWords<DT>];
+    uint32_t last;  // (not WIDE, 16 bits: lane 0's, the one behind the lanes')
+
+    // n: values of the row from the warp's first on, more than 0
+    __device__ __forceinline__ void load(const value_t<DT>* __restrict__ at, uint32_t n, int lane) {
 #pragma unroll
-        for (int i = 0; i < 8; i += V) {
-            float part[V];
-            load_values<DT, V>(row + c + i, part);
+        for (int i = 0; i < kWords<DT>; ++i) w[i] = 0;
+        last = 0;
+        if constexpr (WIDE) {
+            if (lane * 8u < n) {
+                const uint4* from = reinterpret_cast<const uint4*>(at + lane * 8);
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[i + j] = part[j];
+                for (int i = 0; i < kWords<DT>; i += 4) {
+                    const uint4 v = __ldg(from + i / 4);
+                    w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+                }
+            }
+        } else if constexpr (DT == CIERA_FP32) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (lane + 32u * i < n) w[i] = __ldg(reinterpret_cast<const uint32_t*>(at) + lane + 32 * i);
+        } else {
+            // values v0 = 2 * word - odd and v0 + 1, of which the first may be before and the second behind the row
+            const int odd = (int)((uintptr_t)at >> 1 & 1u);
+            const int count = (int)min(n, 256u);
+            const auto word = [&](int i) -> uint32_t {
+                const int v0 = 2 * i - odd;
+                if (v0 >= 0 && v0 + 1 < count) return __ldg(reinterpret_cast<const uint32_t*>(at + v0));
+                const unsigned short* h = reinterpret_cast<const unsigned short*>(at);
+                uint32_t r = 0;
+                if (v0 >= 0 && v0 < count) r = __ldg(h + v0);
+                if (v0 + 1 >= 0 && v0 + 1 < count) r |= (uint32_t)__ldg(h + v0 + 1) << 16;
+                return r;
+            };
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = word(lane + 32 * i);
+            if (odd && lane == 0) last = word(128);
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? ValueOf<DT>::get(row[c + i]) : 0.f;
     }
-}
+    // WIDE, 16 bits: the bits of the largest magnitude as fp32
+    __device__ __forceinline__ uint32_t most() const {
+        const auto two = [](uint32_t a, uint32_t b) {
+            uint32_t r;
+            asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a & 0x7fff7fffu), "r"(b & 0x7fff7fffu));
+            return r;
+        };
+        const uint32_t m = two(two(w[0], w[1]), two(w[2], w[3])), half = max(m & 0xffffu, m >> 16);
+        if constexpr (DT == CIERA_BF16) return half << 16;
+        else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)half)));
+    }
+    // by the whole warp
+    __device__ __forceinline__ void get(const value_t<DT>* __restrict__ at, Staging<DT>& st, float (&v)[8], int lane) {
+        if constexpr (!WIDE) {
+#pragma unroll
+            for (int i = 0; i < kWords<DT>; ++i) st.w[lane + 32 * i] = w[i];
+            if (lane == 0) st.w[32 * kWords<DT>] = last;
+            __syncwarp();
+            const uint4* from = reinterpret_cast<const uint4*>(st.w) + lane * (kWords<DT> / 4);
+#pragma unroll
+            for (int i = 0; i < kWords<DT>; i += 4) {
+                const uint4 x = from[i / 4];
+                w[i] = x.x, w[i + 1] = x.y, w[i + 2] = x.z, w[i + 3] = x.w;
+            }
+            if (DT != CIERA_FP32 && ((uintptr_t)at >> 1 & 1u)) {
+                const uint32_t next = st.w[lane * 4 + 4];
+                w[0] = __byte_perm(w[0], w[1], 0x5432);
+                w[1] = __byte_perm(w[1], w[2], 0x5432);
+                w[2] = __byte_perm(w[2], w[3], 0x5432);
+                w[3] = __byte_perm(w[3], next, 0x5432);
+            }
+            __syncwarp();
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (DT == CIERA_FP32) v[i] = __uint_as_float(w[i]);
+            else if constexpr (DT == CIERA_BF16) v[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+            else v[i] = __half2float(__ushort_as_half((unsigned short)(w[i / 2] >> (16 * (i & 1)))));
+        }
+    }
+};
 
 struct Rows4Args {
     uint64_t x_stride, x_matrix_stride, q_stride, q_matrix_stride, scales_stride, scales_matrix_stride;
     uint64_t x_rows;
     const int32_t* slot_of_row;
     const int32_t* starts;
-    uint32_t rows, cols, col_tiles, units, top_k, n_experts, source_rows;  // units: warps' work in a matrix
+    uint32_t rows, cols, col_tiles, units, each, chunks, top_k, n_experts, source_rows;  // units: warps of a matrix; tiles of each; chunks of a line
     uint8_t* q;
     uint8_t* scales;
 };
@@ -65,113 +143,138 @@ __device__ __forceinline__ bool at_border4(uint32_t amax) {
     return amax < 0x7f800000u && (amax < (32u << 23) || (uint32_t)((amax & 0x7fffffu) - 0x400000u + 256u) <= 512u);
 }
 
-// Whole tokens' worth of a warp: rows r + 32 * j of a block of 128, 256 columns.
-template <int DT, int SRC, int V>
-__global__ void __launch_bounds__(kFp4Threads) quantize4_rows_kernel(const Rows4Args a, const value_t<DT>* __restrict__ x_) {
+// A warp takes rows r + 32 * j of a block of 128 and `each` neighbouring tiles of 256 columns; the next rows' values are on their way
+// (four, or two of gates and ups, which take twice the registers).
+template <int DT, int SRC, bool WIDE>
+__global__ void __launch_bounds__(kFp4Threads, SRC == CIERA_SOURCE_SWIGLU ? 3 : 4) quantize4_rows_kernel(const Rows4Args a, const value_t<DT>* __restrict__ x_) {
+    constexpr bool kSwiglu = SRC == CIERA_SOURCE_SWIGLU;
+    constexpr int kAhead = kSwiglu || DT == CIERA_FP32 ? 2 : 4;
+    __shared__ __align__(16) Staging<DT> staging[WIDE ? 1 : kFp4Threads / 32];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t used = a.starts ? min((uint32_t)max(a.starts[a.n_experts], 0), a.rows) : a.rows;
     const uint32_t unit = blockIdx.x * (kFp4Threads / 32) + warp;
     if (unit >= a.units) return;
-    const uint32_t line = unit / a.col_tiles, tile = unit - line * a.col_tiles;
+    const uint32_t line = unit / a.chunks, tile0 = (unit - line * a.chunks) * a.each, tile1 = min(tile0 + a.each, a.col_tiles);
     const uint32_t rb = line >> 5, r0 = rb * 128u + (line & 31u);
     if (r0 >= used) return;
-    const value_t<DT>* x = x_ + blockIdx.y * a.x_matrix_stride;
-    // lane j: where row j of the four comes from
-    uint32_t from = r0 + 32u * (lane & 3);
-    bool some = from < used;
-    if (a.slot_of_row) {
-        const int32_t slot = some ? a.slot_of_row[from] : -1;
-        some = slot >= 0 && (uint64_t)slot < a.x_rows * a.top_k;
-        if (SRC == CIERA_SOURCE_ROWS) from = some ? (uint32_t)slot / a.top_k : 0u;
+    Staging<DT>& st = staging[WIDE ? 0 : warp];
+    const value_t<DT>* at[4];  // the rows' first tile
+    uint32_t there;            // bit j: row j comes from anywhere
+    {
+        const uint32_t row = r0 + 32u * (lane & 3);
+        bool some = row < used;
+        uint32_t from = row;
+        if (a.slot_of_row) {
+            const int32_t slot = some ? __ldg(a.slot_of_row + row) : -1;
+            some = slot >= 0 && (uint64_t)slot < a.x_rows * a.top_k;
+            if (!kSwiglu) from = some ? (uint32_t)slot / a.top_k : 0u;
+        }
+        there = __ballot_sync(~0u, some) & 15u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) at[j] = x_ + blockIdx.y * a.x_matrix_stride + (uint64_t)__shfl_sync(~0u, from, j) * a.x_stride + tile0 * 256u;
     }
-    const uint32_t there = __ballot_sync(~0u, some);
-    const uint32_t c0 = tile * 256u + lane * 8;
-    float v[4][8];
-    uint32_t some_values = 0;  // bit j: a value of row j is more than a zero times something
-    if constexpr (SRC == CIERA_SOURCE_ROWS) {
+    uint8_t* q = a.q + blockIdx.y * a.q_matrix_stride + (uint64_t)r0 * a.q_stride + tile0 * 128u + lane * 4;
+    RawEight<DT, WIDE> raw[kAhead], raw_up[kSwiglu ? kAhead : 1];
+    const auto load = [&](int to, int j, uint32_t tile) {  // row j's tile
+        if (tile < tile1 && (there >> j & 1u)) {
+            const value_t<DT>* p = at[j] + (tile - tile0) * 256u;
+            raw[to].load(p, a.cols - tile * 256u, lane);
+            if constexpr (kSwiglu) raw_up[to].load(p + a.cols, a.cols - tile * 256u, lane);
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) load(j, j, tile0);
+    for (uint32_t tile = tile0; tile < tile1; ++tile, q += 128) {
+        const uint32_t c0 = tile * 256u + lane * 8;
+        uint32_t bytes = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t f = __shfl_sync(~0u, from, j);
+            constexpr int A = kAhead;
+            const uint32_t row = r0 + 32u * j;
+            uint32_t codes = 0, byte = 127u;
             if (there >> j & 1u) {
-                load_eight<DT, V>(x + (uint64_t)f * a.x_stride, c0, a.cols, v[j]);
-            } else {
+                const value_t<DT>* p = at[j] + (tile - tile0) * 256u;
+                float v[8];
+                uint32_t amax = 0;
+                if constexpr (WIDE && !kSwiglu && DT != CIERA_FP32) amax = raw[j % A].most();
+                raw[j % A].get(p, st, v, lane);
+                bool some = false;  // a value is more than a zero times something
+                if constexpr (kSwiglu) {
+                    float u[8];
+                    raw_up[j % A].get(p + a.cols, st, u, lane);
+                    bool low = false;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t f = __shfl_sync(~0u, from, j);
-            float u[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[j][i] = u[i] = 0.f;
-            if (!(there >> j & 1u)) continue;
-            const value_t<DT>* row = x + (uint64_t)f * a.x_stride;
-            load_eight<DT, V>(row, c0, a.cols, v[j]);
-            load_eight<DT, V>(row + a.cols, c0, a.cols, u);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float g = v[j][i];
-                v[j][i] = swiglu32(g, u[i]);
-                some_values |= (uint32_t)(g != 0.f && u[i] != 0.f) << j;
-                if (g < kLowestGate) v[j][i] = (float)((double)g / (1.0 + exp(-(double)g)) * (double)u[i]);
-            }
-        }
-    }
-    uint32_t bytes = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t row = r0 + 32u * j;
-        uint32_t amax = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) amax = max(amax, magnitude4(v[j][i]));
-        amax = max(amax, __shfl_xor_sync(~0u, amax, 1));
-        amax = max(amax, __shfl_xor_sync(~0u, amax, 2));
-        if constexpr (SRC == CIERA_SOURCE_SWIGLU) {
-            // settled in 64 bits, by the four lanes of each such group
-            const uint32_t has = __ballot_sync(~0u, some_values >> j & 1u) >> (lane & 28) & 15u;
-            const bool settle = at_border4(amax) && has;
-            if (__any_sync(~0u, settle)) {
-                const uint32_t f = __shfl_sync(~0u, from, j);
-                double most = 0.0;
-                if (settle) {
-                    const value_t<DT>* at = x + (uint64_t)f * a.x_stride;
+                    for (int i = 0; i < 8; ++i) {
+                        const float g = v[i];
+                        low |= g < kLowestGate;
+                        some |= g != 0.f && u[i] != 0.f;
+                        v[i] = swiglu32(g, u[i]);
+                    }
+                    if (low) {
 #pragma unroll 1
-                    for (uint32_t c = c0; c < min(c0 + 8u, a.cols); ++c) {
-                        const double g = ValueOf<DT>::get(at[c]), u = ValueOf<DT>::get(at[a.cols + c]);
-                        most = fmax(most, fabs(g / (1.0 + exp(-g)) * u));
+                        for (int i = 0; i < 8; ++i)
+                            if (c0 + i < a.cols) {
+                                const double g = ValueOf<DT>::get(p[lane * 8 + i]);
+                                const float y = (float)(g / (1.0 + exp(-g)) * (double)ValueOf<DT>::get(p[a.cols + lane * 8 + i]));
+#pragma unroll
+                                for (int k = 0; k < 8; ++k)
+                                    if (k == i && g < (double)kLowestGate) v[k] = y;
+                            }
                     }
                 }
-                most = fmax(most, __shfl_xor_sync(~0u, most, 1));
-                most = fmax(most, __shfl_xor_sync(~0u, most, 2));
-                if (settle) amax = __float_as_uint(__double2float_ru(most));
-            }
-        }
-        const uint32_t byte = scale_byte4(amax);
-        uint32_t codes = to_e2m1x8(v[j], inverse_scale4(byte));
-        if (byte == 255u) codes = 0u;
-        bytes |= byte << (8 * j);
-        if (row < used && c0 < a.cols) {
-            uint8_t* to = a.q + blockIdx.y * a.q_matrix_stride + (uint64_t)row * a.q_stride + c0 / 2;
-            if (c0 + 8 <= a.cols) {
-                *reinterpret_cast<uint32_t*>(to) = codes;
+                load(j % A, (j + A) & 3, tile + ((j + A) >> 2));
+                if constexpr (!WIDE || kSwiglu || DT == CIERA_FP32) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) amax = max(amax, magnitude4(v[i]));
+                }
+                amax = max(amax, __shfl_xor_sync(~0u, amax, 1));
+                amax = max(amax, __shfl_xor_sync(~0u, amax, 2));
+                if constexpr (kSwiglu) {
+                    // settled in 64 bits, by the four lanes of each such group
+                    const uint32_t has = __ballot_sync(~0u, some) >> (lane & 28) & 15u;
+                    const bool settle = at_border4(amax) && has;
+                    if (__any_sync(~0u, settle)) {
+                        double most = 0.0;
+                        if (settle) {
+#pragma unroll 1
+                            for (uint32_t c = 0; c < 8 && c0 + c < a.cols; ++c) {
+                                const double g = ValueOf<DT>::get(p[lane * 8 + c]), u = ValueOf<DT>::get(p[a.cols + lane * 8 + c]);
+                                most = fmax(most, fabs(g / (1.0 + exp(-g)) * u));
+                            }
+                        }
+                        most = fmax(most, __shfl_xor_sync(~0u, most, 1));
+                        most = fmax(most, __shfl_xor_sync(~0u, most, 2));
+                        if (settle) amax = __float_as_uint(__double2float_ru(most));
+                    }
+                }
+                byte = scale_byte4(amax);
+                codes = to_e2m1x8(v, inverse_scale4(byte));
+                if (byte == 255u) codes = 0u;
             } else {
-                for (uint32_t i = 0; 2 * i < a.cols - c0; ++i) to[i] = (uint8_t)(codes >> (8 * i));
+                load(j % A, (j + A) & 3, tile + ((j + A) >> 2));
+            }
+            bytes |= byte << (8 * j);
+            if (row < used && c0 < a.cols) {
+                uint8_t* to = q + 32 * j * a.q_stride;
+                if (c0 + 8 <= a.cols) {
+                    *reinterpret_cast<uint32_t*>(to) = codes;
+                } else {
+                    for (uint32_t i = 0; 2 * i < a.cols - c0; ++i) to[i] = (uint8_t)(codes >> (8 * i));
+                }
             }
         }
+        // from a group's bytes of four rows to a row's of four groups, which lane 4 * j of the 16 writes for row j
+        const uint32_t g = lane >> 2;
+        uint32_t t = __shfl_xor_sync(~0u, bytes, 4);
+        bytes = g & 1 ? __byte_perm(t, bytes, 0x7351) : __byte_perm(bytes, t, 0x6240);
+        t = __shfl_xor_sync(~0u, bytes, 8);
+        bytes = g & 2 ? __byte_perm(t, bytes, 0x7632) : __byte_perm(bytes, t, 0x5410);
+        const uint32_t row = r0 + 32u * (g & 3), atom = tile * 2 + (lane >> 4);
+        if (!(lane & 3) && row < used && atom * 128u < a.cols)
+            *reinterpret_cast<uint32_t*>(a.scales + blockIdx.y * a.scales_matrix_stride + (uint64_t)rb * a.scales_stride + (uint64_t)atom * kAtomBytes +
+                                         atom_word(row)) = bytes;
     }
-    // from a group's bytes of four rows to a row's of four groups, which lane 4 * j of the 16 writes for row j
-    const uint32_t g = lane >> 2;
-    uint32_t t = __shfl_xor_sync(~0u, bytes, 4);
-    bytes = g & 1 ? __byte_perm(t, bytes, 0x7351) : __byte_perm(bytes, t, 0x6240);
-    t = __shfl_xor_sync(~0u, bytes, 8);
-    bytes = g & 2 ? __byte_perm(t, bytes, 0x7632) : __byte_perm(bytes, t, 0x5410);
-    const uint32_t row = r0 + 32u * (g & 3), atom = tile * 2 + (lane >> 4);
-    if (!(lane & 3) && row < used && atom * 128u < a.cols)
-        *reinterpret_cast<uint32_t*>(a.scales + blockIdx.y * a.scales_matrix_stride + (uint64_t)rb * a.scales_stride + (uint64_t)atom * kAtomBytes +
-                                     atom_word(row)) = bytes;
 }
 
 struct Turned4Args {
@@ -276,15 +379,19 @@ struct Values4Args {
 // Back: the same rows and columns for a warp as above.
 template <int DT, bool WIDE>
 __global__ void __launch_bounds__(kFp4Threads) values4_kernel(const Values4Args a, value_t<DT>* __restrict__ out_) {
+    __shared__ __align__(16) Staging<DT> staging[WIDE ? 1 : kFp4Threads / 32];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t unit = blockIdx.x * (kFp4Threads / 32) + warp;
     if (unit >= a.units) return;
     const uint32_t line = unit / a.col_tiles, tile = unit - line * a.col_tiles;
     const uint32_t rb = line >> 5, r0 = rb * 128u + (line & 31u), c0 = tile * 256u + lane * 8;
-    if (r0 >= a.rows || c0 >= a.cols) return;
+    const bool inside = c0 < a.cols;
+    if (r0 >= a.rows || (WIDE && !inside)) return;
+    Staging<DT>& st = staging[WIDE ? 0 : warp];
     const uint8_t* q = a.q + blockIdx.y * a.q_matrix_stride + c0 / 2;
-    const uint4 s = *reinterpret_cast<const uint4*>(a.scales + blockIdx.y * a.scales_matrix_stride + (uint64_t)rb * a.scales_stride +
+    uint4 s = make_uint4(0, 0, 0, 0);
+    if (inside) s = *reinterpret_cast<const uint4*>(a.scales + blockIdx.y * a.scales_matrix_stride + (uint64_t)rb * a.scales_stride +
                                                     (uint64_t)(c0 >> 7) * kAtomBytes + (line & 31u) * 16);
     const uint32_t scale[4] = {s.x, s.y, s.z, s.w};
     uint32_t codes[4];
@@ -292,7 +399,7 @@ __global__ void __launch_bounds__(kFp4Threads) values4_kernel(const Values4Args 
     for (int j = 0; j < 4; ++j) {
         const uint32_t row = r0 + 32u * j;
         codes[j] = 0;
-        if (row >= a.rows) continue;
+        if (row >= a.rows || !inside) continue;
         const uint8_t* from = q + (uint64_t)row * a.q_stride;
         if (c0 + 8 <= a.cols) {
             codes[j] = *reinterpret_cast<const uint32_t*>(from);
@@ -314,30 +421,54 @@ __global__ void __launch_bounds__(kFp4Threads) values4_kernel(const Values4Args 
             v[2 * i] = y.x * f;
             v[2 * i + 1] = y.y * f;
         }
-        value_t<DT>* to = out_ + blockIdx.y * a.out_matrix_stride + (uint64_t)row * a.out_stride + c0;
-        if (WIDE && c0 + 8 <= a.cols) {
-            constexpr int kEach = 16 / sizeof(value_t<DT>);
+        value_t<DT>* line_at = out_ + blockIdx.y * a.out_matrix_stride + (uint64_t)row * a.out_stride + tile * 256u;
+        if constexpr (WIDE) {
+            value_t<DT>* to = line_at + lane * 8;
+            if (c0 + 8 <= a.cols) {
+                constexpr int kEach = 16 / sizeof(value_t<DT>);
 #pragma unroll
-            for (int i = 0; i < 8; i += kEach) {
-                float part[kEach];
+                for (int i = 0; i < 8; i += kEach) {
+                    float part[kEach];
 #pragma unroll
-                for (int k = 0; k < kEach; ++k) part[k] = v[i + k];
-                store_values<DT, kEach>(to + i, part);
+                    for (int k = 0; k < kEach; ++k) part[k] = v[i + k];
+                    store_values<DT, kEach>(to + i, part);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c0 + i < a.cols) to[i] = ValueOf<DT>::put(v[i]);
             }
         } else {
+            // through shared memory to neighbouring words by neighbouring lanes, as they are read
+            const uint32_t n = min(a.cols - tile * 256u, 256u);
+            Pack<value_t<DT>, 16 / sizeof(value_t<DT>)>* put = reinterpret_cast<Pack<value_t<DT>, 16 / sizeof(value_t<DT>)>*>(st.w) + lane * (kWords<DT> / 4);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c0 + i < a.cols) to[i] = ValueOf<DT>::put(v[i]);
+            for (int i = 0; i < 8; ++i) put[i * sizeof(value_t<DT>) / 16].v[i % (16 / sizeof(value_t<DT>))] = ValueOf<DT>::put(v[i]);
+            __syncwarp();
+            if constexpr (DT == CIERA_FP32) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (lane + 32u * i < n) reinterpret_cast<uint32_t*>(line_at)[lane + 32 * i] = st.w[lane + 32 * i];
+            } else {
+                const int odd = (int)((uintptr_t)line_at >> 1 & 1u), count = (int)n;
+                const unsigned short* h = reinterpret_cast<const unsigned short*>(st.w);
+                const auto write = [&](int i) {
+                    const int v0 = 2 * i - odd;
+                    if (v0 >= 0 && v0 + 1 < count) {
+                        *reinterpret_cast<uint32_t*>(line_at + v0) = odd ? __byte_perm(st.w[i - 1], st.w[i], 0x5432) : st.w[i];
+                        return;
+                    }
+                    unsigned short* to = reinterpret_cast<unsigned short*>(line_at);
+                    if (v0 >= 0 && v0 < count) to[v0] = h[v0];
+                    if (v0 + 1 >= 0 && v0 + 1 < count) to[v0 + 1] = h[v0 + 1];
+                };
+#pragma unroll
+                for (int i = 0; i < 4; ++i) write(lane + 32 * i);
+                if (odd && lane == 0) write(128);
+            }
+            __syncwarp();
         }
     }
-}
-
-// f(values that may be read at a time as a constant): rows that start at multiples of 8 values, of 2, or of 1
-template <class F>
-static void with_width(bool eight, bool two, F&& f) {
-    if (eight) f(std::integral_constant<int, 8>());
-    else if (two) f(std::integral_constant<int, 2>());
-    else f(std::integral_constant<int, 1>());
 }
 
 // An operand's codes and scales; lines: of atoms.  0, or the status of what is wrong with them.
@@ -351,11 +482,21 @@ static int operand4(const void* q, uint64_t q_stride, uint64_t q_matrix_stride, 
     return CIERA_OK;
 }
 
+// (a tile of a line each)
 static uint64_t warp_units(uint64_t rows, uint64_t cols) {
     return (rows + 127) / 128 * (rows < 32 ? rows : 32) * ((cols + 255) / 256);
 }
 
-// Warps' work has 32 lines for each block of 128 rows; of a single block with fewer rows those that it has.
+// Warps' work: 32 lines for each block of 128 rows (of a single block with fewer rows those that it has), whole if that leaves 24 warps
+// an SM, else in pieces.
+static uint64_t rows_units(uint64_t rows, uint64_t cols, uint64_t matrices, uint32_t* each, uint32_t* chunks) {
+    const uint64_t tiles = (cols + 255) / 256, lines = (rows + 127) / 128 * (rows < 32 ? rows : 32);
+    const uint64_t most = lines * tiles * matrices / (148 * 24);
+    *each = (uint32_t)(most < 1 ? 1 : most > tiles ? tiles : most);
+    *chunks = (uint32_t)((tiles + *each - 1) / *each);
+    return lines * *chunks;
+}
+
 template <int SRC>
 static cudaError_t launch_rows4(const Rows4Args& a, int dtype, const void* x, uint32_t matrices, cudaStream_t s) {
     cudaError_t e = cudaSuccess;
@@ -365,9 +506,10 @@ static cudaError_t launch_rows4(const Rows4Args& a, int dtype, const void* x, ui
         uint64_t at = (uint64_t)x | (a.source_rows > 1 ? a.x_stride * v : 0) | (matrices > 1 ? a.x_matrix_stride * v : 0);
         if (SRC == CIERA_SOURCE_SWIGLU) at |= a.cols * v;
         const dim3 grid((a.units + kFp4Threads / 32 - 1) / (kFp4Threads / 32), matrices);
-        with_width(!(at & 15), !(at & (2 * v - 1)), [&](auto width) {
-            e = launch_after(quantize4_rows_kernel<DT, SRC, decltype(width)::value>, grid, kFp4Threads, 0, s, a, (const value_t<DT>*)x);
-        });
+        // (rows of whole pieces of 16 bytes)
+        const bool wide = !((at | (uint64_t)a.cols * v) & 15) && !(a.cols & 7);
+        e = launch_after(wide ? quantize4_rows_kernel<DT, SRC, true> : quantize4_rows_kernel<DT, SRC, false>, grid, kFp4Threads, 0, s, a,
+                         (const value_t<DT>*)x);
     });
     return e;
 }
@@ -390,10 +532,11 @@ extern "C" int ciera_fp4_quantize_rows(const ciera_fp4_rows* p, void* stream) {
     const int rc = operand4(p->q, p->q_stride, 0, p->scales, p->scales_stride, 0, 1, p->rows, p->cols);
     if (rc) return rc;
     if (!aligned_to(p->x, dtype_bytes(p->dtype)) || !aligned_to(p->slot_of_row, 4) || !aligned_to(p->starts, 4)) return CIERA_ERR_MISALIGNED;
-    const uint64_t units = warp_units(p->rows, p->cols);
+    uint32_t each, chunks;
+    const uint64_t units = rows_units(p->rows, p->cols, 1, &each, &chunks);
     if (units > kMaxExtent) return CIERA_ERR_UNSUPPORTED;
     const Rows4Args a{p->x_stride, 0, p->q_stride, 0, p->scales_stride, 0, p->x_rows, p->slot_of_row, p->starts, (uint32_t)p->rows,
-                      (uint32_t)p->cols, (uint32_t)((p->cols + 255) / 256), (uint32_t)units, p->slot_of_row ? p->top_k : 1u, p->n_experts,
+                      (uint32_t)p->cols, (uint32_t)((p->cols + 255) / 256), (uint32_t)units, each, chunks, p->slot_of_row ? p->top_k : 1u, p->n_experts,
                       (uint32_t)p->x_rows, (uint8_t*)p->q, p->scales};
     const cudaError_t e = swiglu ? launch_rows4<CIERA_SOURCE_SWIGLU>(a, p->dtype, p->x, 1, (cudaStream_t)stream)
                                  : launch_rows4<CIERA_SOURCE_ROWS>(a, p->dtype, p->x, 1, (cudaStream_t)stream);
@@ -417,13 +560,14 @@ extern "C" int ciera_fp4_quantize_matrices(const ciera_fp4_matrices* p, void* st
         const int rc = operand4(p->qt, p->qt_stride, p->qt_matrix_stride, p->scales_t, p->scales_t_stride, p->scales_t_matrix_stride, p->matrices, p->cols, p->rows);
         if (rc) return rc;
     }
-    const uint64_t v = dtype_bytes(p->dtype), units = warp_units(p->rows, p->cols), wide_cols = 256 / v;
+    uint32_t each, chunks;
+    const uint64_t v = dtype_bytes(p->dtype), units = rows_units(p->rows, p->cols, p->matrices, &each, &chunks), wide_cols = 256 / v;
     const uint64_t row_tiles = (p->rows + 127) / 128, col_tiles = (p->cols + wide_cols - 1) / wide_cols;
     if (units > kMaxExtent || row_tiles * col_tiles > kMaxExtent) return CIERA_ERR_UNSUPPORTED;
     cudaError_t e = cudaSuccess;
     if (p->q) {
         const Rows4Args a{p->x_stride, p->x_matrix_stride, p->q_stride, p->q_matrix_stride, p->scales_stride, p->scales_matrix_stride,
-                          p->rows, nullptr, nullptr, (uint32_t)p->rows, (uint32_t)p->cols, (uint32_t)((p->cols + 255) / 256), (uint32_t)units, 1u, 0u,
+                          p->rows, nullptr, nullptr, (uint32_t)p->rows, (uint32_t)p->cols, (uint32_t)((p->cols + 255) / 256), (uint32_t)units, each, chunks, 1u, 0u,
                           (uint32_t)p->rows, (uint8_t*)p->q, p->scales};
         e = launch_rows4<CIERA_SOURCE_ROWS>(a, p->dtype, p->x, p->matrices, (cudaStream_t)stream);
         if (e != cudaSuccess) return record_cuda_error(e);

@@ -11,8 +11,7 @@ constexpr uint32_t kAtomBytes = 512;  // scale bytes of 128 rows and 128 columns
 __device__ __forceinline__ uint32_t scale_byte4(uint32_t amax) {
     if (amax >= 0x7f800000u) return 255u;
     if (amax == 0u) return 127u;
-    const int s = (int)(amax >> 23) - 127 - 2 + ((amax & 0x7fffffu) > 0x400000u ? 1 : 0);
-    return (uint32_t)(max(s, -126) + 127);
+    return (uint32_t)max((int)((amax + 0x3fffffu) >> 23) - 2, 1);  // (a mantissa above 1.5 carries into the exponent)
 }
 // 2^s for a scale byte s + 127; NaN for byte 255
 __device__ __forceinline__ float scale_value(uint32_t byte) {
