@@ -383,11 +383,50 @@ __global__ void __launch_bounds__(kFp4Threads) quantize4_turned_kernel(const Tur
             *reinterpret_cast<uint4*>(tile + r * 64 + ((piece * 4 + 8 * (r >> 5)) & 63)) = v[i];
         }
     } else {
-        for (uint32_t i = threadIdx.x; i < 128 * 64 * kCols; i += kFp4Threads) {
-            const uint32_t r = i / (64 * kCols), c = i % (64 * kCols), w = c / kCols;
-            value_t<DT> v = ValueOf<DT>::put(0.f);
-            if (row0 + r < a.rows && col0 + c < a.cols) v = x[(uint64_t)(row0 + r) * a.x_stride + col0 + c];
-            reinterpret_cast<value_t<DT>*>(tile + r * 64 + ((w + 8 * (r >> 5)) & 63))[c % kCols] = v;
+        // words of 4 bytes, neighbouring ones by neighbouring lanes, 16 rows a warp; a row that starts in the middle of one is shifted on the
+        // way.  (Value by value: 27 matrices of 1373 x 1374 in 126 us with the values back, XXX so.)
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        const int count = (int)min(a.cols - col0, 64u * kCols);
+#pragma unroll 1
+        for (int i0 = 0; i0 < 16; i0 += 4) {
+            uint32_t v[4][3];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t r = warp * 16 + i0 + i;
+                const bool here = row0 + r < a.rows;
+                const value_t<DT>* at = x + (uint64_t)(row0 + r) * a.x_stride + col0;
+                const int odd = DT == CIERA_FP32 ? 0 : (int)((uintptr_t)at >> 1 & 1u);
+                const auto word = [&](int k) -> uint32_t {
+                    const int v0 = k * kCols - odd;
+                    if (!here) return 0;
+                    if constexpr (DT == CIERA_FP32) return v0 < count ? __ldg(reinterpret_cast<const uint32_t*>(at) + v0) : 0u;
+                    if (v0 >= 0 && v0 + 1 < count) return __ldg(reinterpret_cast<const uint32_t*>(at + v0));
+                    const unsigned short* h = reinterpret_cast<const unsigned short*>(at);
+                    uint32_t b = 0;
+                    if (v0 >= 0 && v0 < count) b = __ldg(h + v0);
+                    if (v0 + 1 >= 0 && v0 + 1 < count) b |= (uint32_t)__ldg(h + v0 + 1) << 16;
+                    return b;
+                };
+                v[i][0] = word(lane);
+                v[i][1] = word(lane + 32);
+                v[i][2] = odd && lane == 0 ? word(64) : 0u;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t r = warp * 16 + i0 + i, turn = 8 * (r >> 5);
+                uint32_t lo = v[i][0], hi = v[i][1];
+                if constexpr (DT != CIERA_FP32) {
+                    const value_t<DT>* at = x + (uint64_t)(row0 + r) * a.x_stride + col0;
+                    if ((uintptr_t)at >> 1 & 1u) {
+                        const uint32_t first = __shfl_sync(~0u, hi, 0), last = __shfl_sync(~0u, v[i][2], 0);
+                        const uint32_t lo1 = __shfl_down_sync(~0u, lo, 1), hi1 = __shfl_down_sync(~0u, hi, 1);
+                        lo = __byte_perm(lo, lane == 31 ? first : lo1, 0x5432);
+                        hi = __byte_perm(hi, lane == 31 ? last : hi1, 0x5432);
+                    }
+                }
+                tile[r * 64 + ((lane + turn) & 63)] = lo;
+                tile[r * 64 + ((lane + 32 + turn) & 63)] = hi;
+            }
         }
     }
     __syncthreads();

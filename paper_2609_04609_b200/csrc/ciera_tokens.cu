@@ -220,6 +220,14 @@ __device__ __forceinline__ uint32_t take_part4(float (&v)[4], float inv, float u
     return r;
 }
 
+// What a part leaves fits below a power of two that is known beforehand: of values up to 448 * 2^s e4m3 leaves at most 16 * 2^s, which
+// is less than 448 * 2^(s - 4), and of those up to 6 * 2^s e2m1 leaves 2^s, less than 6 * 2^(s - 2).  So only the first part's
+// power has to be looked for.  (A reduction over 32 lanes for each part: 1 us for the six of one slot, of which a tile has up to 16.)
+template <int BITS>
+__device__ __forceinline__ uint32_t next_byte(uint32_t first, uint32_t p) {
+    return (uint32_t)max((int)first - (int)(p * (BITS == 8 ? 4 : 2)), 1);
+}
+
 // 128 values of a token, four a lane, as parts.
 template <int DT, int BITS>
 __device__ __forceinline__ void make_parts(const TokensArgs& a, const value_t<DT>* __restrict__ x, uint32_t token, uint32_t kb, uint32_t lane) {
@@ -232,32 +240,31 @@ __device__ __forceinline__ void make_parts(const TokensArgs& a, const value_t<DT
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = ValueOf<DT>::get(from[i]);
     }
-    const uint32_t rows = a.n_tokens * P;
+    uint32_t amax = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) amax = max(amax, __shfl_xor_sync(~0u, amax, d));
+    uint32_t first = part_byte<BITS>(amax);
+    const bool bad = first == 255u;  // NaN by its first part's scale; the rest is zeros
+    if (bad) {
+        first = 127u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = 0.f;
+    }
+    uint32_t own = 0;  // lane p: the four groups' bytes of part p
 #pragma unroll
     for (uint32_t p = 0; p < P; ++p) {
-        uint32_t amax = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);
-#pragma unroll
-        for (int d = 1; d < 8; d <<= 1) amax = max(amax, __shfl_xor_sync(~0u, amax, d));
-        const uint32_t byte = part_byte<BITS>(amax), row = token * P + p;
+        const uint32_t byte = next_byte<BITS>(first, p), row = token * P + p;
         const float inv = part_inverse(byte), unit = __uint_as_float(byte << 23);
-        uint32_t word;
-        if constexpr (BITS == 8) word = take_part8(v, inv, unit);
-        else word = take_part4(v, inv, unit);
-        if (byte == 255u) {  // NaN by its scale; nothing is left
-            word = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = 0.f;
-        }
-        if constexpr (BITS == 8) *reinterpret_cast<uint32_t*>(a.x_parts + (uint64_t)row * a.d_model + kb * 128 + lane * 4) = word;
-        else *reinterpret_cast<uint16_t*>(a.x_parts + (uint64_t)row * (a.d_model / 2) + kb * 64 + lane * 2) = (uint16_t)word;
-        // the four groups' bytes
-        uint32_t all = byte << (lane >> 3) * 8;
+        if constexpr (BITS == 8) *reinterpret_cast<uint32_t*>(a.x_parts + (uint64_t)row * a.d_model + kb * 128 + lane * 4) = take_part8(v, inv, unit);
+        else *reinterpret_cast<uint16_t*>(a.x_parts + (uint64_t)row * (a.d_model / 2) + kb * 64 + lane * 2) = (uint16_t)take_part4(v, inv, unit);
+        uint32_t all = (p == 0 && bad ? 255u : byte) << (lane >> 3) * 8;
         all |= __shfl_xor_sync(~0u, all, 8);
         all |= __shfl_xor_sync(~0u, all, 16);
-        if (lane == 0) a.x_scales[(uint64_t)kb * rows + row] = all;
+        if (lane == p) own = all;
     }
+    if (lane < P) a.x_scales[(uint64_t)kb * (a.n_tokens * P) + token * P + lane] = own;
 }
 
 // 32 neighbouring values of the middle, one a lane, as parts at one place; columns f ... of d_ff.
@@ -265,30 +272,31 @@ template <int DT, int BITS>
 __device__ __forceinline__ void put_hidden(const TokensArgs& a, float v, uint32_t place, uint32_t f, uint32_t lane) {
     constexpr uint32_t P = kParts<BITS, DT>;
     const uint32_t rows = a.n_tokens * a.top_k * P;
+    uint32_t first = part_byte<BITS>(__reduce_max_sync(~0u, __float_as_uint(v) & 0x7fffffffu));
+    const bool bad = first == 255u;
+    if (bad) first = 127u, v = 0.f;
+    if (lane < P)
+        reinterpret_cast<uint8_t*>(a.hidden_scales + (uint64_t)(f >> 7) * rows + place * P + lane)[f >> 5 & 3u] =
+            (uint8_t)(lane == 0 && bad ? 255u : next_byte<BITS>(first, lane));
+    if constexpr (BITS == 8) {
+        uint8_t* to = a.hidden + (uint64_t)place * P * a.d_ff + f + lane;
 #pragma unroll
-    for (uint32_t p = 0; p < P; ++p) {
-        const uint32_t amax = __reduce_max_sync(~0u, __float_as_uint(v) & 0x7fffffffu), byte = part_byte<BITS>(amax), row = place * P + p;
-        const float inv = part_inverse(byte), unit = __uint_as_float(byte << 23);
-        const bool bad = byte == 255u;
-        if constexpr (BITS == 8) {
-            const uint8_t q = __nv_cvt_float_to_fp8(v * inv, __NV_SATFINITE, __NV_E4M3);
-            v = fmaf(-__half2float(__half(__nv_cvt_fp8_to_halfraw(q, __NV_E4M3))), unit, v);
-            a.hidden[(uint64_t)row * a.d_ff + f + lane] = bad ? 0 : q;
-        } else {
-            const float other = __shfl_xor_sync(~0u, v, 1);
-            uint32_t q, two;
-            asm("{\n\t.reg .b8 a;\n\t.reg .b16 w;\n\t"
-                "cvt.rn.satfinite.e2m1x2.f32 a, %3, %2;\n\t"
-                "cvt.rn.f16x2.e2m1x2 %1, a;\n\t"
-                "cvt.u16.u8 w, a;\n\tcvt.u32.u16 %0, w;\n\t}"
-                : "=r"(q), "=r"(two)
-                : "f"((lane & 1 ? other : v) * inv), "f"((lane & 1 ? v : other) * inv));
-            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&two));
-            v = fmaf(-(lane & 1 ? y.y : y.x), unit, v);
-            if (!(lane & 1)) a.hidden[(uint64_t)row * (a.d_ff / 2) + f / 2 + lane / 2] = bad ? 0 : (uint8_t)q;
+        for (uint32_t p = 0; p < P; ++p) {
+            const uint32_t byte = next_byte<BITS>(first, p);
+            const uint8_t q = __nv_cvt_float_to_fp8(v * part_inverse(byte), __NV_SATFINITE, __NV_E4M3);
+            v = fmaf(-__half2float(__half(__nv_cvt_fp8_to_halfraw(q, __NV_E4M3))), __uint_as_float(byte << 23), v);
+            to[(uint64_t)p * a.d_ff] = q;
         }
-        if (lane == 0) reinterpret_cast<uint8_t*>(a.hidden_scales + (uint64_t)(f >> 7) * rows + row)[f >> 5 & 3u] = (uint8_t)byte;
-        if (bad) v = 0.f;
+    } else {  // an even lane has its neighbour's value too
+        const float other = __shfl_down_sync(~0u, v, 1);
+        if (lane & 1) return;
+        float pair[4] = {v, other, 0.f, 0.f};
+        uint8_t* to = a.hidden + (uint64_t)place * P * (a.d_ff / 2) + (f + lane) / 2;
+#pragma unroll
+        for (uint32_t p = 0; p < P; ++p) {
+            const uint32_t byte = next_byte<BITS>(first, p);
+            to[(uint64_t)p * (a.d_ff / 2)] = (uint8_t)take_part4(pair, part_inverse(byte), __uint_as_float(byte << 23));
+        }
     }
 }
 
@@ -702,15 +710,20 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
             if (!ok) break;
             tensor_fence_after();
             const uint32_t from = tmem + (quarter << 21) + which * kSumColumns;
-            for (uint32_t slot = 0; slot < slots; ++slot) {
+            constexpr uint32_t kEach = 16 / P;  // slots of 16 columns
+            for (uint32_t slot = 0; slot < slots; slot += kEach) {
                 uint32_t r[16];
                 tmem_load16(from + slot * P, r);
                 tmem_wait_load();
-                float v = __uint_as_float(r[P - 1]);  // small ones first
 #pragma unroll
-                for (int p = (int)P - 2; p >= 0; --p) v += __uint_as_float(r[p]);
-                if (w.up) sm.exchange[slot][quarter * 32 + lane] = v;
-                else a.rows[(uint64_t)(first + slot) * a.d_model + w.tile * 128 + quarter * 32 + lane] = v;
+                for (uint32_t e = 0; e < kEach; ++e) {
+                    if (slot + e >= slots) break;
+                    float v = __uint_as_float(r[e * P + P - 1]);  // small ones first
+#pragma unroll
+                    for (int p = (int)P - 2; p >= 0; --p) v += __uint_as_float(r[e * P + p]);
+                    if (w.up) sm.exchange[slot + e][quarter * 32 + lane] = v;
+                    else a.rows[(uint64_t)(first + slot + e) * a.d_model + w.tile * 128 + quarter * 32 + lane] = v;
+                }
             }
             tensor_fence_before();
             __syncwarp();
