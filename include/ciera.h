@@ -674,7 +674,8 @@ CIERA_API int ciera_fp4_matmul(const ciera_fp4_product* args, void* stream);
  *   x             device, n_tokens rows of d_model values of dtype;  out  the same
  *   logits, bias, experts, weights   as for ciera_route
  *   workspace     device, 16-byte aligned, ciera_expert_tokens_workspace_bytes() of the largest call: zero-filled once, its first
- *                 256 bytes are handed back zero by every call (but one that reports an error); not shared by calls that may overlap
+ *                 CIERA_EXPERT_TOKENS_HEAD bytes are handed back zero by every call (but one that reports an error); not shared by
+ *                 calls that may overlap
  *   status        device int32 or NULL: CIERA_ERR_TIMEOUT if the blocks' bounded wait for each other ran out
  * Arithmetic: fp32 sums of 8-bit (4-bit) tensor products.  The weights are what they are; x and silu(g) * u go into the products as
  * sums of parts in the weights' bits, each below a power of two of its own for 32 values.  8 bits: three parts, of which 2^-12 of a
@@ -684,6 +685,7 @@ CIERA_API int ciera_fp4_matmul(const ciera_fp4_product* args, void* stream);
  * Limits: n_tokens 0 .. CIERA_EXPERT_TOKENS_MAX, d_model and d_ff multiples of 128 up to 65536, config as for ciera_route; weights
  * and their strides as for the products. */
 #define CIERA_EXPERT_TOKENS_MAX 64
+#define CIERA_EXPERT_TOKENS_HEAD 8448
 typedef enum ciera_weights_format { CIERA_WEIGHTS_FP8 = 0, CIERA_WEIGHTS_FP4 = 1 } ciera_weights_format;
 typedef struct ciera_expert_tokens_args {
     ciera_route_config route;

@@ -53,6 +53,7 @@ FP4_GROUP = 32
 FP4_ATOM = 512  # scale bytes of 128 rows and 128 columns
 WEIGHTS_FP8, WEIGHTS_FP4 = 0, 1
 EXPERT_TOKENS_MAX = 64
+EXPERT_TOKENS_HEAD = 8448
 
 
 class RouteConfig(ctypes.Structure):
@@ -192,12 +193,22 @@ for _name, (_args, _res) in _SIGS.items():
 
 EXPORTS = tuple(_SIGS)
 
-# ``ciera_expert_tokens`` with its many arguments packed in one go: a few microseconds less than a structure takes, of a call whose
-# kernels take sixteen.
-_TOKENS = struct.Struct("=32s6i24Q")
-assert _TOKENS.size == ctypes.sizeof(_ExpertTokens)
-_tokens = _lib["ciera_expert_tokens"]
-_tokens.argtypes, _tokens.restype = [ctypes.c_char_p, _vp], _i32
+
+
+def _packed(name: str, layout: str, structure):
+    """An entry point whose arguments are packed in one go, microseconds less than a structure with as many fields takes."""
+    pack = struct.Struct(layout)
+    assert pack.size == ctypes.sizeof(structure)
+    f = _lib[name]
+    f.argtypes, f.restype = [ctypes.c_char_p, _vp], _i32
+    return f, pack.pack
+
+
+_fp4_rows, _pack_fp4_rows = _packed("ciera_fp4_quantize_rows", "=2i7Q2I4Q", _Fp4Rows)
+_fp4_matrices, _pack_fp4_matrices = _packed("ciera_fp4_quantize_matrices", "=iI17Q", _Fp4Matrices)
+_fp4_value, _pack_fp4_value = _packed("ciera_fp4_values", "=iI11Q", _Fp4Values)
+_fp4_product, _pack_fp4_product = _packed("ciera_fp4_matmul", "=2iI4x17Q", _Fp4Product)
+_tokens, _pack_tokens = _packed("ciera_expert_tokens", "=32s6i24Q", _ExpertTokens)
 
 
 class CieraError(RuntimeError):
@@ -710,17 +721,19 @@ def fp4_quantize_rows(x, q, scales, *, kind: int = SOURCE_ROWS, slot_of_row=None
     rows = q.shape[0]
     q_at = _codes(w, device, q, rows, cols)
     s_at = _atom_lines(w, device, scales, rows, cols)
-    slots = begin = None
-    n_experts = 0
+    slots = begin = n_experts = 0
     if slot_of_row is not None:
-        slots = _whole(w, device, slot_of_row, slot_of_row.shape, _I32)
-        if slot_of_row.dim() != 1 or slot_of_row.numel() < rows:
+        n = slot_of_row.numel() if isinstance(slot_of_row, _Tensor) else -1
+        slots = _whole(w, device, slot_of_row, (n,), _I32)
+        if n < rows:
             _refuse(w)
     if starts is not None:
-        n_experts = starts.numel() - 1
+        n_experts = starts.numel() - 1 if isinstance(starts, _Tensor) else 0
         begin = _whole(w, device, starts, (n_experts + 1,), _I32)
-    args = _Fp4Rows(kind, code, rows, cols, x_rows, *x_at, slots, begin, top_k, max(n_experts, 0), *q_at, *s_at)
-    _enqueue(w, device, stream, _lib.ciera_fp4_quantize_rows, args)
+    if not 0 <= kind <= 2 or not 0 <= top_k < 1 << 32:
+        _refuse(w)
+    _enqueue(w, device, stream, _fp4_rows, _pack_fp4_rows(kind, code, rows, cols, x_rows, *x_at, slots, begin, top_k,
+                                                          max(n_experts, 0), *q_at, *s_at))
 
 
 def fp4_quantize_matrices(x, q=None, scales=None, qt=None, scales_t=None, stream=None) -> None:
@@ -733,13 +746,12 @@ def fp4_quantize_matrices(x, q=None, scales=None, qt=None, scales_t=None, stream
     m, r, c = x.shape
     if (q is None) != (scales is None) or (qt is None) != (scales_t is None):
         _refuse(w)
-    none = (None, 0, 0)
-    args = _Fp4Matrices(code, m, r, c, *x_at,
-                        *(none if q is None else _matrices(w, device, q, (m, r, (c + 1) // 2), _U8)),
-                        *(none if q is None else _atom_stack(w, device, scales, m, r, c)),
-                        *(none if qt is None else _matrices(w, device, qt, (m, c, (r + 1) // 2), _U8)),
-                        *(none if qt is None else _atom_stack(w, device, scales_t, m, c, r)))
-    _enqueue(w, device, stream, _lib.ciera_fp4_quantize_matrices, args)
+    at = turned = (0, 0, 0, 0, 0, 0)
+    if q is not None:
+        at = (*_matrices(w, device, q, (m, r, (c + 1) // 2), _U8), *_atom_stack(w, device, scales, m, r, c))
+    if qt is not None:
+        turned = (*_matrices(w, device, qt, (m, c, (r + 1) // 2), _U8), *_atom_stack(w, device, scales_t, m, c, r))
+    _enqueue(w, device, stream, _fp4_matrices, _pack_fp4_matrices(code, m, r, c, *x_at, *at, *turned))
 
 
 def fp4_values(q, scales, out, stream=None) -> None:
@@ -755,7 +767,7 @@ def fp4_values(q, scales, out, stream=None) -> None:
         o_at = (*_matrix(w, device, out, None, out.dtype), 0)
         m, (r, c) = 1, out.shape
         q_at, s_at = (*_codes(w, device, q, r, c), 0), (*_atom_lines(w, device, scales, r, c), 0)
-    _enqueue(w, device, stream, _lib.ciera_fp4_values, _Fp4Values(code, m, r, c, *q_at, *s_at, *o_at))
+    _enqueue(w, device, stream, _fp4_value, _pack_fp4_value(code, m, r, c, *q_at, *s_at, *o_at))
 
 
 def fp4_matmul(a, a_scales, b, b_scales, out, starts=None, status=None, stream=None) -> None:
@@ -768,9 +780,9 @@ def fp4_matmul(a, a_scales, b, b_scales, out, starts=None, status=None, stream=N
     a_at = _matrix(w, device, a, None, _U8)
     m, line = a.shape
     k = 2 * line
-    begin, experts = None, 0
+    begin = experts = 0
     if starts is not None:
-        experts = starts.numel() - 1
+        experts = starts.numel() - 1 if isinstance(starts, _Tensor) else 0
         begin = _whole(w, device, starts, (experts + 1,), _I32)
         b_at = _matrices(w, device, b, None, _U8)
         matrices, n, b_line = b.shape
@@ -784,10 +796,11 @@ def fp4_matmul(a, a_scales, b, b_scales, out, starts=None, status=None, stream=N
     if b_line != line:
         _refuse(w)
     code = _code(w, out)
-    args = _Fp4Product(PRODUCT_DENSE if starts is None else PRODUCT_ROWS, code, max(experts, 0), m, n, k, *a_at,
-                       *_atom_lines(w, device, a_scales, m, k), *b_at, *bs_at, begin,
-                       *_matrix(w, device, out, (m, n), out.dtype), None if status is None else _whole(w, device, status, (1,), _I32))
-    _enqueue(w, device, stream, _lib.ciera_fp4_matmul, args)
+    args = _pack_fp4_product(PRODUCT_DENSE if starts is None else PRODUCT_ROWS, code, max(experts, 0), m, n, k, *a_at,
+                             *_atom_lines(w, device, a_scales, m, k), *b_at, *bs_at, begin,
+                             *_matrix(w, device, out, (m, n), out.dtype),
+                             0 if status is None else _whole(w, device, status, (1,), _I32))
+    _enqueue(w, device, stream, _fp4_product, args)
 
 
 def expert_tokens_workspace_bytes(config: RouteConfig, n_tokens: int, d_model: int, d_ff: int) -> int:
@@ -826,7 +839,7 @@ def expert_tokens(config: RouteConfig, x, logits, bias, w1, w1_scales, w2, w2_sc
               *_matrices(w, device, w2, (e, d, f), _E4M3), *_matrices(w, device, w2_scales, (e, db, fb), _U8))
     choice = (t, k)
     room = workspace.numel()
-    args = _TOKENS.pack(bytes(config), form, code, logits_code, t, d, f, *x_at, *_matrix(w, device, logits, (t, e), logits.dtype),
+    args = _pack_tokens(bytes(config), form, code, logits_code, t, d, f, *x_at, *_matrix(w, device, logits, (t, e), logits.dtype),
                         0 if bias is None else _whole(w, device, bias, (e,), _F32), *at, *_matrix(w, device, out, shape, dtype),
                         _whole(w, device, experts, choice, _I32), _whole(w, device, weights, choice, _F32),
                         _whole(w, device, workspace, (room,), _U8), room,

@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(kFp4Threads, SRC == CIERA_SOURCE_SWIGLU ? 3 : 
 }
 
 // The same for rows of 16-bit values that lie in whole pieces of 16 bytes, which are compared as they are, two at a time.  What four
-// lanes need for each of four rows, the largest magnitude and the scale, each of them works out for one: 200 instructions for 4 rows
+// lanes need for each of four rows, the largest magnitude and the scale, each of them works out for one: 330 instructions for 4 rows
 // of 256 instead of 460, and 32768 rows of 2048 in 34 us instead of 42.
 template <int DT>
 __global__ void __launch_bounds__(kFp4Threads, 4) quantize4_words_kernel(const Rows4Args a, const value_t<DT>* __restrict__ x) {
@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(kFp4Threads) quantize4_turned_kernel(const Tur
         }
     } else {
         // words of 4 bytes, neighbouring ones by neighbouring lanes, 16 rows a warp; a row that starts in the middle of one is shifted on the
-        // way.  (Value by value: 27 matrices of 1373 x 1374 in 126 us with the values back, XXX so.)
+        // way.  (Value by value: 27 matrices of 1373 x 1374 in 126 us with the values back, 102 so.)
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         const int count = (int)min(a.cols - col0, 64u * kCols);
 #pragma unroll 1

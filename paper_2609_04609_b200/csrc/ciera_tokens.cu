@@ -16,8 +16,9 @@
 //   up     tiles of 64 rows of the gate and the same 64 of up; silu(g) * u goes to the workspace as parts again
 //   down   tiles of 128 rows of the output, expert by expert, as fp32 to the workspace
 //   sum    a token's rows, weighted, in the order of its choices
-// with a barrier of all blocks between them, which only the copies of the second operand wait for: those of the weights go on,
-// so that a block's next 100 to 180 KB of them are on their way meanwhile.
+// What one part reads of another's results, only the copies of the second operand wait for: those of the weights go on, so that a
+// block's next 100 to 180 KB of them are on their way meanwhile.  A tile of down waits for its group's tiles of up, which were the
+// first to be made (for all of up: 64 tokens 76 us, XXX so).
 // Tokens of an expert are taken 16 at a time (a group; 11 where there are ten parts): 112 columns.
 #include <type_traits>
 
@@ -34,7 +35,8 @@ constexpr int kMostStages = 10;
 constexpr int kBehind = 5;  // stages whose weights' scales are on their way; fewer than there are stages
 constexpr uint32_t kMaxSlots = CIERA_EXPERT_TOKENS_MAX * 32;
 constexpr uint32_t kMaxColumns = 112;
-constexpr uint32_t kTokenHead = 256;  // bytes of the workspace's counters
+constexpr uint32_t kTokenHead = CIERA_EXPERT_TOKENS_HEAD;  // bytes of the workspace's counters
+static_assert(kTokenHead >= 256 + 4 * kMaxSlots, "a counter for each group");
 constexpr uint32_t kTileBytes = 128 * 128;
 constexpr uint32_t kSumColumns = 112, kTokenScalesAt = 2 * kSumColumns, kTokenTmem = 256;  // of tensor memory: two sums, scales
 
@@ -53,7 +55,8 @@ struct TokensArgs {
     const int32_t* experts;
     const float* weights;
     uint64_t x_stride, out_stride;
-    uint32_t* counters;  // blocks that are done with parts, with up, with down, with all: zero before and after
+    uint32_t* counters;  // blocks that are done with parts, tiles of up, blocks done with down, with all; from 64 on each group's tiles of
+                         // up.  Zero before and after
     int32_t* status;
     uint8_t* x_parts;        // [tokens * parts][d_model], 8 or 4 bits
     uint32_t* x_scales;      // [d_model / 128][tokens * parts]
@@ -356,8 +359,6 @@ struct alignas(16) TokensSmem {
 };
 constexpr uint32_t kStageScales = 4 * 512;  // a stage's scale bytes: two atoms (8 bits: one) of each operand
 // a stage: the weights' tile, the tokens' columns, the scales of both
-static_assert(sizeof(TokensSmem) + 1024 + sizeof(ListScratch) <= 227 * 1024, "more than a block may have");
-
 __device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
@@ -609,7 +610,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         // copies of the tokens' columns and their scale words, behind the blocks that make them; every fourth stage.  (By one warp
         // 64 tokens took 107 us.)
         uint32_t it = 0, s = 0, odd = 1, last = 0;  // last: the warp's stage whose words are on their way
-        bool ok, was_up = true, some = false;
+        bool ok, some = false;
         ok = wait_for_all(a.counters, blocks, abort, a.status);
         fence_async_all();  // (written by threads, read by copies)
         const auto report = [&]() {
@@ -618,14 +619,22 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
             if (lane == 0) mbar_arrive(&sm.full[last]);
             some = false;
         };
+        bool all_up = false;  // of all groups
         while (ok && w.next()) {
-            if (was_up && !w.up) {
-                cp_async_wait<0>();  // (up's last stages, which the blocks' barrier stands behind)
-                if (some) report();
-                was_up = false;
-                ok = wait_for_all(a.counters + 1, blocks, abort, a.status);
+            if (!w.up && !all_up) {
+                uint32_t tiles, whole;
+                asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(tiles) : "l"(a.counters + 64 + w.group) : "memory");
+                asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(whole) : "l"(a.counters + 1) : "memory");
+                all_up = __all_sync(~0u, whole >= sm.lists.groups * w.up_tiles);
+                if (!all_up && !__all_sync(~0u, tiles >= w.up_tiles)) {
+                    if (some) {  // (a tile of up may be waiting for it)
+                        cp_async_wait<0>();
+                        report();
+                    }
+                    ok = wait_for_all(a.counters + 64 + w.group, w.up_tiles, abort, a.status);
+                    if (!ok) break;
+                }
                 fence_async_all();
-                if (!ok) break;
             }
             const uint32_t packed = w.packed(), first = group_first(packed), slots = group_slots(packed);
             const uint32_t atoms = (w.up ? a.d_model : a.d_ff) / 128, rows = a.n_tokens * (w.up ? 1 : a.top_k) * P;
@@ -699,12 +708,8 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
             return r != 0;
         };
         uint32_t tile = 0;
-        bool ok = true, was_up = true;
+        bool ok = true;
         while (w.next()) {
-            if (was_up && !w.up) {
-                done_with(a.counters + 1);
-                was_up = false;
-            }
             const uint32_t which = tile & 1, packed = w.packed(), slots = group_slots(packed), first = group_first(packed);
             ok = all_agree(mbar_wait_soon(&sm.sums_full[which], (tile >> 1) & 1, abort, a.status, kMaxBarrierPolls + w.stages));
             if (!ok) break;
@@ -738,13 +743,15 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
                     put_hidden<DT, BITS>(a, v, first + slot, w.tile * 64 + (quarter & 1) * 32, lane);
                 }
                 all_four();
+                if (tid == 0) {
+                    __threadfence();
+                    atomicAdd(a.counters + 64 + w.group, 1u);
+                    atomicAdd(a.counters + 1, 1u);
+                }
             }
             ++tile;
         }
-        if (ok) {
-            if (was_up) done_with(a.counters + 1);
-            done_with(a.counters + 2);
-        }
+        if (ok) done_with(a.counters + 2);
     }
     __syncthreads();
     if (warp == 2) {
@@ -755,6 +762,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
     __syncthreads();
     if (*abort) return;
     // a token's rows, in the order of its choices; the last block to leave sets the counters back
+    for (uint32_t i = blockIdx.x * kTokenThreads + threadIdx.x; i < sm.lists.groups; i += blocks * kTokenThreads) a.counters[64 + i] = 0;
     if (threadIdx.x == 0 && atomicAdd(a.counters + 3, 1u) == blocks - 1)
         for (int i = 0; i < 4; ++i) a.counters[i] = 0;
     const uint32_t quads = a.d_model / 4;
@@ -813,6 +821,11 @@ template <int DT, int BITS>
 static cudaError_t launch_tokens(TokensArgs a, const ciera_expert_tokens_args* p, int dev, uint32_t sms, cudaStream_t s) {
     static std::atomic<uint64_t> allowed{0};  // devices on which this instance may have its shared memory
     constexpr uint32_t P = kParts<BITS, DT>, kMost = 227 * 1024 - 1024 - sizeof(TokensSmem);
+    // (the lists are made where the ring will be, and stages' scales are reported while there is still room for more)
+    static_assert(kMost - (kTileBytes + kMaxColumns * 128 + kStageScales) >= sizeof(ListScratch) &&
+                      kMostStages * (kTileBytes + 2048 + kStageScales) >= sizeof(ListScratch) &&
+                      kMost / (kTileBytes + kMaxColumns * 128 + kStageScales) > kBehind,
+                  "too short a ring");
     const uint64_t slots = (uint64_t)a.n_tokens * a.top_k, d = a.d_model, f = a.d_ff;
     const TokensRoom room = tokens_room(a.n_tokens, a.top_k, d, f, BITS, P);
     uint8_t* const base = (uint8_t*)p->workspace;
@@ -848,7 +861,6 @@ static cudaError_t launch_tokens(TokensArgs a, const ciera_expert_tokens_args* p
     cfg.gridDim = dim3((uint32_t)(work < sms ? work : sms));
     cfg.blockDim = dim3(kTokenThreads);
     cfg.dynamicSmemBytes = 1024 + a.stages * a.stage_bytes + sizeof(TokensSmem);
-    if (cfg.dynamicSmemBytes < 1024 + sizeof(ListScratch) + sizeof(TokensSmem)) cfg.dynamicSmemBytes = 1024 + sizeof(ListScratch) + sizeof(TokensSmem);
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = 2;

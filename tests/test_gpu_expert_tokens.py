@@ -58,7 +58,7 @@ class Case:
         self.weights = torch.full((t, k), 7.0, device=DEV)
         n = ciera.expert_tokens_workspace_bytes(self.config, t, self.d, self.f)
         self.workspace = torch.zeros(n, dtype=torch.uint8, device=DEV)
-        self.workspace[256:] = 255  # (only the head has to be zero)
+        self.workspace[ciera.EXPERT_TOKENS_HEAD :] = 255  # (only the head has to be zero)
         return self
 
     def run(self, stream=None):
@@ -69,7 +69,9 @@ class Case:
         return self.out
 
     def check(self, tokens=None):
-        assert not self.workspace[:256].any()
+        from paper_2609_04609_b200 import ciera
+
+        assert not self.workspace[: ciera.EXPERT_TOKENS_HEAD].any()
         self._check(tokens)
 
     def _check(self, tokens):
@@ -118,7 +120,8 @@ class Case:
     (1, 8, 2, 128, 128, "bf16"), (1, 64, 8, 256, 128, "fp32"), (3, 4, 2, 384, 256, "fp16"), (8, 16, 4, 640, 384, "bf16"),
     (9, 4, 4, 1152, 128, "bf16"), (17, 2, 2, 256, 640, "fp32"), (64, 4, 2, 384, 256, "bf16"), (33, 64, 8, 128, 384, "fp16"),
     (64, 1, 1, 256, 128, "bf16"), (5, 6, 3, 2176, 128, "bf16"), (2, 3, 1, 4224, 256, "fp32"), (40, 3, 2, 2304, 2176, "bf16"),
-    (64, 40, 32, 128, 128, "bf16"),
+    (64, 40, 32, 128, 128, "bf16"), (64, 1024, 32, 128, 128, "bf16"), (23, 2, 2, 256, 128, "fp32"), (12, 1, 1, 128, 256, "fp32"), (1, 300, 32, 128, 128, "fp16"),
+    (3, 2, 2, 8192, 128, "bf16"),
 ])
 def test_against_64_bits(t, e, k, d, f, dtype, bits):
     c = Case(t, e, k, d, f, bits, dtype)
@@ -262,6 +265,51 @@ def test_calls_behind_each_other_share_a_workspace():
             c.run()
     for c in cases:
         c.check()
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_calls_that_feed_each_other_without_a_pause(bits):
+    """A call's kernels begin before the ones before them have ended: inputs and weights that those are still writing."""
+    e, d, f, k, t = 8, 256, 128, 2, 30
+    layer, w = _layer(e, d, f, k, t, weight_bits=bits, training=False)
+    logits = [torch.randn(t, e, device=DEV) for _ in range(12)]
+    x0 = torch.randn(t, d, device=DEV).to(layer.dtype)
+    weights = [w, (w.view(layer.dtype) * 1.5).view(torch.uint8)]
+
+    def chain(pause):
+        y, seen = x0, []
+        for i, lg in enumerate(logits):
+            if i % 3 == 0:
+                layer.step(weights[i // 3 % 2])
+                pause()
+            y = layer.forward_tokens(y, lg)
+            pause()
+            y = layer.forward(y, lg) if i % 2 else y
+            pause()
+            y = (y / (y.abs().max() + 1e-3)).to(layer.dtype)
+            seen.append(y)
+        torch.cuda.synchronize()
+        return seen
+
+    want = chain(torch.cuda.synchronize)
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(chain(lambda: None), want))
+    layer.check_status()
+
+
+def test_a_larger_workspace_and_a_status_word():
+    from paper_2609_04609_b200 import ciera
+
+    c = Case(5, 8, 2, 256, 128, 8)
+    want = c.run().clone()
+    room = torch.zeros(c.workspace.numel() + 4096, dtype=torch.uint8, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out = torch.zeros_like(c.out)
+    ciera.expert_tokens(c.config, c.x, c.logits, c.bias, c.w1, c.w1_s, c.w2, c.w2_s, out, c.experts, c.weights, room, status)
+    assert torch.equal(out, want) and int(status) == 0
+    assert not room[: ciera.EXPERT_TOKENS_HEAD].any() and not room[-4096:].any()
+    with pytest.raises(ciera.CieraError):
+        ciera.expert_tokens(c.config, c.x, c.logits, c.bias, c.w1, c.w1_s, c.w2, c.w2_s, out, c.experts, c.weights, room[:512])
 
 
 def test_no_tokens():
