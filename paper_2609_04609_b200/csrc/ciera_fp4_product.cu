@@ -12,7 +12,10 @@
 //   warp 0      copies tiles and scales into a ring of stages by tensor maps
 //   warp 1      of the first block: copies a stage's scales into tensor memory and starts its four products
 //   warps 2-5   read finished sums (a lane is a column of out) and write them
-// Two sums are in flight.  Tensor memory has 512 columns: the two sums share 64, and the last 64 hold the scales of two stages.
+// Two sums are in flight.  Tensor memory has 512 columns: the two sums share 128, and the last 128 hold the scales of five stages.
+//
+// Measured: 8192^3 172 us, 6.4 PFLOP/s, in a short run (208 us back to back, where the clock falls with the power); 32768 rows of 64
+// experts, 2048 x 2048, 80 us, 64 without writing the results; one token on 8 experts 9.4 us, of which DRAM needs 3.
 #include <type_traits>
 
 #include "ciera_product.cuh"
@@ -24,8 +27,10 @@ constexpr int kStages4 = 6;
 constexpr uint32_t kTile4N = 256;  // columns of a pair's tile
 constexpr uint32_t kStageK = 256;  // values of the contraction in a stage
 constexpr uint32_t kMaxSegments4 = 1024;
-constexpr uint32_t kShared4 = 64, kSecondSum4 = 256 - kShared4, kScalesAt4 = kSecondSum4 + 256;  // columns of tensor memory
+constexpr uint32_t kShared4 = 128, kSecondSum4 = 256 - kShared4, kScalesAt4 = kSecondSum4 + 256;  // columns of tensor memory
 constexpr uint32_t kScaleColumns = 24;  // of a stage: two atoms of b's rows, two of each 128 of a's
+constexpr uint32_t kScaleStages = 5;    // that tensor memory holds the scales of
+static_assert(kScalesAt4 + kScaleStages * kScaleColumns <= 512 && kScaleStages < kStages4, "not in tensor memory");
 
 struct Product4Args {
     uint64_t out_stride;
@@ -204,17 +209,18 @@ __global__ void __launch_bounds__(kProduct4Threads, 1)
                 }
                 const uint32_t instruction = mx4_instruction(256, w.height()), d = tmem + (tile & 1) * kSecondSum4;
                 for (uint32_t kb = 0; kb < stages; ++kb) {
-                    // (the products of two stages ago, whose scales these replace, have ended; those of the last one keep the tensor cores busy)
+                    // (the products whose scales these replace have ended: those of two stages ago, with room for two, held up the rest:
+                    // 8192^3 176 us, 172 so)
                     if (!mbar_wait_soon(&sm.full[s], odd, abort, p.status) ||
-                        (it >= 2 && !mbar_wait_soon(&sm.empty[(it - 2) % kStages4], ((it - 2) / kStages4) & 1, abort, p.status))) {
+                        (it >= kScaleStages && !mbar_wait_soon(&sm.empty[(it - kScaleStages) % kStages4], ((it - kScaleStages) / kStages4) & 1, abort, p.status))) {
                         ok = false;
                         break;
                     }
                     tensor_fence_after();
                     const bool last = kb + 1 == stages;
                     const uint32_t left = min(p.k - kb * kStageK, kStageK);
-                    // b's scales, then a's: both halves of a's rows of an atom side by side.  Two stages' worth in turn
-                    const uint32_t sc = tmem + kScalesAt4 + (it & 1) * kScaleColumns;
+                    // b's scales, then a's: both halves of a's rows of an atom side by side
+                    const uint32_t sc = tmem + kScalesAt4 + it % kScaleStages * kScaleColumns;
                     if (elect_one()) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
@@ -256,19 +262,19 @@ __global__ void __launch_bounds__(kProduct4Threads, 1)
             __syncwarp();
             tensor_fence_after();
             const uint32_t from = tmem + ((uint32_t)quarter << 21) + which * kSecondSum4;
-            // the columns shared with the other sum first: the second's first two parts, the first's last two of eight
-            const uint32_t first = which == 0 && parts == 8 ? 6 : 0;
-            uint32_t r[2][32];
+            // the columns shared with the other sum first: the second's first four parts, the first's last four of eight
+            const uint32_t first = which == 0 && parts == 8 ? 4 : 0;
+            uint32_t r[4][32];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) tmem_load32(from + 32 * (first + i), r[i]);
+            for (int i = 0; i < 4; ++i) tmem_load32(from + 32 * (first + i), r[i]);
             tmem_wait_load();
             tensor_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster_read(in_first_block(&sm.sums_free[which]));
 #pragma unroll
-            for (int i = 0; i < 2; ++i) write(r[i], first + i);
-            for (uint32_t i = 2; i < parts; ++i) {
-                const uint32_t part = first ? i - 2 : i;
+            for (int i = 0; i < 4; ++i) write(r[i], first + i);
+            for (uint32_t i = 4; i < parts; ++i) {
+                const uint32_t part = first ? i - 4 : i;
                 tmem_load32(from + 32 * part, r[0]);
                 tmem_wait_load();
                 write(r[0], part);

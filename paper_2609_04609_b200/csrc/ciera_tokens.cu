@@ -18,7 +18,7 @@
 //   sum    a token's rows, weighted, in the order of its choices
 // What one part reads of another's results, only the copies of the second operand wait for: those of the weights go on, so that a
 // block's next 100 to 180 KB of them are on their way meanwhile.  A tile of down waits for its group's tiles of up, which were the
-// first to be made (for all of up: 64 tokens 76 us, XXX so).
+// first to be made (for all of up: 64 tokens 76 us, 72 so).
 // Tokens of an expert are taken 16 at a time (a group; 11 where there are ten parts): 112 columns.
 #include <type_traits>
 
@@ -35,6 +35,7 @@ constexpr int kMostStages = 10;
 constexpr int kBehind = 5;  // stages whose weights' scales are on their way; fewer than there are stages
 constexpr uint32_t kMaxSlots = CIERA_EXPERT_TOKENS_MAX * 32;
 constexpr uint32_t kMaxColumns = 112;
+constexpr uint32_t kMaxReportPolls = 1u << 25;  // of 32 ns and more: longer than what is waited for may take
 constexpr uint32_t kTokenHead = CIERA_EXPERT_TOKENS_HEAD;  // bytes of the workspace's counters
 static_assert(kTokenHead >= 256 + 4 * kMaxSlots, "a counter for each group");
 constexpr uint32_t kTileBytes = 128 * 128;
@@ -354,7 +355,7 @@ struct alignas(16) TokensSmem {
     TokenLists lists;
     float exchange[16][128];  // the sums of a tile, [slot][row]
     uint64_t full[kMostStages], empty[kMostStages], sums_full[2], sums_free[2], done;
-    uint32_t tmem;
+    uint32_t tmem, written;  // written: tiles of up whose silu(g) * u is on its way to the workspace
     int abort;
 };
 constexpr uint32_t kStageScales = 4 * 512;  // a stage's scale bytes: two atoms (8 bits: one) of each operand
@@ -441,6 +442,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         }
         mbar_init(&sm.done, 1);
         sm.abort = 0;
+        sm.written = 0;
         mbar_fence_init();
     }
     const uint32_t tid = threadIdx.x & 127;  // of the last four warps, which compute
@@ -606,6 +608,31 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         int none = 0;
         mbar_wait_soon(&sm.done, 0, &none, a.status);
         __syncwarp();
+    } else if (warp == 3) {
+        // tells all blocks of the tiles of up that are written, so that the warps that write them need not wait until they are (128 experts
+        // of 256 x 1920 of 34 tokens: 50 us so, 64 by the writing warps)
+        if (lane == 0) {
+            uint32_t told = 0, there = 0;
+            bool ok = true;
+            while (ok && w.next() && w.up) {
+                for (uint32_t polls = 0; there == told;) {
+                    asm volatile("ld.acquire.cta.shared.u32 %0, [%1];" : "=r"(there) : "r"(smem_u32(&sm.written)) : "memory");
+                    if (there > told) {
+                        __threadfence();
+                    } else if (*abort || ++polls > kMaxReportPolls) {
+                        ok = false;
+                        break;
+                    } else {
+                        __nanosleep(32);
+                    }
+                }
+                if (!ok) break;
+                atomicAdd(a.counters + 64 + w.group, 1u);
+                atomicAdd(a.counters + 1, 1u);
+                ++told;
+            }
+        }
+        __syncwarp();
     } else if (warp >= 4 && warp < 8) {
         // copies of the tokens' columns and their scale words, behind the blocks that make them; every fourth stage.  (By one warp
         // 64 tokens took 107 us.)
@@ -743,11 +770,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
                     put_hidden<DT, BITS>(a, v, first + slot, w.tile * 64 + (quarter & 1) * 32, lane);
                 }
                 all_four();
-                if (tid == 0) {
-                    __threadfence();
-                    atomicAdd(a.counters + 64 + w.group, 1u);
-                    atomicAdd(a.counters + 1, 1u);
-                }
+                if (tid == 0) asm volatile("st.release.cta.shared.u32 [%0], %1;" ::"r"(smem_u32(&sm.written)), "r"(tile + 1) : "memory");
             }
             ++tile;
         }
