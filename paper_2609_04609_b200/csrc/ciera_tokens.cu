@@ -39,7 +39,11 @@ constexpr uint32_t kMaxReportPolls = 1u << 25;  // of 32 ns and more: longer tha
 constexpr uint32_t kTokenHead = CIERA_EXPERT_TOKENS_HEAD;  // bytes of the workspace's counters
 static_assert(kTokenHead >= 256 + 4 * kMaxSlots, "a counter for each group");
 constexpr uint32_t kTileBytes = 128 * 128;
-constexpr uint32_t kSumColumns = 112, kTokenScalesAt = 2 * kSumColumns, kTokenTmem = 256;  // of tensor memory: two sums, scales
+// Tensor memory: two sums, and the scales of more stages than the ring has, so that the products of a stage whose place a later one's
+// scales take have ended when that one has come.  (Four or two stages' scales, and a wait for them: 0.5 us a call.)
+constexpr uint32_t kSumColumns = 112, kTokenScalesAt = 2 * kSumColumns, kTokenTmem = 512;
+constexpr uint32_t kScaleBuffers = 16;
+static_assert(kScaleBuffers > kMostStages && kTokenScalesAt + kScaleBuffers * 16 <= kTokenTmem, "not in tensor memory");
 
 // Parts of a value and slots of a group.
 template <int BITS, int DT>
@@ -421,7 +425,6 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
                   value_t<DT>* __restrict__ out) {
     constexpr uint32_t P = kParts<BITS, DT>;
     constexpr uint32_t kAtoms = BITS == 8 ? 1 : 2;        // of a stage and operand
-    constexpr uint32_t kBuffers = BITS == 8 ? 4 : 2;      // stages whose scales tensor memory holds
     extern __shared__ uint8_t tokens_smem[];
     uint8_t* ring = tokens_smem + (-smem_u32(tokens_smem) & 1023u);
     TokensSmem& sm = *reinterpret_cast<TokensSmem*>(ring + a.stages * a.stage_bytes);
@@ -561,7 +564,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         cp_async_wait<0>();
         while (behind) report();
     } else if (warp == 2) {
-        uint32_t it = 0, s = 0, odd = 0, tile = 0, before = 0, before_odd = 0;  // before: the stage kBuffers ago
+        uint32_t it = 0, s = 0, odd = 0, tile = 0;
         bool ok = true;
         const uint32_t stage_units = a.stage_bytes / 16;
         const uint64_t da0 = operand_descriptor(ring), db0 = operand_descriptor(ring + kTileBytes), ds0 = scales_descriptor(scales_of(0));
@@ -572,14 +575,12 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
             const uint32_t n = (group_slots(w.packed()) * P + 15) / 16 * 16, d = tmem + which * kSumColumns;
             const uint32_t instruction = BITS == 8 ? mx_instruction(128, n, 0) : mx4_instruction(128, n);
             for (uint32_t k = 0; k < w.stages; ++k, ++it) {
-                // (the products whose scales these replace have ended)
-                if (!mbar_wait_soon(&sm.full[s], odd, abort, a.status) || (it >= kBuffers && !mbar_wait_soon(&sm.empty[before], before_odd, abort, a.status))) {
+                if (!mbar_wait_soon(&sm.full[s], odd, abort, a.status)) {
                     ok = false;
                     break;
                 }
-                if (it >= kBuffers && ++before == a.stages) before = 0, before_odd ^= 1;
                 tensor_fence_after();
-                const uint32_t sc = tmem + kTokenScalesAt + (it % kBuffers) * (8 * kAtoms);
+                const uint32_t sc = tmem + kTokenScalesAt + (it % kScaleBuffers) * (8 * kAtoms);
                 const uint32_t left = w.up ? a.d_model - k * 128 * kAtoms : a.d_ff - k * 128 * kAtoms;  // of the contraction
                 if (elect_one()) {
                     const uint64_t da = da0 + s * stage_units, db = db0 + s * stage_units, ds = ds0 + s * stage_units;
