@@ -26,6 +26,7 @@
 #include "ciera_fp8.cuh"
 #include "ciera_product.cuh"
 #include "ciera_swiglu.cuh"
+#include "ciera_tokens_end.hpp"
 
 namespace ciera {
 
@@ -418,6 +419,78 @@ struct TokenWalk {
     __device__ uint32_t packed() const { return l.group[group]; }
 };
 
+// The end of a call (ciera_tokens_end.hpp).
+template <int DT>
+struct TokensEnd {
+    const TokensArgs& a;
+    TokensSmem& sm;
+    value_t<DT>* out;
+    uint32_t tmem;
+    bool frees;  // the warp that has allocated tensor memory
+
+    __device__ __forceinline__ void join() {
+        __syncthreads();
+        if (frees) {
+            tensor_fence_after();
+            tmem_free_one(tmem, kTokenTmem);
+        }
+    }
+    __device__ __forceinline__ bool all_done() {
+        volatile int* abort = &sm.abort;
+        if (threadIdx.x == 0 && !*abort) wait_for_all(a.counters + 2, gridDim.x, abort, a.status);
+        __syncthreads();
+        return !*abort;
+    }
+    __device__ __forceinline__ void ticket() {
+        if (threadIdx.x == 0) {
+            __threadfence();
+            if (atomicAdd(a.counters + 3, 1u) == gridDim.x - 1) {
+                __threadfence();
+                for (int i = 0; i < 4; ++i) a.counters[i] = 0;
+            }
+        }
+    }
+    __device__ __forceinline__ void clear() {
+        for (uint32_t i = blockIdx.x * kTokenThreads + threadIdx.x; i < sm.lists.groups; i += gridDim.x * kTokenThreads) a.counters[64 + i] = 0;
+    }
+    // a token's rows, in the order of its choices
+    __device__ __forceinline__ void sum() {
+        const uint32_t quads = a.d_model / 4;
+        for (uint32_t i = blockIdx.x * kTokenThreads + threadIdx.x; i < a.n_tokens * quads; i += gridDim.x * kTokenThreads) {
+            const uint32_t token = i / quads, c = (i - token * quads) * 4;
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            for (uint32_t j0 = 0; j0 < a.top_k; j0 += 8) {
+                float4 r[8];
+                float wt[8];
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) {
+                    const uint32_t place = j0 + j < a.top_k ? sm.lists.place[token * a.top_k + j0 + j] : 0xffffu;
+                    r[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    wt[j] = 0.f;
+                    if (place != 0xffffu) {
+                        r[j] = __ldcg(reinterpret_cast<const float4*>(a.rows + (uint64_t)place * a.d_model + c));
+                        wt[j] = __ldg(a.weights + token * a.top_k + j0 + j);
+                    }
+                }
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) {
+                    v[0] = fmaf(wt[j], r[j].x, v[0]);
+                    v[1] = fmaf(wt[j], r[j].y, v[1]);
+                    v[2] = fmaf(wt[j], r[j].z, v[2]);
+                    v[3] = fmaf(wt[j], r[j].w, v[3]);
+                }
+            }
+            value_t<DT>* to = out + token * a.out_stride + c;
+            if (a.out_wide) {
+                store_values<DT, 4>(to, v);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) to[j] = ValueOf<DT>::put(v[j]);
+            }
+        }
+    }
+};
+
 template <int DT, int BITS>
 __global__ void __launch_bounds__(kTokenThreads, 1)
     tokens_kernel(const TokensArgs a, const __grid_constant__ CUtensorMap w1_map, const __grid_constant__ CUtensorMap w2_map,
@@ -628,8 +701,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
                     }
                 }
                 if (!ok) break;
-                atomicAdd(a.counters + 64 + w.group, 1u);
-                atomicAdd(a.counters + 1, 1u);
+                tell([&]() { atomicAdd(a.counters + 64 + w.group, 1u); }, []() { __threadfence(); }, [&]() { atomicAdd(a.counters + 1, 1u); });
                 ++told;
             }
         }
@@ -649,7 +721,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         };
         bool all_up = false;  // of all groups
         while (ok && w.next()) {
-            if (!w.up && !all_up) {
+            if (!w.up && !all_up && takes_part(it, w.stages, warp & 3, kColumnWarps)) {
                 uint32_t tiles, whole;
                 asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(tiles) : "l"(a.counters + 64 + w.group) : "memory");
                 asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(whole) : "l"(a.counters + 1) : "memory");
@@ -777,51 +849,8 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         }
         if (ok) done_with(a.counters + 2);
     }
-    __syncthreads();
-    if (warp == 2) {
-        tensor_fence_after();
-        tmem_free_one(tmem, kTokenTmem);
-    }
-    if (threadIdx.x == 0 && !*abort) wait_for_all(a.counters + 2, blocks, abort, a.status);
-    __syncthreads();
-    if (*abort) return;
-    // a token's rows, in the order of its choices; the last block to leave sets the counters back
-    for (uint32_t i = blockIdx.x * kTokenThreads + threadIdx.x; i < sm.lists.groups; i += blocks * kTokenThreads) a.counters[64 + i] = 0;
-    if (threadIdx.x == 0 && atomicAdd(a.counters + 3, 1u) == blocks - 1)
-        for (int i = 0; i < 4; ++i) a.counters[i] = 0;
-    const uint32_t quads = a.d_model / 4;
-    for (uint32_t i = blockIdx.x * kTokenThreads + threadIdx.x; i < a.n_tokens * quads; i += blocks * kTokenThreads) {
-        const uint32_t token = i / quads, c = (i - token * quads) * 4;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (uint32_t j0 = 0; j0 < a.top_k; j0 += 8) {
-            float4 r[8];
-            float wt[8];
-#pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) {
-                const uint32_t place = j0 + j < a.top_k ? sm.lists.place[token * a.top_k + j0 + j] : 0xffffu;
-                r[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-                wt[j] = 0.f;
-                if (place != 0xffffu) {
-                    r[j] = __ldcg(reinterpret_cast<const float4*>(a.rows + (uint64_t)place * a.d_model + c));
-                    wt[j] = __ldg(a.weights + token * a.top_k + j0 + j);
-                }
-            }
-#pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) {
-                v[0] = fmaf(wt[j], r[j].x, v[0]);
-                v[1] = fmaf(wt[j], r[j].y, v[1]);
-                v[2] = fmaf(wt[j], r[j].z, v[2]);
-                v[3] = fmaf(wt[j], r[j].w, v[3]);
-            }
-        }
-        value_t<DT>* to = out + token * a.out_stride + c;
-        if (a.out_wide) {
-            store_values<DT, 4>(to, v);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) to[j] = ValueOf<DT>::put(v[j]);
-        }
-    }
+    TokensEnd<DT> end{a, sm, out, tmem, warp == 2};
+    end_call(end);
 }
 
 struct TokensRoom {  // offsets of the workspace's parts

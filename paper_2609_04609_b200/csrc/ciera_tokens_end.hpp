@@ -1,0 +1,46 @@
+// How a call of the layer for a few tokens ends on the counters that its blocks wait for one another by.  They are zero before a
+// call and have to be zero behind it, so somebody sets them back, and nobody may be reading or adding then.  Plain C++ over an object
+// that does it, so that every order in which blocks get there can be played through on the CPU.
+//
+//   b.join()       all warps of the block are behind their last wait for a counter and their last addition to one
+//   b.all_done()   waits until every block's tiles are done; false: given up, and the counters stay as they are
+//   b.ticket()     takes the next number, behind join(); who has the last one, and so is behind every block's join(), sets the blocks'
+//                  counters back
+//   b.clear()      sets a share of the groups' counters back
+//   b.sum()        the block's share of the output
+//
+// The groups' counters are set back by all blocks, and only behind all tiles, not behind the other blocks' warps.  So nobody may be
+// reading one who is not needed for a tile (takes_part), and an addition to one has to be behind nobody's back: it is there before
+// what tells of all groups together, by which a reader may have gone instead.
+#pragma once
+
+#ifdef __CUDACC__
+#define CIERA_ON_BOTH __host__ __device__ __forceinline__
+#else
+#define CIERA_ON_BOTH inline
+#endif
+
+namespace ciera {
+
+// Whether one of `warps` warps (a power of two), which take stages in turn, has one of a tile's, the first of which is stage `it`.
+CIERA_ON_BOTH bool takes_part(unsigned it, unsigned stages, unsigned warp, unsigned warps) { return ((warp - it) & (warps - 1)) < stages; }
+
+// Tells of a written tile of a group: `group` adds to the group's counter, `whole` to that of all groups.
+template <class Group, class Fence, class Whole>
+CIERA_ON_BOTH void tell(Group group, Fence fence, Whole whole) {
+    group();
+    fence();
+    whole();
+}
+
+template <class Block>
+CIERA_ON_BOTH bool end_call(Block& b) {
+    b.join();
+    if (!b.all_done()) return false;
+    b.ticket();
+    b.clear();
+    b.sum();
+    return true;
+}
+
+}  // namespace ciera

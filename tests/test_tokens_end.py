@@ -1,0 +1,45 @@
+"""The end of a call of the layer for a few tokens (``csrc/ciera_tokens_end.hpp``, which the kernel runs) on the CPU: no warp waits for a counter
+that has been set back, and all counters are zero behind the call, in whatever order its blocks get there."""
+import os
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+CSRC = os.path.join(HERE, "..", "paper_2609_04609_b200", "csrc")
+ORDERS = 40000
+
+
+@pytest.fixture(scope="module")
+def play(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("tokens_end") / "tokens_end")
+    subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-Werror", "-Wno-cast-function-type", "-I", CSRC, os.path.join(HERE, "tokens_end.cpp"), "-o", exe],
+                   check=True)
+
+    def run(blocks, rule, orders):
+        out = subprocess.run([exe, str(blocks), str(rule), str(orders)], check=True, capture_output=True, text=True).stdout
+        return [int(w) for w in out.split()]
+
+    return run
+
+
+@pytest.mark.parametrize("blocks", [1, 2, 3, 5])
+def test_nobody_waits_for_good_and_all_is_zero(play, blocks):
+    assert play(blocks, 0, ORDERS) == [ORDERS, 0, 0]
+
+
+def test_the_model_sees_a_warp_that_waits_without_a_part(play):
+    assert play(3, 1, ORDERS)[1] > 0
+
+
+def test_the_model_sees_additions_that_come_late(play):
+    assert play(3, 2, ORDERS)[2] > 0
+
+
+def test_the_kernel_goes_by_this():
+    with open(os.path.join(CSRC, "ciera_tokens.cu")) as f:
+        source = f.read()
+    assert "end_call(end)" in source and "tell([&]" in source and "takes_part(it, w.stages, warp & 3, kColumnWarps)" in source
+    lo = source.index("struct TokensEnd")
+    rest = source[:lo] + source[source.index("\n};", lo) :]
+    assert "a.counters[" not in rest  # nobody else sets one back
