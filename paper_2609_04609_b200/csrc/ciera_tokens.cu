@@ -36,7 +36,7 @@ constexpr int kMostStages = 10;
 constexpr int kBehind = 5;  // stages whose weights' scales are on their way; fewer than there are stages
 constexpr uint32_t kMaxSlots = CIERA_EXPERT_TOKENS_MAX * 32;
 constexpr uint32_t kMaxColumns = 112;
-constexpr uint32_t kMaxReportPolls = 1u << 25;  // of 32 ns and more: longer than what is waited for may take
+constexpr uint32_t kMaxReportPolls = 1u << 25;  // of some tens of ns: about as long as the other waits (1.3 s and more)
 constexpr uint32_t kTokenHead = CIERA_EXPERT_TOKENS_HEAD;  // bytes of the workspace's counters
 static_assert(kTokenHead >= 256 + 4 * kMaxSlots, "a counter for each group");
 constexpr uint32_t kTileBytes = 128 * 128;
@@ -373,17 +373,19 @@ __device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
                  : "memory");
     return ok != 0;
 }
-// All blocks have added to a counter.  false: the bounded wait ran out, or another of the block's has.
-__device__ __forceinline__ bool wait_for_all(const uint32_t* counter, uint32_t blocks, volatile int* abort, int32_t* status) {
-    for (uint32_t polls = 0; polls < kMaxPolls; ++polls) {
-        uint32_t seen;
-        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(counter) : "memory");
-        if (seen >= blocks) return true;
-        if (*abort) return false;
-    }
+// A wait of the block has run out: its other waits end too, and the caller is told.
+__device__ __forceinline__ void give_up(volatile int* abort, int32_t* status) {
     *abort = 1;
     if (status) atomicCAS(status, 0, (int32_t)CIERA_ERR_TIMEOUT);
-    return false;
+}
+// All blocks have added to a counter.  false: the bounded wait ran out, or another of the block's has.
+__device__ __forceinline__ bool wait_for_all(const uint32_t* counter, uint32_t blocks, volatile int* abort, int32_t* status) {
+    const auto there = [&]() {
+        uint32_t seen;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(counter) : "memory");
+        return seen >= blocks;
+    };
+    return poll(kMaxPolls, there, [&]() { return *abort != 0; }, [&]() { give_up(abort, status); });
 }
 __device__ __forceinline__ void fence_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
@@ -687,20 +689,16 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         // of 256 x 1920 of 34 tokens: 50 us so, 64 by the writing warps)
         if (lane == 0) {
             uint32_t told = 0, there = 0;
-            bool ok = true;
-            while (ok && w.next() && w.up) {
-                for (uint32_t polls = 0; there == told;) {
+            while (w.next() && w.up) {
+                const auto written = [&]() {
+                    if (there > told) return true;
                     asm volatile("ld.acquire.cta.shared.u32 %0, [%1];" : "=r"(there) : "r"(smem_u32(&sm.written)) : "memory");
-                    if (there > told) {
-                        __threadfence();
-                    } else if (*abort || ++polls > kMaxReportPolls) {
-                        ok = false;
-                        break;
-                    } else {
-                        __nanosleep(32);
-                    }
-                }
-                if (!ok) break;
+                    if (there == told) __nanosleep(32);
+                    return there > told;
+                };
+                const bool fresh = there == told;
+                if (!poll(kMaxReportPolls, written, [&]() { return *abort != 0; }, [&]() { give_up(abort, a.status); })) break;
+                if (fresh) __threadfence();
                 tell([&]() { atomicAdd(a.counters + 64 + w.group, 1u); }, []() { __threadfence(); }, [&]() { atomicAdd(a.counters + 1, 1u); });
                 ++told;
             }

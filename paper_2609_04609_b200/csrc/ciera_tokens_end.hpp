@@ -1,4 +1,4 @@
-// How a call of the layer for a few tokens ends on the counters that its blocks wait for one another by.  They are zero before a
+// The waits of the layer for a few tokens, and how a call ends on the counters that its blocks wait for one another by.  They are zero before a
 // call and have to be zero behind it, so somebody sets them back, and nobody may be reading or adding then.  Plain C++ over an object
 // that does it, so that every order in which blocks get there can be played through on the CPU.
 //
@@ -21,6 +21,18 @@
 #endif
 
 namespace ciera {
+
+// A bounded wait.  True once there() is; false when another of the block's waits has run out, or when this one does, which give_up() then
+// tells the block and the caller.
+template <class There, class GivenUp, class GiveUp>
+CIERA_ON_BOTH bool poll(unsigned most, There there, GivenUp given_up, GiveUp give_up) {
+    for (unsigned i = 0; i < most; ++i) {
+        if (there()) return true;
+        if (given_up()) return false;
+    }
+    give_up();
+    return false;
+}
 
 // Whether one of `warps` warps (a power of two), which take stages in turn, has one of a tile's, the first of which is stage `it`.
 CIERA_ON_BOTH bool takes_part(unsigned it, unsigned stages, unsigned warp, unsigned warps) { return ((warp - it) & (warps - 1)) < stages; }

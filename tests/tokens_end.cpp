@@ -3,6 +3,7 @@
 // block's: two warps that take stages in turn and wait for that group, one that tells of the block's own tile by two additions, which
 // nothing but a fence orders, and the rest, which tells that the block is done and ends the call.
 //   tokens_end BLOCKS RULE ORDERS   RULE 0: the header's; 1, 2: what it must not be (the model has to see it)
+//   tokens_end wait MOST THERE GIVEN_UP
 // prints how many orders there were, in how many a warp waited for a value that had been set back, and in how many a counter was not
 // zero behind the call.
 #include <stdio.h>
@@ -83,7 +84,16 @@ struct Block {
     void sum() { step(); }
 };
 
+// the bounded wait: prints whether it came true, after how many looks, and how often it gave up
+static int waits(unsigned most, unsigned there, unsigned given_up) {
+    unsigned looks = 0, told = 0;
+    const bool ok = ciera::poll(most, [&] { return ++looks == there; }, [&] { return looks == given_up; }, [&] { ++told; });
+    printf("%d %u %u\n", ok, looks, told);
+    return 0;
+}
+
 int main(int argc, char** argv) {
+    if (argc == 5) return waits((unsigned)atoi(argv[2]), (unsigned)atoi(argv[3]), (unsigned)atoi(argv[4]));
     if (argc != 4) return 2;
     blocks = atoi(argv[1]);
     const int rule = atoi(argv[2]);
