@@ -674,9 +674,11 @@ CIERA_API int ciera_fp4_matmul(const ciera_fp4_product* args, void* stream);
  *   x             device, n_tokens rows of d_model values of dtype;  out  the same
  *   logits, bias, experts, weights   as for ciera_route
  *   workspace     device, 16-byte aligned, ciera_expert_tokens_workspace_bytes() of the largest call: zero-filled once, its first
- *                 CIERA_EXPERT_TOKENS_HEAD bytes are handed back zero by every call (but one that reports an error); not shared by
+ *                 CIERA_EXPERT_TOKENS_HEAD bytes are handed back zero by every call but one that was given up; not shared by
  *                 calls that may overlap
- *   status        device int32 or NULL: CIERA_ERR_TIMEOUT if the blocks' bounded wait for each other ran out
+ *   status        device int32 or NULL: CIERA_ERR_TIMEOUT if a bounded wait of the blocks for each other ran out.  Such a call
+ *                 leaves parts of out as they were, and so does every later call on this workspace, which reports the same, until
+ *                 those bytes have been zero-filled again
  * Arithmetic: fp32 sums of 8-bit (4-bit) tensor products.  The weights are what they are; x and silu(g) * u go into the products as
  * sums of parts in the weights' bits, each below a power of two of its own for 32 values.  8 bits: three parts, of which 2^-12 of a
  * value is left out at most and 2^-14 on the average (fp32: five, 2^-20 and 2^-24); bf16 and fp16 values of x are exact next to others

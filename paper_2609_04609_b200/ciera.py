@@ -815,7 +815,7 @@ def expert_tokens(config: RouteConfig, x, logits, bias, w1, w1_scales, w2, w2_sc
     Weights in 8 bits: ``w1`` e4m3 [E, 2 d_ff, d_model] with a scale for each 128 x 128 block, ``w2`` [E, d_model, d_ff].  In 4 bits:
     uint8, half as wide, with scales [E, rows / 128, cols / 128, 512].  ``workspace`` uint8
     [expert_tokens_workspace_bytes(config, T, d_model, d_ff) or more], zeros before the first call; every call leaves it fit for the
-    next."""
+    next, but for one that was given up (``status`` ERR_TIMEOUT), behind which it has to be filled with zeros again."""
     w = "ciera_expert_tokens"
     device = _device_of(w, x)
     dtype = x.dtype

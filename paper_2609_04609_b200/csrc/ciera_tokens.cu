@@ -36,7 +36,7 @@ constexpr int kMostStages = 10;
 constexpr int kBehind = 5;  // stages whose weights' scales are on their way; fewer than there are stages
 constexpr uint32_t kMaxSlots = CIERA_EXPERT_TOKENS_MAX * 32;
 constexpr uint32_t kMaxColumns = 112;
-constexpr uint32_t kMaxReportPolls = 1u << 25;  // of some tens of ns: about as long as the other waits (1.3 s and more)
+constexpr uint32_t kMaxReportPolls = 1u << 25;  // of some tens of ns: longer than what is waited for may take
 constexpr uint32_t kTokenHead = CIERA_EXPERT_TOKENS_HEAD;  // bytes of the workspace's counters
 static_assert(kTokenHead >= 256 + 4 * kMaxSlots, "a counter for each group");
 constexpr uint32_t kTileBytes = 128 * 128;
@@ -378,12 +378,14 @@ __device__ __forceinline__ void give_up(volatile int* abort, int32_t* status) {
     *abort = 1;
     if (status) atomicCAS(status, 0, (int32_t)CIERA_ERR_TIMEOUT);
 }
-// All blocks have added to a counter.  false: the bounded wait ran out, or another of the block's has.
+// All blocks have added to a counter.  false: the bounded wait ran out, or another of the block's has, or a call before this one was given
+// up and the workspace has not been zeros since.
 __device__ __forceinline__ bool wait_for_all(const uint32_t* counter, uint32_t blocks, volatile int* abort, int32_t* status) {
     const auto there = [&]() {
         uint32_t seen;
         asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(counter) : "memory");
-        return seen >= blocks;
+        if (seen >= kSpoiled) give_up(abort, status);
+        return seen >= blocks && seen < kSpoiled;
     };
     return poll(kMaxPolls, there, [&]() { return *abort != 0; }, [&]() { give_up(abort, status); });
 }
@@ -436,6 +438,9 @@ struct TokensEnd {
             tensor_fence_after();
             tmem_free_one(tmem, kTokenTmem);
         }
+    }
+    __device__ __forceinline__ void spoil() {
+        if (threadIdx.x == 0) atomicOr(a.counters, kSpoiled);
     }
     __device__ __forceinline__ bool all_done() {
         volatile int* abort = &sm.abort;

@@ -8,6 +8,7 @@
 //                  counters back
 //   b.clear()      sets a share of the groups' counters back
 //   b.sum()        the block's share of the output
+//   b.spoil()      marks the counters of a call that was given up, so that none that comes behind it goes by them
 //
 // The groups' counters are set back by all blocks, and only behind all tiles, not behind the other blocks' warps.  So nobody may be
 // reading one who is not needed for a tile (takes_part), and an addition to one has to be behind nobody's back: it is there before
@@ -34,6 +35,9 @@ CIERA_ON_BOTH bool poll(unsigned most, There there, GivenUp given_up, GiveUp giv
     return false;
 }
 
+// The first counter of a call that was given up: no call gets there by adding.
+constexpr unsigned kSpoiled = 1u << 31;
+
 // Whether one of `warps` warps (a power of two), which take stages in turn, has one of a tile's, the first of which is stage `it`.
 CIERA_ON_BOTH bool takes_part(unsigned it, unsigned stages, unsigned warp, unsigned warps) { return ((warp - it) & (warps - 1)) < stages; }
 
@@ -48,7 +52,10 @@ CIERA_ON_BOTH void tell(Group group, Fence fence, Whole whole) {
 template <class Block>
 CIERA_ON_BOTH bool end_call(Block& b) {
     b.join();
-    if (!b.all_done()) return false;
+    if (!b.all_done()) {
+        b.spoil();
+        return false;
+    }
     b.ticket();
     b.clear();
     b.sum();

@@ -251,6 +251,6 @@ class ExpertLayer:
         s = int(self.status.item())
         if s != 0:
             self.status.zero_()
-            self.few_workspace.zero_()  # (a call that gave up leaves its counters as they are)
+            self.few_workspace.zero_()  # (calls behind one that gave up give up too until then)
             torch.cuda.synchronize(self.device)
             raise ciera.CieraError("device status", s)

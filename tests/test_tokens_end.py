@@ -18,7 +18,7 @@ def play(tmp_path_factory):
 
     def run(*what):
         out = subprocess.run([exe, *map(str, what)], check=True, capture_output=True, text=True).stdout
-        return [int(w) for w in out.split()]
+        return [int(w) if w.isdigit() else w for w in out.split()]
 
     return run
 
@@ -45,12 +45,16 @@ def test_a_wait_that_runs_out_is_told(play, most, there, given_up, want):
     assert play("wait", most, there, given_up) == want
 
 
+def test_a_block_that_gives_up_spoils_the_counters_and_writes_nothing(play):
+    assert play("give_up") == ["join", "spoil"]
+
+
 def test_the_kernel_goes_by_this():
     with open(os.path.join(CSRC, "ciera_tokens.cu")) as f:
         source = f.read()
     assert "end_call(end)" in source and "tell([&]" in source and "takes_part(it, w.stages, warp & 3, kColumnWarps)" in source
     # both waits for other threads' words, those for all blocks and those for written tiles
-    assert source.count("poll(k") == 2 and source.count("give_up(abort, ") == 2 and "kMaxReportPolls)" not in source
+    assert "poll(kMaxPolls, " in source and "poll(kMaxReportPolls, " in source
     lo = source.index("struct TokensEnd")
     rest = source[:lo] + source[source.index("\n};", lo) :]
     assert "a.counters[" not in rest  # nobody else sets one back

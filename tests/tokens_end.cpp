@@ -3,6 +3,7 @@
 // block's: two warps that take stages in turn and wait for that group, one that tells of the block's own tile by two additions, which
 // nothing but a fence orders, and the rest, which tells that the block is done and ends the call.
 //   tokens_end BLOCKS RULE ORDERS   RULE 0: the header's; 1, 2: what it must not be (the model has to see it)
+//   tokens_end give_up
 //   tokens_end wait MOST THERE GIVEN_UP
 // prints how many orders there were, in how many a warp waited for a value that had been set back, and in how many a counter was not
 // zero behind the call.
@@ -82,6 +83,7 @@ struct Block {
     }
     void clear() { counters[kGroups + (rank + 2) % blocks] = 0; }  // (told of by one block, read by another)
     void sum() { step(); }
+    void spoil() {}
 };
 
 // the bounded wait: prints whether it came true, after how many looks, and how often it gave up
@@ -92,7 +94,21 @@ static int waits(unsigned most, unsigned there, unsigned given_up) {
     return 0;
 }
 
+// a block that gives up: prints what it is asked for
+struct GivesUp {
+    void join() { printf("join "); }
+    bool all_done() { return false; }
+    void spoil() { printf("spoil\n"); }
+    void ticket() { printf("ticket "); }
+    void clear() { printf("clear "); }
+    void sum() { printf("sum "); }
+};
+
 int main(int argc, char** argv) {
+    if (argc == 2) {
+        GivesUp b;
+        return ciera::end_call(b) ? 1 : 0;
+    }
     if (argc == 5) return waits((unsigned)atoi(argv[2]), (unsigned)atoi(argv[3]), (unsigned)atoi(argv[4]));
     if (argc != 4) return 2;
     blocks = atoi(argv[1]);
