@@ -321,9 +321,6 @@ __device__ __forceinline__ void pdl_wait() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
-// the argument checks of ciera_route
-int check_route(const ciera_route_config* config, int dtype, const void* logits_dev, uint64_t n_tokens, uint64_t logits_stride,
-                const float* bias_dev, const int32_t* experts_dev, const float* weights_dev);
 int check_launch();                            // cudaGetLastError -> status
 void count_plan(int change);                   // plans that exist
 // the persistent sender kernel with HashCache in place of the exponent cache (ciera_encode.cu)

@@ -82,15 +82,12 @@ template <int N>
 __device__ __forceinline__ void bulk_wait_all() {
     asm volatile("cp.async.bulk.wait_group %0;" ::"n"(N) : "memory");
 }
-// per-thread asynchronous global -> shared copies of 4, 8 or 16 bytes (no registers held while in flight)
+// per-thread asynchronous global -> shared copies of 4 or 16 bytes (no registers held while in flight)
 __device__ __forceinline__ void cp_async4(void* smem_dst, const void* gsrc) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(smem_dst)), "l"(gsrc) : "memory");
 }
 __device__ __forceinline__ void cp_async16(void* smem_dst, const void* gsrc) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(smem_dst)), "l"(gsrc) : "memory");
-}
-__device__ __forceinline__ void cp_async8(void* smem_dst, const void* gsrc) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(smem_dst)), "l"(gsrc) : "memory");
 }
 // the first `bytes` (0 .. 16) of 16 bytes; the others are not read and arrive as zero
 __device__ __forceinline__ void cp_async16_first(void* smem_dst, const void* gsrc, uint32_t bytes) {

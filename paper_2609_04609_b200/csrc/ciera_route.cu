@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "ciera_numeric.cuh"
+#include "ciera_route.cuh"
 
 namespace ciera {
 

@@ -25,6 +25,7 @@
 #include "ciera_fp4.cuh"
 #include "ciera_fp8.cuh"
 #include "ciera_product.cuh"
+#include "ciera_route.cuh"
 #include "ciera_swiglu.cuh"
 #include "ciera_tokens_end.hpp"
 
@@ -344,6 +345,10 @@ __device__ __forceinline__ void map_load3_one(void* dst, const void* map, int32_
                      smem_u32(dst)),
                  "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
                  : "memory");
+}
+// an asynchronous copy of 8 bytes (cp_async4 and cp_async16 have the others)
+__device__ __forceinline__ void cp_async8(void* smem_dst, const void* gsrc) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(smem_dst)), "l"(gsrc) : "memory");
 }
 // 16 columns of the warp's 32 lanes
 __device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t (&r)[16]) {
