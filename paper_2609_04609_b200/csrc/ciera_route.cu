@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
                      const float* __restrict__ bias, int32_t* __restrict__ experts, float* __restrict__ weights) {
     extern __shared__ __align__(16) float route_smem[];
     __shared__ int chosen[kRouteWarps][32];
-    pdl_wait();
+    pdl_wait();  // first of all: ciera_route.cuh says who goes by that
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t E = a.n_experts, e0 = lane * EPL;
     float* scratch = route_smem + warp * 2 * E;

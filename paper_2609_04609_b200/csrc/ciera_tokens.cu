@@ -240,7 +240,7 @@ __device__ __forceinline__ uint32_t next_byte(uint32_t first, uint32_t p) {
 
 // 128 values of a token, four a lane, as parts.
 template <int DT, int BITS>
-__device__ __forceinline__ void make_parts(const TokensArgs& a, const value_t<DT>* __restrict__ x, uint32_t token, uint32_t kb, uint32_t lane) {
+__device__ __forceinline__ void make_parts(const TokensArgs& a, const value_t<DT>* x, uint32_t token, uint32_t kb, uint32_t lane) {
     constexpr uint32_t P = kParts<BITS, DT>;
     float v[4];
     const value_t<DT>* from = x + token * a.x_stride + kb * 128 + lane * 4;
@@ -428,7 +428,8 @@ struct TokenWalk {
     __device__ uint32_t packed() const { return l.group[group]; }
 };
 
-// The end of a call (ciera_tokens_end.hpp).
+// The end of a call (ciera_tokens_end.hpp).  (The router writes its choice and weights while this kernel runs, so they are not read as what
+// nobody writes.)
 template <int DT>
 struct TokensEnd {
     const TokensArgs& a;
@@ -481,7 +482,7 @@ struct TokensEnd {
                     wt[j] = 0.f;
                     if (place != 0xffffu) {
                         r[j] = __ldcg(reinterpret_cast<const float4*>(a.rows + (uint64_t)place * a.d_model + c));
-                        wt[j] = __ldg(a.weights + token * a.top_k + j0 + j);
+                        wt[j] = a.weights[token * a.top_k + j0 + j];
                     }
                 }
 #pragma unroll
@@ -506,7 +507,7 @@ struct TokensEnd {
 template <int DT, int BITS>
 __global__ void __launch_bounds__(kTokenThreads, 1)
     tokens_kernel(const TokensArgs a, const __grid_constant__ CUtensorMap w1_map, const __grid_constant__ CUtensorMap w2_map,
-                  const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap hidden_map, const value_t<DT>* __restrict__ x,
+                  const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap hidden_map, const value_t<DT>* x,
                   value_t<DT>* __restrict__ out) {
     constexpr uint32_t P = kParts<BITS, DT>;
     constexpr uint32_t kAtoms = BITS == 8 ? 1 : 2;        // of a stage and operand
@@ -547,7 +548,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         tensor_fence_before();
     } else if (warp >= 8) {
         // Before the router has ended: it lets this kernel begin when all that came before it has, the call before this one and whatever
-        // wrote x.
+        // wrote x (ciera_route.cuh).
         const uint32_t kbs = a.d_model / 128;
         for (uint32_t u = blockIdx.x * 4 + (warp & 3); u < a.n_tokens * kbs; u += gridDim.x * 4) make_parts<DT, BITS>(a, x, u / kbs, u % kbs, lane);
         done_with(a.counters);
