@@ -700,19 +700,20 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         // of 256 x 1920 of 34 tokens: 50 us so, 64 by the writing warps)
         if (lane == 0) {
             uint32_t told = 0, there = 0;
-            while (w.next() && w.up) {
+            const auto next = [&]() {
+                if (!w.next() || !w.up) return false;
+                if (there > told) return true;
                 const auto written = [&]() {
-                    if (there > told) return true;
                     asm volatile("ld.acquire.cta.shared.u32 %0, [%1];" : "=r"(there) : "r"(smem_u32(&sm.written)) : "memory");
-                    if (there == told) __nanosleep(32);
-                    return there > told;
+                    if (there > told) return true;
+                    __nanosleep(32);
+                    return false;
                 };
-                const bool fresh = there == told;
-                if (!poll(kMaxReportPolls, written, [&]() { return *abort != 0; }, [&]() { give_up(abort, a.status); })) break;
-                if (fresh) __threadfence();
-                tell([&]() { atomicAdd(a.counters + 64 + w.group, 1u); }, []() { __threadfence(); }, [&]() { atomicAdd(a.counters + 1, 1u); });
-                ++told;
-            }
+                if (!poll(kMaxReportPolls, written, [&]() { return *abort != 0; }, [&]() { give_up(abort, a.status); })) return false;
+                __threadfence();
+                return true;
+            };
+            tell(next, [&]() { atomicAdd(a.counters + 64 + w.group, 1u), ++told; }, []() { __threadfence(); }, [&]() { if (told) atomicAdd(a.counters + 1, told); });
         }
         __syncwarp();
     } else if (warp >= 4 && warp < 8) {

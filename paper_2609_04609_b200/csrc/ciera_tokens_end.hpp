@@ -41,10 +41,11 @@ constexpr unsigned kSpoiled = 1u << 31;
 // Whether one of `warps` warps (a power of two), which take stages in turn, has one of a tile's, the first of which is stage `it`.
 CIERA_ON_BOTH bool takes_part(unsigned it, unsigned stages, unsigned warp, unsigned warps) { return ((warp - it) & (warps - 1)) < stages; }
 
-// Tells of a written tile of a group: `group` adds to the group's counter, `whole` to that of all groups.
-template <class Group, class Fence, class Whole>
-CIERA_ON_BOTH void tell(Group group, Fence fence, Whole whole) {
-    group();
+// Tells of a block's written tiles: next() waits for one, group() adds it to its group's counter; behind the last whole() adds all of them to
+// that of all groups.  (A fence for each tile: 2 us more for five tokens on 256 experts.)
+template <class Next, class Group, class Fence, class Whole>
+CIERA_ON_BOTH void tell(Next next, Group group, Fence fence, Whole whole) {
+    while (next()) group();
     fence();
     whole();
 }

@@ -52,7 +52,7 @@ def test_a_block_that_gives_up_spoils_the_counters_and_writes_nothing(play):
 def test_the_kernel_goes_by_this():
     with open(os.path.join(CSRC, "ciera_tokens.cu")) as f:
         source = f.read()
-    assert "end_call(end)" in source and "tell([&]" in source and "takes_part(it, w.stages, warp & 3, kColumnWarps)" in source
+    assert "end_call(end)" in source and "tell(next, [&]" in source and "takes_part(it, w.stages, warp & 3, kColumnWarps)" in source
     # both waits for other threads' words, those for all blocks and those for written tiles
     assert "poll(kMaxPolls, " in source and "poll(kMaxReportPolls, " in source
     lo = source.index("struct TokensEnd")

@@ -123,7 +123,8 @@ int main(int argc, char** argv) {
         std::vector<int> ended(blocks, 0), copied(blocks, 0);
         for (int r = 0; r < blocks; ++r) {
             spawn([r, rule, &ended] {
-                ciera::tell([&] { add(r, kGroups + r); }, [&] { if (rule != 2) fence(r); }, [&] { add(r, kWhole); });
+                int tiles = 0;
+                ciera::tell([&] { return tiles++ == 0; }, [&] { add(r, kGroups + r); }, [&] { if (rule != 2) fence(r); }, [&] { add(r, kWhole); });
                 ++ended[r];
             });
             for (unsigned warp = 0; warp < 2; ++warp)
