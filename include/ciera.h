@@ -669,8 +669,8 @@ CIERA_API int ciera_fp4_matmul(const ciera_fp4_product* args, void* stream);
  *   experts, weights = ciera_route(logits, bias);   out[t] = sum over j of weights[t, j] * W2 (silu(g) * u),  (g, u) = W1 x[t]
  * with W1 [2 * d_ff, d_model] (gate above up) and W2 [d_model, d_ff] of the choice's expert; choices of -1 are passed over, a
  * token without any gets zeros.  The matrices stay in 8 bits (CIERA_WEIGHTS_FP8: e4m3 with a scale for each 128 x 128 block, as
- * ciera_fp8_quantize_blocks makes them) or 4 (CIERA_WEIGHTS_FP4, scales_stride and so on as above); x keeps its own precision,
- * other than in ciera_fp8_matmul.  An expert's matrices are read once for up to 16 of its tokens (11 in fp32 on 4 bits).
+ * ciera_fp8_quantize_blocks makes them) or 4 (CIERA_WEIGHTS_FP4, scales_stride and so on as above); x is not rounded to them, other
+ * than in ciera_fp8_matmul.  An expert's matrices are read once for up to 16 of its tokens (12 in fp32 on 4 bits).
  *   x             device, n_tokens rows of d_model values of dtype;  out  the same
  *   logits, bias, experts, weights   as for ciera_route
  *   workspace     device, 16-byte aligned, ciera_expert_tokens_workspace_bytes() of the largest call: zero-filled once, its first
@@ -680,9 +680,10 @@ CIERA_API int ciera_fp4_matmul(const ciera_fp4_product* args, void* stream);
  *                 leaves parts of out as they were, and so does every later call on this workspace, which reports the same, until
  *                 those bytes have been zero-filled again
  * Arithmetic: fp32 sums of 8-bit (4-bit) tensor products.  The weights are what they are; x and silu(g) * u go into the products as
- * sums of parts in the weights' bits, each below a power of two of its own for 32 values.  8 bits: three parts, of which 2^-12 of a
- * value is left out at most and 2^-14 on the average (fp32: five, 2^-20 and 2^-24); bf16 and fp16 values of x are exact next to others
- * within 2^15.  4 bits: six parts, seven for fp16 and ten for fp32: 2^-11.6, 2^-13.6 and 2^-19.6 of the largest of 32 at most.  A
+ * sums of parts in the weights' bits, each with a power of two for 32 neighbouring values.  8 bits: five parts, which leave out at most
+ * 2^-24 of a value or 2^-36 of the largest of its 32, whichever is more; bf16 (fp16) values of x are exact beside others up to 2^26
+ * (2^23) times as large.  4 bits: seven parts, which leave out 2^-19 of the largest of the 32 at most, bf16 (fp16) values exact beside
+ * others up to 2^11 (2^8) times as large; fp32 nine parts and 2^-25.  (What is below 2^-127 counts for nothing.)  A
  * token with an infinity or a NaN gets NaN, and nobody else does.  Results do not depend on the other tokens of a call.
  * Limits: n_tokens 0 .. CIERA_EXPERT_TOKENS_MAX, d_model and d_ff multiples of 128 up to 65536, config as for ciera_route; weights
  * and their strides as for the products. */

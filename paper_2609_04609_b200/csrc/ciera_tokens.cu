@@ -3,11 +3,12 @@
 // What it costs is reading the matrices of the experts that are reached, once: one token of 8 experts of 2048 x 1024 reads 50 MB
 // in 8 bits and multiplies each weight once.  So the weights go from memory to the tensor cores without passing through a
 // register: a tile of 128 rows comes by tensor map and is the first operand as it is, in 8 bits (kind::mxf8f6f4) or 4 (kind::mxf4),
-// with its powers of two; the tokens are the second operand, in the same bits.  A token's values keep their own precision there: they
-// come as a sum of parts, each rounded to 8 or 4 bits below a power of two of its own for 32 values, every part a column of the
-// product, whose sums are added in the end.  An e4m3 part leaves 2^-4 of a value at most (bf16 takes two, fp16 three), so three leave
-// 2^-12, on the average 2^-14; an e2m1 part leaves 1/3 of the largest of 32 at most and each further one a quarter of that, so six
-// leave 2^-11.6, on the average 2^-13.
+// with its powers of two; the tokens are the second operand, in the same bits.  A token's values are not rounded to those: they come as
+// a sum of parts, each rounded to 8 or 4 bits below a power of two of its own for 32 values, every part a column of the product,
+// whose sums are added in the end.  An e4m3 part has four bits and a sign, so five take all 24 of a 32-bit value, x's or the middle's.  An
+// e2m1 part takes three bits below the largest of 32: seven leave 2^-19 of that at most, what rounding a value 2^10 times smaller to bf16
+// does, and nine (fp32) 2^-25.  (Three and six, 2^-14 of a value and 2^-13 of the largest: 64 tokens in 8 bits 72.1 us, 73.9 so;
+// 34 of 128 experts of 256 x 1920 47.6, 57.9; in 4 bits 64 tokens 51.1, 52.4.  Nine in 4 bits for all types: 56.5.)
 // (With weights made fp16 in registers and 16-bit tensor products the same took 300 instructions for 2 KB: one token 24 us, 64
 // tokens 164 us.)
 //
@@ -17,9 +18,9 @@
 //   down   tiles of 128 rows of the output, expert by expert, as fp32 to the workspace
 //   sum    a token's rows, weighted, in the order of its choices
 // What one part reads of another's results, only the copies of the second operand wait for: those of the weights go on, so that a
-// block's next 100 to 180 KB of them are on their way meanwhile.  A tile of down waits for its group's tiles of up, which were the
+// block's next 96 to 160 KB of them are on their way meanwhile.  A tile of down waits for its group's tiles of up, which were the
 // first to be made (for all of up: 64 tokens 76 us, 72 so).
-// Tokens of an expert are taken 16 at a time (a group; 11 where there are ten parts): 112 columns.
+// Tokens of an expert are taken 16 at a time (a group; 12 where there are nine parts): 112 columns.
 #include <type_traits>
 
 #include "ciera_fp4.cuh"
@@ -49,7 +50,7 @@ static_assert(kScaleBuffers > kMostStages && kTokenScalesAt + kScaleBuffers * 16
 
 // Parts of a value and slots of a group.
 template <int BITS, int DT>
-constexpr int kParts = BITS == 8 ? (DT == CIERA_FP32 ? 5 : 3) : (DT == CIERA_FP32 ? 10 : DT == CIERA_FP16 ? 7 : 6);
+constexpr int kParts = BITS == 8 ? 5 : DT == CIERA_FP32 ? 9 : 7;
 template <int BITS, int DT>
 constexpr uint32_t kGroupSlots = kMaxColumns / kParts<BITS, DT> < 16 ? kMaxColumns / kParts<BITS, DT> : 16;
 
@@ -138,7 +139,7 @@ __device__ __forceinline__ void make_lists(TokenLists& l, ListScratch& s, const 
         if (id[j] >= 0 && rank[j] == 0) s.count[chunk * E + id[j]] = (uint16_t)__popc(same);
     }
     __syncthreads();
-    // an expert's slots before each 32, then places and groups before each expert, a thread for each (of 256 at a time): slots in the
+    // an expert's slots before each 32, then places and groups before each expert, a thread for each (of 384 at a time): slots in the
     // low half, groups in the high one
     uint32_t base = 0;
     for (uint32_t e0 = 0; e0 < E; e0 += kTokenThreads) {
@@ -230,12 +231,14 @@ __device__ __forceinline__ uint32_t take_part4(float (&v)[4], float inv, float u
     return r;
 }
 
-// What a part leaves fits below a power of two that is known beforehand: of values up to 448 * 2^s e4m3 leaves at most 16 * 2^s, which
-// is less than 448 * 2^(s - 4), and of those up to 6 * 2^s e2m1 leaves 2^s, less than 6 * 2^(s - 2).  So only the first part's
-// power has to be looked for.  (A reduction over 32 lanes for each part: 1 us for the six of one slot, of which a tile has up to 16.)
+// What a part leaves fits below a power of two that is known beforehand, so only the first part's has to be looked for.  Of values up to
+// 448 * 2^s e4m3 leaves at most 16 * 2^s = 256 * 2^(s - 4), and of those up to 256 units 8, which is 256 of a unit 32 times smaller.  Of
+// values up to 6 * 2^s e2m1 leaves at most 2^s = 4 * 2^(s - 2), and of those up to 4 units 1/2, which is 4 of a unit 8 times smaller.
+// (A reduction over 32 lanes for each part: 1 us for the six of one slot, of which a tile has up to 16.)
 template <int BITS>
 __device__ __forceinline__ uint32_t next_byte(uint32_t first, uint32_t p) {
-    return (uint32_t)max((int)first - (int)(p * (BITS == 8 ? 4 : 2)), 1);
+    const int below = p == 0 ? 0 : BITS == 8 ? 4 + 5 * (int)(p - 1) : 2 + 3 * (int)(p - 1);
+    return (uint32_t)max((int)first - below, 1);
 }
 
 // 128 values of a token, four a lane, as parts.
@@ -866,7 +869,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
 struct TokensRoom {  // offsets of the workspace's parts
     uint64_t x_parts, x_scales, hidden, hidden_scales, rows, all;
 };
-// `parts`: ten suffice for every type and format (five of 8 bits take as much room as ten of 4)
+// `parts`: ten of 4 bits suffice for every type and format (five of 8 bits take as much room)
 static TokensRoom tokens_room(uint64_t tokens, uint64_t top_k, uint64_t d, uint64_t f, uint64_t bits, uint64_t parts) {
     const uint64_t slots = tokens * top_k;
     const auto up = [](uint64_t v) { return (v + 255) / 256 * 256; };
