@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(kFp4Threads, SRC == CIERA_SOURCE_SWIGLU ? 3 : 
                         const float g = v[i];
                         low |= g < kLowestGate;
                         some |= g != 0.f && u[i] != 0.f;
-                        v[i] = swiglu32(g, u[i]);
+                        v[i] = swiglu32_any(g, u[i]);
                     }
                     if (low) {
 #pragma unroll 1

@@ -21,5 +21,8 @@ __device__ __forceinline__ float2 sigmoid32(float g) {
     return make_float2(s, e * s);  // (a NaN is not seen here; g itself is a factor of all that this goes into)
 }
 __device__ __forceinline__ float swiglu32(float g, float u) { return g * sigmoid32(g).x * u; }
+// The same with the gate last: g * sigmoid(g) of a gate below 2^-126 has lost bits, of the least one all, which a large u would bring back,
+// while sigmoid(g) * u is below 2^-126 only where the result counts for nothing beside the least power of two of a group.
+__device__ __forceinline__ float swiglu32_any(float g, float u) { return g * (sigmoid32(g).x * u); }
 
 }  // namespace ciera
