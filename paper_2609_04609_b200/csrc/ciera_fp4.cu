@@ -599,9 +599,12 @@ static uint64_t warp_units(uint64_t rows, uint64_t cols) {
     return (rows + 127) / 128 * (rows < 32 ? rows : 32) * ((cols + 255) / 256);
 }
 
-// Warps' work: 32 lines for each block of 128 rows (of a single block with fewer rows those that it has), whole if that leaves 24 warps
-// an SM, else in pieces.
-static uint64_t rows_units(uint64_t rows, uint64_t cols, uint64_t matrices, uint32_t* each, uint32_t* chunks, uint32_t warps = 24) {
+// Warps' work: 32 lines for each block of 128 rows (of a single block with fewer rows those that it has), whole if that leaves `warps`
+// warps for each of the 148 SMs over the whole call, else in pieces.  Long pieces have the next tile's values on their way, short ones end
+// together: 24 for rows as they are, which have four rows ahead (32768 gathered rows of 2048 29.7 us, with 48 29.9, with 96 32.2), 96 for
+// silu(g) * u, which has two and more to do for each (8008 rows of 1001 27.2 us, with 48 30.1; 32768 of 1024 50.7, with 48 52.1, with 192 54.8).
+constexpr uint32_t kRowWarps = 24, kSwigluWarps = 96;
+static uint64_t rows_units(uint64_t rows, uint64_t cols, uint64_t matrices, uint32_t* each, uint32_t* chunks, uint32_t warps) {
     const uint64_t tiles = (cols + 255) / 256, lines = (rows + 127) / 128 * (rows < 32 ? rows : 32);
     const uint64_t most = lines * tiles * matrices / (148 * warps);
     *each = (uint32_t)(most < 1 ? 1 : most > tiles ? tiles : most);
@@ -652,7 +655,7 @@ extern "C" int ciera_fp4_quantize_rows(const ciera_fp4_rows* p, void* stream) {
     if (rc) return rc;
     if (!aligned_to(p->x, dtype_bytes(p->dtype)) || !aligned_to(p->slot_of_row, 4) || !aligned_to(p->starts, 4)) return CIERA_ERR_MISALIGNED;
     uint32_t each, chunks;
-    const uint64_t units = rows_units(p->rows, p->cols, 1, &each, &chunks, swiglu ? 96 : 24);
+    const uint64_t units = rows_units(p->rows, p->cols, 1, &each, &chunks, swiglu ? kSwigluWarps : kRowWarps);
     if (units > kMaxExtent) return CIERA_ERR_UNSUPPORTED;
     const Rows4Args a{p->x_stride, 0, p->q_stride, 0, p->scales_stride, 0, p->x_rows, p->slot_of_row, p->starts, (uint32_t)p->rows,
                       (uint32_t)p->cols, (uint32_t)((p->cols + 255) / 256), (uint32_t)units, each, chunks, p->slot_of_row ? p->top_k : 1u, p->n_experts,
@@ -680,7 +683,7 @@ extern "C" int ciera_fp4_quantize_matrices(const ciera_fp4_matrices* p, void* st
         if (rc) return rc;
     }
     uint32_t each, chunks;
-    const uint64_t v = dtype_bytes(p->dtype), units = rows_units(p->rows, p->cols, p->matrices, &each, &chunks), wide_cols = 256 / v;
+    const uint64_t v = dtype_bytes(p->dtype), units = rows_units(p->rows, p->cols, p->matrices, &each, &chunks, kRowWarps), wide_cols = 256 / v;
     const uint64_t row_tiles = (p->rows + 127) / 128, col_tiles = (p->cols + wide_cols - 1) / wide_cols;
     if (units > kMaxExtent || row_tiles * col_tiles > kMaxExtent) return CIERA_ERR_UNSUPPORTED;
     cudaError_t e = cudaSuccess;
