@@ -14,8 +14,8 @@
 //   warps 2-5   read finished sums (a lane is a column of out) and write them
 // Two sums are in flight.  Tensor memory has 512 columns: the two sums share 128, and the last 128 hold the scales of five stages.
 //
-// Measured: 8192^3 172 us, 6.4 PFLOP/s, in a short run (208 us back to back, where the clock falls with the power); 32768 rows of 64
-// experts, 2048 x 2048, 80 us, 64 without writing the results; one token on 8 experts 9.4 us, of which DRAM needs 3.
+// Measured: 8192^3 174 to 177 us, 6.3 PFLOP/s, in a short run (208 us back to back, where the clock falls with the power); 32768 rows of
+// 64 experts, 2048 x 2048, 79 us, 64 without writing the results (97 back to back); one token on 8 experts 9.6 us, of which DRAM needs 3.
 #include <type_traits>
 
 #include "ciera_product.cuh"
@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(kProduct4Threads, 1)
                 const uint32_t instruction = mx4_instruction(256, w.height()), d = tmem + (tile & 1) * kSecondSum4;
                 for (uint32_t kb = 0; kb < stages; ++kb) {
                     // (the products whose scales these replace have ended: those of two stages ago, with room for two, held up the rest:
-                    // 8192^3 176 us, 172 so)
+                    // 8192^3 176 us in a short run, 172 so; no difference back to back)
                     if (!mbar_wait_soon(&sm.full[s], odd, abort, p.status) ||
                         (it >= kScaleStages && !mbar_wait_soon(&sm.empty[(it - kScaleStages) % kStages4], ((it - kScaleStages) / kStages4) & 1, abort, p.status))) {
                         ok = false;
