@@ -671,7 +671,7 @@ CIERA_API int ciera_fp4_matmul(const ciera_fp4_product* args, void* stream);
  * token without any gets zeros.  The matrices stay in 8 bits (CIERA_WEIGHTS_FP8: e4m3 with a scale for each 128 x 128 block, as
  * ciera_fp8_quantize_blocks makes them) or 4 (CIERA_WEIGHTS_FP4, scales_stride and so on as above); x is not rounded to them, other
  * than in ciera_fp8_matmul.  An expert's matrices are read once for up to 16 of its tokens (12 in fp32 on 4 bits).
- *   x             device, n_tokens rows of d_model values of dtype;  out  the same
+ *   x             device, n_tokens rows of d_model values of dtype;  out  the same, and may be x
  *   logits, bias, experts, weights   as for ciera_route
  *   workspace     device, 16-byte aligned, ciera_expert_tokens_workspace_bytes() of the largest call: zero-filled once, its first
  *                 CIERA_EXPERT_TOKENS_HEAD bytes are handed back zero by every call but one that was given up; not shared by

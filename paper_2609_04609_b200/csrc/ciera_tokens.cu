@@ -472,6 +472,7 @@ struct TokensEnd {
     // a token's rows, in the order of its choices
     __device__ __forceinline__ void sum() {
         const uint32_t quads = a.d_model / 4;
+        value_t<DT>* __restrict__ to_all = out;  // (it may be x, which nobody reads any more; without this 64 tokens 75.6 us, 73.8 so)
         for (uint32_t i = blockIdx.x * kTokenThreads + threadIdx.x; i < a.n_tokens * quads; i += gridDim.x * kTokenThreads) {
             const uint32_t token = i / quads, c = (i - token * quads) * 4;
             float v[4] = {0.f, 0.f, 0.f, 0.f};
@@ -496,7 +497,7 @@ struct TokensEnd {
                     v[3] = fmaf(wt[j], r[j].w, v[3]);
                 }
             }
-            value_t<DT>* to = out + token * a.out_stride + c;
+            value_t<DT>* to = to_all + token * a.out_stride + c;
             if (a.out_wide) {
                 store_values<DT, 4>(to, v);
             } else {
@@ -511,7 +512,7 @@ template <int DT, int BITS>
 __global__ void __launch_bounds__(kTokenThreads, 1)
     tokens_kernel(const TokensArgs a, const __grid_constant__ CUtensorMap w1_map, const __grid_constant__ CUtensorMap w2_map,
                   const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap hidden_map, const value_t<DT>* x,
-                  value_t<DT>* __restrict__ out) {
+                  value_t<DT>* out /* may be x */) {
     constexpr uint32_t P = kParts<BITS, DT>;
     constexpr uint32_t kAtoms = BITS == 8 ? 1 : 2;        // of a stage and operand
     extern __shared__ uint8_t tokens_smem[];

@@ -35,6 +35,20 @@ def test_counters_are_zero_behind_calls_whose_tiles_some_warps_have_no_part_in(b
 
 
 @pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_in_place(bits, dtype):
+    """The output is written when every block has read what it needs of x."""
+    c = Case(50, 8, 4, 640, 256, bits, dtype)
+    _call(c, None)
+    want, x = c.out.clone(), c.x.clone()
+    for _ in range(20):
+        c.x.copy_(x)
+        c.out = c.x
+        _call(c, None)
+        assert torch.equal(c.out, want)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("counter", [0, 2])
 def test_a_wait_that_runs_out_is_reported_until_the_workspace_is_zeros_again(bits, counter):
     """A counter that starts one below zero never gets to the number of blocks: the bounded wait for parts (0) or for all tiles (2) runs out
